@@ -357,6 +357,186 @@ sf_status sf_kv_quantize_fp8(const sf_attn_desc* desc, const void* k_pool, const
                              void* k_pool8, void* v_pool8, float* k_scale, float* v_scale, void* stream);
 
 /*
+ * Store of new tokens into an fp8 cache: what lets it grow token by token
+ * (a decode step, E_s = 1) or by blocks (a prompt, a re-prefill). Sequence s
+ * holds L_s = seq_lens[s] tokens of which the last E_s = q_lens[s] are new;
+ * new token j has row cu_s + j of k_new and v_new (bf16 [T][Hkv][D], T = sum_s
+ * E_s, cu_s as in extend attention) and goes to slot p % 16 of page
+ * block_table[s][p / 16] for position p = L_s - E_s + j.
+ *
+ * For every (page, KV head) tile that new tokens land in, keys and values
+ * separately: m = max |x| over its new values, s = its scale; fp32, every
+ * operation correctly rounded.
+ *   No code that it holds (slots of earlier tokens) is nonzero, as in a page
+ *   without earlier tokens (whose old codes and scale are not read):
+ *     scale = max(m, 2^-100) / 448, new codes E4M3(x * (448 / max(m, 2^-100)));
+ *     m = 0: scale 1, codes 0. (sf_kv_quantize_fp8's codes and scale for
+ *     m >= 2^-100.)
+ *   Else, k = the least integer >= 0 with m / (448 s) <= 2^k:
+ *     scale = s 2^k; held codes become E4M3(value * 2^-k) (exact unless
+ *     subnormal), new ones E4M3(x * (1 / (s 2^k))).
+ * Slots of the tile that hold no token get code 0. Rounding is to nearest,
+ * ties to even. Values must be finite and held scales in [2^-110, 2^110].
+ * new_pages (device int32 [B], may be NULL): new_pages[s] >= 0 is the page of
+ * sequence s's last token (one that opens a page), which the call records in
+ * block_table[s][(L_s - 1) / 16]; all other entries must be there. No page
+ * that tokens land in may be part of two sequences.
+ */
+typedef struct sf_store_info {
+  int32_t num_rows;          /* work rows (one workgroup each, or more) */
+  int32_t num_q_rows;        /* T */
+  uint64_t work_bytes;       /* num_rows * 32 */
+  uint64_t desc_key;         /* fingerprint of the descriptor */
+} sf_store_info;
+
+/*
+ * Builds the store's work list on the host (no device calls): int32 rows of 8,
+ * sequence by sequence: seq, first page, pages, position of the first new
+ * token, L_s, cu_s, 0, 0; each a run of the pages that new tokens land in, of
+ * one page, or of up to 4 where there are more than 2048 in all.
+ * Lengths: 0 <= E_s <= L_s <= min(16 * block_table_stride, 2^30), T * Hq * D
+ * < 2^31. work_host NULL only reports the sizes; SF_ERR_CAPACITY if
+ * work_capacity_bytes < info->work_bytes.
+ */
+sf_status sf_kv_store_fp8_plan(const sf_attn_desc* desc, const int32_t* seq_lens_host, const int32_t* q_lens_host,
+                               int32_t* work_host, uint64_t work_capacity_bytes, sf_store_info* info);
+
+/* Enqueues the store (one launch; the work list as for sf_decode_attn).
+ * Errors as sf_decode_attn. */
+sf_status sf_kv_store_fp8(const sf_attn_desc* desc, const sf_store_info* info, const int32_t* work_host,
+                          int32_t* work_dev, const void* k_new, const void* v_new, const int32_t* new_pages,
+                          void* k_pool8, void* v_pool8, float* k_scale, float* v_scale, int32_t* block_table,
+                          void* stream);
+
+/*
+ * Attention weights of cached keys. What a cache of bounded size goes by when
+ * it gives up tokens: for every cached key t of (sequence s, KV head kvh), over
+ * the new tokens j (rows as in extend attention) and the group's query heads h,
+ *   u[t] = sum of exp(softmax_scale * sum_d q[r,h,d] K_s[t,d] - lse[r,h]),  t <= P_s + j
+ *   weights_out = (t < held_s ? weights : 0) + u[t]
+ * with lse from the attention of the same rows over the same cache (a decode
+ * step is E_s = 1). weights, weights_out: fp32 [num_pages][Hkv][16], by page and
+ * slot as the cache (they may be one array). Keys t >= held_s have not been
+ * weighed before: what stands in weights for them is not read, and positions
+ * (int32 [num_pages][Hkv][16], may be NULL) gets first_pos_s + t - held_s.
+ * Rows whose lse is not finite add nothing. Sequences with E_s = 0 are left
+ * out, and so is every slot past L_s. All sums are fp32 in an order that does
+ * not change from run to run. No page may be part of two sequences.
+ */
+typedef struct sf_weights_info {
+  int32_t num_items;         /* work items (one 256-thread workgroup each) */
+  int32_t num_merge;         /* items cut into parts */
+  int32_t num_slots;         /* their parts */
+  int32_t item_pages;        /* pages per item, at most: a multiple of 16 up to 64 */
+  int32_t num_q_rows;        /* T */
+  int32_t reserved;          /* 0 */
+  uint64_t work_bytes;       /* (num_items + num_merge) * 64 */
+  uint64_t workspace_bytes;  /* num_slots * item_pages * 64 */
+  uint64_t desc_key;         /* fingerprint of the descriptor */
+} sf_weights_info;
+
+/*
+ * Builds the work list on the host (no device calls). held_lens_host NULL:
+ * held_s = L_s - E_s (every token before this call has been weighed).
+ * first_pos_host NULL: first_pos_s = held_s. 0 <= held_s <= L_s; positions stay
+ * below 2^31; the other lengths as sf_kv_store_fp8_plan. opts (may be NULL):
+ * num_cus only.
+ * Rule: each (sequence, block of item_pages pages, KV head) is an item that
+ * walks the new tokens t0 .. E_s - 1 that see its first key. If no sequence
+ * has more than 64 query rows per KV head, item_pages is the number of pages over
+ * 8 num_cus, rounded up to a multiple of 16, at least 16 and at most 64; else it
+ * is 16, and walks are cut into the fewest equal parts of at most
+ * max(1, floor(16 m / g)) tokens, m = max(8, floor(row tiles of all items / (8
+ * num_cus))), with ceil(tokens g / 16) row tiles per item.
+ * Work list, int32 rows of 16: num_items rows seq, kv_head, first page, end
+ * page, first token, end token, part slot (-1: uncut), L_s, P_s, cu_s, held_s,
+ * first_pos_s, 0 ..; then num_merge rows with the first part slot and the
+ * number of parts in place of the tokens.
+ */
+sf_status sf_key_weights_plan(const sf_attn_desc* desc, const int32_t* seq_lens_host, const int32_t* q_lens_host,
+                              const int32_t* held_lens_host, const int32_t* first_pos_host, const sf_plan_opts* opts,
+                              int32_t* work_host, uint64_t work_capacity_bytes, sf_weights_info* info);
+
+/* Enqueues the weights pass (one launch, or two where walks are cut). k_pool
+ * holds bf16 keys if k_scale is NULL, else E4M3 codes with k_scale as for
+ * sf_decode_attn_fp8. Arrays 16-byte aligned (lse, k_scale, block_table: 4).
+ * Errors as sf_decode_attn. */
+sf_status sf_key_weights(const sf_attn_desc* desc, const sf_weights_info* info, const int32_t* work_host,
+                         int32_t* work_dev, const void* q, const float* lse, const void* k_pool, const float* k_scale,
+                         const int32_t* block_table, const float* weights, float* weights_out, int32_t* positions,
+                         void* workspace, uint64_t workspace_bytes, void* stream);
+
+/*
+ * Eviction by accumulated attention weight. Every (sequence, KV head) keeps
+ * n_s = min(keep_lens[s], L_s) of its L_s cached tokens, those in the first n_s
+ * slots after the call: the ones whose position is below `sinks` or among the
+ * last `recent` before end_s, and of the others the heaviest (weights; a NaN
+ * counts as lightest), the lower slot among equals. Attention does not depend
+ * on the order of the keys, so kept tokens in the first n_s slots stay where
+ * they are, and the i-th kept token behind them (by slot) moves to the i-th
+ * freed slot, key, value, weight and position. The sequence then has n_s
+ * tokens (the next one goes to slot n_s, at position end_s); its pages from
+ * ceil(n_s / 16) on are free (sf_page_table_truncate).
+ * weights_out and positions_out may be the input arrays; else slots 0 .. n_s - 1
+ * of every sequence are written to them. In an fp8 cache (k_scale and v_scale
+ * not NULL) a moved token's values code * scale are stored as new ones by
+ * sf_kv_store_fp8's rule, the tokens that the tile holds besides (slots below
+ * L_s) being the held ones; the tiles without a freed slot do not change.
+ * Slots from n_s on keep no meaning. No page may be part of two sequences.
+ */
+typedef struct sf_evict_info {
+  int32_t num_seqs;
+  int32_t num_moves;         /* work rows of the moves */
+  int32_t sinks, recent;     /* as given to the plan */
+  int32_t boundary;          /* some sequence gives up tokens and its n_s ends inside a page */
+  int32_t hole_pages;        /* Hkv * sum_s ceil(n_s / 16) */
+  uint64_t work_bytes;       /* (num_seqs + num_moves) * 32 */
+  uint64_t workspace_bytes;  /* hole_pages * 8, rounded up to 256, + Hkv * sum_s min(n_s, L_s - n_s) * 4 */
+  uint64_t desc_key;         /* fingerprint of the descriptor */
+} sf_evict_info;
+
+/*
+ * Builds the work list on the host (no device calls). ends_host NULL: end_s =
+ * L_s (nothing was evicted before). SF_ERR_INVALID_ARG for a negative length,
+ * sinks or recent, L_s > min(16 * block_table_stride, 2^30), end_s < L_s, and
+ * n_s < min(L_s, sinks + recent). Work list, int32 rows of 8: num_seqs rows L_s,
+ * n_s, first hole page, first tail, end_s, 0 ..; then the moves, runs of one of the
+ * first ceil(n_s / 16) pages, or of up to 4 where there are more than 2048 in all: seq, first page,
+ * pages, 0 ...
+ */
+sf_status sf_kv_evict_plan(const sf_attn_desc* desc, const int32_t* seq_lens_host, const int32_t* keep_lens_host,
+                           const int32_t* ends_host, int32_t sinks, int32_t recent, int32_t* work_host,
+                           uint64_t work_capacity_bytes, sf_evict_info* info);
+
+/* Enqueues the eviction (two launches; three for an fp8 cache with a budget
+ * inside a page). Arrays 16-byte aligned (scales, block_table: 4). Errors as
+ * sf_decode_attn. */
+sf_status sf_kv_evict(const sf_attn_desc* desc, const sf_evict_info* info, const int32_t* work_host, int32_t* work_dev,
+                      void* k_pool, void* v_pool, float* k_scale, float* v_scale, const int32_t* block_table,
+                      const float* weights, const int32_t* positions, float* weights_out, int32_t* positions_out,
+                      void* workspace, uint64_t workspace_bytes, void* stream);
+
+/* The same three through a runner: planned into its ring, which the kernels
+ * read in place, in its workspace, in order with its steps. Arguments as
+ * the plan's and the call's, lengths and new_pages on the host (new_pages_host
+ * may be NULL). SF_ERR_UNSUPPORTED, with nothing launched, on a stream that is
+ * being captured into a graph. Other errors as theirs and sf_runner_step. */
+sf_status sf_runner_store_fp8(sf_runner* runner, const sf_attn_desc* desc, const int32_t* seq_lens_host,
+                              const int32_t* q_lens_host, const void* k_new, const void* v_new,
+                              const int32_t* new_pages_host, void* k_pool8, void* v_pool8, float* k_scale,
+                              float* v_scale, int32_t* block_table, void* stream);
+sf_status sf_runner_key_weights(sf_runner* runner, const sf_attn_desc* desc, const int32_t* seq_lens_host,
+                                const int32_t* q_lens_host, const int32_t* held_lens_host,
+                                const int32_t* first_pos_host, const void* q, const float* lse, const void* k_pool,
+                                const float* k_scale, const int32_t* block_table, const float* weights,
+                                float* weights_out, int32_t* positions, void* stream);
+sf_status sf_runner_evict(sf_runner* runner, const sf_attn_desc* desc, const int32_t* seq_lens_host,
+                          const int32_t* keep_lens_host, const int32_t* ends_host, int32_t sinks, int32_t recent,
+                          void* k_pool, void* v_pool, float* k_scale, float* v_scale, const int32_t* block_table,
+                          const float* weights, const int32_t* positions, float* weights_out, int32_t* positions_out,
+                          void* stream);
+
+/*
  * Extend (re-prefill) attention. A trajectory interrupted for a model update
  * or migrated to another instance has its KV cache recomputed before its
  * generation resumes (partial rollout and migration, Sec. 2.3; prefill and
@@ -524,6 +704,16 @@ sf_status sf_page_pool_release(sf_page_pool* pool, const int32_t* pages, int32_t
 sf_status sf_page_table_step(sf_page_pool* pool, int32_t* block_table, int32_t stride,
                              int32_t num_seqs, const int32_t* prev_lens, const int32_t* lens,
                              int32_t appending, int32_t* new_pages);
+
+/*
+ * The pages that an eviction frees: sequence s goes from lens[s] to keep[s] <=
+ * lens[s] tokens and returns the pages ceil(keep / 16) .. ceil(lens / 16) - 1
+ * of its block-table row to the pool (ascending sequence order, each in
+ * block-table order); their entries become -1. All or nothing, errors as
+ * sf_page_table_step.
+ */
+sf_status sf_page_table_truncate(sf_page_pool* pool, int32_t* block_table, int32_t stride, int32_t num_seqs,
+                                 const int32_t* lens, const int32_t* keep);
 
 /*
  * Host check of a block table before it is used on the device: the kernels

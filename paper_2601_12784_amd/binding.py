@@ -62,6 +62,22 @@ class sf_extend_info(ctypes.Structure):
                 ("work_bytes", ctypes.c_uint64), ("desc_key", ctypes.c_uint64)]
 
 
+class sf_store_info(ctypes.Structure):
+    _fields_ = [("num_rows", ctypes.c_int32), ("num_q_rows", ctypes.c_int32), ("work_bytes", ctypes.c_uint64),
+                ("desc_key", ctypes.c_uint64)]
+
+
+class sf_weights_info(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("num_items", "num_merge", "num_slots", "item_pages", "num_q_rows",
+                                              "reserved")] + \
+               [(n, ctypes.c_uint64) for n in ("work_bytes", "workspace_bytes", "desc_key")]
+
+
+class sf_evict_info(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("num_seqs", "num_moves", "sinks", "recent", "boundary", "hole_pages")] + \
+               [(n, ctypes.c_uint64) for n in ("work_bytes", "workspace_bytes", "desc_key")]
+
+
 class sf_runner_extras(ctypes.Structure):
     _fields_ = [("k_new", ctypes.c_void_p), ("v_new", ctypes.c_void_p), ("new_pages_host", ctypes.c_void_p),
                 ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p), ("attn_start", ctypes.c_void_p),
@@ -141,6 +157,17 @@ def lib():
     for fn in ("sf_page_pool_claim", "sf_page_pool_release"):
         getattr(L, fn).argtypes = [vp, vp, ctypes.c_int32]
     L.sf_page_pool_alloc.argtypes = [vp, ctypes.c_int32, vp]
+    i32, u64, desc = ctypes.c_int32, ctypes.c_uint64, P(sf_attn_desc)
+    L.sf_kv_store_fp8_plan.argtypes = [desc, vp, vp, vp, u64, P(sf_store_info)]
+    L.sf_kv_store_fp8.argtypes = [desc, P(sf_store_info)] + [vp] * 11
+    L.sf_key_weights_plan.argtypes = [desc, vp, vp, vp, vp, P(sf_plan_opts), vp, u64, P(sf_weights_info)]
+    L.sf_key_weights.argtypes = [desc, P(sf_weights_info)] + [vp] * 11 + [u64, vp]
+    L.sf_kv_evict_plan.argtypes = [desc, vp, vp, vp, i32, i32, vp, u64, P(sf_evict_info)]
+    L.sf_kv_evict.argtypes = [desc, P(sf_evict_info)] + [vp] * 12 + [u64, vp]
+    L.sf_runner_store_fp8.argtypes = [vp, desc] + [vp] * 11
+    L.sf_runner_key_weights.argtypes = [vp, desc] + [vp] * 13
+    L.sf_runner_evict.argtypes = [vp, desc, vp, vp, vp, i32, i32] + [vp] * 10
+    L.sf_page_table_truncate.argtypes = [vp, vp, i32, i32, vp, vp]
     L.sf_page_table_step.argtypes = [vp, vp, ctypes.c_int32, ctypes.c_int32, vp, vp, ctypes.c_int32, vp]
     L.sf_cost_throughput.argtypes = [P(sf_cost_model), P(sf_instance_state)]
     L.sf_cost_marginal_gain.argtypes = [P(sf_cost_model), P(sf_instance_state), ctypes.c_double]
@@ -156,7 +183,10 @@ def lib():
                "sf_page_pool_release", "sf_page_table_step", "sf_route", "sf_extend_attn_plan",
                "sf_extend_attn", "sf_decode_attn_fp8", "sf_kv_quantize_fp8", "sf_runner_create",
                "sf_runner_step", "sf_runner_extend", "sf_runner_plan", "sf_debug_extend_plan",
-               "sf_debug_runner_reserve", "sf_runner_reserve_batch", "sf_debug_stream_read", "sf_decode_attn_scratch"):
+               "sf_debug_runner_reserve", "sf_runner_reserve_batch", "sf_debug_stream_read", "sf_decode_attn_scratch",
+               "sf_kv_store_fp8_plan", "sf_kv_store_fp8", "sf_key_weights_plan", "sf_key_weights", "sf_kv_evict_plan",
+               "sf_kv_evict", "sf_runner_store_fp8", "sf_runner_key_weights", "sf_runner_evict",
+               "sf_page_table_truncate"):
         getattr(L, fn).restype = ctypes.c_int
     L.sf_status_string.argtypes = [ctypes.c_int]
     L.sf_status_string.restype = ctypes.c_char_p
@@ -395,6 +425,144 @@ def sf_decode_attn_append(desc, info, work_host, work_dev, q, k_new, v_new, new_
         ctypes.byref(desc), ctypes.byref(info), _addr(work_host), _addr(work_dev), _addr(q), _addr(k_new),
         _addr(v_new), _addr(new_pages), _addr(k_pool), _addr(v_pool), _addr(block_table), _addr(out),
         _addr(lse), _addr(workspace), ws_bytes, _stream(stream)))
+
+
+def _host_i32(x, name, n):
+    """x as a host int32 array with an entry per sequence (None stays None)."""
+    if x is None:
+        return None
+    if isinstance(x, torch.Tensor):
+        x = x.cpu().numpy()
+    x = x if isinstance(x, np.ndarray) and x.dtype == np.int32 and x.flags.c_contiguous else np.ascontiguousarray(x, np.int32)
+    if x.shape != (n,):
+        raise ValueError(f"{name} must have one entry per sequence")
+    return x
+
+
+def _planned(name, info, call, work_host):
+    """call(work, capacity) into work_host, or into an array of the size it asks for."""
+    if work_host is None:
+        _check(name, call(None, 0))
+        work_host = np.empty(max(1, info.work_bytes // 4), dtype=np.int32)
+    cap = work_host.numel() * 4 if isinstance(work_host, torch.Tensor) else work_host.nbytes
+    _check(name, call(_addr(work_host), cap))
+    return info, work_host
+
+
+def _check_work(info, work_dev, workspace=None):
+    """The device work list and workspace of a planned call; returns the workspace's bytes."""
+    _dev(work_dev, "work_dev", torch.int32)
+    if work_dev.numel() * 4 < info.work_bytes:
+        raise ValueError("work_dev is smaller than the plan")
+    if workspace is None:
+        return 0
+    _dev(workspace, "workspace", workspace.dtype)
+    return workspace.numel() * workspace.element_size()
+
+
+def _check_pools(n, hkv, d, k_pool, v_pool, block_table, batch, fp8):
+    """A cache's pools (v_pool may be None) and block table; fp8: (k_scale, v_scale), None for a bf16 cache."""
+    if fp8 is None:
+        _dev(k_pool, "k_pool", torch.bfloat16, (n, hkv, d // 8, PAGE, 8))
+        if v_pool is not None:
+            _dev(v_pool, "v_pool", torch.bfloat16, (n, hkv, d, PAGE))
+    else:
+        _dev(k_pool, "k_pool8", torch.uint8, (n, hkv, PAGE * d))
+        _dev(fp8[0], "k_scale", torch.float32, (n, hkv))
+        if v_pool is not None:
+            _dev(v_pool, "v_pool8", torch.uint8, (n, hkv, PAGE * d))
+            _dev(fp8[1], "v_scale", torch.float32, (n, hkv))
+    _dev(block_table, "block_table", torch.int32, (batch, block_table.shape[1]))
+
+
+def _check_slots(n, hkv, weights, weights_out, positions, positions_out=None):
+    for t, name in ((weights, "weights"), (weights_out, "weights_out")):
+        _dev(t, name, torch.float32, (n, hkv, PAGE))
+    for t, name in ((positions, "positions"), (positions_out, "positions_out")):
+        if t is not None:
+            _dev(t, name, torch.int32, (n, hkv, PAGE))
+
+
+def sf_kv_store_fp8_plan(desc, seq_lens, q_lens, work_host=None):
+    """Plans the store of the last q_lens[s] of seq_lens[s] tokens into an fp8 cache. Returns (info, work_host)."""
+    lens, qls = _host_i32(seq_lens, "seq_lens", desc.num_seqs), _host_i32(q_lens, "q_lens", desc.num_seqs)
+    info = sf_store_info()
+    return _planned("sf_kv_store_fp8_plan", info, lambda w, cap: lib().sf_kv_store_fp8_plan(
+        ctypes.byref(desc), _host_addr(lens), _host_addr(qls), w, cap, ctypes.byref(info)), work_host)
+
+
+def sf_kv_store_fp8(desc, info, work_host, work_dev, k_new, v_new, new_pages, k_pool8, v_pool8, k_scale, v_scale,
+                    block_table, stream=None):
+    """Enqueues the store of new tokens (k_new, v_new: bf16 [T, Hkv, D]) into an fp8 cache whose tiles' scales grow.
+    new_pages: device int32 [B] (-1 = no new page) or None."""
+    hkv, d = desc.num_kv_heads, desc.head_dim
+    _dev(k_new, "k_new", torch.bfloat16, (info.num_q_rows, hkv, d))
+    _dev(v_new, "v_new", torch.bfloat16, (info.num_q_rows, hkv, d))
+    if new_pages is not None:
+        _dev(new_pages, "new_pages", torch.int32, (desc.num_seqs,))
+    _check_pools(desc.num_pages, hkv, d, k_pool8, v_pool8, block_table, desc.num_seqs, (k_scale, v_scale))
+    _check_work(info, work_dev)
+    _check("sf_kv_store_fp8", lib().sf_kv_store_fp8(
+        ctypes.byref(desc), ctypes.byref(info), _addr(work_host), _addr(work_dev), _addr(k_new), _addr(v_new),
+        _addr(new_pages), _addr(k_pool8), _addr(v_pool8), _addr(k_scale), _addr(v_scale), _addr(block_table),
+        _stream(stream)))
+
+
+def sf_key_weights_plan(desc, seq_lens, q_lens, held_lens=None, first_pos=None, opts=None, work_host=None):
+    """Plans the weights pass of the last q_lens[s] of seq_lens[s] tokens' query rows. Returns (info, work_host)."""
+    n = desc.num_seqs
+    lens, qls = _host_i32(seq_lens, "seq_lens", n), _host_i32(q_lens, "q_lens", n)
+    held, pos = _host_i32(held_lens, "held_lens", n), _host_i32(first_pos, "first_pos", n)
+    info = sf_weights_info()
+    return _planned("sf_key_weights_plan", info, lambda w, cap: lib().sf_key_weights_plan(
+        ctypes.byref(desc), _host_addr(lens), _host_addr(qls), _addr(held), _addr(pos),
+        None if opts is None else ctypes.byref(opts), w, cap, ctypes.byref(info)), work_host)
+
+
+def sf_key_weights(desc, info, work_host, work_dev, q, lse, k_pool, block_table, weights, weights_out=None,
+                   positions=None, k_scale=None, workspace=None, stream=None):
+    """Enqueues the weights pass: every cached key's attention weight, summed over the rows of q (bf16 [T, Hq, D], lse
+    fp32 [T, Hq]), added to `weights` (fp32 [N, Hkv, 16]) into weights_out (default: weights itself). positions
+    (int32 [N, Hkv, 16]) takes those of keys weighed first. k_scale: k_pool is an fp8 cache's."""
+    weights_out = weights if weights_out is None else weights_out
+    hq, hkv, d = desc.num_q_heads, desc.num_kv_heads, desc.head_dim
+    _dev(q, "q", torch.bfloat16, (info.num_q_rows, hq, d))
+    _dev(lse, "lse", torch.float32, (info.num_q_rows, hq))
+    _check_pools(desc.num_pages, hkv, d, k_pool, None, block_table, desc.num_seqs, None if k_scale is None else (k_scale,))
+    _check_slots(desc.num_pages, hkv, weights, weights_out, positions)
+    ws_bytes = _check_work(info, work_dev, workspace)
+    _check("sf_key_weights", lib().sf_key_weights(
+        ctypes.byref(desc), ctypes.byref(info), _addr(work_host), _addr(work_dev), _addr(q), _addr(lse), _addr(k_pool),
+        _addr(k_scale), _addr(block_table), _addr(weights), _addr(weights_out), _addr(positions), _addr(workspace),
+        ws_bytes, _stream(stream)))
+
+
+def sf_kv_evict_plan(desc, seq_lens, keep_lens, ends=None, sinks=0, recent=0, work_host=None):
+    """Plans an eviction from seq_lens[s] to at most keep_lens[s] tokens. Returns (info, work_host)."""
+    n = desc.num_seqs
+    lens, keep = _host_i32(seq_lens, "seq_lens", n), _host_i32(keep_lens, "keep_lens", n)
+    end = _host_i32(ends, "ends", n)
+    info = sf_evict_info()
+    return _planned("sf_kv_evict_plan", info, lambda w, cap: lib().sf_kv_evict_plan(
+        ctypes.byref(desc), _host_addr(lens), _host_addr(keep), _addr(end), int(sinks), int(recent), w, cap,
+        ctypes.byref(info)), work_host)
+
+
+def sf_kv_evict(desc, info, work_host, work_dev, k_pool, v_pool, block_table, weights, positions, weights_out=None,
+                positions_out=None, fp8=None, workspace=None, stream=None):
+    """Enqueues the eviction: every (sequence, KV head) keeps its heaviest tokens, in its first slots. fp8: (k_scale,
+    v_scale) of an fp8 cache. weights_out and positions_out default to weights and positions themselves."""
+    weights_out = weights if weights_out is None else weights_out
+    positions_out = positions if positions_out is None else positions_out
+    hkv, d = desc.num_kv_heads, desc.head_dim
+    _check_pools(desc.num_pages, hkv, d, k_pool, v_pool, block_table, desc.num_seqs, fp8)
+    _check_slots(desc.num_pages, hkv, weights, weights_out, positions, positions_out)
+    ws_bytes = _check_work(info, work_dev, workspace)
+    k_scale, v_scale = fp8 if fp8 is not None else (None, None)
+    _check("sf_kv_evict", lib().sf_kv_evict(
+        ctypes.byref(desc), ctypes.byref(info), _addr(work_host), _addr(work_dev), _addr(k_pool), _addr(v_pool),
+        _addr(k_scale), _addr(v_scale), _addr(block_table), _addr(weights), _addr(positions), _addr(weights_out),
+        _addr(positions_out), _addr(workspace), ws_bytes, _stream(stream)))
 
 
 def sf_extend_attn_plan(desc: sf_attn_desc, seq_lens, q_lens, work_host=None):
@@ -980,9 +1148,8 @@ class DecodeAttention:
         new_pages a host int32 [B] array (-1 = the token's page is already
         held), uploaded together with the work list. fp8 = (k_scale, v_scale)
         makes k_pool / v_pool an fp8 cache (uint8 E4M3 codes [N, Hkv, 16*D],
-        fp32 scales [N, Hkv]); it cannot be combined with append."""
-        if fp8 is not None and append is not None:
-            raise ValueError("the fp8 cache has no appending step")
+        fp32 scales [N, Hkv]). With both, the newest tokens are stored first
+        (sf_kv_store_fp8's rule) and attended as stored."""
         b = q.shape[0]
         main = stream.cuda_stream if stream else _current_stream(self.device)
         if out is None:
@@ -1009,7 +1176,7 @@ class DecodeAttention:
             if pages.shape != (b,):
                 raise ValueError("new_pages must have one entry per sequence")
             ex.k_new, ex.v_new, ex.new_pages_host = k_new.data_ptr(), v_new.data_ptr(), _host_addr(pages)
-            if lse is None:  # the merge reads lse back: keep one of our own
+            if lse is None and fp8 is None:  # the merge reads lse back: keep one of our own
                 if self._lse is None or self._lse.numel() < b * self.hq:
                     self._lse = torch.empty(b * self.hq * 5 // 4 + 64, dtype=torch.float32, device=self.device)
                 lse = self._lse[: b * self.hq].view(b, self.hq)
@@ -1033,6 +1200,72 @@ class DecodeAttention:
             ctypes.byref(ex), main, ctypes.byref(info)))
         self.last_info = sf_plan_info.from_buffer_copy(info)
         return out
+
+    def _call_desc(self, k_pool, block_table, seq_lens, scale):
+        """(desc, lengths) of a call besides the steps."""
+        lens = _host_i32(seq_lens, "seq_lens", block_table.shape[0])
+        desc = make_desc(lens.size, self.hq, self.hkv, self.d, block_table.shape[1], k_pool.shape[0], scale)
+        return desc, lens
+
+    def store_fp8(self, k_new, v_new, k_pool8, v_pool8, fp8, block_table, seq_lens, q_lens, new_pages=None, stream=None):
+        """Stores the last q_lens[s] of seq_lens[s] tokens (k_new, v_new: bf16 [T, Hkv, D]) into an fp8 cache, fp8 =
+        (k_scale, v_scale), through the runner (sf_runner_store_fp8). new_pages: host int32 [B], the page of a
+        sequence's last token where that opens one, else -1; None: every page is in the block table."""
+        desc, lens = self._call_desc(k_pool8, block_table, seq_lens, 1.0)
+        qls, pages = _host_i32(q_lens, "q_lens", lens.size), _host_i32(new_pages, "new_pages", lens.size)
+        rows = int(qls.sum())
+        _dev(k_new, "k_new", torch.bfloat16, (rows, self.hkv, self.d))
+        _dev(v_new, "v_new", torch.bfloat16, (rows, self.hkv, self.d))
+        _check_pools(desc.num_pages, self.hkv, self.d, k_pool8, v_pool8, block_table, lens.size, fp8)
+        if DEBUG_CHECKS:
+            named = np.zeros(lens.size, bool) if pages is None else pages >= 0
+            check_block_table(desc, block_table, np.where(qls > 0, lens - named, 0))
+            if pages is not None and np.any((pages < -1) | (pages >= desc.num_pages)):
+                raise ValueError("new_pages holds a page id outside the pool")
+        _check("sf_runner_store_fp8", self.L.sf_runner_store_fp8(
+            self._runner(None), ctypes.byref(desc), _host_addr(lens), _host_addr(qls), k_new.data_ptr(), v_new.data_ptr(),
+            _addr(pages), k_pool8.data_ptr(), v_pool8.data_ptr(), fp8[0].data_ptr(), fp8[1].data_ptr(),
+            block_table.data_ptr(), stream.cuda_stream if stream else _current_stream(self.device)))
+
+    def key_weights(self, q, lse, k_pool, block_table, seq_lens, q_lens, scale, weights, weights_out=None,
+                    positions=None, held_lens=None, first_pos=None, k_scale=None, stream=None):
+        """Adds every cached key's attention weight, summed over the query rows of the last q_lens[s] of seq_lens[s]
+        tokens and over the heads of its group, to weights (sf_key_weights, through the runner)."""
+        weights_out = weights if weights_out is None else weights_out
+        desc, lens = self._call_desc(k_pool, block_table, seq_lens, scale)
+        n = lens.size
+        qls, held, pos = (_host_i32(x, name, n) for x, name in ((q_lens, "q_lens"), (held_lens, "held_lens"),
+                                                                (first_pos, "first_pos")))
+        rows = int(qls.sum())
+        _dev(q, "q", torch.bfloat16, (rows, self.hq, self.d))
+        _dev(lse, "lse", torch.float32, (rows, self.hq))
+        _check_pools(desc.num_pages, self.hkv, self.d, k_pool, None, block_table, n, None if k_scale is None else (k_scale,))
+        _check_slots(desc.num_pages, self.hkv, weights, weights_out, positions)
+        if DEBUG_CHECKS:
+            check_block_table(desc, block_table, np.where(qls > 0, lens, 0))
+        _check("sf_runner_key_weights", self.L.sf_runner_key_weights(
+            self._runner(None), ctypes.byref(desc), _host_addr(lens), _host_addr(qls), _addr(held), _addr(pos), q.data_ptr(),
+            lse.data_ptr(), k_pool.data_ptr(), _addr(k_scale), block_table.data_ptr(), weights.data_ptr(),
+            weights_out.data_ptr(), _addr(positions), stream.cuda_stream if stream else _current_stream(self.device)))
+
+    def evict(self, k_pool, v_pool, block_table, seq_lens, keep_lens, weights, positions, weights_out=None,
+              positions_out=None, ends=None, sinks=0, recent=0, fp8=None, stream=None):
+        """Evicts down to at most keep_lens[s] tokens per (sequence, KV head) (sf_kv_evict, through the runner): the
+        positions below `sinks` and the last `recent` before ends[s] (default: seq_lens) stay, then the heaviest."""
+        weights_out = weights if weights_out is None else weights_out
+        positions_out = positions if positions_out is None else positions_out
+        desc, lens = self._call_desc(k_pool, block_table, seq_lens, 1.0)
+        keep, end = _host_i32(keep_lens, "keep_lens", lens.size), _host_i32(ends, "ends", lens.size)
+        _check_pools(desc.num_pages, self.hkv, self.d, k_pool, v_pool, block_table, lens.size, fp8)
+        _check_slots(desc.num_pages, self.hkv, weights, weights_out, positions, positions_out)
+        if DEBUG_CHECKS:
+            check_block_table(desc, block_table, lens)
+        k_scale, v_scale = fp8 if fp8 is not None else (None, None)
+        _check("sf_runner_evict", self.L.sf_runner_evict(
+            self._runner(None), ctypes.byref(desc), _host_addr(lens), _host_addr(keep), _addr(end), int(sinks), int(recent),
+            k_pool.data_ptr(), v_pool.data_ptr(), _addr(k_scale), _addr(v_scale), block_table.data_ptr(), weights.data_ptr(),
+            positions.data_ptr(), weights_out.data_ptr(), positions_out.data_ptr(),
+            stream.cuda_stream if stream else _current_stream(self.device)))
 
     def __del__(self):
         L = getattr(self, "L", None)
@@ -1078,6 +1311,15 @@ class PageTable:
             lens.ctypes.data, int(bool(appending)), self.new_pages.ctypes.data))
         self.prev = lens
         return self.new_pages
+
+
+    def truncate(self, keep) -> None:
+        """After an eviction: the sequences hold keep tokens, and the pages behind them go back to the pool
+        (the library's sf_page_table_truncate on the host table; the next advance continues from keep)."""
+        keep = _host_i32(keep, "keep", self.prev.size)
+        _check("sf_page_table_truncate", self.pool._L.sf_page_table_truncate(
+            self.pool._p, self.bt.ctypes.data, self.bt.shape[1], keep.size, self.prev.ctypes.data, keep.ctypes.data))
+        self.prev = keep.copy()
 
 
 class DecodeLoopRunner:

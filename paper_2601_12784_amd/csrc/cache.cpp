@@ -1,0 +1,425 @@
+// A cache of bounded size: host planners and entry points of the store into
+// an fp8 cache, the weights of cached keys and the eviction that goes by them.
+// The rules are stated in sf_decode_attn.h next to their plan functions.
+#include <algorithm>
+#include <climits>
+#include <cstdint>
+#include <cstring>
+
+#include "sf_internal.h"
+
+static_assert(sizeof(sf_store_info) == 24, "sf_store_info layout is part of the ABI");
+static_assert(sizeof(sf_weights_info) == 48, "sf_weights_info layout is part of the ABI");
+static_assert(sizeof(sf_evict_info) == 48, "sf_evict_info layout is part of the ABI");
+
+using namespace sf;
+
+namespace {
+
+constexpr int32_t kMaxTokens = 1 << 30;   // per sequence: token and page numbers stay far from 2^31
+
+bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+int32_t pages_of(int32_t tokens) { return (tokens + kPage - 1) / kPage; }
+sf_status from_hip(hipError_t e) { return e == hipSuccess ? SF_OK : SF_ERR_HIP; }
+
+// Pages per work-list row: one wave per tile has the most parallelism, and a
+// long list is cheaper to make and read in runs of four.
+constexpr int64_t kSinglePages = 2048;
+int32_t run_of(int64_t pages) { return pages > kSinglePages ? 4 : 1; }
+
+void put_row(int32_t*& at, int32_t a, int32_t b, int32_t c, int32_t d, int32_t e, int32_t f) {
+  const int32_t row[kItemInts] = {a, b, c, d, e, f, 0, 0};
+  std::memcpy(at, row, sizeof row);
+  at += kItemInts;
+}
+
+sf_status check_lengths(const sf_attn_desc* desc, const int32_t* seq_lens, const int32_t* q_lens, int64_t* rows) {
+  const sf_status st = check_extend_lengths(desc, seq_lens, q_lens, rows);
+  if (st != SF_OK) return st;
+  for (int32_t s = 0; s < desc->num_seqs; ++s)
+    if (seq_lens[s] > kMaxTokens) return SF_ERR_INVALID_ARG;
+  return SF_OK;
+}
+
+}  // namespace
+
+// ---------------------------------------------------------------------------
+// store into an fp8 cache
+// ---------------------------------------------------------------------------
+extern "C" sf_status sf_kv_store_fp8_plan(const sf_attn_desc* desc, const int32_t* seq_lens_host,
+                                          const int32_t* q_lens_host, int32_t* work_host, uint64_t work_capacity_bytes,
+                                          sf_store_info* info) {
+  if (!info) return SF_ERR_INVALID_ARG;
+  int64_t tokens = 0;
+  sf_status st = check_lengths(desc, seq_lens_host, q_lens_host, &tokens);
+  if (st != SF_OK) return st;
+  const int32_t* news = q_lens_host;
+  auto touched = [&](int32_t s) {
+    return news[s] == 0 ? 0 : pages_of(seq_lens_host[s]) - (seq_lens_host[s] - news[s]) / kPage;
+  };
+  int64_t pages = 0, rows = 0;
+  for (int32_t s = 0; s < desc->num_seqs; ++s) pages += touched(s);
+  const int32_t run = run_of(pages);
+  for (int32_t s = 0; s < desc->num_seqs; ++s) rows += (touched(s) + run - 1) / run;
+  info->num_rows = int32_t(rows);   // at most 16 per token, and T Hq D < 2^31
+  info->num_q_rows = int32_t(tokens);
+  info->work_bytes = uint64_t(rows) * kItemInts * 4;
+  info->desc_key = desc_key(desc);
+  if (!work_host) return SF_OK;
+  if (work_capacity_bytes < info->work_bytes) return SF_ERR_CAPACITY;
+  int32_t qrow = 0;
+  for (int32_t s = 0; s < desc->num_seqs; qrow += news[s++]) {
+    const int32_t first = seq_lens_host[s] - news[s], begin = first / kPage, end = begin + touched(s);
+    for (int32_t p = begin; p < end; p += run)
+      put_row(work_host, s, p, std::min(run, end - p), first, seq_lens_host[s], qrow);
+  }
+  return SF_OK;
+}
+
+sf_status sf::store8_args(const sf_attn_desc* desc, const int32_t* work_dev, const void* k_new, const void* v_new,
+                          const int32_t* new_pages, void* k_pool8, void* v_pool8, float* k_scale, float* v_scale,
+                          int32_t* block_table, Store8Args* args) {
+  if (!work_dev || !k_new || !v_new || !k_pool8 || !v_pool8 || !k_scale || !v_scale || !block_table)
+    return SF_ERR_INVALID_ARG;
+  if (!aligned16(work_dev) || !aligned16(k_new) || !aligned16(v_new) || !aligned16(k_pool8) || !aligned16(v_pool8) ||
+      !aligned4(k_scale) || !aligned4(v_scale) || !aligned4(block_table) || (new_pages && !aligned4(new_pages)))
+    return SF_ERR_INVALID_ARG;
+  Store8Args a = {};
+  a.rows = work_dev;
+  a.k_new = static_cast<const uint16_t*>(k_new);
+  a.v_new = static_cast<const uint16_t*>(v_new);
+  a.new_pages = new_pages;
+  a.k_pool = static_cast<uint8_t*>(k_pool8);
+  a.v_pool = static_cast<uint8_t*>(v_pool8);
+  a.k_scale = k_scale;
+  a.v_scale = v_scale;
+  a.block_table = block_table;
+  a.num_kv_heads = desc->num_kv_heads;
+  a.head_dim = desc->head_dim;
+  a.bt_stride = desc->block_table_stride;
+  *args = a;
+  return SF_OK;
+}
+
+extern "C" sf_status sf_kv_store_fp8(const sf_attn_desc* desc, const sf_store_info* info, const int32_t* work_host,
+                                     int32_t* work_dev, const void* k_new, const void* v_new, const int32_t* new_pages,
+                                     void* k_pool8, void* v_pool8, float* k_scale, float* v_scale, int32_t* block_table,
+                                     void* stream) {
+  sf_status st = validate_desc(desc);
+  if (st != SF_OK) return st;
+  if (!info) return SF_ERR_INVALID_ARG;
+  if (info->desc_key != desc_key(desc) || info->num_rows < 0 || info->num_q_rows < 0 ||
+      info->work_bytes != uint64_t(info->num_rows) * kItemInts * 4)
+    return SF_ERR_PLAN_MISMATCH;
+  if (info->num_rows == 0) return SF_OK;
+  Store8Args a;
+  if ((st = store8_args(desc, work_dev, k_new, v_new, new_pages, k_pool8, v_pool8, k_scale, v_scale, block_table, &a)) !=
+      SF_OK)
+    return st;
+  a.num_rows = info->num_rows;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if (work_host && hipMemcpyAsync(work_dev, work_host, info->work_bytes, hipMemcpyHostToDevice, s) != hipSuccess)
+    return SF_ERR_HIP;
+  return from_hip(launch_store_fp8(a, s));
+}
+
+// ---------------------------------------------------------------------------
+// weights of cached keys
+// ---------------------------------------------------------------------------
+namespace {
+
+// A work item is a block of pages of one (sequence, KV head), 64 keys per wave
+// at a time; its cost is the walk over its query rows, 16 per tile. Few rows
+// (a decode step's one token) are bound by reading the keys: blocks of up to 64
+// pages, as few as still give every compute unit eight. Many rows (prompts) take
+// blocks of 16 pages, one walk per wave, and walks longer than about an eighth of a
+// compute unit's share are cut into parts, so that no walk is longer than the rest.
+constexpr int32_t kItemPages = 4 * kWeightPages;
+constexpr int32_t kMaxItemPages = 4 * kItemPages;
+constexpr int32_t kShortRows = 64;
+constexpr int64_t kItemsPerCu = 8;
+constexpr int64_t kShortestPart = 8;   // row tiles
+
+struct WeightCut {
+  int32_t item_pages;
+  int64_t part_tokens;
+};
+
+template <class F>   // f(sequence, first page, end page, first token that sees the block, parts)
+void for_weight_items(const sf_attn_desc* d, const int32_t* lens, const int32_t* news, const WeightCut& cut, F f) {
+  for (int32_t s = 0; s < d->num_seqs; ++s) {
+    if (news[s] == 0) continue;
+    const int32_t pages = pages_of(lens[s]), prefix = lens[s] - news[s];
+    for (int32_t p = 0; p < pages; p += cut.item_pages) {
+      const int32_t t0 = std::max(0, p * kPage - prefix);
+      f(s, p, std::min(pages, p + cut.item_pages), t0, int32_t((news[s] - t0 + cut.part_tokens - 1) / cut.part_tokens));
+    }
+  }
+}
+
+WeightCut choose_weight_cut(const sf_attn_desc* d, const int32_t* lens, const int32_t* news, int32_t num_cus) {
+  const int64_t g = d->num_q_heads / d->num_kv_heads, hkv = d->num_kv_heads, cus = num_cus;
+  int64_t pages = 0, most = 0;
+  for (int32_t s = 0; s < d->num_seqs; ++s) {
+    if (news[s] == 0) continue;
+    pages += pages_of(lens[s]);
+    most = std::max<int64_t>(most, news[s] * g);
+  }
+  WeightCut cut = {kItemPages, INT32_MAX};
+  if (most <= kShortRows) {
+    const int64_t each = (pages * hkv / (kItemsPerCu * cus) + kItemPages - 1) / kItemPages * kItemPages;
+    cut.item_pages = int32_t(std::min<int64_t>(kMaxItemPages, std::max<int64_t>(kItemPages, each)));
+    return cut;
+  }
+  int64_t tiles = 0;
+  for_weight_items(d, lens, news, cut,
+                   [&](int32_t s, int32_t, int32_t, int32_t t0, int32_t) { tiles += ((news[s] - t0) * g + 15) / 16; });
+  const int64_t part = std::max(kShortestPart, tiles * hkv / (kItemsPerCu * cus));
+  cut.part_tokens = std::max<int64_t>(1, part * 16 / g);
+  return cut;
+}
+
+}  // namespace
+
+extern "C" sf_status sf_key_weights_plan(const sf_attn_desc* desc, const int32_t* seq_lens_host,
+                                         const int32_t* q_lens_host, const int32_t* held_lens_host,
+                                         const int32_t* first_pos_host, const sf_plan_opts* opts, int32_t* work_host,
+                                         uint64_t work_capacity_bytes, sf_weights_info* info) {
+  if (!info) return SF_ERR_INVALID_ARG;
+  int64_t tokens = 0;
+  sf_status st = check_lengths(desc, seq_lens_host, q_lens_host, &tokens);
+  if (st != SF_OK) return st;
+  if (opts && opts->num_cus < 0) return SF_ERR_INVALID_ARG;
+  const int32_t *lens = seq_lens_host, *news = q_lens_host;
+  for (int32_t s = 0; s < desc->num_seqs; ++s) {
+    const int32_t held = held_lens_host ? held_lens_host[s] : lens[s] - news[s];
+    const int32_t pos = first_pos_host ? first_pos_host[s] : held;
+    if (held < 0 || held > lens[s] || pos < 0 || int64_t(pos) + (lens[s] - held) > INT32_MAX) return SF_ERR_INVALID_ARG;
+  }
+  const WeightCut cut =
+      choose_weight_cut(desc, lens, news, opts && opts->num_cus > 0 ? opts->num_cus : kDefaultNumCus);
+  const int32_t hkv = desc->num_kv_heads;
+  int64_t items = 0, merges = 0, slots = 0;
+  for_weight_items(desc, lens, news, cut, [&](int32_t, int32_t, int32_t, int32_t, int32_t parts) {
+    items += int64_t(parts) * hkv;
+    if (parts > 1) merges += hkv, slots += int64_t(parts) * hkv;
+  });
+  if (items + merges > INT32_MAX / kWeightInts) return SF_ERR_INVALID_ARG;
+  info->num_items = int32_t(items);
+  info->num_merge = int32_t(merges);
+  info->num_slots = int32_t(slots);
+  info->item_pages = cut.item_pages;
+  info->num_q_rows = int32_t(tokens);
+  info->reserved = 0;
+  info->work_bytes = uint64_t(items + merges) * kWeightInts * 4;
+  info->workspace_bytes = uint64_t(slots) * cut.item_pages * kPage * 4;
+  info->desc_key = desc_key(desc);
+  if (!work_host) return SF_OK;
+  if (work_capacity_bytes < info->work_bytes) return SF_ERR_CAPACITY;
+  int32_t *item = work_host, *merge = work_host + items * kWeightInts;
+  int32_t slot = 0, last = 0;
+  int64_t qrow = 0;
+  for_weight_items(desc, lens, news, cut, [&](int32_t s, int32_t pb, int32_t pe, int32_t t0, int32_t parts) {
+    for (; last < s; ++last) qrow += news[last];
+    const int32_t held = held_lens_host ? held_lens_host[s] : lens[s] - news[s];
+    const int32_t pos = first_pos_host ? first_pos_host[s] : held;
+    for (int32_t h = 0; h < hkv; ++h) {
+      int32_t row[kWeightInts] = {s, h, pb, pe, 0, 0, -1, lens[s], lens[s] - news[s], int32_t(qrow), held, pos};
+      if (parts > 1) {
+        row[4] = slot;
+        row[5] = parts;
+        std::memcpy(merge, row, sizeof row);
+        merge += kWeightInts;
+      }
+      const int64_t span = news[s] - t0;
+      for (int32_t i = 0; i < parts; ++i) {
+        row[4] = t0 + int32_t(span * i / parts);
+        row[5] = t0 + int32_t(span * (i + 1) / parts);
+        row[6] = parts > 1 ? slot++ : -1;
+        std::memcpy(item, row, sizeof row);
+        item += kWeightInts;
+      }
+    }
+  });
+  return SF_OK;
+}
+
+sf_status sf::weight_args(const sf_attn_desc* desc, const sf_weights_info* info, const int32_t* work_dev, const void* q,
+                          const float* lse, const void* k_pool, const float* k_scale, const int32_t* block_table,
+                          const float* weights, float* weights_out, int32_t* positions, void* workspace,
+                          WeightArgs* args) {
+  if (!work_dev || !q || !lse || !k_pool || !block_table || !weights || !weights_out) return SF_ERR_INVALID_ARG;
+  if (!aligned16(work_dev) || !aligned16(q) || !aligned4(lse) || !aligned16(k_pool) || !aligned4(k_scale) ||
+      !aligned4(block_table) || !aligned16(weights) || !aligned16(weights_out) || !aligned16(positions) ||
+      (info->workspace_bytes && (!workspace || !aligned16(workspace))))
+    return SF_ERR_INVALID_ARG;
+  WeightArgs a = {};
+  a.items = work_dev;
+  a.num_items = info->num_items;
+  a.merge_rows = work_dev + int64_t(info->num_items) * kWeightInts;
+  a.num_merge = info->num_merge;
+  a.q = static_cast<const uint16_t*>(q);
+  a.lse = lse;
+  a.k_pool = static_cast<const uint16_t*>(k_pool);
+  a.k_scale = k_scale;
+  a.block_table = block_table;
+  a.w_in = weights;
+  a.w_out = weights_out;
+  a.positions = positions;
+  a.part = static_cast<float*>(workspace);
+  a.part_keys = info->item_pages * kPage;
+  a.num_q_heads = desc->num_q_heads;
+  a.num_kv_heads = desc->num_kv_heads;
+  a.group = desc->num_q_heads / desc->num_kv_heads;
+  a.inv_group = uint32_t((65536 + a.group - 1) / a.group);
+  a.head_dim = desc->head_dim;
+  a.bt_stride = desc->block_table_stride;
+  a.scale_log2 = float(double(desc->softmax_scale) * 1.4426950408889634074);
+  *args = a;
+  return SF_OK;
+}
+
+extern "C" sf_status sf_key_weights(const sf_attn_desc* desc, const sf_weights_info* info, const int32_t* work_host,
+                                    int32_t* work_dev, const void* q, const float* lse, const void* k_pool,
+                                    const float* k_scale, const int32_t* block_table, const float* weights,
+                                    float* weights_out, int32_t* positions, void* workspace, uint64_t workspace_bytes,
+                                    void* stream) {
+  sf_status st = validate_desc(desc);
+  if (st != SF_OK) return st;
+  if (!info) return SF_ERR_INVALID_ARG;
+  if (info->desc_key != desc_key(desc) || info->num_items < 0 || info->num_merge < 0 || info->num_slots < 0 ||
+      info->reserved != 0 || info->item_pages < kItemPages || info->item_pages > kMaxItemPages ||
+      info->work_bytes != (uint64_t(info->num_items) + info->num_merge) * kWeightInts * 4 ||
+      info->workspace_bytes != uint64_t(info->num_slots) * info->item_pages * kPage * 4)
+    return SF_ERR_PLAN_MISMATCH;
+  if (info->num_items == 0) return SF_OK;
+  WeightArgs a;
+  if ((st = weight_args(desc, info, work_dev, q, lse, k_pool, k_scale, block_table, weights, weights_out, positions,
+                        workspace, &a)) != SF_OK)
+    return st;
+  if (workspace_bytes < info->workspace_bytes) return SF_ERR_CAPACITY;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if (work_host && hipMemcpyAsync(work_dev, work_host, info->work_bytes, hipMemcpyHostToDevice, s) != hipSuccess)
+    return SF_ERR_HIP;
+  return from_hip(launch_key_weights(a, s));
+}
+
+// ---------------------------------------------------------------------------
+// eviction
+// ---------------------------------------------------------------------------
+extern "C" sf_status sf_kv_evict_plan(const sf_attn_desc* desc, const int32_t* seq_lens_host,
+                                      const int32_t* keep_lens_host, const int32_t* ends_host, int32_t sinks,
+                                      int32_t recent, int32_t* work_host, uint64_t work_capacity_bytes,
+                                      sf_evict_info* info) {
+  if (!info) return SF_ERR_INVALID_ARG;
+  sf_status st = validate_desc(desc);
+  if (st != SF_OK) return st;
+  if (sinks < 0 || recent < 0 || (desc->num_seqs > 0 && (!seq_lens_host || !keep_lens_host))) return SF_ERR_INVALID_ARG;
+  const int64_t hkv = desc->num_kv_heads;
+  int64_t pages = 0, tails = 0;
+  for (int32_t s = 0; s < desc->num_seqs; ++s) {
+    const int32_t L = seq_lens_host[s], end = ends_host ? ends_host[s] : L;
+    if (L < 0 || L > kMaxTokens || int64_t(L) > int64_t(kPage) * desc->block_table_stride ||
+        (L > 0 && desc->num_pages == 0) || end < L)
+      return SF_ERR_INVALID_ARG;
+    const int32_t n = std::min(keep_lens_host[s], L);
+    if (n < 0 || n < std::min<int64_t>(L, int64_t(sinks) + recent)) return SF_ERR_INVALID_ARG;
+    pages += pages_of(n);
+    tails += std::min(n, L - n);
+  }
+  const int32_t run = run_of(pages);
+  int64_t moves = 0;
+  bool boundary = false;
+  for (int32_t s = 0; s < desc->num_seqs; ++s) {
+    const int32_t n = std::min(keep_lens_host[s], seq_lens_host[s]);
+    moves += (pages_of(n) + run - 1) / run;
+    boundary = boundary || (n < seq_lens_host[s] && n % kPage != 0);
+  }
+  if (pages * hkv > INT32_MAX / 2 || tails * hkv > INT32_MAX || int64_t(desc->num_seqs) * hkv > INT32_MAX ||
+      desc->num_seqs + moves > INT32_MAX / kItemInts)
+    return SF_ERR_INVALID_ARG;
+  info->num_seqs = desc->num_seqs;
+  info->num_moves = int32_t(moves);
+  info->sinks = sinks;
+  info->recent = recent;
+  info->boundary = boundary ? 1 : 0;
+  info->hole_pages = int32_t(pages * hkv);
+  info->work_bytes = (uint64_t(desc->num_seqs) + uint64_t(moves)) * kItemInts * 4;
+  info->workspace_bytes = align256(uint64_t(pages) * hkv * 8) + uint64_t(tails) * hkv * 4;
+  info->desc_key = desc_key(desc);
+  if (!work_host) return SF_OK;
+  if (work_capacity_bytes < info->work_bytes) return SF_ERR_CAPACITY;
+  int32_t *row = work_host, *move = work_host + int64_t(desc->num_seqs) * kItemInts;
+  int64_t hole = 0, tail = 0;
+  for (int32_t s = 0; s < desc->num_seqs; ++s) {
+    const int32_t L = seq_lens_host[s], n = std::min(keep_lens_host[s], L), np = pages_of(n);
+    put_row(row, L, n, int32_t(hole), int32_t(tail), ends_host ? ends_host[s] : L, 0);
+    hole += np * hkv;
+    tail += std::min(n, L - n) * hkv;
+    for (int32_t p = 0; p < np; p += run) put_row(move, s, p, std::min(run, np - p), 0, 0, 0);
+  }
+  return SF_OK;
+}
+
+sf_status sf::evict_args(const sf_attn_desc* desc, const sf_evict_info* info, const int32_t* work_dev, void* k_pool,
+                         void* v_pool, float* k_scale, float* v_scale, const int32_t* block_table, const float* weights,
+                         const int32_t* positions, float* weights_out, int32_t* positions_out, void* workspace,
+                         EvictArgs* args) {
+  if ((k_scale == nullptr) != (v_scale == nullptr)) return SF_ERR_INVALID_ARG;
+  if (!work_dev || !k_pool || !v_pool || !block_table || !weights || !positions || !weights_out || !positions_out ||
+      !workspace)
+    return SF_ERR_INVALID_ARG;
+  if (!aligned16(work_dev) || !aligned16(k_pool) || !aligned16(v_pool) || !aligned4(k_scale) || !aligned4(v_scale) ||
+      !aligned4(block_table) || !aligned16(weights) || !aligned16(positions) || !aligned16(weights_out) ||
+      !aligned16(positions_out) || !aligned16(workspace))
+    return SF_ERR_INVALID_ARG;
+  EvictArgs a = {};
+  a.rows = work_dev;
+  a.num_seqs = info->num_seqs;
+  a.num_moves = info->num_moves;
+  a.boundary = info->boundary != 0;
+  a.k_pool = k_pool;
+  a.v_pool = v_pool;
+  a.k_scale = k_scale;
+  a.v_scale = v_scale;
+  a.block_table = block_table;
+  a.w_in = weights;
+  a.pos_in = positions;
+  a.w_out = weights_out;
+  a.pos_out = positions_out;
+  a.holes = static_cast<uint32_t*>(workspace);
+  a.tails = reinterpret_cast<int32_t*>(static_cast<char*>(workspace) + align256(uint64_t(info->hole_pages) * 8));
+  a.sinks = info->sinks;
+  a.recent = info->recent;
+  a.num_kv_heads = desc->num_kv_heads;
+  a.head_dim = desc->head_dim;
+  a.bt_stride = desc->block_table_stride;
+  *args = a;
+  return SF_OK;
+}
+
+extern "C" sf_status sf_kv_evict(const sf_attn_desc* desc, const sf_evict_info* info, const int32_t* work_host,
+                                 int32_t* work_dev, void* k_pool, void* v_pool, float* k_scale, float* v_scale,
+                                 const int32_t* block_table, const float* weights, const int32_t* positions,
+                                 float* weights_out, int32_t* positions_out, void* workspace, uint64_t workspace_bytes,
+                                 void* stream) {
+  sf_status st = validate_desc(desc);
+  if (st != SF_OK) return st;
+  if (!info) return SF_ERR_INVALID_ARG;
+  if (info->desc_key != desc_key(desc) || info->num_seqs != desc->num_seqs || info->num_moves < 0 || info->sinks < 0 ||
+      info->recent < 0 || info->hole_pages < 0 ||
+      info->work_bytes != (uint64_t(info->num_seqs) + uint64_t(info->num_moves)) * kItemInts * 4 ||
+      info->workspace_bytes < align256(uint64_t(info->hole_pages) * 8))
+    return SF_ERR_PLAN_MISMATCH;
+  if (info->num_moves == 0) return SF_OK;
+  EvictArgs a;
+  if ((st = evict_args(desc, info, work_dev, k_pool, v_pool, k_scale, v_scale, block_table, weights, positions,
+                       weights_out, positions_out, workspace, &a)) != SF_OK)
+    return st;
+  if (workspace_bytes < info->workspace_bytes) return SF_ERR_CAPACITY;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if (work_host && hipMemcpyAsync(work_dev, work_host, info->work_bytes, hipMemcpyHostToDevice, s) != hipSuccess)
+    return SF_ERR_HIP;
+  return from_hip(launch_evict(a, s));
+}

@@ -29,9 +29,19 @@ struct Item {
   int32_t seq, kvh, t0, nt, prefix, qrow0, steps;
 };
 
-// Checks the lengths and counts the query rows.
-sf_status check_lengths(const sf_attn_desc* desc, const int32_t* seq_lens_host, const int32_t* q_lens_host,
-                        int64_t* rows) {
+void fill_info(const sf_attn_desc* desc, int64_t items, int64_t rows, sf_extend_info* info) {
+  info->num_items = int32_t(items);
+  info->tokens_per_item = kExtendRows / (desc->num_q_heads / desc->num_kv_heads);
+  info->num_q_rows = int32_t(rows);
+  info->reserved = 0;
+  info->work_bytes = uint64_t(items) * kItemInts * 4;
+  info->desc_key = desc_key(desc);
+}
+
+}  // namespace
+
+sf_status sf::check_extend_lengths(const sf_attn_desc* desc, const int32_t* seq_lens_host, const int32_t* q_lens_host,
+                                   int64_t* rows) {
   sf_status st = validate_desc(desc);
   if (st != SF_OK) return st;
   if (desc->num_seqs > 0 && (!seq_lens_host || !q_lens_host)) return SF_ERR_INVALID_ARG;
@@ -46,17 +56,6 @@ sf_status check_lengths(const sf_attn_desc* desc, const int32_t* seq_lens_host, 
   return SF_OK;
 }
 
-void fill_info(const sf_attn_desc* desc, int64_t items, int64_t rows, sf_extend_info* info) {
-  info->num_items = int32_t(items);
-  info->tokens_per_item = kExtendRows / (desc->num_q_heads / desc->num_kv_heads);
-  info->num_q_rows = int32_t(rows);
-  info->reserved = 0;
-  info->work_bytes = uint64_t(items) * kItemInts * 4;
-  info->desc_key = desc_key(desc);
-}
-
-}  // namespace
-
 extern "C" sf_status sf_extend_attn_plan(const sf_attn_desc* desc, const int32_t* seq_lens_host,
                                          const int32_t* q_lens_host, int32_t* work_host,
                                          uint64_t work_capacity_bytes, sf_extend_info* info) {
@@ -64,7 +63,7 @@ extern "C" sf_status sf_extend_attn_plan(const sf_attn_desc* desc, const int32_t
   sf_status st = validate_desc(desc);
   if (st != SF_OK) return st;
   if (!info) return SF_ERR_INVALID_ARG;
-  if ((st = check_lengths(desc, seq_lens_host, q_lens_host, &rows)) != SF_OK) return st;
+  if ((st = check_extend_lengths(desc, seq_lens_host, q_lens_host, &rows)) != SF_OK) return st;
   const int32_t per_item = kExtendRows / (desc->num_q_heads / desc->num_kv_heads);
 
   std::vector<Item> items;
@@ -268,7 +267,7 @@ sf_status sf::extend_plan_parts(const sf_attn_desc* desc, const int32_t* seq_len
                                 int32_t num_cus, bool store, int32_t* work, uint64_t capacity, ExtendPlan* plan,
                                 sf_extend_info* info) {
   int64_t q_rows = 0;
-  sf_status st = check_lengths(desc, seq_lens_host, q_lens_host, &q_rows);
+  sf_status st = check_extend_lengths(desc, seq_lens_host, q_lens_host, &q_rows);
   if (st != SF_OK) return st;
   const int32_t g = desc->num_q_heads / desc->num_kv_heads, hkv = desc->num_kv_heads;
   const int32_t *lens = seq_lens_host, *news = q_lens_host;

@@ -1,0 +1,405 @@
+// Eviction from a paged cache by accumulated attention weight.
+//
+// Each (sequence, KV head) keeps n of its L cached keys. Softmax attention does
+// not depend on the order of its keys (their positions are in the keys), so
+// nothing is compacted: a kept key in the first n slots stays where it is, and
+// the i-th kept key behind them moves into the i-th freed slot. That moves at
+// most min(n, L - n) tokens, for a cache that gives up a page at a time 16 of
+// n, where keeping the order would move nearly all of them; and in an 8-bit
+// cache a token is rounded again only when it moves. The positions array keeps
+// what the slot no longer says.
+//
+// Launch 1, one workgroup per (sequence, KV head), a thread per page: the n-th
+// largest key of (weight, lowest slot first) by four passes of 8 bits over the
+// weights' order-preserving integers, then for every page of the first n slots
+// the freed slots' mask and number, and the list of kept slots behind. Bound by
+// latency: the weights and positions come from L2 after the first pass.
+// Launch 2, a wave per (page, KV head, keys or values) of the first n slots:
+// gathers its page's new tokens. Bound by memory; a bf16 value tile is
+// dim-major, so a token's values are 2 bytes of D 32-byte rows, and a page with
+// one freed slot reads and writes its whole tile.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "fp8_tile.h"
+#include "sf_internal.h"
+
+namespace sf {
+namespace {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(4))) const int32_t* const_i32_ptr;
+__device__ __forceinline__ const_i32_ptr as_constant(const int32_t* p) { return (const_i32_ptr)(p); }
+
+// Sequence row of the work list: L, n, first page of the moves' masks, first
+// entry of the moves' sources (both per KV head 0), end (next position), 0 ..
+constexpr int kRowInts = kItemInts;
+
+template <int kThreads>
+struct BlockScan {
+  int32_t wave_sum[kThreads / 64];
+};
+
+// Exclusive prefix sum of x over the workgroup's threads, and the total.
+template <int kThreads>
+__device__ __forceinline__ int block_scan(int x, BlockScan<kThreads>& lds, int& total) {
+  const int lane = int(threadIdx.x) & 63;
+  const int wave = int(threadIdx.x) >> 6;
+  int incl = x;
+#pragma unroll
+  for (int off = 1; off < 64; off <<= 1) {
+    const int y = __shfl_up(incl, off);
+    if (lane >= off) incl += y;
+  }
+  __syncthreads();   // the sums of the scan before have been read
+  if (lane == 63) lds.wave_sum[wave] = incl;
+  __syncthreads();
+  int before = 0;
+  total = 0;
+#pragma unroll
+  for (int w = 0; w < kThreads / 64; ++w) {
+    if (w < wave) before += lds.wave_sum[w];
+    total += lds.wave_sum[w];
+  }
+  return before + incl - x;
+}
+
+// Integers in the order of the weights: a protected position above all, NaN below all.
+__device__ __forceinline__ uint32_t rank_key(float w, int pos, int sinks, int recent_from) {
+  if (pos < sinks || pos >= recent_from) return 0xFFFFFFFFu;
+  if (w != w) return 0u;
+  const uint32_t b = __builtin_bit_cast(uint32_t, w + 0.f);   // -0 is 0
+  return b & 0x80000000u ? ~b : b | 0x80000000u;
+}
+
+template <int kThreads>
+__global__ __launch_bounds__(kThreads) void evict_select_kernel(EvictArgs a) {
+  __shared__ int32_t hist[256];
+  __shared__ int32_t found[2];
+  __shared__ BlockScan<kThreads> scan;
+  const int seq = int(blockIdx.x) / a.num_kv_heads;
+  const int kvh = int(blockIdx.x) % a.num_kv_heads;
+  const const_i32_ptr row = as_constant(a.rows) + size_t(seq) * kRowInts;
+  const int len = row[0];
+  const int n = row[1];
+  if (n == 0) return;
+  const int keep_pages = (n + kPage - 1) / kPage;
+  uint32_t* holes = a.holes + 2 * (size_t(row[2]) + size_t(kvh) * keep_pages);
+  const int tid = int(threadIdx.x);
+  if (n == len) {   // nothing to give up
+    for (int p = tid; p < keep_pages; p += kThreads) holes[2 * p] = holes[2 * p + 1] = 0;
+    return;
+  }
+  int32_t* tails = a.tails + size_t(row[3]) + size_t(kvh) * min(n, len - n);
+  const int recent_from = a.recent > 0 ? row[4] - a.recent : INT32_MAX;
+  const int pages = (len + kPage - 1) / kPage;
+  const const_i32_ptr bt = as_constant(a.block_table) + size_t(seq) * a.bt_stride;
+
+  // The 16 keys of page p (0 past the end of the sequence: counted nowhere).
+  auto load = [&](int p, uint32_t* key) {
+    const size_t at = (size_t(bt[p]) * a.num_kv_heads + kvh) * kPage;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const f32x4 w = *reinterpret_cast<const f32x4*>(a.w_in + at + 4 * q);
+      const i32x4 pos = *reinterpret_cast<const i32x4*>(a.pos_in + at + 4 * q);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) key[4 * q + e] = rank_key(w[e], pos[e], a.sinks, recent_from);
+    }
+  };
+  uint32_t cached[kPage];   // of this thread's first page
+  if (tid < pages) load(tid, cached);
+
+  // The n-th largest key, 8 bits at a time from the top.
+  uint32_t prefix = 0;
+  int want = n;   // keys still to be found among those with this prefix
+  for (int shift = 24; shift >= 0; shift -= 8) {
+    for (int i = tid; i < 256; i += kThreads) hist[i] = 0;
+    __syncthreads();
+    for (int p = tid; p < pages; p += kThreads) {
+      uint32_t key[kPage];
+      if (p == tid) {
+#pragma unroll
+        for (int j = 0; j < kPage; ++j) key[j] = cached[j];
+      } else {
+        load(p, key);
+      }
+      const int valid = min(len - p * kPage, kPage);
+#pragma unroll
+      for (int j = 0; j < kPage; ++j)
+        if (j < valid && (shift == 24 || (key[j] >> ((shift + 8) & 31)) == (prefix >> ((shift + 8) & 31))))
+          atomicAdd(&hist[(key[j] >> shift) & 255u], 1);
+    }
+    __syncthreads();
+    // keys with a larger digit than d, by a scan from the top
+    if (tid < 64) {
+      int four[4], sum = 0;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) sum += four[q] = hist[255 - (4 * tid + q)];
+      int incl = sum;
+#pragma unroll
+      for (int off = 1; off < 64; off <<= 1) {
+        const int y = __shfl_up(incl, off);
+        if (tid >= off) incl += y;
+      }
+      int above = incl - sum;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        if (above < want && above + four[q] >= want) {   // exactly one digit
+          found[0] = 255 - (4 * tid + q);
+          found[1] = above;
+        }
+        above += four[q];
+      }
+    }
+    __syncthreads();
+    prefix |= uint32_t(found[0]) << shift;
+    want -= found[1];
+    __syncthreads();   // before `found` and `hist` are written again
+  }
+
+  // Keys above the threshold stay, and the first `want` equal ones.
+  int equal_before = 0, hole_before = 0, tail_before = 0;
+  for (int base = 0; base < pages; base += kThreads) {
+    const int p = base + tid;
+    uint32_t key[kPage];
+    int valid = 0;
+    if (p < pages) {
+      if (base == 0) {
+#pragma unroll
+        for (int j = 0; j < kPage; ++j) key[j] = cached[j];
+      } else {
+        load(p, key);
+      }
+      valid = min(len - p * kPage, kPage);
+    }
+    uint32_t above = 0, equal = 0;
+#pragma unroll
+    for (int j = 0; j < kPage; ++j) {
+      if (j >= valid) break;
+      above |= uint32_t(key[j] > prefix) << j;
+      equal |= uint32_t(key[j] == prefix) << j;
+    }
+    int total;
+    int rank = equal_before + block_scan<kThreads>(__popc(equal), scan, total);
+    equal_before += total;
+    uint32_t kept = above;
+    for (uint32_t m = equal; m != 0; m &= m - 1, ++rank)
+      if (rank < want) kept |= m & (0u - m);
+    const uint32_t all = (1u << valid) - 1u;
+    const int front = min(max(n - p * kPage, 0), valid);   // slots of this page among the first n
+    const uint32_t front_mask = (1u << front) - 1u;
+    const uint32_t hole = all & front_mask & ~kept;
+    uint32_t tail = kept & ~front_mask;
+    const int hole_at = hole_before + block_scan<kThreads>(__popc(hole), scan, total);
+    hole_before += total;
+    int tail_at = tail_before + block_scan<kThreads>(__popc(tail), scan, total);
+    tail_before += total;
+    if (p < keep_pages) {
+      holes[2 * p] = hole;
+      holes[2 * p + 1] = uint32_t(hole_at);
+    }
+    for (; tail != 0; tail &= tail - 1) tails[tail_at++] = p * kPage + __ffs(tail) - 1;
+  }
+}
+
+constexpr int kMoveWaves = 4;
+
+// kPhase of an fp8 cache: the page that holds slot n keeps both freed slots and
+// sources of other pages' moves, which must read its codes by the scale that
+// they have; it is left to a launch of its own behind the others (kBoundary).
+template <int D, bool kFp8, bool kBoundary>
+__global__ __launch_bounds__(64 * kMoveWaves) void evict_move_kernel(EvictArgs a) {
+  constexpr int kPieces = D / 64;
+  const int lane = int(threadIdx.x) & 63;
+  const int col = lane & 15;
+  const int grp = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
+  const int hkv = a.num_kv_heads;
+  int seq, pb, np;
+  if constexpr (kBoundary) {
+    seq = int(blockIdx.x);
+    pb = 0;
+    np = 1;
+  } else {
+    const const_i32_ptr item = as_constant(a.rows) + (size_t(a.num_seqs) + blockIdx.x) * kRowInts;
+    seq = item[0];
+    pb = item[1];
+    np = item[2];
+  }
+  const const_i32_ptr row = as_constant(a.rows) + size_t(seq) * kRowInts;
+  const int len = row[0];
+  const int n = row[1];
+  if constexpr (kBoundary) {
+    if (n % kPage == 0 || n == len) return;
+    pb = n / kPage;
+  }
+  const int keep_pages = (n + kPage - 1) / kPage;
+  const const_i32_ptr bt = as_constant(a.block_table) + size_t(seq) * a.bt_stride;
+  const int moves = min(n, len - n);
+  for (int i = int(blockIdx.y) * kMoveWaves + wave; i < np * hkv * 2; i += int(gridDim.y) * kMoveWaves) {
+    const int pg = pb + i / (2 * hkv);
+    const int rem = i % (2 * hkv);
+    const bool is_v = rem >= hkv;
+    const int kvh = is_v ? rem - hkv : rem;
+    if (kFp8 && !kBoundary && n < len && (pg + 1) * kPage > n) continue;
+    const const_i32_ptr hole = (const_i32_ptr)(a.holes) + 2 * (size_t(row[2]) + size_t(kvh) * keep_pages + pg);
+    const uint32_t mask = uint32_t(hole[0]);
+    if (mask == 0 && (is_v || a.w_out == a.w_in) && (is_v || a.pos_out == a.pos_in)) continue;
+    const int32_t* tails = a.tails + size_t(row[3]) + size_t(kvh) * moves + hole[1];
+    const int page = bt[pg];
+    const size_t dst_tile = size_t(page) * hkv + kvh;
+    // Lane t (every 16 lanes alike): where the token of slot t comes from.
+    const bool moved = (mask >> col) & 1u;
+    int src = 0;
+    if (moved) src = tails[__popc(mask & ((1u << col) - 1u))];
+    const int src_page = moved ? a.block_table[size_t(seq) * a.bt_stride + src / kPage] : page;
+    const int src_slot = moved ? src % kPage : col;
+    const size_t src_tile = size_t(src_page) * hkv + kvh;
+    if (!is_v && lane < kPage && pg * kPage + lane < n) {
+      const size_t from = src_tile * kPage + src_slot, to = dst_tile * kPage + lane;
+      const float w = a.w_in[from];
+      const int32_t pos = a.pos_in[from];
+      a.w_out[to] = w;
+      a.pos_out[to] = pos;
+    }
+    if (mask == 0) continue;
+    if constexpr (kFp8) {
+      uint8_t* pool = static_cast<uint8_t*>(is_v ? a.v_pool : a.k_pool);
+      float* scales = is_v ? a.v_scale : a.k_scale;
+      uint8_t* dst = pool + dst_tile * (kPage * D);
+      tile_u32x4 codes[kPieces];
+      float x[kPieces][16];
+#pragma unroll
+      for (int p = 0; p < kPieces; ++p) {
+        codes[p] = *reinterpret_cast<const tile_u32x4*>(dst + 1024 * p + 16 * lane);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) x[p][e] = 0.f;
+      }
+      const float old_scale = scales[dst_tile];
+      if (!is_v) {
+        if (moved) {
+          const float s = scales[src_tile];
+          const uint8_t* from = pool + src_tile * (kPage * D) + (grp * kPage + src_slot) * 16;
+#pragma unroll
+          for (int p = 0; p < kPieces; ++p) {
+            const tile_u32x4 w = *reinterpret_cast<const tile_u32x4*>(from + 1024 * p);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) x[p][e] = fp8_value(w[e >> 2], e & 3) * s;
+          }
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int t = 4 * grp + e;
+          const int from_slot = __shfl(src_slot, t);
+          const int from_page = __shfl(src_page, t);
+          if (!((mask >> t) & 1u)) continue;
+          const size_t tile = size_t(from_page) * hkv + kvh;
+          const float s = scales[tile];
+          const uint8_t* from = pool + tile * (kPage * D) + ((from_slot >> 2) * kPage + col) * 16;
+          const int shift = 8 * (from_slot & 3);
+#pragma unroll
+          for (int p = 0; p < kPieces; ++p) {
+            const tile_u32x4 w = *reinterpret_cast<const tile_u32x4*>(from + 1024 * p);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[p][4 * j + e] = fp8_value(w[j] >> shift, 0) * s;
+          }
+        }
+      }
+      const uint32_t live = (1u << min(len - pg * kPage, kPage)) - 1u;
+      const uint32_t keep = fp8_slot_bytes(live & ~mask, is_v, lane);
+#pragma unroll
+      for (int p = 0; p < kPieces; ++p)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) codes[p][j] &= keep;
+      fp8_store_tile<D>(codes, x, fp8_slot_bytes(mask, is_v, lane), old_scale, dst, scales + dst_tile, lane);
+    } else if (!is_v) {
+      // keys: 16-byte pieces of 8 dims, four tokens at a time
+      constexpr int kKeyPieces = D / 8;
+      uint16_t* pool = static_cast<uint16_t*>(a.k_pool);
+      u32x4 v[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int t = 4 * j + grp;
+        const int from_slot = __shfl(src_slot, t);
+        const int from_page = __shfl(src_page, t);
+        if (((mask >> t) & 1u) && col < kKeyPieces)
+          v[j] = *reinterpret_cast<const u32x4*>(pool + (size_t(from_page) * hkv + kvh) * (kPage * D) +
+                                                 (col * kPage + from_slot) * 8);
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int t = 4 * j + grp;
+        if (((mask >> t) & 1u) && col < kKeyPieces)
+          *reinterpret_cast<u32x4*>(pool + dst_tile * (kPage * D) + (col * kPage + t) * 8) = v[j];
+      }
+    } else {
+      // values: a lane takes whole dims (32-byte rows of 16 slots)
+      uint16_t* pool = static_cast<uint16_t*>(a.v_pool);
+      uint16_t* dst = pool + dst_tile * (kPage * D) + lane * kPage;
+      uint32_t word[kPieces][8];
+      uint32_t fresh[kPieces][16];
+#pragma unroll
+      for (int t = 0; t < kPage; ++t) {
+        if (!((mask >> t) & 1u)) continue;   // wave-uniform
+        const int from_slot = __builtin_amdgcn_readlane(src_slot, t);
+        const int from_page = __builtin_amdgcn_readlane(src_page, t);
+        const uint16_t* from = pool + (size_t(from_page) * hkv + kvh) * (kPage * D) + lane * kPage + from_slot;
+#pragma unroll
+        for (int p = 0; p < kPieces; ++p) fresh[p][t] = from[64 * p * kPage];
+      }
+#pragma unroll
+      for (int p = 0; p < kPieces; ++p)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const u32x4 w = *reinterpret_cast<const u32x4*>(dst + 64 * p * kPage + 8 * h);
+#pragma unroll
+          for (int q = 0; q < 4; ++q) word[p][4 * h + q] = w[q];
+        }
+#pragma unroll
+      for (int t = 0; t < kPage; ++t) {
+        if (!((mask >> t) & 1u)) continue;
+#pragma unroll
+        for (int p = 0; p < kPieces; ++p) {
+          uint32_t& w = word[p][t >> 1];
+          w = t & 1 ? (w & 0xFFFFu) | (fresh[p][t] << 16) : (w & 0xFFFF0000u) | fresh[p][t];
+        }
+      }
+#pragma unroll
+      for (int p = 0; p < kPieces; ++p)
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+          *reinterpret_cast<u32x4*>(dst + 64 * p * kPage + 8 * h) =
+              u32x4{word[p][4 * h], word[p][4 * h + 1], word[p][4 * h + 2], word[p][4 * h + 3]};
+    }
+  }
+}
+
+template <int D, bool kFp8>
+hipError_t launch_moves(const EvictArgs& a, hipStream_t stream) {
+  const int groups = (2 * a.num_kv_heads + kMoveWaves - 1) / kMoveWaves;
+  const int gy = groups < 65535 ? groups : 65535;
+  if (a.num_moves > 0) {
+    hipLaunchKernelGGL((evict_move_kernel<D, kFp8, false>), dim3(a.num_moves, gy), dim3(64 * kMoveWaves), 0, stream, a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  if (!kFp8 || !a.boundary) return hipSuccess;
+  hipLaunchKernelGGL((evict_move_kernel<D, kFp8, true>), dim3(a.num_seqs, gy), dim3(64 * kMoveWaves), 0, stream, a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_evict(const EvictArgs& a, hipStream_t stream) {
+  if (a.num_moves == 0) return hipSuccess;
+  hipLaunchKernelGGL(evict_select_kernel<256>, dim3(a.num_seqs * a.num_kv_heads), dim3(256), 0, stream, a);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  if (a.k_scale) return a.head_dim == 128 ? launch_moves<128, true>(a, stream) : launch_moves<64, true>(a, stream);
+  return a.head_dim == 128 ? launch_moves<128, false>(a, stream) : launch_moves<64, false>(a, stream);
+}
+
+}  // namespace sf

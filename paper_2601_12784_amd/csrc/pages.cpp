@@ -139,6 +139,30 @@ extern "C" sf_status sf_page_table_step(sf_page_pool* pool, int32_t* block_table
   return SF_OK;
 }
 
+extern "C" sf_status sf_page_table_truncate(sf_page_pool* pool, int32_t* block_table, int32_t stride,
+                                            int32_t num_seqs, const int32_t* lens, const int32_t* keep) {
+  if (!pool || !block_table || stride < 1 || num_seqs < 0) return SF_ERR_INVALID_ARG;
+  if (num_seqs > 0 && (!lens || !keep)) return SF_ERR_INVALID_ARG;
+  const int64_t max_len = int64_t(stride) * kPage;
+  auto pages_of = [](int32_t tokens) { return int32_t((int64_t(tokens) + kPage - 1) / kPage); };
+  thread_local std::vector<int32_t> gone;
+  gone.clear();
+  for (int32_t s = 0; s < num_seqs; ++s)
+    if (keep[s] < 0 || keep[s] > lens[s] || lens[s] > max_len) return SF_ERR_INVALID_ARG;
+  try {
+    for (int32_t s = 0; s < num_seqs; ++s)
+      for (int32_t j = pages_of(keep[s]); j < pages_of(lens[s]); ++j)
+        gone.push_back(block_table[int64_t(s) * stride + j]);
+  } catch (...) {
+    return SF_ERR_CAPACITY;
+  }
+  const sf_status st = sf_page_pool_release(pool, gone.data(), int32_t(gone.size()));
+  if (st != SF_OK) return st;
+  for (int32_t s = 0; s < num_seqs; ++s)
+    for (int32_t j = pages_of(keep[s]); j < pages_of(lens[s]); ++j) block_table[int64_t(s) * stride + j] = -1;
+  return SF_OK;
+}
+
 extern "C" sf_status sf_check_block_table(const sf_attn_desc* desc, const int32_t* block_table_host,
                                           const int32_t* seq_lens_host, int32_t* bad_seq) {
   if (bad_seq) *bad_seq = -1;

@@ -665,7 +665,8 @@ sf::ReserveBytes sf::reserve_bytes(const sf_attn_desc* shape, const sf_plan_opts
   auto plan = [&](int64_t workers, int64_t segments, int64_t cut_segments, int64_t cut, bool appending) {
     partials = std::max(partials, cut_segments);
     rows = std::max(rows, workers + segments + cut);
-    if (appending) append_rows = std::max(append_rows, workers + 2 * segments + cut);
+    // over an fp8 cache: a store row per sequence
+    append_rows = std::max(append_rows, workers + segments + cut + (appending ? segments : int64_t(num_seqs)));
   };
   const bool known = total_pages >= 0;
   auto slices = [&](int64_t w, int64_t least, bool appending) {

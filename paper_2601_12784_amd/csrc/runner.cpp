@@ -175,6 +175,83 @@ sf_status grow_device(sf_runner* r, void** ptr, uint64_t* have, uint64_t bytes, 
   return SF_OK;
 }
 
+bool same_shape(const sf_runner* r, const sf_attn_desc* desc) {
+  return desc->num_q_heads == r->shape.num_q_heads && desc->num_kv_heads == r->shape.num_kv_heads &&
+         desc->head_dim == r->shape.head_dim && desc->page_size == r->shape.page_size;
+}
+
+// Takes the next ring slot for a call on `main`: after the step that last read
+// it has ended. A mark stands for steps of one stream: a new stream closes the run.
+sf_status open_slot(sf_runner* r, hipStream_t main, Pinned** slot) {
+  Pinned& pin = r->ring[r->steps % kRing];
+  sf_status st = pin.used ? wait_step(r, pin.last_step) : SF_OK;
+  if (st != SF_OK) return st;
+  pin.used = false;
+  if (r->unmarked < r->steps && main != r->last_stream && (st = mark_steps(r)) != SF_OK) return st;
+  *slot = &pin;
+  return SF_OK;
+}
+
+// Counts a call whose launches may have been enqueued and read the slot, with
+// what they returned.
+sf_status close_slot(sf_runner* r, hipStream_t main, Pinned& pin, sf_status st) {
+  pin.used = true;
+  pin.last_step = r->steps;
+  r->last_stream = main;
+  ++r->steps;
+  if (r->steps - r->unmarked >= kMarkEvery && mark_steps(r) != SF_OK) {
+    // Without the mark nothing orders a later rewrite of these slots after
+    // the steps' reads: wait for the stream instead.
+    (void)hipStreamSynchronize(main);
+    for (auto& p : r->ring) p.used = false;
+    r->unmarked = r->steps;
+    if (st == SF_OK) st = SF_ERR_HIP;
+  }
+  return st;
+}
+
+// Slots are reused by waiting on the host, which a graph's replays would not.
+sf_status not_capturing(hipStream_t main) {
+  hipStreamCaptureStatus capturing = hipStreamCaptureStatusNone;
+  if (hipStreamIsCapturing(main, &capturing) != hipSuccess) return SF_ERR_HIP;
+  return capturing == hipStreamCaptureStatusNone ? SF_OK : SF_ERR_UNSUPPORTED;
+}
+
+// Makes the runner's device current for a call, and the caller's again after it.
+struct OnDevice {
+  int before = -1;
+  sf_status st = SF_OK;
+  explicit OnDevice(int device) {
+    int now = device;
+    if (hipGetDevice(&now) != hipSuccess || (now != device && hipSetDevice(device) != hipSuccess)) st = SF_ERR_HIP;
+    if (st == SF_OK && now != device) before = now;
+  }
+  ~OnDevice() {
+    if (before >= 0) (void)hipSetDevice(before);
+  }
+};
+
+// A call of a runner besides its steps: plan(work, capacity) into the next slot
+// (grown and planned again if it is too small; bytes() afterwards are what the
+// slot must hold), `workspace` bytes, then launch(slot as the kernels address it).
+template <class Plan, class Bytes, class Workspace, class Launch>
+sf_status run_in_slot(sf_runner* r, hipStream_t main, Plan plan, Bytes bytes, Workspace workspace, Launch launch) {
+  const OnDevice on(r->device);
+  if (on.st != SF_OK) return on.st;
+  sf_status st = not_capturing(main);
+  Pinned* pin = nullptr;
+  if (st != SF_OK || (st = open_slot(r, main, &pin)) != SF_OK) return st;
+  st = plan(pin->ptr, pin->bytes);
+  if (st == SF_ERR_CAPACITY || (st == SF_OK && pin->bytes < bytes())) {
+    if ((st = grow_pinned(*pin, bytes())) != SF_OK) return st;
+    st = plan(pin->ptr, pin->bytes);
+  }
+  if (st != SF_OK) return st;
+  if (bytes() == 0) return SF_OK;
+  if ((st = grow_device(r, &r->workspace, &r->workspace_bytes, workspace(), main)) != SF_OK) return st;
+  return close_slot(r, main, *pin, launch(pin->ptr, pin->dev));
+}
+
 // Waits for the device where calls have no event.
 sf_status wait_unmarked(Lent& l) {
   if (l.unmarked == 0) return SF_OK;
@@ -270,33 +347,32 @@ extern "C" sf_status sf_runner_step(sf_runner* r, const sf_attn_desc* desc, cons
                                     const int32_t* block_table, float* out, float* lse,
                                     const sf_runner_extras* extras, void* stream, sf_plan_info* info_out) {
   if (!r || !desc || (desc->num_seqs > 0 && !seq_lens_host)) return SF_ERR_INVALID_ARG;
-  if (desc->num_q_heads != r->shape.num_q_heads || desc->num_kv_heads != r->shape.num_kv_heads ||
-      desc->head_dim != r->shape.head_dim || desc->page_size != r->shape.page_size)
-    return SF_ERR_INVALID_ARG;
-  const bool append = extras && extras->k_new;
+  if (!same_shape(r, desc)) return SF_ERR_INVALID_ARG;
   const bool fp8 = extras && extras->k_scale;
-  if (extras && (append && fp8)) return SF_ERR_INVALID_ARG;
+  const bool store = fp8 && extras->k_new;   // an appending step over an fp8 cache: stored, then attended
+  const bool append = extras && extras->k_new && !store;
   if (append && !lse) return SF_ERR_INVALID_ARG;
   hipStream_t main = static_cast<hipStream_t>(stream);
 
   // 1. plan into the next ring slot (after the step that last read it has
   //    ended); grow it and plan again only if the plan does not fit
-  Pinned& pin = r->ring[r->steps % kRing];
-  sf_status st = pin.used ? wait_step(r, pin.last_step) : SF_OK;
+  Pinned* slot = nullptr;
+  sf_status st = open_slot(r, main, &slot);
   if (st != SF_OK) return st;
-  pin.used = false;
-  // A mark stands for steps of one stream: a new stream closes the run.
-  if (r->unmarked < r->steps && main != r->last_stream && (st = mark_steps(r)) != SF_OK) return st;
+  Pinned& pin = *slot;
   // Appending: after the work list, copies of the rows the merge launch acts
   // on (pairs with one segment and len > 0, at most one per item), then
   // new_pages. The work list ends with the combine rows, so the merge
   // launch's rows are one contiguous range, which the attention launch
-  // copies to device memory (RowCopy).
-  const uint64_t pages_bytes = append ? (uint64_t(desc->num_seqs) * 4 + 31) / 32 * 32 : 0;
+  // copies to device memory (RowCopy). Over an fp8 cache: the rows of the
+  // store launch (one per sequence with a token), then new_pages.
+  const uint64_t pages_bytes = append || store ? (uint64_t(desc->num_seqs) * 4 + 31) / 32 * 32 : 0;
   sf_plan_info info;
   const sf::StepKind kind = fp8 ? sf::StepKind::kFp8 : append ? sf::StepKind::kAppend : sf::StepKind::kPlain;
   st = sf::decode_plan_runner(desc, seq_lens_host, &r->opts, kind, pin.ptr, pin.bytes, &info);
-  auto need = [&]() { return info.work_bytes + (append ? uint64_t(info.num_work) * 32 + pages_bytes : 0); };
+  auto need = [&]() {
+    return info.work_bytes + pages_bytes + (append ? uint64_t(info.num_work) : store ? uint64_t(desc->num_seqs) : 0) * 32;
+  };
   if (st == SF_ERR_CAPACITY || (st == SF_OK && pin.bytes < need())) {
     if ((st = grow_pinned(pin, need())) != SF_OK) return st;
     st = sf::decode_plan_runner(desc, seq_lens_host, &r->opts, kind, pin.ptr, pin.bytes, &info);
@@ -319,9 +395,35 @@ extern "C" sf_status sf_runner_step(sf_runner* r, const sf_attn_desc* desc, cons
     pages_off = info.work_bytes + uint64_t(num_single) * 32;
     std::memcpy(base + pages_off, extras->new_pages_host, uint64_t(desc->num_seqs) * 4);
   }
+  int32_t num_store = 0;
+  if (store && desc->num_seqs > 0) {
+    if (!extras->new_pages_host) return SF_ERR_INVALID_ARG;
+    char* base = reinterpret_cast<char*>(pin.ptr);
+    int32_t* row = reinterpret_cast<int32_t*>(base + info.work_bytes);
+    for (int32_t s = 0; s < desc->num_seqs; ++s) {
+      const int32_t L = seq_lens_host[s];
+      if (L <= 0) continue;
+      const int32_t r8[sf::kItemInts] = {s, (L - 1) / sf::kPage, 1, L - 1, L, s, 0, 0};
+      std::memcpy(row + int64_t(num_store++) * sf::kItemInts, r8, sizeof r8);
+    }
+    pages_off = info.work_bytes + uint64_t(num_store) * 32;
+    std::memcpy(base + pages_off, extras->new_pages_host, uint64_t(desc->num_seqs) * 4);
+  }
   if (info_out) *info_out = info;
   r->last = info;
   if (info.num_workers == 0) return SF_OK;
+  sf::Store8Args store_args = {};
+  if (num_store > 0) {
+    const char* base = reinterpret_cast<const char*>(pin.dev);
+    if ((st = sf::check_step_args(desc, &info, pin.dev, q, k_pool, v_pool, block_table, out, lse, nullptr, nullptr,
+                                  nullptr, extras->k_scale, extras->v_scale)) != SF_OK ||
+        (st = sf::store8_args(desc, reinterpret_cast<const int32_t*>(base + info.work_bytes), extras->k_new,
+                              extras->v_new, reinterpret_cast<const int32_t*>(base + pages_off),
+                              const_cast<void*>(k_pool), const_cast<void*>(v_pool), const_cast<float*>(extras->k_scale),
+                              const_cast<float*>(extras->v_scale), const_cast<int32_t*>(block_table), &store_args)) != SF_OK)
+      return st;
+    store_args.num_rows = num_store;
+  }
 
   // 2. workspace (grown only while idle): the partial results, then the
   //    device copy of what the merge launch reads from the ring: the combine
@@ -353,23 +455,77 @@ extern "C" sf_status sf_runner_step(sf_runner* r, const sf_attn_desc* desc, cons
                                      const_cast<int32_t*>(block_table), out, lse, r->workspace,
                                      r->workspace_bytes, stream, cp, ev0, ev1, shared);
   } else {
+    if (num_store > 0 && sf::launch_store_fp8(store_args, main) != hipSuccess) return close_slot(r, main, pin, SF_ERR_HIP);
     st = sf::decode_attn_rows(desc, &info, work, q, k_pool, v_pool, fp8 ? extras->k_scale : nullptr,
                               fp8 ? extras->v_scale : nullptr, block_table, out, lse, r->workspace,
                               r->workspace_bytes, stream, cp, ev0, ev1, shared);
   }
-  pin.used = true;
-  pin.last_step = r->steps;
-  r->last_stream = main;
-  ++r->steps;
-  if (r->steps - r->unmarked >= kMarkEvery && mark_steps(r) != SF_OK) {
-    // Without the mark nothing orders a later rewrite of these slots after
-    // the steps' reads: wait for the stream instead.
-    (void)hipStreamSynchronize(main);
-    for (auto& p : r->ring) p.used = false;
-    r->unmarked = r->steps;
-    if (st == SF_OK) st = SF_ERR_HIP;
-  }
-  return st;
+  return close_slot(r, main, pin, st);
+}
+
+extern "C" sf_status sf_runner_store_fp8(sf_runner* r, const sf_attn_desc* desc, const int32_t* seq_lens_host,
+                                         const int32_t* q_lens_host, const void* k_new, const void* v_new,
+                                         const int32_t* new_pages_host, void* k_pool8, void* v_pool8, float* k_scale,
+                                         float* v_scale, int32_t* block_table, void* stream) {
+  if (!r || !desc || !same_shape(r, desc)) return SF_ERR_INVALID_ARG;
+  hipStream_t main = static_cast<hipStream_t>(stream);
+  sf_store_info info = {};
+  const uint64_t pages_bytes = new_pages_host && desc->num_seqs > 0 ? (uint64_t(desc->num_seqs) * 4 + 31) / 32 * 32 : 0;
+  return run_in_slot(
+      r, main,
+      [&](int32_t* work, uint64_t bytes) {
+        return sf_kv_store_fp8_plan(desc, seq_lens_host, q_lens_host, work, bytes, &info);
+      },
+      [&] { return info.num_rows > 0 ? info.work_bytes + pages_bytes : 0; }, [] { return uint64_t(0); },
+      [&](int32_t* host, const int32_t* dev) {
+        const int32_t* pages = nullptr;
+        if (pages_bytes) {
+          std::memcpy(host + info.work_bytes / 4, new_pages_host, uint64_t(desc->num_seqs) * 4);
+          pages = dev + info.work_bytes / 4;
+        }
+        return sf_kv_store_fp8(desc, &info, nullptr, const_cast<int32_t*>(dev), k_new, v_new, pages, k_pool8, v_pool8,
+                               k_scale, v_scale, block_table, stream);
+      });
+}
+
+extern "C" sf_status sf_runner_key_weights(sf_runner* r, const sf_attn_desc* desc, const int32_t* seq_lens_host,
+                                           const int32_t* q_lens_host, const int32_t* held_lens_host,
+                                           const int32_t* first_pos_host, const void* q, const float* lse,
+                                           const void* k_pool, const float* k_scale, const int32_t* block_table,
+                                           const float* weights, float* weights_out, int32_t* positions, void* stream) {
+  if (!r || !desc || !same_shape(r, desc)) return SF_ERR_INVALID_ARG;
+  sf_weights_info info = {};
+  return run_in_slot(
+      r, static_cast<hipStream_t>(stream),
+      [&](int32_t* work, uint64_t bytes) {
+        return sf_key_weights_plan(desc, seq_lens_host, q_lens_host, held_lens_host, first_pos_host, &r->opts, work,
+                                   bytes, &info);
+      },
+      [&] { return info.work_bytes; }, [&] { return info.workspace_bytes; },
+      [&](int32_t*, const int32_t* dev) {
+        return sf_key_weights(desc, &info, nullptr, const_cast<int32_t*>(dev), q, lse, k_pool, k_scale, block_table,
+                              weights, weights_out, positions, r->workspace, r->workspace_bytes, stream);
+      });
+}
+
+extern "C" sf_status sf_runner_evict(sf_runner* r, const sf_attn_desc* desc, const int32_t* seq_lens_host,
+                                     const int32_t* keep_lens_host, const int32_t* ends_host, int32_t sinks,
+                                     int32_t recent, void* k_pool, void* v_pool, float* k_scale, float* v_scale,
+                                     const int32_t* block_table, const float* weights, const int32_t* positions,
+                                     float* weights_out, int32_t* positions_out, void* stream) {
+  if (!r || !desc || !same_shape(r, desc)) return SF_ERR_INVALID_ARG;
+  sf_evict_info info = {};
+  return run_in_slot(
+      r, static_cast<hipStream_t>(stream),
+      [&](int32_t* work, uint64_t bytes) {
+        return sf_kv_evict_plan(desc, seq_lens_host, keep_lens_host, ends_host, sinks, recent, work, bytes, &info);
+      },
+      [&] { return info.num_moves > 0 ? info.work_bytes : 0; }, [&] { return info.workspace_bytes; },
+      [&](int32_t*, const int32_t* dev) {
+        return sf_kv_evict(desc, &info, nullptr, const_cast<int32_t*>(dev), k_pool, v_pool, k_scale, v_scale,
+                           block_table, weights, positions, weights_out, positions_out, r->workspace,
+                           r->workspace_bytes, stream);
+      });
 }
 
 // Extend attention, in memory that the caller lends: the pinned part is cut

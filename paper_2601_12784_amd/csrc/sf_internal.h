@@ -148,6 +148,95 @@ struct QuantArgs {
   int32_t head_dim;
 };
 
+// Store of new tokens into an fp8 cache (sf_kv_store_fp8).
+struct Store8Args {
+  const int32_t* rows;        // seq, first page, pages, first new position, end position, query row of the first, 0, 0
+  int32_t num_rows;
+  const uint16_t* k_new;      // [T][Hkv][D]
+  const uint16_t* v_new;
+  const int32_t* new_pages;   // [B] page newly given to a sequence's last token, -1 = none; may be NULL
+  uint8_t* k_pool;
+  uint8_t* v_pool;
+  float* k_scale;
+  float* v_scale;
+  int32_t* block_table;
+  int32_t num_kv_heads;
+  int32_t head_dim;
+  int32_t bt_stride;
+};
+sf_status store8_args(const sf_attn_desc* desc, const int32_t* work_dev, const void* k_new, const void* v_new,
+                      const int32_t* new_pages, void* k_pool8, void* v_pool8, float* k_scale, float* v_scale,
+                      int32_t* block_table, Store8Args* args);
+hipError_t launch_store_fp8(const Store8Args& a, hipStream_t stream);
+
+// Attention weights of cached keys (sf_key_weights).
+constexpr int kWeightInts = 16;   // int32 fields per work-list row
+constexpr int kWeightPages = 4;   // pages a wave holds at a time (64 keys)
+struct WeightArgs {
+  // rows: seq, kv_head, first page, end page, first token, end token (of the new ones), part slot (-1: written
+  // directly), L, P, query row of the sequence's first new token, held, position of key `held`, 0 ..
+  const int32_t* items;
+  int32_t num_items;
+  const int32_t* merge_rows;  // the same with first part slot and parts in place of the tokens
+  int32_t num_merge;
+  const uint16_t* q;          // [T][Hq][D]
+  const float* lse;           // [T][Hq]
+  const uint16_t* k_pool;
+  const float* k_scale;       // fp8 cache, else NULL
+  const int32_t* block_table;
+  const float* w_in;          // [num_pages][Hkv][16]
+  float* w_out;
+  int32_t* positions;         // [num_pages][Hkv][16] or NULL
+  float* part;                // [slots][part_keys]
+  int32_t part_keys;
+  int32_t num_q_heads;
+  int32_t num_kv_heads;
+  int32_t group;
+  uint32_t inv_group;         // ceil(2^16 / group)
+  int32_t head_dim;
+  int32_t bt_stride;
+  float scale_log2;
+};
+sf_status weight_args(const sf_attn_desc* desc, const sf_weights_info* info, const int32_t* work_dev, const void* q,
+                      const float* lse, const void* k_pool, const float* k_scale, const int32_t* block_table,
+                      const float* weights, float* weights_out, int32_t* positions, void* workspace, WeightArgs* args);
+hipError_t launch_key_weights(const WeightArgs& a, hipStream_t stream);
+
+// Eviction (sf_kv_evict).
+struct EvictArgs {
+  // num_seqs rows: L, n, first page of holes, first entry of tails (of KV head 0), next position, 0, 0, 0; then
+  // num_moves rows: seq, first page, pages, 0 ..
+  const int32_t* rows;
+  int32_t num_seqs;
+  int32_t num_moves;
+  bool boundary;              // some sequence's n ends inside a page
+  void* k_pool;
+  void* v_pool;
+  float* k_scale;             // fp8 cache, else NULL
+  float* v_scale;
+  const int32_t* block_table;
+  const float* w_in;          // [num_pages][Hkv][16]
+  const int32_t* pos_in;
+  float* w_out;
+  int32_t* pos_out;
+  uint32_t* holes;            // (mask of freed slots, freed slots before it) per page of the first n slots
+  int32_t* tails;             // kept slots behind the first n, ascending
+  int32_t sinks;
+  int32_t recent;
+  int32_t num_kv_heads;
+  int32_t head_dim;
+  int32_t bt_stride;
+};
+sf_status evict_args(const sf_attn_desc* desc, const sf_evict_info* info, const int32_t* work_dev, void* k_pool,
+                     void* v_pool, float* k_scale, float* v_scale, const int32_t* block_table, const float* weights,
+                     const int32_t* positions, float* weights_out, int32_t* positions_out, void* workspace,
+                     EvictArgs* args);
+hipError_t launch_evict(const EvictArgs& a, hipStream_t stream);
+
+// Checks the lengths of an extend-like call and counts its query rows.
+sf_status check_extend_lengths(const sf_attn_desc* desc, const int32_t* seq_lens_host, const int32_t* q_lens_host,
+                               int64_t* rows);
+
 struct GatherArgs {
   const uint16_t* k_pool;
   const uint16_t* v_pool;
