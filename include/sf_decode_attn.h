@@ -257,7 +257,8 @@ typedef struct sf_runner_extras {
   const void* k_new;             /* appending step (sf_decode_attn_append's arguments) */
   const void* v_new;
   const int32_t* new_pages_host; /* host int32 [num_seqs], copied next to the work list */
-  const float* k_scale;          /* fp8 cache (sf_decode_attn_fp8's scales); not with k_new */
+  const float* k_scale;          /* fp8 cache (sf_decode_attn_fp8's scales). With k_new: the newest tokens are
+                                    first stored by sf_kv_store_fp8's rule, which writes these */
   const float* v_scale;
   void* attn_start;              /* optional hipEvent_t: takes the attention kernel's own start time */
   void* attn_end;                /* optional hipEvent_t: takes its end time (before the merge) */
@@ -307,7 +308,9 @@ sf_status sf_runner_plan(const sf_attn_desc* desc, const int32_t* seq_lens_host,
 /* One decode step: desc (its head counts, head_dim and page size as at
  * creation), seq_lens_host (host int32 [num_seqs]) and the device tensors as
  * for sf_decode_attn; extras may be NULL. *info (may be NULL) receives the
- * step's plan. lse is required for an appending step. An fp8 step whose
+ * step's plan. lse is required for an appending step over bf16 pools. An appending
+ * step over an fp8 cache launches the store, then the fp8 step (kind 1), which attends
+ * to the newest token as stored. An fp8 step whose
  * runner options leave workers_per_cu at 0 plans 8 workers per CU (two waves
  * per SIMD: its blocks move half the bytes). */
 sf_status sf_runner_step(sf_runner* runner, const sf_attn_desc* desc, const int32_t* seq_lens_host,
@@ -609,6 +612,25 @@ sf_status sf_extend_attn(const sf_attn_desc* desc, const sf_extend_info* info, c
                          float* lse, void* stream);
 
 /*
+ * Extend attention over an fp8 cache (pools and scales as for
+ * sf_decode_attn_fp8), with sf_extend_attn_plan's plan: the attention above over
+ * the cached values code * scale. The new tokens' keys and values are in the
+ * cache before the call (sf_kv_store_fp8), so every row attends to its own
+ * token, too, as stored. out is fp32 [T][Hq][D], or bf16 if out_bf16 is 1 (rounded once,
+ * to nearest even). Numerics: scores from bf16 q and the codes, exact in bf16,
+ * with fp32 accumulation, the page's key scale applied in fp32; softmax weights
+ * and values enter the P.V product as fp16, values as code * scale over a power of
+ * two that is at least the largest value scale that the walk has met. Within
+ * 2^-14 of that largest scale, the error is at most 2^-10 times sum_t p_t |V_t| /
+ * sum_t p_t plus fp32 rounding; lse is fp32 throughout. Errors as
+ * sf_decode_attn_fp8, and SF_ERR_INVALID_ARG for another out_bf16 than 0 and 1.
+ */
+sf_status sf_extend_attn_fp8(const sf_attn_desc* desc, const sf_extend_info* info, const int32_t* work_host,
+                             int32_t* work_dev, const void* q, const void* k_pool8, const void* v_pool8,
+                             const float* k_scale, const float* v_scale, const int32_t* block_table, void* out,
+                             int32_t out_bf16, float* lse, void* stream);
+
+/*
  * Extend attention through a runner (sf_runner_create): plans, stores the new
  * tokens if given, and attends, in one call. out, lse and the pools as
  * sf_extend_attn; the runner's own plan differs from sf_extend_attn_plan's
@@ -656,6 +678,14 @@ sf_status sf_runner_extend(sf_runner* runner, const sf_attn_desc* desc, const in
                            const int32_t* q_lens_host, const void* q, const void* k_new, const void* v_new,
                            void* k_pool, void* v_pool, const int32_t* block_table, float* out, float* lse,
                            sf_runner_memory* memory, void* stream, sf_extend_info* info);
+
+/* The same over an fp8 cache: sf_kv_store_fp8 of k_new and v_new (unless both
+ * are NULL), then sf_extend_attn_fp8, with the runner's own plan. */
+sf_status sf_runner_extend_fp8(sf_runner* runner, const sf_attn_desc* desc, const int32_t* seq_lens_host,
+                               const int32_t* q_lens_host, const void* q, const void* k_new, const void* v_new,
+                               void* k_pool8, void* v_pool8, const int32_t* block_table, void* out, float* lse,
+                               sf_runner_memory* memory, void* stream, sf_extend_info* info, float* k_scale,
+                               float* v_scale, int32_t out_bf16);
 
 /*
  * Host page allocator for the KV pool. A trajectory's cache grows by one

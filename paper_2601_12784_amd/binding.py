@@ -167,6 +167,8 @@ def lib():
     L.sf_runner_store_fp8.argtypes = [vp, desc] + [vp] * 11
     L.sf_runner_key_weights.argtypes = [vp, desc] + [vp] * 13
     L.sf_runner_evict.argtypes = [vp, desc, vp, vp, vp, i32, i32] + [vp] * 10
+    L.sf_extend_attn_fp8.argtypes = [desc, P(sf_extend_info)] + [vp] * 9 + [i32, vp, vp]
+    L.sf_runner_extend_fp8.argtypes = [vp, desc] + [vp] * 10 + [P(sf_runner_memory), vp, P(sf_extend_info), vp, vp, i32]
     L.sf_page_table_truncate.argtypes = [vp, vp, i32, i32, vp, vp]
     L.sf_page_table_step.argtypes = [vp, vp, ctypes.c_int32, ctypes.c_int32, vp, vp, ctypes.c_int32, vp]
     L.sf_cost_throughput.argtypes = [P(sf_cost_model), P(sf_instance_state)]
@@ -186,7 +188,7 @@ def lib():
                "sf_debug_runner_reserve", "sf_runner_reserve_batch", "sf_debug_stream_read", "sf_decode_attn_scratch",
                "sf_kv_store_fp8_plan", "sf_kv_store_fp8", "sf_key_weights_plan", "sf_key_weights", "sf_kv_evict_plan",
                "sf_kv_evict", "sf_runner_store_fp8", "sf_runner_key_weights", "sf_runner_evict",
-               "sf_page_table_truncate"):
+               "sf_page_table_truncate", "sf_extend_attn_fp8", "sf_runner_extend_fp8"):
         getattr(L, fn).restype = ctypes.c_int
     L.sf_status_string.argtypes = [ctypes.c_int]
     L.sf_status_string.restype = ctypes.c_char_p
@@ -584,14 +586,17 @@ def sf_extend_attn_plan(desc: sf_attn_desc, seq_lens, q_lens, work_host=None):
     return info, work_host
 
 
-def _check_extend(desc, rows, q, k_pool, v_pool, block_table, out, lse, k_new, v_new):
+def _check_extend(desc, rows, q, k_pool, v_pool, block_table, out, lse, k_new, v_new, fp8=None):
     """The tensors of an extend call over `rows` new tokens."""
     hq, hkv, d = desc.num_q_heads, desc.num_kv_heads, desc.head_dim
     _dev(q, "q", torch.bfloat16, (rows, hq, d))
-    _dev(k_pool, "k_pool", torch.bfloat16, (desc.num_pages, hkv, d // 8, PAGE, 8))
-    _dev(v_pool, "v_pool", torch.bfloat16, (desc.num_pages, hkv, d, PAGE))
+    if fp8 is None:
+        _dev(k_pool, "k_pool", torch.bfloat16, (desc.num_pages, hkv, d // 8, PAGE, 8))
+        _dev(v_pool, "v_pool", torch.bfloat16, (desc.num_pages, hkv, d, PAGE))
+    else:
+        _check_pools(desc.num_pages, hkv, d, k_pool, v_pool, block_table, desc.num_seqs, fp8)
     _dev(block_table, "block_table", torch.int32, (desc.num_seqs, desc.block_table_stride))
-    _dev(out, "out", torch.float32, (rows, hq, d))
+    _dev(out, "out", out.dtype if fp8 is not None and out.dtype is torch.bfloat16 else torch.float32, (rows, hq, d))
     if lse is not None:
         _dev(lse, "lse", torch.float32, (rows, hq))
     if (k_new is None) != (v_new is None):
@@ -613,6 +618,18 @@ def sf_extend_attn(desc, info, work_host, work_dev, q, k_pool, v_pool, block_tab
         ctypes.byref(desc), ctypes.byref(info), _addr(work_host), _addr(work_dev), _addr(q), _addr(k_new),
         _addr(v_new), _addr(k_pool), _addr(v_pool), _addr(block_table), _addr(out), _addr(lse),
         _stream(stream)))
+
+
+def sf_extend_attn_fp8(desc, info, work_host, work_dev, q, k_pool8, v_pool8, k_scale, v_scale, block_table, out,
+                       lse=None, stream=None):
+    """Enqueues extend attention over an fp8 cache that holds the new tokens already (sf_kv_store_fp8). q, out:
+    [T, Hq, D]; out fp32 or bf16."""
+    _check_extend(desc, info.num_q_rows, q, k_pool8, v_pool8, block_table, out, lse, None, None, (k_scale, v_scale))
+    _check_work(info, work_dev)
+    _check("sf_extend_attn_fp8", lib().sf_extend_attn_fp8(
+        ctypes.byref(desc), ctypes.byref(info), _addr(work_host), _addr(work_dev), _addr(q), _addr(k_pool8),
+        _addr(v_pool8), _addr(k_scale), _addr(v_scale), _addr(block_table), _addr(out),
+        int(out.dtype is torch.bfloat16), _addr(lse), _stream(stream)))
 
 
 _cus = {}
@@ -805,12 +822,13 @@ class ExtendAttention:
             if at != self._at:
                 self._at, self._block = at, self._scratch.get(at[:3])
             block = self._block
+        call = self._L.sf_runner_extend if len(args) == 15 else self._L.sf_runner_extend_fp8
         if block is None:
-            st = self._L.sf_runner_extend(*args)
+            st = call(*args)
         else:
             kept = m.device, m.device_bytes
             m.device, m.device_bytes, m.device_per_call = block.next(), block.nbytes, 1
-            st = self._L.sf_runner_extend(*args)
+            st = call(*args)
             m.device, m.device_bytes, m.device_per_call = *kept, 0
         if self._large is None:
             self._large = m.need_device > m.device_bytes
@@ -821,7 +839,9 @@ class ExtendAttention:
         return st
 
     def __call__(self, q, k_pool, v_pool, block_table, seq_lens, q_lens, scale, out=None, lse=None,
-                 k_new=None, v_new=None, stream=None):
+                 k_new=None, v_new=None, stream=None, fp8=None):
+        """fp8 = (k_scale, v_scale): k_pool and v_pool are an fp8 cache, which k_new and v_new are stored into by
+        sf_kv_store_fp8's rule, and out may be bf16."""
         lens = np.ascontiguousarray(np.asarray(seq_lens), dtype=np.int32)
         qls = np.ascontiguousarray(np.asarray(q_lens), dtype=np.int32)
         if lens.ndim != 1 or lens.shape != qls.shape:
@@ -832,9 +852,9 @@ class ExtendAttention:
             check_block_table(desc, block_table, np.where(qls > 0, lens, 0))
         if out is None:
             out = torch.empty((rows, self.hq, self.d), dtype=torch.float32, device=self.device)
-        _check_extend(desc, rows, q, k_pool, v_pool, block_table, out, lse, k_new, v_new)
+        _check_extend(desc, rows, q, k_pool, v_pool, block_table, out, lse, k_new, v_new, fp8)
         info = sf_extend_info()
-        tensors = (q, k_pool, v_pool, block_table, out, lse, k_new, v_new)
+        tensors = (q, k_pool, v_pool, block_table, out, lse, k_new, v_new, fp8)
         try:
             if not self._lent:
                 if torch.cuda.is_current_stream_capturing():   # nothing is created in a capture
@@ -844,6 +864,8 @@ class ExtendAttention:
             args = (self._runner, ctypes.byref(desc), _host_addr(lens), _host_addr(qls), q.data_ptr(), _addr(k_new),
                     _addr(v_new), k_pool.data_ptr(), v_pool.data_ptr(), block_table.data_ptr(), out.data_ptr(), _addr(lse),
                     ctypes.byref(self._memory), _stream(stream), ctypes.byref(info))
+            if fp8 is not None:
+                args += (fp8[0].data_ptr(), fp8[1].data_ptr(), int(out.dtype is torch.bfloat16))
             st = self._run(args, stream)
             if st == CAPACITY:
                 self._grow(stream)
@@ -857,8 +879,11 @@ class ExtendAttention:
             info = self._call_captured(desc, lens, qls, tensors, stream)
         else:
             _check("sf_runner_extend", st)
-            if self._spare[4] < info.work_bytes:   # captured calls took it
-                self._spare = self._room(info.work_bytes)
+            need = info.work_bytes
+            if fp8 is not None:   # a captured call takes the store's list, too, which the runner's plan holds
+                need = max(need, int(self._memory.need_slot))
+            if self._spare[4] < need:   # captured calls took it
+                self._spare = self._room(need)
         self.last_info = info
         return out
 
@@ -884,17 +909,36 @@ class ExtendAttention:
         self._captured.append((host, dev))
         return host, dev
 
-    def _call_captured(self, desc, lens, qls, tensors, stream):
+    def _launch_whole(self, desc, lens, qls, tensors, stream, lists):
+        """sf_extend_attn, or the store and sf_extend_attn_fp8, on lists(work list) -> (pinned or None, device)."""
         info, work = sf_extend_attn_plan(desc, lens, qls)
-        if info.num_items > 0:
-            sf_extend_attn(desc, info, *self._captured_list(work[: info.work_bytes // 4]), *tensors, stream=stream)
+        if info.num_items == 0:
+            return info
+        fp8 = tensors[-1]
+        if fp8 is None:
+            sf_extend_attn(desc, info, *lists(work[: info.work_bytes // 4]), *tensors[:-1], stream=stream)
+            return info
+        q, k_pool, v_pool, block_table, out, lse, k_new, v_new = tensors[:-1]
+        if k_new is not None:
+            sinfo, rows = sf_kv_store_fp8_plan(desc, lens, qls)
+            sf_kv_store_fp8(desc, sinfo, *lists(rows[: sinfo.work_bytes // 4]), k_new, v_new, None, k_pool, v_pool, *fp8,
+                            block_table, stream=stream)
+        sf_extend_attn_fp8(desc, info, *lists(work[: info.work_bytes // 4]), q, k_pool, v_pool, *fp8, block_table, out,
+                           lse, stream=stream)
         return info
 
+    def _call_captured(self, desc, lens, qls, tensors, stream):
+        return self._launch_whole(desc, lens, qls, tensors, stream, self._captured_list)
+
     def _call_whole(self, desc, lens, qls, tensors, stream):
-        info, work = sf_extend_attn_plan(desc, lens, qls)
-        dev = torch.from_numpy(work).to(self.device)   # uploaded when this returns
-        sf_extend_attn(desc, info, None, dev, *tensors, stream=stream)
-        if stream is not None:   # the list belongs to the current stream
+        kept = []
+
+        def lists(work):
+            kept.append(torch.from_numpy(work).to(self.device))   # uploaded when this returns
+            return None, kept[-1]
+
+        info = self._launch_whole(desc, lens, qls, tensors, stream, lists)
+        if stream is not None:   # the lists belong to the current stream
             torch.cuda.ExternalStream(_stream(stream), device=self.device).synchronize()
         return info
 

@@ -400,10 +400,11 @@ sf_status sf::extend_args(const sf_attn_desc* desc, const int32_t* work_dev, con
   return SF_OK;
 }
 
-extern "C" sf_status sf_extend_attn(const sf_attn_desc* desc, const sf_extend_info* info,
+static sf_status extend_attn(const sf_attn_desc* desc, const sf_extend_info* info,
                                     const int32_t* work_host, int32_t* work_dev, const void* q,
                                     const void* k_new, const void* v_new, void* k_pool, void* v_pool,
-                                    const int32_t* block_table, float* out, float* lse, void* stream) {
+                                    const int32_t* block_table, float* out, float* lse, void* stream, const float* k_scale = nullptr,
+                             const float* v_scale = nullptr, bool out_bf16 = false) {
   sf_status st = validate_desc(desc);
   if (st != SF_OK) return st;
   if (!info) return SF_ERR_INVALID_ARG;
@@ -417,12 +418,34 @@ extern "C" sf_status sf_extend_attn(const sf_attn_desc* desc, const sf_extend_in
   if ((st = extend_args(desc, work_dev, q, k_new, v_new, k_pool, v_pool, block_table, out, lse, &a)) != SF_OK)
     return st;
   a.num_items = info->num_items;
+  a.k_scale = k_scale;
+  a.v_scale = v_scale;
+  a.out_bf16 = out_bf16;
   hipStream_t s = static_cast<hipStream_t>(stream);
   if (work_host) {
     hipError_t e = hipMemcpyAsync(work_dev, work_host, info->work_bytes, hipMemcpyHostToDevice, s);
     if (e != hipSuccess) return SF_ERR_HIP;
   }
   return launch_extend(a, s) == hipSuccess ? SF_OK : SF_ERR_HIP;
+}
+
+extern "C" sf_status sf_extend_attn(const sf_attn_desc* desc, const sf_extend_info* info,
+                                    const int32_t* work_host, int32_t* work_dev, const void* q,
+                                    const void* k_new, const void* v_new, void* k_pool, void* v_pool,
+                                    const int32_t* block_table, float* out, float* lse, void* stream) {
+  return extend_attn(desc, info, work_host, work_dev, q, k_new, v_new, k_pool, v_pool, block_table, out, lse, stream);
+}
+
+extern "C" sf_status sf_extend_attn_fp8(const sf_attn_desc* desc, const sf_extend_info* info, const int32_t* work_host,
+                                        int32_t* work_dev, const void* q, const void* k_pool8, const void* v_pool8,
+                                        const float* k_scale, const float* v_scale, const int32_t* block_table,
+                                        void* out, int32_t out_bf16, float* lse, void* stream) {
+  if ((out_bf16 | 1) != 1) return SF_ERR_INVALID_ARG;
+  if (info && info->num_items > 0 && (!k_scale || !v_scale || !aligned4(k_scale) || !aligned4(v_scale)))
+    return SF_ERR_INVALID_ARG;
+  return extend_attn(desc, info, work_host, work_dev, q, nullptr, nullptr, const_cast<void*>(k_pool8),
+                     const_cast<void*>(v_pool8), block_table, static_cast<float*>(out), lse, stream, k_scale, v_scale,
+                     out_bf16 != 0);
 }
 
 extern "C" sf_status sf_debug_extend_plan(const sf_attn_desc* desc, const int32_t* seq_lens_host,

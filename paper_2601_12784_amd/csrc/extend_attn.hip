@@ -119,9 +119,25 @@ __device__ __forceinline__ uint32_t bf16x2_to_f16x2(uint32_t w) {
   return pack_f16(__builtin_bit_cast(float, w << 16), __builtin_bit_cast(float, w & 0xFFFF0000u));
 }
 
+// Two E4M3 codes (the low or the high two of four) as bf16 and as fp32, both exact.
+template <bool kHigh>
+__device__ __forceinline__ uint32_t fp8x2_to_bf16x2(uint32_t codes4) {
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes4, 1.0f, kHigh));
+}
+template <bool kHigh>
+__device__ __forceinline__ f32x2 fp8x2_to_f32x2(uint32_t codes4) {
+  return __builtin_bit_cast(f32x2, __builtin_amdgcn_cvt_pk_f32_fp8(int(codes4), kHigh));
+}
+
 // Element offset of a (page, KV head) tile in either pool.
 __device__ __forceinline__ size_t tile_base(int32_t page, int32_t num_kv_heads, int32_t kvh, int d) {
   return (size_t(page) * num_kv_heads + kvh) * size_t(kPage * d);
+}
+
+// Four floats to bf16, round to nearest even.
+__device__ __forceinline__ u32x2 pack_bf16x4(f32x4 v) {
+  typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+  return __builtin_bit_cast(u32x2, __builtin_convertvector(v, bf16x4));
 }
 
 // V in LDS, both pages of a step interleaved: dim d owns 64 bytes, four
@@ -132,10 +148,10 @@ __device__ __forceinline__ size_t tile_base(int32_t page, int32_t num_kv_heads, 
 // distinct 16-byte bank groups.
 __device__ __forceinline__ int v_swizzle(int d) { return (d >> 1) & 3; }
 
-template <int D, int kStageWaves>
+template <int D, int kStageWaves, bool kFp8 = false>
 struct Tiles {
-  static constexpr int kElems = kPage * D;            // bf16 per (page, KV head) tile
-  static constexpr int kChunks = kElems / 8;          // 16-byte pieces per tile
+  static constexpr int kElems = kPage * D;            // elements per (page, KV head) tile
+  static constexpr int kChunks = kElems / (kFp8 ? 16 : 8);   // 16-byte pieces per tile in the pool
   // A step stages four tiles (K and V of two pages); each is moved by
   // kStageWaves / 4 waves, kWaveChunks wave-wide 1 KiB chunks (64 pieces) each.
   static constexpr int kWaveChunks = kChunks / 64 / (kStageWaves / 4);
@@ -207,14 +223,33 @@ __device__ __forceinline__ float row_max(const TileWeights& t) {
   return fmaxf(mx, __shfl_xor(mx, 32));
 }
 
+// The factors of a step's two pages that turn raw scores into log2 units: the
+// softmax scale, and over an fp8 cache the page's key scale with it.
+template <bool kFp8>
+struct PageFactors {
+  float c0, c1;
+  __device__ __forceinline__ float of(int e) const { return e < 4 || !kFp8 ? c0 : c1; }
+};
+
+// Row maximum of a step in log2 units, in every lane of the row.
+template <bool kFp8>
+__device__ __forceinline__ float scaled_row_max(const TileWeights& t, PageFactors<kFp8> c) {
+  if constexpr (!kFp8) return row_max(t) * c.c0;
+  const float a = fmaxf(fmaxf(t.sc[0], t.sc[1]), fmaxf(t.sc[2], t.sc[3])) * c.c0;
+  const float b = fmaxf(fmaxf(t.sc[4], t.sc[5]), fmaxf(t.sc[6], t.sc[7])) * c.c1;
+  float mx = fmaxf(a, b);
+  mx = fmaxf(mx, __shfl_xor(mx, 16));
+  return fmaxf(mx, __shfl_xor(mx, 32));
+}
+
 // Part 1: exponentiate against the current reference.
-template <bool kMasked>
+template <bool kMasked, bool kFp8>
 __device__ __forceinline__ TileWeights exponentiate(const f32x4& s0, const f32x4& s1, int key0, int grp, int limit,
-                                                    float c, float m) {
+                                                    PageFactors<kFp8> c, float m) {
   TileWeights t;
   take_scores<kMasked>(t, s0, s1, key0, grp, limit);
 #pragma unroll
-  for (int e = 0; e < 8; ++e) t.p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(t.sc[e], c, -m));
+  for (int e = 0; e < 8; ++e) t.p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(t.sc[e], c.of(e), -m));
   t.part = weight_sum(t.p);
   // Also true for inf (the first step, m = -inf) and NaN (-inf * 0 for a
   // zero scale), which settle() sorts out.
@@ -224,10 +259,10 @@ __device__ __forceinline__ TileWeights exponentiate(const f32x4& s0, const f32x4
 
 // Part 2: move the reference if needed (rare), then add the sum and pack the
 // weights as the P^T operand.
-template <int D, bool kMasked>
-__device__ __forceinline__ u32x4 settle(TileWeights& t, float c, float& m, float& lsum, f32x4* o) {
+template <int D, bool kMasked, bool kFp8>
+__device__ __forceinline__ u32x4 settle(TileWeights& t, PageFactors<kFp8> c, float& m, float& lsum, f32x4* o) {
   if (__any(t.need)) {
-    const float mx_s = row_max(t) * c;
+    const float mx_s = scaled_row_max(t, c);
     const bool grow = mx_s > m;   // NaN (fully masked, zero scale) compares false
     const float mnew = grow ? mx_s : m;
     const float alpha = __builtin_amdgcn_exp2f(m - mnew);
@@ -236,7 +271,7 @@ __device__ __forceinline__ u32x4 settle(TileWeights& t, float c, float& m, float
 #pragma unroll
     for (int jb = 0; jb < D / 16; ++jb) o[jb] *= alpha;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) t.p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(t.sc[e], c, -m));
+    for (int e = 0; e < 8; ++e) t.p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(t.sc[e], c.of(e), -m));
     t.part = weight_sum(t.p);
   }
   if constexpr (kMasked) {
@@ -249,18 +284,29 @@ __device__ __forceinline__ u32x4 settle(TileWeights& t, float c, float& m, float
                pack_f16(t.p[6], t.p[7])};
 }
 
-template <int D, int kWaves>
+// Over an fp8 cache (kFp8) only the staging differs. Codes are widened on the
+// way into LDS: keys to bf16, exact, with the page's scale left to the factor of
+// its scores; values to fp16 times their page's scale over a reference, one
+// rounding. The reference is a power of two, at least the largest value scale of
+// the walk so far (so no product leaves fp16's range, and pages of any smaller
+// scale keep their precision down to 2^-14 of it); it goes with the step's key scales
+// through LDS, and a wave rescales its O where it has moved, which the scales'
+// spread makes rare. The pool's 16-byte pieces are half as many, so the staging
+// waves take one each at D = 128, and four waves are enough at D = 64.
+template <int D, int kWaves, bool kFp8>
 __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(Build<kWaves>::kPerSimd, Build<kWaves>::kPerSimd)))
 void extend_attn_kernel(ExtendArgs a) {
   constexpr int KB = D / 32;
   constexpr int JB = D / 16;
-  constexpr int kStageWaves = Build<kWaves>::kStageWaves;
+  constexpr int kStageWaves = kFp8 && D == 64 ? 4 : Build<kWaves>::kStageWaves;
   constexpr int kAhead = Build<kWaves>::kAhead;
-  constexpr int TE = Tiles<D, kStageWaves>::kElems;
-  constexpr int NC = Tiles<D, kStageWaves>::kWaveChunks;
+  constexpr int TE = Tiles<D, kStageWaves, kFp8>::kElems;
+  constexpr int NC = Tiles<D, kStageWaves, kFp8>::kWaveChunks;
   constexpr int kWaveRows = 16 * kRowTiles;
   // [buffer][K page 0 | K page 1 | V of both pages, interleaved]
   __shared__ __attribute__((aligned(16))) uint16_t lds[2][4 * TE];
+  // fp8: [buffer][key scale of page 0 | of page 1 | value reference | unused]
+  __shared__ __attribute__((aligned(16))) float lds_scale[2][4];
 
   const const_i32_ptr item = as_constant(a.items) + size_t(blockIdx.x) * kItemInts;
   const int seq = item[0];
@@ -341,8 +387,23 @@ void extend_attn_kernel(ExtendArgs a) {
   int skey[NC];    // V: first token of the piece within the step's 32 keys
 #pragma unroll
   for (int q = 0; q < NC; ++q) {
-    soff[q] = (((wave % kPerTile) * NC + q) * 64 + lane) * 8;
-    if (stile < 2) {
+    soff[q] = (((wave % kPerTile) * NC + q) * 64 + lane) * (kFp8 ? 16 : 8);   // fp8: bytes
+    if constexpr (kFp8) {
+      // Piece p of a tile, of lane (grp, col): a key piece holds dims 64p + 8grp
+      // .. + 7 of token col, then the same of 64p + 32; a value piece tokens
+      // 4grp .. + 3 of dims 64p + 16j + col, j = 0 .. 3 (32 * 16 elements apart).
+      const int p = (wave % kPerTile) * NC + q;
+      if (stile < 2) {
+        sdst0[q] = stile * TE + ((8 * p + grp) * kPage + col) * 8;
+        sdst1[q] = sdst0[q] + 4 * kPage * 8;
+        skey[q] = 0;
+      } else {
+        const int d = 64 * p + col;
+        sdst0[q] = 2 * TE + d * 32 + (grp ^ v_swizzle(d)) * 8 + (stile - 2) * 4;
+        sdst1[q] = 0;
+        skey[q] = (stile - 2) * kPage + 4 * grp;
+      }
+    } else if (stile < 2) {
       sdst0[q] = stile * TE + soff[q];
       sdst1[q] = 0;
       skey[q] = 0;
@@ -357,11 +418,32 @@ void extend_attn_kernel(ExtendArgs a) {
       skey[q] = pg * kPage + 8 * c;
     }
   }
-  u32x4 pre[kAhead][NC];
-  auto fetch = [&](u32x4* x, int js) {
+  struct Fetched {
+    u32x4 x[NC];
+    float own, most;   // fp8: the tile's scale, and the larger of both pages' value scales
+  };
+  Fetched pre[kAhead];
+  constexpr float kNoReference = 0x1p-126f;
+  float vstage = kNoReference;   // fp8: the value reference, as the staging waves and
+  float vref = kNoReference;     // as the computing waves know it
+  typedef __attribute__((address_space(4))) const float* const_f32_ptr;
+  auto fetch = [&](Fetched& f, int js) {
     if (js >= nsteps) return;
+    u32x4* x = f.x;
     const int pg0 = 2 * js;
     const int p0 = bt[pg0];
+    if constexpr (kFp8) {
+      const int p1 = pg0 + 1 < npages ? bt[pg0 + 1] : p0;
+      const size_t tile0 = size_t(p0) * a.num_kv_heads + kvh, tile1 = size_t(p1) * a.num_kv_heads + kvh;
+      const const_f32_ptr scales = (const_f32_ptr)(stile < 2 ? a.k_scale : a.v_scale);
+      const float s0 = scales[tile0], s1 = scales[tile1];
+      f.own = stile & 1 ? s1 : s0;
+      f.most = fmaxf(s0, s1);
+      const uint8_t* src = reinterpret_cast<const uint8_t*>(spool) + (stile & 1 ? tile1 : tile0) * size_t(kPage * D);
+#pragma unroll
+      for (int q = 0; q < NC; ++q) x[q] = *reinterpret_cast<const u32x4*>(src + soff[q]);
+      return;
+    }
     const int page = (stile & 1) && pg0 + 1 < npages ? bt[pg0 + 1] : p0;
     const uint16_t* src = spool + tile_base(page, a.num_kv_heads, kvh, D);
 #pragma unroll
@@ -372,8 +454,48 @@ void extend_attn_kernel(ExtendArgs a) {
   // their interleaved slots; in the step that reaches kend, V tokens at or
   // past it are zeroed first (they may be stale or NaN, and a zero weight
   // times NaN is still NaN).
-  auto stage = [&](uint16_t* L, const u32x4* px, int js) {
+  auto stage = [&](int buffer, const Fetched& f, int js) {
     if (js >= nsteps) return;
+    uint16_t* L = lds[buffer];
+    const u32x4* px = f.x;
+    if constexpr (kFp8) {
+      const bool first = wave % kPerTile == 0 && lane == 0;
+      if (stile < 2) {
+        if (first) lds_scale[buffer][stile] = f.own;
+#pragma unroll
+        for (int q = 0; q < NC; ++q) {
+          const u32x4 x = px[q];
+          *reinterpret_cast<u32x4*>(L + sdst0[q]) = u32x4{fp8x2_to_bf16x2<false>(x[0]), fp8x2_to_bf16x2<true>(x[0]),
+                                                          fp8x2_to_bf16x2<false>(x[1]), fp8x2_to_bf16x2<true>(x[1])};
+          *reinterpret_cast<u32x4*>(L + sdst1[q]) = u32x4{fp8x2_to_bf16x2<false>(x[2]), fp8x2_to_bf16x2<true>(x[2]),
+                                                          fp8x2_to_bf16x2<false>(x[3]), fp8x2_to_bf16x2<true>(x[3])};
+        }
+        return;
+      }
+      if (f.most > vstage) {   // the next power of two (scales are at most 2^110)
+        const uint32_t b = __builtin_bit_cast(uint32_t, f.most);
+        vstage = __builtin_bit_cast(float, ((b >> 23) + ((b & 0x7FFFFFu) ? 1u : 0u)) << 23);
+      }
+      const float r = f.own * __builtin_bit_cast(float, 0x7F000000u - __builtin_bit_cast(uint32_t, vstage));   // over it, exact
+      if (first && stile == 2) lds_scale[buffer][2] = vstage;
+      const int left = kend - js * kStepKeys;   // keys of the step that exist
+#pragma unroll
+      for (int q = 0; q < NC; ++q) {
+        uint32_t keep = 0xFFFFFFFFu;
+        if (left < kStepKeys) {
+          const int n = left - skey[q];
+          keep = n >= 4 ? 0xFFFFFFFFu : n <= 0 ? 0u : (1u << (8 * n)) - 1u;
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const uint32_t w = px[q][j] & keep;
+          const f32x2 lo = fp8x2_to_f32x2<false>(w), hi = fp8x2_to_f32x2<true>(w);
+          *reinterpret_cast<u32x2*>(L + sdst0[q] + j * 16 * 32) =
+              u32x2{pack_f16(lo[0] * r, lo[1] * r), pack_f16(hi[0] * r, hi[1] * r)};
+        }
+      }
+      return;
+    }
     if (stile < 2) {
 #pragma unroll
       for (int q = 0; q < NC; ++q) *reinterpret_cast<u32x4*>(L + sdst0[q]) = px[q];
@@ -419,17 +541,36 @@ void extend_attn_kernel(ExtendArgs a) {
       }
     }
   };
-  auto compute = [&](const uint16_t* L, int key0) {
+  auto factors = [&](int buffer) {
+    if constexpr (!kFp8) return PageFactors<kFp8>{c, c};
+    return PageFactors<kFp8>{c * __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, lds_scale[buffer][0]))),
+                             c * __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, lds_scale[buffer][1])))};
+  };
+  auto compute = [&](int buffer, int key0) {
+    const uint16_t* L = lds[buffer];
     f32x4 s0[kRowTiles], s1[kRowTiles];
     scores(L, s0, s1);
+    const PageFactors<kFp8> cf = factors(buffer);
+    if constexpr (kFp8) {
+      const float v =
+          __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, lds_scale[buffer][2])));
+      if (v != vref) {
+        const float f = vref / v;   // a power of two; O is 0 before the first step
+#pragma unroll
+        for (int rt = 0; rt < kRowTiles; ++rt)
+#pragma unroll
+          for (int jb = 0; jb < JB; ++jb) o[rt][jb] *= f;
+        vref = v;
+      }
+    }
     const int vo = 2 * TE + col * 32 + (grp ^ v_swizzle(col)) * 8;
     auto tail = [&](auto masked_tag) {
       constexpr bool kMasked = decltype(masked_tag)::value;
       u32x4 pf[kRowTiles];
 #pragma unroll
       for (int rt = 0; rt < kRowTiles; ++rt) {
-        TileWeights t = exponentiate<kMasked>(s0[rt], s1[rt], key0, grp, limit[rt], c, m[rt]);
-        pf[rt] = settle<D, kMasked>(t, c, m[rt], lsum[rt], o[rt]);
+        TileWeights t = exponentiate<kMasked>(s0[rt], s1[rt], key0, grp, limit[rt], cf, m[rt]);
+        pf[rt] = settle<D, kMasked>(t, cf, m[rt], lsum[rt], o[rt]);
       }
 #pragma unroll
       for (int jb = 0; jb < JB; ++jb) {
@@ -446,22 +587,23 @@ void extend_attn_kernel(ExtendArgs a) {
 
   if (stager) {
     const bool first = begin > 0 && stile < 2;   // the keys of step 0, for a later part's reference
-    u32x4 k0[NC];
+    Fetched k0;
     if (first) fetch(k0, 0);
     fetch(pre[0], begin);
     if constexpr (kAhead == 2) fetch(pre[1], begin + 1);
-    if (first) stage(lds[1], k0, 0);
-    stage(lds[0], pre[0], begin);
+    if (first) stage(1, k0, 0);
+    stage(0, pre[0], begin);
   }
   __syncthreads();
   if (begin > 0) {
     f32x4 s0[kRowTiles], s1[kRowTiles];
     scores(lds[1], s0, s1);
+    const PageFactors<kFp8> cf = factors(1);
 #pragma unroll
     for (int rt = 0; rt < kRowTiles; ++rt) {
       TileWeights t;
       take_scores<true>(t, s0[rt], s1[rt], 0, grp, limit[rt]);
-      const float mx_s = row_max(t) * c;
+      const float mx_s = scaled_row_max(t, cf);
       m[rt] = mx_s > m[rt] ? mx_s : m[rt];   // as settle() moves it
     }
     __syncthreads();   // before the next step is staged over these keys
@@ -470,15 +612,15 @@ void extend_attn_kernel(ExtendArgs a) {
   // One step from buffer `cur` while the next is staged into `nxt` and, two
   // ahead, the one after it is fetched; the loop is unrolled by two so that
   // both buffers' addresses (and prefetch registers) are constants.
-  auto interval = [&](int js, const uint16_t* cur, uint16_t* nxt, u32x4* fetched, u32x4* next) {
+  auto interval = [&](int js, int cur, int nxt, Fetched& fetched, const Fetched& next) {
     if (stager) fetch(fetched, js + kAhead);
     if (js * kStepKeys <= wave_kmax) compute(cur, js * kStepKeys);
     if (stager) stage(nxt, next, js + 1);
     __syncthreads();
   };
   for (int js = begin; js < nsteps; js += 2) {
-    interval(js, lds[0], lds[1], pre[0], pre[kAhead - 1]);
-    if (js + 1 < nsteps) interval(js + 1, lds[1], lds[0], pre[kAhead - 1], pre[0]);
+    interval(js, 0, 1, pre[0], pre[kAhead - 1]);
+    if (js + 1 < nsteps) interval(js + 1, 1, 0, pre[kAhead - 1], pre[0]);
   }
 
   // Lane holds O[row col][16*jb + 4*grp + i] of each row tile.
@@ -493,7 +635,15 @@ void extend_attn_kernel(ExtendArgs a) {
     const size_t orow = size_t(qrow0 + t0 + tok) * a.num_q_heads + head;
     // A part's result goes to its partial slot, with its lse in log2 units
     // (o = 0 and lse = -inf for a row with no key in the part).
-    const float inv = slot >= 0 && lt == 0.f ? 0.f : 1.f / lt;
+    float inv = slot >= 0 && lt == 0.f ? 0.f : 1.f / lt;
+    if constexpr (kFp8) inv *= vref;
+    if (kFp8 && slot < 0 && a.out_bf16) {
+      uint16_t* dst = reinterpret_cast<uint16_t*>(a.out) + orow * D + 4 * grp;
+#pragma unroll
+      for (int jb = 0; jb < JB; ++jb) *reinterpret_cast<u32x2*>(dst + 16 * jb) = pack_bf16x4(o[rt][jb] * inv);
+      if (a.lse && grp == 0) a.lse[orow] = (m[rt] + __log2f(lt)) * kLn2;
+      continue;
+    }
     float* dst = (slot >= 0 ? a.part_o + (size_t(slot) * (kWaves * kWaveRows) + r) * D : a.out + orow * D) + 4 * grp;
 #pragma unroll
     for (int jb = 0; jb < JB; ++jb) *reinterpret_cast<f32x4*>(dst + 16 * jb) = o[rt][jb] * inv;
@@ -543,7 +693,10 @@ __global__ __launch_bounds__(kMergeThreads) void extend_merge_kernel(ExtendArgs 
   }
   const int tok = r / g;
   const size_t orow = size_t(qrow + tok) * a.num_q_heads + kvh * g + (r - tok * g);
-  *reinterpret_cast<f32x4*>(a.out + orow * D + 4 * d4) = acc * (1.f / wsum);
+  if (a.out_bf16)
+    *reinterpret_cast<u32x2*>(reinterpret_cast<uint16_t*>(a.out) + orow * D + 4 * d4) = pack_bf16x4(acc * (1.f / wsum));
+  else
+    *reinterpret_cast<f32x4*>(a.out + orow * D + 4 * d4) = acc * (1.f / wsum);
   if (a.lse && d4 == 0) a.lse[orow] = (mx + __log2f(wsum)) * kLn2;
 }
 
@@ -712,9 +865,11 @@ hipError_t launch_extend_d(const ExtendArgs& a, hipStream_t stream, hipEvent_t d
   if (e != hipSuccess) return e;
   const hipEvent_t attention_done = a.num_merge > 0 ? nullptr : done;
   if (a.parts && a.part_rows == kExtendSmallRows)
-    e = launch(extend_attn_kernel<D, 4>, dim3(a.num_items), dim3(256), stream, attention_done, a);
+    e = launch(a.k_scale ? extend_attn_kernel<D, 4, true> : extend_attn_kernel<D, 4, false>, dim3(a.num_items), dim3(256),
+               stream, attention_done, a);
   else
-    e = launch(extend_attn_kernel<D, 12>, dim3(a.num_items), dim3(768), stream, attention_done, a);
+    e = launch(a.k_scale ? extend_attn_kernel<D, 12, true> : extend_attn_kernel<D, 12, false>, dim3(a.num_items), dim3(768),
+               stream, attention_done, a);
   if (e != hipSuccess || a.num_merge == 0) return e;
   constexpr int kRowsPerBlock = kMergeThreads / (D / 4);
   return launch(extend_merge_kernel<D>, dim3(a.num_merge, (a.part_rows + kRowsPerBlock - 1) / kRowsPerBlock),

@@ -33,6 +33,8 @@ constexpr int kWaves = 4;
 template <int D>
 __global__ __launch_bounds__(64 * kWaves) void kv_store_fp8_kernel(Store8Args a) {
   constexpr int kPieces = D / 64;
+  int i0 = (int(blockIdx.y) * int(gridDim.x) + int(blockIdx.x)) * 64 * kWaves + int(threadIdx.x);
+  const int copied = i0 < a.copy_ints ? a.copy_src[i0] : 0;
   const const_i32_ptr row = as_constant(a.rows) + size_t(blockIdx.x) * kItemInts;
   const int seq = row[0];
   const int pb = row[1];
@@ -112,6 +114,9 @@ __global__ __launch_bounds__(64 * kWaves) void kv_store_fp8_kernel(Store8Args a)
     fp8_store_tile<D>(codes, x, fp8_slot_bytes(new_slots, is_v, lane), old_scale, dst, scale, lane);
     if (opened && rem == 0 && lane == 0) a.block_table[entry0 + pg] = page;
   }
+  if (i0 < a.copy_ints) a.copy_dst[i0] = copied;
+  const int stride = int(gridDim.x) * int(gridDim.y) * 64 * kWaves;
+  for (i0 += stride; i0 < a.copy_ints; i0 += stride) a.copy_dst[i0] = a.copy_src[i0];
 }
 
 }  // namespace

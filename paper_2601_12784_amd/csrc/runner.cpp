@@ -530,15 +530,14 @@ extern "C" sf_status sf_runner_evict(sf_runner* r, const sf_attn_desc* desc, con
 
 // Extend attention, in memory that the caller lends: the pinned part is cut
 // into slots that the plans go round, the device part is the workspace.
-extern "C" sf_status sf_runner_extend(sf_runner* r, const sf_attn_desc* desc, const int32_t* seq_lens_host,
-                                      const int32_t* q_lens_host, const void* q, const void* k_new,
-                                      const void* v_new, void* k_pool, void* v_pool, const int32_t* block_table,
-                                      float* out, float* lse, sf_runner_memory* memory, void* stream,
-                                      sf_extend_info* info_out) {
+static sf_status runner_extend(sf_runner* r, const sf_attn_desc* desc, const int32_t* seq_lens_host,
+                               const int32_t* q_lens_host, const void* q, const void* k_new,
+                               const void* v_new, void* k_pool, void* v_pool, const int32_t* block_table,
+                               float* out, float* lse, sf_runner_memory* memory, void* stream,
+                               sf_extend_info* info_out, float* k_scale = nullptr, float* v_scale = nullptr,
+                               bool out_bf16 = false) {
   if (!r || !desc || !info_out || !memory) return SF_ERR_INVALID_ARG;
-  if (desc->num_q_heads != r->shape.num_q_heads || desc->num_kv_heads != r->shape.num_kv_heads ||
-      desc->head_dim != r->shape.head_dim || desc->page_size != r->shape.page_size)
-    return SF_ERR_INVALID_ARG;
+  if (!same_shape(r, desc)) return SF_ERR_INVALID_ARG;
   if ((reinterpret_cast<uintptr_t>(memory->pinned) | reinterpret_cast<uintptr_t>(memory->device)) & 15u)
     return SF_ERR_INVALID_ARG;
   hipStream_t main = static_cast<hipStream_t>(stream);
@@ -600,6 +599,14 @@ extern "C" sf_status sf_runner_extend(sf_runner* r, const sf_attn_desc* desc, co
   sf::ExtendArgs a;
   if ((st = sf::extend_args(desc, work_dev, q, k_new, v_new, k_pool, v_pool, block_table, out, lse, &a)) != SF_OK)
     return st;
+  a.k_scale = k_scale;
+  a.v_scale = v_scale;
+  a.out_bf16 = out_bf16;
+  sf::Store8Args store8 = {};
+  if (k_scale && store &&
+      (st = sf::store8_args(desc, work_dev, k_new, v_new, nullptr, k_pool, v_pool, k_scale, v_scale,
+                            const_cast<int32_t*>(block_table), &store8)) != SF_OK)
+    return st;
   // Calls of another stream may still use the device memory: they are waited
   // for (calls on one stream are in order by themselves).
   if (main != lent.last_stream && lent.last_stream != kNoStream) {
@@ -630,7 +637,19 @@ extern "C" sf_status sf_runner_extend(sf_runner* r, const sf_attn_desc* desc, co
     a.items = a.copy_dst;
   }
   a.merge_rows = a.items + int64_t(plan.num_parts) * sf::kItemInts;
-  if (sf::launch_extend(a, main, mark ? lent.done[slot] : nullptr) != hipSuccess) {
+  hipError_t launched = hipSuccess;
+  if (k_scale && store) {   // a store launch of its own, with the same rows and side job
+    store8.rows = a.store_rows;
+    store8.num_rows = plan.num_store;
+    store8.copy_src = a.copy_src;
+    store8.copy_dst = a.copy_dst;
+    store8.copy_ints = a.copy_ints;
+    a.k_new = a.v_new = nullptr;
+    a.num_store = a.copy_ints = 0;
+    launched = sf::launch_store_fp8(store8, main);
+  }
+  if (launched == hipSuccess) launched = sf::launch_extend(a, main, mark ? lent.done[slot] : nullptr);
+  if (launched != hipSuccess) {
     // An earlier launch of the call may read the slot, with no event behind it.
     (void)hipStreamSynchronize(main);
     return SF_ERR_HIP;
@@ -645,6 +664,27 @@ extern "C" sf_status sf_runner_extend(sf_runner* r, const sf_attn_desc* desc, co
   }
   ++lent.next;
   return SF_OK;
+}
+
+extern "C" sf_status sf_runner_extend(sf_runner* r, const sf_attn_desc* desc, const int32_t* seq_lens_host,
+                                      const int32_t* q_lens_host, const void* q, const void* k_new,
+                                      const void* v_new, void* k_pool, void* v_pool, const int32_t* block_table,
+                                      float* out, float* lse, sf_runner_memory* memory, void* stream,
+                                      sf_extend_info* info_out) {
+  return runner_extend(r, desc, seq_lens_host, q_lens_host, q, k_new, v_new, k_pool, v_pool, block_table, out, lse,
+                       memory, stream, info_out);
+}
+
+extern "C" sf_status sf_runner_extend_fp8(sf_runner* r, const sf_attn_desc* desc, const int32_t* seq_lens_host,
+                                          const int32_t* q_lens_host, const void* q, const void* k_new,
+                                          const void* v_new, void* k_pool8, void* v_pool8, const int32_t* block_table,
+                                          void* out, float* lse, sf_runner_memory* memory, void* stream,
+                                          sf_extend_info* info_out, float* k_scale, float* v_scale, int32_t out_bf16) {
+  if (!k_scale || !v_scale || ((reinterpret_cast<uintptr_t>(k_scale) | reinterpret_cast<uintptr_t>(v_scale)) & 3u) ||
+      (out_bf16 | 1) != 1)
+    return SF_ERR_INVALID_ARG;
+  return runner_extend(r, desc, seq_lens_host, q_lens_host, q, k_new, v_new, k_pool8, v_pool8, block_table,
+                       static_cast<float*>(out), lse, memory, stream, info_out, k_scale, v_scale, out_bf16 != 0);
 }
 
 namespace {

@@ -163,6 +163,9 @@ struct Store8Args {
   int32_t num_kv_heads;
   int32_t head_dim;
   int32_t bt_stride;
+  const int32_t* copy_src;    // optional side job: ints from pinned host memory to the device, for the launch behind
+  int32_t* copy_dst;
+  int32_t copy_ints;
 };
 sf_status store8_args(const sf_attn_desc* desc, const int32_t* work_dev, const void* k_new, const void* v_new,
                       const int32_t* new_pages, void* k_pool8, void* v_pool8, float* k_scale, float* v_scale,
@@ -287,6 +290,11 @@ struct ExtendArgs {
   const int32_t* copy_src;    // the part and merge rows in pinned host memory
   int32_t* copy_dst;          // and their device copy
   int32_t copy_ints;
+  // fp8 cache (NULL otherwise): the pools hold E4M3 codes, these the scales;
+  // out is bf16 where out_bf16 is set.
+  const float* k_scale;
+  const float* v_scale;
+  bool out_bf16;
 };
 
 // Rows (tokens x query heads of a group) of one extend work item: of the plan
