@@ -1370,10 +1370,13 @@ class DecodeLoopRunner:
     """Multi-step decode over a growing paged cache: per step, PageTable
     bookkeeping on the host, then append-then-attend and the merge of split
     sequences on the GPU. The first step (the prompt) only attends.
-    block_table is the device table the kernels read and extend."""
+    block_table is the device table the kernels read and extend. With fp8 =
+    (k_scale, v_scale) the pools are an fp8 cache. A loop with a budget calls
+    key_weights after its steps and evict every so many of them; the lengths of
+    the step after an eviction go on from the kept tokens."""
 
     def __init__(self, num_q_heads, num_kv_heads, head_dim, k_pool, v_pool, block_table, bt_host, lens0,
-                 scale, device=None, num_cus=None, attn=None):
+                 scale, device=None, num_cus=None, attn=None, fp8=None):
         """attn: an existing DecodeAttention of the same head geometry to reuse
         (its native runner keeps its pinned ring and workspace across loops)."""
         if attn is not None and (attn.hq, attn.hkv, attn.d) != (int(num_q_heads), int(num_kv_heads), int(head_dim)):
@@ -1381,6 +1384,8 @@ class DecodeLoopRunner:
         self.attn = attn or DecodeAttention(num_q_heads, num_kv_heads, head_dim, device=device, num_cus=num_cus)
         self.k_pool, self.v_pool, self.block_table, self.scale = k_pool, v_pool, block_table, float(scale)
         self.table = PageTable(k_pool.shape[0], bt_host, lens0)
+        self.fp8 = fp8
+        self.evicted = np.zeros(self.table.prev.size, dtype=np.int32)   # tokens given up so far, per sequence
         self.steps = 0
 
     @property
@@ -1404,6 +1409,25 @@ class DecodeLoopRunner:
             self.attn._host_checked = True
         append = (k_new, v_new, new_pages) if appending else None
         out = self.attn(q, self.k_pool, self.v_pool, self.block_table, lens.astype(np.int32), self.scale,
-                        out=out, lse=lse, stream=stream, attn_events=attn_events, append=append)
+                        out=out, lse=lse, stream=stream, attn_events=attn_events, append=append, fp8=self.fp8)
         self.steps += 1
         return out
+
+    def key_weights(self, q, lse, weights, positions, stream=None):
+        """Adds the last step's attention weights (its q and lse) to weights; the tokens that it appended, or before
+        the first one every token, start there and get their positions."""
+        lens = self.table.prev
+        held = np.where(lens > 0, lens - 1, 0).astype(np.int32) if self.steps > 1 else np.zeros_like(lens)
+        self.attn.key_weights(q, lse, self.k_pool, self.block_table, lens, (lens > 0).astype(np.int32), self.scale, weights,
+                              positions=positions, held_lens=held, first_pos=held + self.evicted,
+                              k_scale=None if self.fp8 is None else self.fp8[0], stream=stream)
+
+    def evict(self, keep, weights, positions, sinks=0, recent=0, stream=None):
+        """Evicts every running sequence to at most keep tokens and frees the pages behind them. Returns the lengths."""
+        lens = self.table.prev
+        kept = np.minimum(lens, keep).astype(np.int32)
+        self.attn.evict(self.k_pool, self.v_pool, self.block_table, lens, kept, weights, positions,
+                        ends=lens + self.evicted, sinks=sinks, recent=recent, fp8=self.fp8, stream=stream)
+        self.table.truncate(kept)
+        self.evicted = self.evicted + (lens - kept)
+        return kept
