@@ -427,12 +427,12 @@ sf_status sf_kv_store_fp8(const sf_attn_desc* desc, const sf_store_info* info, c
  * not change from run to run. No page may be part of two sequences.
  */
 typedef struct sf_weights_info {
-  int32_t num_items;         /* work items (one 256-thread workgroup each) */
+  int32_t num_items;         /* rows of items (steps = 0: one 256-thread workgroup each) */
   int32_t num_merge;         /* items cut into parts */
   int32_t num_slots;         /* their parts */
-  int32_t item_pages;        /* pages per item, at most: a multiple of 16 up to 64 */
+  int32_t item_pages;        /* pages per item, at most: 16 */
   int32_t num_q_rows;        /* T */
-  int32_t reserved;          /* 0 */
+  int32_t steps;             /* > 0: waves that stream equal shares of the keys (rule below) */
   uint64_t work_bytes;       /* (num_items + num_merge) * 64 */
   uint64_t workspace_bytes;  /* num_slots * item_pages * 64 */
   uint64_t desc_key;         /* fingerprint of the descriptor */
@@ -444,17 +444,21 @@ typedef struct sf_weights_info {
  * first_pos_host NULL: first_pos_s = held_s. 0 <= held_s <= L_s; positions stay
  * below 2^31; the other lengths as sf_kv_store_fp8_plan. opts (may be NULL):
  * num_cus only.
- * Rule: each (sequence, block of item_pages pages, KV head) is an item that
- * walks the new tokens t0 .. E_s - 1 that see its first key. If no sequence
- * has more than 64 query rows per KV head, item_pages is the number of pages over
- * 8 num_cus, rounded up to a multiple of 16, at least 16 and at most 64; else it
- * is 16, and walks are cut into the fewest equal parts of at most
- * max(1, floor(16 m / g)) tokens, m = max(8, floor(row tiles of all items / (8
- * num_cus))), with ceil(tokens g / 16) row tiles per item.
+ * Rule. If no sequence has more than 16 query rows per KV head (a decode step):
+ * the blocks of four pages (the last of a pair shorter) of the pairs (sequence
+ * with E_s > 0, KV head), in that order end to end, are N; W = min(8 num_cus, N)
+ * waves take the blocks [floor(N w / W), floor(N (w + 1) / W)), cut at pair ends
+ * into segments. Rows 0 .. W - 1 are the waves' first segments, the others follow
+ * wave by wave; steps = W, and int 12 of a row is that of the wave's next segment, or -1.
+ * Else each (sequence, block of 16 pages, KV head) is an item that walks the new
+ * tokens t0 .. E_s - 1 that see its first key; walks are cut into the fewest equal
+ * parts of at most max(1, floor(16 m / g)) tokens, m = max(8, floor(row tiles of all items /
+ * (8 num_cus))), with ceil(tokens g / 16) row tiles per item. Items with the most
+ * row tiles come first; equal ones keep the order sequence, block, KV head, part.
  * Work list, int32 rows of 16: num_items rows seq, kv_head, first page, end
  * page, first token, end token, part slot (-1: uncut), L_s, P_s, cu_s, held_s,
- * first_pos_s, 0 ..; then num_merge rows with the first part slot and the
- * number of parts in place of the tokens.
+ * first_pos_s, next row (0 with steps = 0), 0 ..; then num_merge rows with the first part slot
+ * and the number of parts in place of the tokens.
  */
 sf_status sf_key_weights_plan(const sf_attn_desc* desc, const int32_t* seq_lens_host, const int32_t* q_lens_host,
                               const int32_t* held_lens_host, const int32_t* first_pos_host, const sf_plan_opts* opts,

@@ -221,34 +221,50 @@ def store_plan(seq_lens, q_lens):
 
 
 def weights_plan(seq_lens, q_lens, hq, hkv, held=None, first_pos=None, num_cus=256):
-    """(items, merges, pages per item)."""
+    """(items, merges, waves)."""
     g = hq // hkv
     cu = cu_lens(q_lens)
     live = [s for s in range(len(seq_lens)) if q_lens[s] > 0]
-    pages = sum(_pages(seq_lens[s]) for s in live)
-    if max([q_lens[s] * g for s in live], default=0) <= 64:
-        size, tokens = min(64, max(16, -(-(pages * hkv // (8 * num_cus)) // 16) * 16)), None
-    else:
-        size = 16
-        tiles = sum(-(-((q_lens[s] - max(0, p * PAGE - (seq_lens[s] - q_lens[s]))) * g) // 16)
-                    for s in live for p in range(0, _pages(seq_lens[s]), 16))
-        tokens = max(1, max(8, tiles * hkv // (8 * num_cus)) * 16 // g)
+
+    def row(s, h, p0, p1, t0, t1, slot, following=0):
+        h0 = seq_lens[s] - q_lens[s] if held is None else held[s]
+        return [s, h, p0, p1, t0, t1, slot, seq_lens[s], seq_lens[s] - q_lens[s], int(cu[s]), h0,
+                h0 if first_pos is None else first_pos[s], following, 0, 0, 0]
+
+    if max([q_lens[s] * g for s in live], default=0) <= 16:
+        blocks = [(s, h, p) for s in live for h in range(hkv) for p in range(0, _pages(seq_lens[s]), 4)]
+        waves = min(8 * num_cus, len(blocks))
+        first, rest = [], []
+        for w in range(waves):
+            mine = blocks[len(blocks) * w // waves: len(blocks) * (w + 1) // waves]
+            pairs = sorted(set((s, h) for s, h, _ in mine))
+            segments = []
+            for s, h in pairs:
+                p = [x[2] for x in mine if x[:2] == (s, h)]
+                segments.append(row(s, h, p[0], min(_pages(seq_lens[s]), p[-1] + 4), 0, q_lens[s], -1, -1))
+            at = [w] + [waves + len(rest) + i for i in range(len(segments) - 1)]
+            for i, r in enumerate(segments[:-1]):
+                r[12] = at[i + 1]
+            first.append(segments[0])
+            rest += segments[1:]
+        return first + rest, [], waves
+    tiles = sum(-(-((q_lens[s] - max(0, p * PAGE - (seq_lens[s] - q_lens[s]))) * g) // 16)
+                for s in live for p in range(0, _pages(seq_lens[s]), 16))
+    tokens = max(1, max(8, tiles * hkv // (8 * num_cus)) * 16 // g)
     items, merges, slot = [], [], 0
     for s in live:
         L, e = seq_lens[s], q_lens[s]
-        h0 = L - e if held is None else held[s]
-        tail = [L, L - e, int(cu[s]), h0, h0 if first_pos is None else first_pos[s], 0, 0, 0, 0]
-        for p in range(0, _pages(L), size):
-            t0 = max(0, p * PAGE - (L - e))
-            parts = 1 if tokens is None else -(-(e - t0) // tokens)
+        for p in range(0, _pages(L), 16):
+            t0, end = max(0, p * PAGE - (L - e)), min(_pages(L), p + 16)
+            parts = -(-(e - t0) // tokens)
             for h in range(hkv):
-                head = [s, h, p, min(_pages(L), p + size)]
                 if parts > 1:
-                    merges.append(head + [slot, parts, -1] + tail)
+                    merges.append(row(s, h, p, end, slot, parts, -1))
                 for i in range(parts):
-                    items.append(head + [t0 + (e - t0) * i // parts, t0 + (e - t0) * (i + 1) // parts, slot if parts > 1 else -1] + tail)
+                    items.append(row(s, h, p, end, t0 + (e - t0) * i // parts, t0 + (e - t0) * (i + 1) // parts, slot if parts > 1 else -1))
                     slot += parts > 1
-    return items, merges, size
+    items.sort(key=lambda r: -(-((r[5] - r[4]) * g) // 16), reverse=True)   # the most row tiles first
+    return items, merges, 0
 
 
 def evict_plan(seq_lens, keep_lens, hkv, ends=None):

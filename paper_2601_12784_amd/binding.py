@@ -69,7 +69,7 @@ class sf_store_info(ctypes.Structure):
 
 class sf_weights_info(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("num_items", "num_merge", "num_slots", "item_pages", "num_q_rows",
-                                              "reserved")] + \
+                                              "steps")] + \
                [(n, ctypes.c_uint64) for n in ("work_bytes", "workspace_bytes", "desc_key")]
 
 

@@ -5,6 +5,7 @@
 #include <climits>
 #include <cstdint>
 #include <cstring>
+#include <vector>
 
 #include "sf_internal.h"
 
@@ -129,55 +130,84 @@ extern "C" sf_status sf_kv_store_fp8(const sf_attn_desc* desc, const sf_store_in
 // ---------------------------------------------------------------------------
 namespace {
 
-// A work item is a block of pages of one (sequence, KV head), 64 keys per wave
-// at a time; its cost is the walk over its query rows, 16 per tile. Few rows
-// (a decode step's one token) are bound by reading the keys: blocks of up to 64
-// pages, as few as still give every compute unit eight. Many rows (prompts) take
-// blocks of 16 pages, one walk per wave, and walks longer than about an eighth of a
+// A decode step (at most 16 query rows per (sequence, KV head), one row tile) is
+// bound by reading the keys: the pairs' keys, in blocks of four pages laid end to end,
+// are cut into equal slices, one per wave, two waves per SIMD (one takes as long, three
+// per two SIMDs 10 % longer).
+// Other calls are made of items, a block of 16 pages of one (sequence, KV head), whose cost is
+// the walk over its query rows, 16 per tile. Walks longer than about an eighth of a
 // compute unit's share are cut into parts, so that no walk is longer than the rest.
 constexpr int32_t kItemPages = 4 * kWeightPages;
-constexpr int32_t kMaxItemPages = 4 * kItemPages;
-constexpr int32_t kShortRows = 64;
+constexpr int32_t kStepRows = 16;
+constexpr int64_t kStepWavesPerCu = 8;
 constexpr int64_t kItemsPerCu = 8;
 constexpr int64_t kShortestPart = 8;   // row tiles
 
-struct WeightCut {
-  int32_t item_pages;
-  int64_t part_tokens;
-};
-
-template <class F>   // f(sequence, first page, end page, first token that sees the block, parts)
-void for_weight_items(const sf_attn_desc* d, const int32_t* lens, const int32_t* news, const WeightCut& cut, F f) {
+// Calls f(sequence, first page, end page, first token that sees the block, parts) for every item.
+template <class F>
+void for_weight_items(const sf_attn_desc* d, const int32_t* lens, const int32_t* news, int64_t part_tokens, F f) {
   for (int32_t s = 0; s < d->num_seqs; ++s) {
     if (news[s] == 0) continue;
     const int32_t pages = pages_of(lens[s]), prefix = lens[s] - news[s];
-    for (int32_t p = 0; p < pages; p += cut.item_pages) {
+    for (int32_t p = 0; p < pages; p += kItemPages) {
       const int32_t t0 = std::max(0, p * kPage - prefix);
-      f(s, p, std::min(pages, p + cut.item_pages), t0, int32_t((news[s] - t0 + cut.part_tokens - 1) / cut.part_tokens));
+      f(s, p, std::min(pages, p + kItemPages), t0, int32_t((news[s] - t0 + part_tokens - 1) / part_tokens));
     }
   }
 }
 
-WeightCut choose_weight_cut(const sf_attn_desc* d, const int32_t* lens, const int32_t* news, int32_t num_cus) {
-  const int64_t g = d->num_q_heads / d->num_kv_heads, hkv = d->num_kv_heads, cus = num_cus;
-  int64_t pages = 0, most = 0;
-  for (int32_t s = 0; s < d->num_seqs; ++s) {
-    if (news[s] == 0) continue;
-    pages += pages_of(lens[s]);
-    most = std::max<int64_t>(most, news[s] * g);
+struct WeightRow {
+  int32_t v[kWeightInts];
+};
+
+// What the rows of a sequence have in common.
+struct WeightSeqs {
+  const int32_t *lens, *news, *held, *pos;
+  WeightRow row(int32_t s, int32_t h, int32_t pb, int32_t pe, int32_t t0, int32_t t1, int32_t slot, int64_t qrow) const {
+    const int32_t from = held ? held[s] : lens[s] - news[s];
+    return {{s, h, pb, pe, t0, t1, slot, lens[s], lens[s] - news[s], int32_t(qrow), from, pos ? pos[s] : from}};
   }
-  WeightCut cut = {kItemPages, INT32_MAX};
-  if (most <= kShortRows) {
-    const int64_t each = (pages * hkv / (kItemsPerCu * cus) + kItemPages - 1) / kItemPages * kItemPages;
-    cut.item_pages = int32_t(std::min<int64_t>(kMaxItemPages, std::max<int64_t>(kItemPages, each)));
-    return cut;
+};
+
+int32_t blocks_of(int32_t tokens) { return (pages_of(tokens) + kWeightPages - 1) / kWeightPages; }
+
+// A decode step's rows: wave w's first segment is row w, the others follow the
+// first `waves` rows. Returns the number of rows; work may be NULL.
+int64_t plan_weight_steps(const sf_attn_desc* d, const WeightSeqs& q, int64_t blocks, int64_t waves, int32_t* work) {
+  int64_t extra = waves, done = 0, wave = 0, qrow = 0;
+  int64_t cut = blocks / waves, rest = 0;   // the wave's end, floor(blocks (wave + 1) / waves), stepped without divisions
+  const int64_t step = blocks / waves, over = blocks % waves;
+  rest = over;
+  int64_t at = 0, last = -1;   // row of the next segment; the wave's last row so far
+  for (int32_t s = 0; s < d->num_seqs; qrow += q.news[s++]) {
+    if (q.news[s] == 0) continue;
+    const int32_t pages = pages_of(q.lens[s]), n = blocks_of(q.lens[s]);
+    for (int32_t h = 0; h < d->num_kv_heads; ++h)
+      for (int32_t b = 0; b < n;) {
+        const int32_t take = int32_t(std::min<int64_t>(n - b, cut - done));
+        if (work) {
+          WeightRow r = q.row(s, h, b * kWeightPages, std::min(pages, (b + take) * kWeightPages), 0, q.news[s], -1, qrow);
+          r.v[12] = -1;
+          std::memcpy(work + at * kWeightInts, &r, sizeof r);
+          if (last >= 0) work[last * kWeightInts + 12] = int32_t(at);
+        }
+        b += take;
+        done += take;
+        if (done == cut) {   // the next wave starts
+          at = ++wave;
+          last = -1;
+          cut += step;
+          if ((rest += over) >= waves) {
+            rest -= waves;
+            ++cut;
+          }
+        } else {
+          last = at;
+          at = extra++;
+        }
+      }
   }
-  int64_t tiles = 0;
-  for_weight_items(d, lens, news, cut,
-                   [&](int32_t s, int32_t, int32_t, int32_t t0, int32_t) { tiles += ((news[s] - t0) * g + 15) / 16; });
-  const int64_t part = std::max(kShortestPart, tiles * hkv / (kItemsPerCu * cus));
-  cut.part_tokens = std::max<int64_t>(1, part * 16 / g);
-  return cut;
+  return extra;
 }
 
 }  // namespace
@@ -191,54 +221,91 @@ extern "C" sf_status sf_key_weights_plan(const sf_attn_desc* desc, const int32_t
   sf_status st = check_lengths(desc, seq_lens_host, q_lens_host, &tokens);
   if (st != SF_OK) return st;
   if (opts && opts->num_cus < 0) return SF_ERR_INVALID_ARG;
+  const WeightSeqs q = {seq_lens_host, q_lens_host, held_lens_host, first_pos_host};
   const int32_t *lens = seq_lens_host, *news = q_lens_host;
+  const int64_t g = desc->num_q_heads / desc->num_kv_heads, hkv = desc->num_kv_heads;
+  const int64_t cus = opts && opts->num_cus > 0 ? opts->num_cus : kDefaultNumCus;
+  int64_t blocks = 0, most = 0;
   for (int32_t s = 0; s < desc->num_seqs; ++s) {
     const int32_t held = held_lens_host ? held_lens_host[s] : lens[s] - news[s];
     const int32_t pos = first_pos_host ? first_pos_host[s] : held;
     if (held < 0 || held > lens[s] || pos < 0 || int64_t(pos) + (lens[s] - held) > INT32_MAX) return SF_ERR_INVALID_ARG;
+    if (news[s] == 0) continue;
+    blocks += blocks_of(lens[s]) * hkv;
+    most = std::max<int64_t>(most, news[s] * g);
   }
-  const WeightCut cut =
-      choose_weight_cut(desc, lens, news, opts && opts->num_cus > 0 ? opts->num_cus : kDefaultNumCus);
-  const int32_t hkv = desc->num_kv_heads;
+  info->num_items = info->num_merge = info->num_slots = info->steps = 0;
+  info->item_pages = kItemPages;
+  info->num_q_rows = int32_t(tokens);
+  info->work_bytes = info->workspace_bytes = 0;
+  info->desc_key = desc_key(desc);
+  if (blocks == 0) return SF_OK;
+
+  if (most <= kStepRows) {
+    const int64_t waves = std::min(kStepWavesPerCu * cus, blocks);
+    if (waves + blocks > INT32_MAX / kWeightInts) return SF_ERR_INVALID_ARG;
+    const int64_t rows = plan_weight_steps(desc, q, blocks, waves, nullptr);
+    info->num_items = int32_t(rows);
+    info->steps = int32_t(waves);
+    info->work_bytes = uint64_t(rows) * kWeightInts * 4;
+    if (!work_host) return SF_OK;
+    if (work_capacity_bytes < info->work_bytes) return SF_ERR_CAPACITY;
+    plan_weight_steps(desc, q, blocks, waves, work_host);
+    return SF_OK;
+  }
+
+  int64_t tiles = 0;
+  for_weight_items(desc, lens, news, INT32_MAX,
+                   [&](int32_t s, int32_t, int32_t, int32_t t0, int32_t) { tiles += ((news[s] - t0) * g + 15) / 16; });
+  const int64_t part = std::max(kShortestPart, tiles * hkv / (kItemsPerCu * cus));
+  const int64_t part_tokens = std::max<int64_t>(1, part * 16 / g);
   int64_t items = 0, merges = 0, slots = 0;
-  for_weight_items(desc, lens, news, cut, [&](int32_t, int32_t, int32_t, int32_t, int32_t parts) {
-    items += int64_t(parts) * hkv;
-    if (parts > 1) merges += hkv, slots += int64_t(parts) * hkv;
+  for_weight_items(desc, lens, news, part_tokens, [&](int32_t, int32_t, int32_t, int32_t, int32_t parts) {
+    items += parts * hkv;
+    if (parts > 1) merges += hkv, slots += parts * hkv;
   });
   if (items + merges > INT32_MAX / kWeightInts) return SF_ERR_INVALID_ARG;
   info->num_items = int32_t(items);
   info->num_merge = int32_t(merges);
   info->num_slots = int32_t(slots);
-  info->item_pages = cut.item_pages;
-  info->num_q_rows = int32_t(tokens);
-  info->reserved = 0;
   info->work_bytes = uint64_t(items + merges) * kWeightInts * 4;
-  info->workspace_bytes = uint64_t(slots) * cut.item_pages * kPage * 4;
-  info->desc_key = desc_key(desc);
+  info->workspace_bytes = uint64_t(slots) * kItemPages * kPage * 4;
   if (!work_host) return SF_OK;
   if (work_capacity_bytes < info->work_bytes) return SF_ERR_CAPACITY;
-  int32_t *item = work_host, *merge = work_host + items * kWeightInts;
+  // Items with the most row tiles first (a counting sort; equal ones keep the order sequence, block, KV head, part).
+  auto tiles_of = [&](int64_t n) { return size_t((n * g + 15) / 16); };
+  auto part_begin = [](int32_t t0, int64_t span, int32_t i, int32_t parts) { return t0 + int32_t(span * i / parts); };
+  std::vector<int64_t> at;
+  try {
+    at.assign(tiles_of(std::min(part_tokens, tokens)) + 1, 0);
+  } catch (...) {
+    return SF_ERR_CAPACITY;
+  }
+  for_weight_items(desc, lens, news, part_tokens, [&](int32_t s, int32_t, int32_t, int32_t t0, int32_t parts) {
+    for (int32_t i = 0; i < parts; ++i)
+      at[tiles_of(part_begin(t0, news[s] - t0, i + 1, parts) - part_begin(t0, news[s] - t0, i, parts))] += hkv;
+  });
+  for (int64_t i = int64_t(at.size()) - 1, sum = 0; i >= 0; --i) {
+    const int64_t n = at[size_t(i)];
+    at[size_t(i)] = sum;
+    sum += n;
+  }
+  int32_t* merge = work_host + items * kWeightInts;
   int32_t slot = 0, last = 0;
   int64_t qrow = 0;
-  for_weight_items(desc, lens, news, cut, [&](int32_t s, int32_t pb, int32_t pe, int32_t t0, int32_t parts) {
+  for_weight_items(desc, lens, news, part_tokens, [&](int32_t s, int32_t pb, int32_t pe, int32_t t0, int32_t parts) {
     for (; last < s; ++last) qrow += news[last];
-    const int32_t held = held_lens_host ? held_lens_host[s] : lens[s] - news[s];
-    const int32_t pos = first_pos_host ? first_pos_host[s] : held;
     for (int32_t h = 0; h < hkv; ++h) {
-      int32_t row[kWeightInts] = {s, h, pb, pe, 0, 0, -1, lens[s], lens[s] - news[s], int32_t(qrow), held, pos};
       if (parts > 1) {
-        row[4] = slot;
-        row[5] = parts;
-        std::memcpy(merge, row, sizeof row);
+        const WeightRow r = q.row(s, h, pb, pe, slot, parts, -1, qrow);
+        std::memcpy(merge, &r, sizeof r);
         merge += kWeightInts;
       }
       const int64_t span = news[s] - t0;
       for (int32_t i = 0; i < parts; ++i) {
-        row[4] = t0 + int32_t(span * i / parts);
-        row[5] = t0 + int32_t(span * (i + 1) / parts);
-        row[6] = parts > 1 ? slot++ : -1;
-        std::memcpy(item, row, sizeof row);
-        item += kWeightInts;
+        const WeightRow r = q.row(s, h, pb, pe, part_begin(t0, span, i, parts), part_begin(t0, span, i + 1, parts),
+                                  parts > 1 ? slot++ : -1, qrow);
+        std::memcpy(work_host + at[tiles_of(r.v[5] - r.v[4])]++ * kWeightInts, &r, sizeof r);
       }
     }
   });
@@ -257,6 +324,7 @@ sf_status sf::weight_args(const sf_attn_desc* desc, const sf_weights_info* info,
   WeightArgs a = {};
   a.items = work_dev;
   a.num_items = info->num_items;
+  a.steps = info->steps;
   a.merge_rows = work_dev + int64_t(info->num_items) * kWeightInts;
   a.num_merge = info->num_merge;
   a.q = static_cast<const uint16_t*>(q);
@@ -289,7 +357,7 @@ extern "C" sf_status sf_key_weights(const sf_attn_desc* desc, const sf_weights_i
   if (st != SF_OK) return st;
   if (!info) return SF_ERR_INVALID_ARG;
   if (info->desc_key != desc_key(desc) || info->num_items < 0 || info->num_merge < 0 || info->num_slots < 0 ||
-      info->reserved != 0 || info->item_pages < kItemPages || info->item_pages > kMaxItemPages ||
+      info->steps < 0 || info->steps > info->num_items || (info->steps > 0 && info->num_merge > 0) || info->item_pages != kItemPages ||
       info->work_bytes != (uint64_t(info->num_items) + info->num_merge) * kWeightInts * 4 ||
       info->workspace_bytes != uint64_t(info->num_slots) * info->item_pages * kPage * 4)
     return SF_ERR_PLAN_MISMATCH;

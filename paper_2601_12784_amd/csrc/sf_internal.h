@@ -180,6 +180,7 @@ struct WeightArgs {
   // directly), L, P, query row of the sequence's first new token, held, position of key `held`, 0 ..
   const int32_t* items;
   int32_t num_items;
+  int32_t steps;              // > 0: waves that stream the keys of at most 16 rows each (int 12: the row that follows, -1)
   const int32_t* merge_rows;  // the same with first part slot and parts in place of the tokens
   int32_t num_merge;
   const uint16_t* q;          // [T][Hq][D]

@@ -53,17 +53,22 @@ def test_store_plan(lens, news):
 def test_weights_plan(lens, news, heads):
     hq, hkv = heads
     info, work = B.sf_key_weights_plan(_desc(lens, hq, hkv), lens, news)
-    items, merges, size = R.weights_plan(lens, news, hq, hkv)
-    assert (info.num_items, info.num_merge) == (len(items), len(merges))
+    items, merges, waves = R.weights_plan(lens, news, hq, hkv)
+    assert (info.num_items, info.num_merge, info.steps) == (len(items), len(merges), waves)
     assert _rows(work, info, 16) == items + merges
-    if items:
-        assert info.item_pages == size
-    # the parts of every (sequence, KV head) cover its keys' query rows once
     seen = {}
-    for s, h, p0, p1, t0, t1, slot, L, P, cu, held, pos, *rest in items:
-        assert 0 <= t0 < t1 <= news[s] and 0 <= p0 < p1 <= -(-L // 16) and p1 - p0 <= size and rest == [0] * 4
-        seen.setdefault((s, h, p0), []).append((t0, t1))
+    for s, h, p0, p1, t0, t1, slot, L, P, cu, held, pos, following, *rest in items:
+        assert 0 <= t0 < t1 <= news[s] and 0 <= p0 < p1 <= -(-L // 16) and rest == [0] * 3
+        seen.setdefault((s, h) if waves else (s, h, p0), []).append((p0, p1) if waves else (t0, t1))
+    if waves:   # the segments of every (sequence, KV head) cover its pages once
+        for (s, h), spans in seen.items():
+            spans.sort()
+            assert spans[0][0] == 0 and spans[-1][1] == -(-lens[s] // 16)
+            assert all(a[1] == b[0] for a, b in zip(spans, spans[1:]))
+        return
+    # the parts of every block of keys cover the query rows that see it once
     for (s, h, p0), spans in seen.items():
+        spans.sort()
         assert spans[0][0] == max(0, p0 * 16 - (lens[s] - news[s])) and spans[-1][1] == news[s]
         assert all(a[1] == b[0] for a, b in zip(spans, spans[1:]))
 

@@ -421,6 +421,7 @@ WEIGHTS = [
     ([90, 33, 17, 48, 20], [20, 1, 17, 16, 0]),
     ([700, 65], [700, 65]),
     ([5000], [3]),
+    ([9000, 4000], [1, 1]),
     ([1030, 16], [40, 9]),
 ]
 
@@ -474,6 +475,9 @@ def test_key_weights(heads, fp8, lens, news):
     assert np.array_equal(pos, want_pos)
     again, _ = run_weights(*args, runner=False, in_place=True)
     assert np.array_equal(again[touched], got[touched])           # in place, by the plan form: the same bits
+    one, pos = run_weights(*args, runner=False, opts=B.make_opts(num_cus=1))   # eight waves, many blocks of keys each
+    check(one[touched], want[touched], tol[touched], "weights, one compute unit")
+    assert np.array_equal(pos, want_pos)
 
 
 def test_key_weights_cut_walks_are_the_same_up_to_rounding():
