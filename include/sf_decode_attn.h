@@ -497,6 +497,8 @@ typedef struct sf_evict_info {
   int32_t sinks, recent;     /* as given to the plan */
   int32_t boundary;          /* some sequence gives up tokens and its n_s ends inside a page */
   int32_t hole_pages;        /* Hkv * sum_s ceil(n_s / 16) */
+  int32_t num_long;          /* sequences of more than 4096 tokens */
+  int32_t reserved;          /* 0 */
   uint64_t work_bytes;       /* (num_seqs + num_moves) * 32 */
   uint64_t workspace_bytes;  /* hole_pages * 8, rounded up to 256, + Hkv * sum_s min(n_s, L_s - n_s) * 4 */
   uint64_t desc_key;         /* fingerprint of the descriptor */
@@ -507,9 +509,9 @@ typedef struct sf_evict_info {
  * L_s (nothing was evicted before). SF_ERR_INVALID_ARG for a negative length,
  * sinks or recent, L_s > min(16 * block_table_stride, 2^30), end_s < L_s, and
  * n_s < min(L_s, sinks + recent). Work list, int32 rows of 8: num_seqs rows L_s,
- * n_s, first hole page, first tail, end_s, 0 ..; then the moves, runs of one of the
+ * n_s, first hole page, first tail, end_s, s, 0, 0, those of more than 4096 tokens first; then the moves, runs of one of the
  * first ceil(n_s / 16) pages, or of up to 4 where there are more than 2048 in all: seq, first page,
- * pages, 0 ...
+ * pages, L_s, n_s, first hole page, first tail, 0.
  */
 sf_status sf_kv_evict_plan(const sf_attn_desc* desc, const int32_t* seq_lens_host, const int32_t* keep_lens_host,
                            const int32_t* ends_host, int32_t sinks, int32_t recent, int32_t* work_host,

@@ -272,8 +272,8 @@ def evict_plan(seq_lens, keep_lens, hkv, ends=None):
     run = 4 if sum(_pages(x) for x in n) > 2048 else 1
     rows, moved, hole, tail = [], [], 0, 0
     for s, L in enumerate(seq_lens):
-        rows.append([L, n[s], hole, tail, L if ends is None else ends[s], 0, 0, 0])
+        rows.append([L, n[s], hole, tail, L if ends is None else ends[s], s, 0, 0])
+        moved += [[s, p, min(run, _pages(n[s]) - p), L, n[s], hole, tail, 0] for p in range(0, _pages(n[s]), run)]
         hole += _pages(n[s]) * hkv
         tail += min(n[s], L - n[s]) * hkv
-        moved += [[s, p, min(run, _pages(n[s]) - p), 0, 0, 0, 0, 0] for p in range(0, _pages(n[s]), run)]
-    return rows, moved, hole, tail
+    return sorted(rows, key=lambda r: r[0] <= 4096), moved, hole, tail

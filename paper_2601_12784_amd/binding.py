@@ -74,7 +74,8 @@ class sf_weights_info(ctypes.Structure):
 
 
 class sf_evict_info(ctypes.Structure):
-    _fields_ = [(n, ctypes.c_int32) for n in ("num_seqs", "num_moves", "sinks", "recent", "boundary", "hole_pages")] + \
+    _fields_ = [(n, ctypes.c_int32) for n in ("num_seqs", "num_moves", "sinks", "recent", "boundary", "hole_pages", "num_long",
+                                              "reserved")] + \
                [(n, ctypes.c_uint64) for n in ("work_bytes", "workspace_bytes", "desc_key")]
 
 

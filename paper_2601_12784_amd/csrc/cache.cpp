@@ -11,7 +11,7 @@
 
 static_assert(sizeof(sf_store_info) == 24, "sf_store_info layout is part of the ABI");
 static_assert(sizeof(sf_weights_info) == 48, "sf_weights_info layout is part of the ABI");
-static_assert(sizeof(sf_evict_info) == 48, "sf_evict_info layout is part of the ABI");
+static_assert(sizeof(sf_evict_info) == 56, "sf_evict_info layout is part of the ABI");
 
 using namespace sf;
 
@@ -27,10 +27,10 @@ sf_status from_hip(hipError_t e) { return e == hipSuccess ? SF_OK : SF_ERR_HIP; 
 // Pages per work-list row: one wave per tile has the most parallelism, and a
 // long list is cheaper to make and read in runs of four.
 constexpr int64_t kSinglePages = 2048;
-int32_t run_of(int64_t pages) { return pages > kSinglePages ? 4 : 1; }
+int32_t run_of(int64_t pages) { return pages > kSinglePages ? kMaxRun : 1; }
 
-void put_row(int32_t*& at, int32_t a, int32_t b, int32_t c, int32_t d, int32_t e, int32_t f) {
-  const int32_t row[kItemInts] = {a, b, c, d, e, f, 0, 0};
+void put_row(int32_t*& at, int32_t a, int32_t b, int32_t c, int32_t d, int32_t e, int32_t f, int32_t g = 0) {
+  const int32_t row[kItemInts] = {a, b, c, d, e, f, g, 0};
   std::memcpy(at, row, sizeof row);
   at += kItemInts;
 }
@@ -398,10 +398,12 @@ extern "C" sf_status sf_kv_evict_plan(const sf_attn_desc* desc, const int32_t* s
   }
   const int32_t run = run_of(pages);
   int64_t moves = 0;
+  int32_t num_long = 0;
   bool boundary = false;
   for (int32_t s = 0; s < desc->num_seqs; ++s) {
     const int32_t n = std::min(keep_lens_host[s], seq_lens_host[s]);
     moves += (pages_of(n) + run - 1) / run;
+    num_long += seq_lens_host[s] > kEvictLong;
     boundary = boundary || (n < seq_lens_host[s] && n % kPage != 0);
   }
   if (pages * hkv > INT32_MAX / 2 || tails * hkv > INT32_MAX || int64_t(desc->num_seqs) * hkv > INT32_MAX ||
@@ -413,19 +415,21 @@ extern "C" sf_status sf_kv_evict_plan(const sf_attn_desc* desc, const int32_t* s
   info->recent = recent;
   info->boundary = boundary ? 1 : 0;
   info->hole_pages = int32_t(pages * hkv);
+  info->num_long = num_long;
+  info->reserved = 0;
   info->work_bytes = (uint64_t(desc->num_seqs) + uint64_t(moves)) * kItemInts * 4;
   info->workspace_bytes = align256(uint64_t(pages) * hkv * 8) + uint64_t(tails) * hkv * 4;
   info->desc_key = desc_key(desc);
   if (!work_host) return SF_OK;
   if (work_capacity_bytes < info->work_bytes) return SF_ERR_CAPACITY;
-  int32_t *row = work_host, *move = work_host + int64_t(desc->num_seqs) * kItemInts;
+  int32_t *long_row = work_host, *row = work_host + int64_t(num_long) * kItemInts, *move = work_host + int64_t(desc->num_seqs) * kItemInts;
   int64_t hole = 0, tail = 0;
   for (int32_t s = 0; s < desc->num_seqs; ++s) {
     const int32_t L = seq_lens_host[s], n = std::min(keep_lens_host[s], L), np = pages_of(n);
-    put_row(row, L, n, int32_t(hole), int32_t(tail), ends_host ? ends_host[s] : L, 0);
+    put_row(L > kEvictLong ? long_row : row, L, n, int32_t(hole), int32_t(tail), ends_host ? ends_host[s] : L, s);
+    for (int32_t p = 0; p < np; p += run) put_row(move, s, p, std::min(run, np - p), L, n, int32_t(hole), int32_t(tail));
     hole += np * hkv;
     tail += std::min(n, L - n) * hkv;
-    for (int32_t p = 0; p < np; p += run) put_row(move, s, p, std::min(run, np - p), 0, 0, 0);
   }
   return SF_OK;
 }
@@ -447,6 +451,7 @@ sf_status sf::evict_args(const sf_attn_desc* desc, const sf_evict_info* info, co
   a.num_seqs = info->num_seqs;
   a.num_moves = info->num_moves;
   a.boundary = info->boundary != 0;
+  a.num_long = info->num_long;
   a.k_pool = k_pool;
   a.v_pool = v_pool;
   a.k_scale = k_scale;
@@ -476,7 +481,7 @@ extern "C" sf_status sf_kv_evict(const sf_attn_desc* desc, const sf_evict_info* 
   if (st != SF_OK) return st;
   if (!info) return SF_ERR_INVALID_ARG;
   if (info->desc_key != desc_key(desc) || info->num_seqs != desc->num_seqs || info->num_moves < 0 || info->sinks < 0 ||
-      info->recent < 0 || info->hole_pages < 0 ||
+      info->recent < 0 || info->hole_pages < 0 || info->num_long < 0 || info->num_long > info->num_seqs || info->reserved != 0 ||
       info->work_bytes != (uint64_t(info->num_seqs) + uint64_t(info->num_moves)) * kItemInts * 4 ||
       info->workspace_bytes < align256(uint64_t(info->hole_pages) * 8))
     return SF_ERR_PLAN_MISMATCH;

@@ -72,13 +72,20 @@ __device__ __forceinline__ Fp8Scale fp8_new_scale(float scale, bool used, float 
   return r;
 }
 
-// Stores a tile: codes it holds (zero outside the held slots), its scale, and
-// the values x of the slots whose bytes are set in fresh (x: 16 per piece, in
-// the order of the codes; 0 elsewhere). The whole wave calls it.
+// Stores a tile: `old` is what it holds (with `read`; else nothing of it is
+// kept), of which the bytes set in keep belong to held slots, old_scale its
+// scale, and x the values of the slots whose bytes are set in fresh (16 per
+// piece, in the order of the codes; 0 elsewhere). The whole wave calls it. Lanes
+// whose pieces stay as they are write nothing: a single token then touches a
+// quarter of the tile.
 template <int D>
-__device__ __forceinline__ void fp8_store_tile(tile_u32x4 (&codes)[D / 64], const float (&x)[D / 64][16], uint32_t fresh,
-                                               float old_scale, uint8_t* tile, float* scale, int lane) {
+__device__ __forceinline__ void fp8_store_tile(const tile_u32x4 (&old)[D / 64], bool read, uint32_t keep,
+                                               const float (&x)[D / 64][16], uint32_t fresh, float old_scale,
+                                               uint8_t* tile, float* scale, int lane) {
   constexpr int kPieces = D / 64;
+  tile_u32x4 codes[kPieces];
+#pragma unroll
+  for (int p = 0; p < kPieces; ++p) codes[p] = old[p] & keep;
   uint32_t any = 0;
   float top = 0.f;
 #pragma unroll
@@ -103,9 +110,19 @@ __device__ __forceinline__ void fp8_store_tile(tile_u32x4 (&codes)[D / 64], cons
                                    x[p][4 * j + 3] * s.factor);
       codes[p][j] = (w & ~fresh) | (n & fresh);
     }
-    *reinterpret_cast<tile_u32x4*>(tile + 1024 * p + 16 * lane) = codes[p];
   }
-  if (lane == 0) *scale = s.scale;
+  if (!read) {   // wave-uniform
+#pragma unroll
+    for (int p = 0; p < kPieces; ++p) *reinterpret_cast<tile_u32x4*>(tile + 1024 * p + 16 * lane) = codes[p];
+  } else {
+#pragma unroll
+    for (int p = 0; p < kPieces; ++p) {
+      const tile_u32x4 changed = codes[p] ^ old[p];
+      if ((changed[0] | changed[1] | changed[2] | changed[3]) != 0)
+        *reinterpret_cast<tile_u32x4*>(tile + 1024 * p + 16 * lane) = codes[p];
+    }
+  }
+  if (lane == 0 && (!read || s.scale != old_scale)) *scale = s.scale;
 }
 
 }  // namespace sf

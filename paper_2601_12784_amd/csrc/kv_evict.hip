@@ -30,11 +30,13 @@ namespace {
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x8 __attribute__((ext_vector_type(8), aligned(16)));
 typedef __attribute__((address_space(4))) const int32_t* const_i32_ptr;
 __device__ __forceinline__ const_i32_ptr as_constant(const int32_t* p) { return (const_i32_ptr)(p); }
 
 // Sequence row of the work list: L, n, first page of the moves' masks, first
-// entry of the moves' sources (both per KV head 0), end (next position), 0 ..
+// entry of the moves' sources (both of KV head 0), end (next position), sequence, 0, 0;
+// the long sequences first
 constexpr int kRowInts = kItemInts;
 
 template <int kThreads>
@@ -74,16 +76,19 @@ __device__ __forceinline__ uint32_t rank_key(float w, int pos, int sinks, int re
   return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 
+constexpr int kSelectShort = kEvictLong / kPage, kSelectLong = 1024;   // threads
+
 template <int kThreads>
 __global__ __launch_bounds__(kThreads) void evict_select_kernel(EvictArgs a) {
   __shared__ int32_t hist[256];
   __shared__ int32_t found[2];
   __shared__ BlockScan<kThreads> scan;
-  const int seq = int(blockIdx.x) / a.num_kv_heads;
   const int kvh = int(blockIdx.x) % a.num_kv_heads;
-  const const_i32_ptr row = as_constant(a.rows) + size_t(seq) * kRowInts;
+  const const_i32_ptr row =
+      as_constant(a.rows) + size_t((kThreads == kSelectLong ? 0 : a.num_long) + int(blockIdx.x) / a.num_kv_heads) * kRowInts;
   const int len = row[0];
   const int n = row[1];
+  const int seq = row[5];
   if (n == 0) return;
   const int keep_pages = (n + kPage - 1) / kPage;
   uint32_t* holes = a.holes + 2 * (size_t(row[2]) + size_t(kvh) * keep_pages);
@@ -115,7 +120,7 @@ __global__ __launch_bounds__(kThreads) void evict_select_kernel(EvictArgs a) {
   uint32_t prefix = 0;
   int want = n;   // keys still to be found among those with this prefix
   for (int shift = 24; shift >= 0; shift -= 8) {
-    for (int i = tid; i < 256; i += kThreads) hist[i] = 0;
+    if (tid < 256) hist[tid] = 0;
     __syncthreads();
     for (int p = tid; p < pages; p += kThreads) {
       uint32_t key[kPage];
@@ -156,7 +161,6 @@ __global__ __launch_bounds__(kThreads) void evict_select_kernel(EvictArgs a) {
     __syncthreads();
     prefix |= uint32_t(found[0]) << shift;
     want -= found[1];
-    __syncthreads();   // before `found` and `hist` are written again
   }
 
   // Keys above the threshold stay, and the first `want` equal ones.
@@ -205,174 +209,194 @@ __global__ __launch_bounds__(kThreads) void evict_select_kernel(EvictArgs a) {
 }
 
 constexpr int kMoveWaves = 4;
+constexpr int kMoveRun = kMaxRun;   // pages of a row, at most
 
-// kPhase of an fp8 cache: the page that holds slot n keeps both freed slots and
+// One tile of page pg (pool page `page`). Lane t (every 16 lanes alike): slot t
+// takes the token of slot `source` of the sequence, in pool page src_page, if its bit is set in mask.
+template <int D, bool kFp8>
+__device__ __forceinline__ void move_tile(const EvictArgs& a, int pg, int kvh, bool is_v, int len, int n, uint32_t mask,
+                                          int source, int page, int src_page, int lane) {
+  constexpr int kPieces = D / 64;
+  const int col = lane & 15;
+  const int grp = lane >> 4;
+  const int hkv = a.num_kv_heads;
+  const bool moved = (mask >> col) & 1u;
+  const int src_slot = moved ? source % kPage : col;
+  const size_t dst_tile = size_t(page) * hkv + kvh;
+  const size_t src_tile = size_t(src_page) * hkv + kvh;
+  if (!is_v && lane < kPage && pg * kPage + lane < n && (mask != 0 || a.w_out != a.w_in || a.pos_out != a.pos_in)) {
+    const size_t from = src_tile * kPage + src_slot, to = dst_tile * kPage + lane;
+    const float w = a.w_in[from];
+    const int32_t pos = a.pos_in[from];
+    a.w_out[to] = w;
+    a.pos_out[to] = pos;
+  }
+  if (mask == 0) return;
+  if constexpr (kFp8) {
+    uint8_t* pool = static_cast<uint8_t*>(is_v ? a.v_pool : a.k_pool);
+    float* scales = is_v ? a.v_scale : a.k_scale;
+    uint8_t* dst = pool + dst_tile * (kPage * D);
+    tile_u32x4 codes[kPieces];
+    float x[kPieces][16];
+#pragma unroll
+    for (int p = 0; p < kPieces; ++p) {
+      codes[p] = *reinterpret_cast<const tile_u32x4*>(dst + 1024 * p + 16 * lane);
+#pragma unroll
+      for (int e = 0; e < 16; ++e) x[p][e] = 0.f;
+    }
+    const float old_scale = scales[dst_tile];
+    if (!is_v) {
+      if (moved) {
+        const float s = scales[src_tile];
+        const uint8_t* from = pool + src_tile * (kPage * D) + (grp * kPage + src_slot) * 16;
+#pragma unroll
+        for (int p = 0; p < kPieces; ++p) {
+          const tile_u32x4 w = *reinterpret_cast<const tile_u32x4*>(from + 1024 * p);
+#pragma unroll
+          for (int e = 0; e < 16; ++e) x[p][e] = fp8_value(w[e >> 2], e & 3) * s;
+        }
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int t = 4 * grp + e;
+        const int from_slot = __shfl(src_slot, t);
+        const int from_page = __shfl(src_page, t);
+        if (!((mask >> t) & 1u)) continue;
+        const size_t tile = size_t(from_page) * hkv + kvh;
+        const float s = scales[tile];
+        const uint8_t* from = pool + tile * (kPage * D) + ((from_slot >> 2) * kPage + col) * 16;
+        const int shift = 8 * (from_slot & 3);
+#pragma unroll
+        for (int p = 0; p < kPieces; ++p) {
+          const tile_u32x4 w = *reinterpret_cast<const tile_u32x4*>(from + 1024 * p);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) x[p][4 * j + e] = fp8_value(w[j] >> shift, 0) * s;
+        }
+      }
+    }
+    const uint32_t live = (1u << min(len - pg * kPage, kPage)) - 1u;
+    fp8_store_tile<D>(codes, true, fp8_slot_bytes(live & ~mask, is_v, lane), x, fp8_slot_bytes(mask, is_v, lane),
+                      old_scale, dst, scales + dst_tile, lane);
+  } else if (!is_v) {
+    // Keys: a lane's pieces are all of slot col, from its own tile or the
+    // token's; the tile goes out whole (16 bytes here and there would be read
+    // and written as whole lines all the same).
+    uint16_t* pool = static_cast<uint16_t*>(a.k_pool);
+    u32x4 v[D / 32];
+#pragma unroll
+    for (int p = 0; p < D / 32; ++p)
+      v[p] = *reinterpret_cast<const u32x4*>(pool + src_tile * (kPage * D) + ((4 * p + grp) * kPage + src_slot) * 8);
+#pragma unroll
+    for (int p = 0; p < D / 32; ++p)
+      *reinterpret_cast<u32x4*>(pool + dst_tile * (kPage * D) + (64 * p + lane) * 8) = v[p];
+  } else {
+    // Values: a lane takes whole dims (32-byte rows of 16 slots). Every tile
+    // that tokens come from is read once, the next one requested before the
+    // tokens of this one are picked out: their slots are the same for all
+    // lanes, so they are register indexes. (Read token by token, two bytes of
+    // each row, the long-tail batch's moves took 562 us.)
+    uint16_t* pool = static_cast<uint16_t*>(a.v_pool);
+    uint16_t* dst = pool + dst_tile * (kPage * D) + lane * kPage;
+    u32x8 row[kPieces], from[kPieces], next[kPieces];
+    auto read = [&](const uint16_t* tile, u32x8* x) {
+#pragma unroll
+      for (int p = 0; p < kPieces; ++p) x[p] = *reinterpret_cast<const u32x8*>(tile + 64 * p * kPage);
+    };
+    auto tile_of = [&](uint32_t m) {   // of the lowest slot in m
+      const int t = __ffs(m) - 1;
+      return pool + (size_t(__builtin_amdgcn_readlane(src_page, t)) * hkv + kvh) * (kPage * D) + lane * kPage;
+    };
+    // the slots whose tokens come from the same page as that of the lowest one
+    auto same_page = [&](uint32_t m) {
+      const int page_of = __builtin_amdgcn_readlane(src_page, __ffs(m) - 1);
+      return uint32_t(__ballot(src_page == page_of) & 0xFFFFu) & m;
+    };
+    uint32_t left = __builtin_amdgcn_readfirstlane(mask);
+    read(dst, row);
+    read(tile_of(left), from);
+    while (left != 0) {
+      const uint32_t now = same_page(left);
+      left &= ~now;
+      if (left != 0) read(tile_of(left), next);
+      for (uint32_t m = now; m != 0; m &= m - 1) {
+        const int t = __ffs(m) - 1;
+        const int s = __builtin_amdgcn_readlane(src_slot, t);
+#pragma unroll
+        for (int p = 0; p < kPieces; ++p) {
+          const uint32_t x = (s & 1 ? from[p][s >> 1] >> 16 : from[p][s >> 1] & 0xFFFFu);
+          const uint32_t w = row[p][t >> 1];
+          row[p][t >> 1] = t & 1 ? (w & 0xFFFFu) | (x << 16) : (w & 0xFFFF0000u) | x;
+        }
+      }
+#pragma unroll
+      for (int p = 0; p < kPieces; ++p) from[p] = next[p];
+    }
+#pragma unroll
+    for (int p = 0; p < kPieces; ++p) *reinterpret_cast<u32x8*>(dst + 64 * p * kPage) = row[p];
+  }
+}
+
+// Of an fp8 cache the page that holds slot n keeps both freed slots and
 // sources of other pages' moves, which must read its codes by the scale that
 // they have; it is left to a launch of its own behind the others (kBoundary).
 template <int D, bool kFp8, bool kBoundary>
 __global__ __launch_bounds__(64 * kMoveWaves) void evict_move_kernel(EvictArgs a) {
-  constexpr int kPieces = D / 64;
   const int lane = int(threadIdx.x) & 63;
   const int col = lane & 15;
-  const int grp = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
   const int hkv = a.num_kv_heads;
-  int seq, pb, np;
+  // A row has all that its workgroup needs: it may lie in host memory.
+  const const_i32_ptr item = as_constant(a.rows) + (kBoundary ? size_t(blockIdx.x) : size_t(a.num_seqs) + blockIdx.x) * kRowInts;
+  int seq, pb, np, len, n, hole_base, tail_base;
   if constexpr (kBoundary) {
-    seq = int(blockIdx.x);
-    pb = 0;
+    seq = item[5];
+    len = item[0];
+    n = item[1];
+    hole_base = item[2];
+    tail_base = item[3];
+    pb = n / kPage;
     np = 1;
+    if (n % kPage == 0 || n == len) return;
   } else {
-    const const_i32_ptr item = as_constant(a.rows) + (size_t(a.num_seqs) + blockIdx.x) * kRowInts;
     seq = item[0];
     pb = item[1];
     np = item[2];
-  }
-  const const_i32_ptr row = as_constant(a.rows) + size_t(seq) * kRowInts;
-  const int len = row[0];
-  const int n = row[1];
-  if constexpr (kBoundary) {
-    if (n % kPage == 0 || n == len) return;
-    pb = n / kPage;
+    len = item[3];
+    n = item[4];
+    hole_base = item[5];
+    tail_base = item[6];
   }
   const int keep_pages = (n + kPage - 1) / kPage;
   const const_i32_ptr bt = as_constant(a.block_table) + size_t(seq) * a.bt_stride;
   const int moves = min(n, len - n);
-  for (int i = int(blockIdx.y) * kMoveWaves + wave; i < np * hkv * 2; i += int(gridDim.y) * kMoveWaves) {
-    const int pg = pb + i / (2 * hkv);
-    const int rem = i % (2 * hkv);
+  // A wave takes one (KV head, keys or values) of all the run's pages. What it
+  // takes to find the tokens (freed slots, sources, their pages: three dependent
+  // reads) is requested for all of them before the first tile is moved.
+  for (int rem = int(blockIdx.y) * kMoveWaves + wave; rem < hkv * 2; rem += int(gridDim.y) * kMoveWaves) {
     const bool is_v = rem >= hkv;
     const int kvh = is_v ? rem - hkv : rem;
-    if (kFp8 && !kBoundary && n < len && (pg + 1) * kPage > n) continue;
-    const const_i32_ptr hole = (const_i32_ptr)(a.holes) + 2 * (size_t(row[2]) + size_t(kvh) * keep_pages + pg);
-    const uint32_t mask = uint32_t(hole[0]);
-    if (mask == 0 && (is_v || a.w_out == a.w_in) && (is_v || a.pos_out == a.pos_in)) continue;
-    const int32_t* tails = a.tails + size_t(row[3]) + size_t(kvh) * moves + hole[1];
-    const int page = bt[pg];
-    const size_t dst_tile = size_t(page) * hkv + kvh;
-    // Lane t (every 16 lanes alike): where the token of slot t comes from.
-    const bool moved = (mask >> col) & 1u;
-    int src = 0;
-    if (moved) src = tails[__popc(mask & ((1u << col) - 1u))];
-    const int src_page = moved ? a.block_table[size_t(seq) * a.bt_stride + src / kPage] : page;
-    const int src_slot = moved ? src % kPage : col;
-    const size_t src_tile = size_t(src_page) * hkv + kvh;
-    if (!is_v && lane < kPage && pg * kPage + lane < n) {
-      const size_t from = src_tile * kPage + src_slot, to = dst_tile * kPage + lane;
-      const float w = a.w_in[from];
-      const int32_t pos = a.pos_in[from];
-      a.w_out[to] = w;
-      a.pos_out[to] = pos;
+    const const_i32_ptr hole = (const_i32_ptr)(a.holes) + 2 * (size_t(hole_base) + size_t(kvh) * keep_pages + pb);
+    const int32_t* tails = a.tails + size_t(tail_base) + size_t(kvh) * moves;
+    uint32_t masks[kMoveRun];
+    int sources[kMoveRun], pages[kMoveRun], source_pages[kMoveRun];
+#pragma unroll
+    for (int j = 0; j < kMoveRun; ++j) {
+      const bool here = j < np && !(kFp8 && !kBoundary && n < len && (pb + j + 1) * kPage > n);
+      masks[j] = here ? uint32_t(hole[2 * j]) : 0u;
+      pages[j] = bt[j < np ? pb + j : pb];
+      // Lane t (every 16 lanes alike): the slot that slot t's token comes from.
+      const bool moved = (masks[j] >> col) & 1u;
+      sources[j] = moved ? tails[hole[2 * j + 1] + __popc(masks[j] & ((1u << col) - 1u))] : 0;
     }
-    if (mask == 0) continue;
-    if constexpr (kFp8) {
-      uint8_t* pool = static_cast<uint8_t*>(is_v ? a.v_pool : a.k_pool);
-      float* scales = is_v ? a.v_scale : a.k_scale;
-      uint8_t* dst = pool + dst_tile * (kPage * D);
-      tile_u32x4 codes[kPieces];
-      float x[kPieces][16];
 #pragma unroll
-      for (int p = 0; p < kPieces; ++p) {
-        codes[p] = *reinterpret_cast<const tile_u32x4*>(dst + 1024 * p + 16 * lane);
+    for (int j = 0; j < kMoveRun; ++j)
+      source_pages[j] = (masks[j] >> col) & 1u ? a.block_table[size_t(seq) * a.bt_stride + sources[j] / kPage] : pages[j];
 #pragma unroll
-        for (int e = 0; e < 16; ++e) x[p][e] = 0.f;
-      }
-      const float old_scale = scales[dst_tile];
-      if (!is_v) {
-        if (moved) {
-          const float s = scales[src_tile];
-          const uint8_t* from = pool + src_tile * (kPage * D) + (grp * kPage + src_slot) * 16;
-#pragma unroll
-          for (int p = 0; p < kPieces; ++p) {
-            const tile_u32x4 w = *reinterpret_cast<const tile_u32x4*>(from + 1024 * p);
-#pragma unroll
-            for (int e = 0; e < 16; ++e) x[p][e] = fp8_value(w[e >> 2], e & 3) * s;
-          }
-        }
-      } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int t = 4 * grp + e;
-          const int from_slot = __shfl(src_slot, t);
-          const int from_page = __shfl(src_page, t);
-          if (!((mask >> t) & 1u)) continue;
-          const size_t tile = size_t(from_page) * hkv + kvh;
-          const float s = scales[tile];
-          const uint8_t* from = pool + tile * (kPage * D) + ((from_slot >> 2) * kPage + col) * 16;
-          const int shift = 8 * (from_slot & 3);
-#pragma unroll
-          for (int p = 0; p < kPieces; ++p) {
-            const tile_u32x4 w = *reinterpret_cast<const tile_u32x4*>(from + 1024 * p);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) x[p][4 * j + e] = fp8_value(w[j] >> shift, 0) * s;
-          }
-        }
-      }
-      const uint32_t live = (1u << min(len - pg * kPage, kPage)) - 1u;
-      const uint32_t keep = fp8_slot_bytes(live & ~mask, is_v, lane);
-#pragma unroll
-      for (int p = 0; p < kPieces; ++p)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) codes[p][j] &= keep;
-      fp8_store_tile<D>(codes, x, fp8_slot_bytes(mask, is_v, lane), old_scale, dst, scales + dst_tile, lane);
-    } else if (!is_v) {
-      // keys: 16-byte pieces of 8 dims, four tokens at a time
-      constexpr int kKeyPieces = D / 8;
-      uint16_t* pool = static_cast<uint16_t*>(a.k_pool);
-      u32x4 v[4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int t = 4 * j + grp;
-        const int from_slot = __shfl(src_slot, t);
-        const int from_page = __shfl(src_page, t);
-        if (((mask >> t) & 1u) && col < kKeyPieces)
-          v[j] = *reinterpret_cast<const u32x4*>(pool + (size_t(from_page) * hkv + kvh) * (kPage * D) +
-                                                 (col * kPage + from_slot) * 8);
-      }
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int t = 4 * j + grp;
-        if (((mask >> t) & 1u) && col < kKeyPieces)
-          *reinterpret_cast<u32x4*>(pool + dst_tile * (kPage * D) + (col * kPage + t) * 8) = v[j];
-      }
-    } else {
-      // values: a lane takes whole dims (32-byte rows of 16 slots)
-      uint16_t* pool = static_cast<uint16_t*>(a.v_pool);
-      uint16_t* dst = pool + dst_tile * (kPage * D) + lane * kPage;
-      uint32_t word[kPieces][8];
-      uint32_t fresh[kPieces][16];
-#pragma unroll
-      for (int t = 0; t < kPage; ++t) {
-        if (!((mask >> t) & 1u)) continue;   // wave-uniform
-        const int from_slot = __builtin_amdgcn_readlane(src_slot, t);
-        const int from_page = __builtin_amdgcn_readlane(src_page, t);
-        const uint16_t* from = pool + (size_t(from_page) * hkv + kvh) * (kPage * D) + lane * kPage + from_slot;
-#pragma unroll
-        for (int p = 0; p < kPieces; ++p) fresh[p][t] = from[64 * p * kPage];
-      }
-#pragma unroll
-      for (int p = 0; p < kPieces; ++p)
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const u32x4 w = *reinterpret_cast<const u32x4*>(dst + 64 * p * kPage + 8 * h);
-#pragma unroll
-          for (int q = 0; q < 4; ++q) word[p][4 * h + q] = w[q];
-        }
-#pragma unroll
-      for (int t = 0; t < kPage; ++t) {
-        if (!((mask >> t) & 1u)) continue;
-#pragma unroll
-        for (int p = 0; p < kPieces; ++p) {
-          uint32_t& w = word[p][t >> 1];
-          w = t & 1 ? (w & 0xFFFFu) | (fresh[p][t] << 16) : (w & 0xFFFF0000u) | fresh[p][t];
-        }
-      }
-#pragma unroll
-      for (int p = 0; p < kPieces; ++p)
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-          *reinterpret_cast<u32x4*>(dst + 64 * p * kPage + 8 * h) =
-              u32x4{word[p][4 * h], word[p][4 * h + 1], word[p][4 * h + 2], word[p][4 * h + 3]};
+    for (int j = 0; j < kMoveRun; ++j) {
+      if (j >= np) break;
+      if (kFp8 && !kBoundary && n < len && (pb + j + 1) * kPage > n) continue;
+      move_tile<D, kFp8>(a, pb + j, kvh, is_v, len, n, masks[j], sources[j], pages[j], source_pages[j], lane);
     }
   }
 }
@@ -395,7 +419,15 @@ hipError_t launch_moves(const EvictArgs& a, hipStream_t stream) {
 
 hipError_t launch_evict(const EvictArgs& a, hipStream_t stream) {
   if (a.num_moves == 0) return hipSuccess;
-  hipLaunchKernelGGL(evict_select_kernel<256>, dim3(a.num_seqs * a.num_kv_heads), dim3(256), 0, stream, a);
+  // A thread keeps its first page's keys in registers, and reads the others
+  // again at each of the five passes: sequences of more pages than a small
+  // workgroup has threads go to a launch of large ones (long-tail batch, both on
+  // 256 threads 64 us, both on 1024 63).
+  if (a.num_long < a.num_seqs)
+    hipLaunchKernelGGL(evict_select_kernel<kSelectShort>, dim3((a.num_seqs - a.num_long) * a.num_kv_heads), dim3(kSelectShort),
+                       0, stream, a);
+  if (a.num_long > 0)
+    hipLaunchKernelGGL(evict_select_kernel<kSelectLong>, dim3(a.num_long * a.num_kv_heads), dim3(kSelectLong), 0, stream, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   if (a.k_scale) return a.head_dim == 128 ? launch_moves<128, true>(a, stream) : launch_moves<64, true>(a, stream);

@@ -11,8 +11,8 @@
 // at every growth.
 //
 // One wave per tile, which it reads (where it holds tokens), requantizes in
-// registers and writes whole: 1 KiB per wave store instead of 16-byte keys
-// 256 bytes apart and single value bytes. Values of new tokens are read two
+// registers and writes in 16-byte pieces, the changed ones: whole fresh pages
+// go out as 1 KiB per wave store. Values of new tokens are read two
 // bytes at a time (16 lanes, 32 contiguous bytes per token), which is not what
 // bounds it: memory is.
 #include <hip/hip_runtime.h>
@@ -67,7 +67,6 @@ __global__ __launch_bounds__(64 * kWaves) void kv_store_fp8_kernel(Store8Args a)
     float* scale = (is_v ? a.v_scale : a.k_scale) + size_t(page) * hkv + kvh;
     tile_u32x4 codes[kPieces];
     float old_scale = 1.f;
-    const uint32_t keep = fp8_slot_bytes(held_slots, is_v, lane);
 #pragma unroll
     for (int p = 0; p < kPieces; ++p) codes[p] = tile_u32x4{0u, 0u, 0u, 0u};
     if (s0 > 0) {
@@ -77,41 +76,44 @@ __global__ __launch_bounds__(64 * kWaves) void kv_store_fp8_kernel(Store8Args a)
     }
     // new-token row of slot s0; slot s is row s - s0
     const uint16_t* src = (is_v ? a.v_new : a.k_new) + size_t(qrow + (lo - first)) * tok_stride + size_t(kvh) * D;
+    // Slots without a new token read the nearest one that has: without branches
+    // all of a lane's reads are in flight at once.
     float x[kPieces][16];
-#pragma unroll
-    for (int p = 0; p < kPieces; ++p)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) x[p][e] = 0.f;
     if (is_v) {
+      uint16_t raw[kPieces][16];
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const int s = 4 * grp + e;
-        if (s < s0 || s >= s1) continue;
-        const uint16_t* v = src + size_t(s - s0) * tok_stride + col;
+        const uint16_t* v = src + size_t(min(max(4 * grp + e, s0), s1 - 1) - s0) * tok_stride + col;
 #pragma unroll
         for (int p = 0; p < kPieces; ++p)
 #pragma unroll
-          for (int j = 0; j < 4; ++j) x[p][4 * j + e] = bf16_value(v[64 * p + 16 * j]);
+          for (int j = 0; j < 4; ++j) raw[p][4 * j + e] = v[64 * p + 16 * j];
       }
-    } else if (col >= s0 && col < s1) {
-      const uint16_t* k = src + size_t(col - s0) * tok_stride + 8 * grp;
 #pragma unroll
       for (int p = 0; p < kPieces; ++p)
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const tile_u32x4 w = *reinterpret_cast<const tile_u32x4*>(k + 64 * p + 32 * h);
+        for (int e = 0; e < 16; ++e) {
+          const int s = 4 * grp + (e & 3);
+          x[p][e] = s >= s0 && s < s1 ? bf16_value(raw[p][e]) : 0.f;
+        }
+    } else {
+      const bool there = col >= s0 && col < s1;
+      const uint16_t* k = src + size_t(min(max(col, s0), s1 - 1) - s0) * tok_stride + 8 * grp;
+      tile_u32x4 raw[kPieces][2];
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            x[p][8 * h + 2 * j] = bf16_value(w[j] & 0xFFFFu);
-            x[p][8 * h + 2 * j + 1] = bf16_value(w[j] >> 16);
-          }
+      for (int p = 0; p < kPieces; ++p)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) raw[p][h] = *reinterpret_cast<const tile_u32x4*>(k + 64 * p + 32 * h);
+#pragma unroll
+      for (int p = 0; p < kPieces; ++p)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const uint32_t w = raw[p][e >> 3][(e >> 1) & 3];
+          x[p][e] = there ? bf16_value(e & 1 ? w >> 16 : w & 0xFFFFu) : 0.f;
         }
     }
-#pragma unroll
-    for (int p = 0; p < kPieces; ++p)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) codes[p][j] &= keep;
-    fp8_store_tile<D>(codes, x, fp8_slot_bytes(new_slots, is_v, lane), old_scale, dst, scale, lane);
+    fp8_store_tile<D>(codes, s0 > 0, fp8_slot_bytes(held_slots, is_v, lane), x, fp8_slot_bytes(new_slots, is_v, lane),
+                      old_scale, dst, scale, lane);
     if (opened && rem == 0 && lane == 0) a.block_table[entry0 + pg] = page;
   }
   if (i0 < a.copy_ints) a.copy_dst[i0] = copied;

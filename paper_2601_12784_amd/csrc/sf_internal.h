@@ -207,13 +207,16 @@ sf_status weight_args(const sf_attn_desc* desc, const sf_weights_info* info, con
 hipError_t launch_key_weights(const WeightArgs& a, hipStream_t stream);
 
 // Eviction (sf_kv_evict).
+constexpr int kEvictLong = 4096;   // tokens: a page per thread of a small workgroup
+constexpr int kMaxRun = 4;   // pages of a work row, at most (store and moves)
 struct EvictArgs {
-  // num_seqs rows: L, n, first page of holes, first entry of tails (of KV head 0), next position, 0, 0, 0; then
-  // num_moves rows: seq, first page, pages, 0 ..
+  // num_seqs rows: L, n, first page of holes, first entry of tails (of KV head 0), next position, seq, 0, 0; then
+  // num_moves rows: seq, first page, pages, L, n, first page of holes, first entry of tails, 0
   const int32_t* rows;
   int32_t num_seqs;
   int32_t num_moves;
   bool boundary;              // some sequence's n ends inside a page
+  int32_t num_long;           // sequences of more than kEvictLong tokens, the first rows
   void* k_pool;
   void* v_pool;
   float* k_scale;             // fp8 cache, else NULL

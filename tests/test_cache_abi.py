@@ -37,7 +37,7 @@ def _rows(work, info, ints):
 def test_struct_sizes():
     assert ctypes.sizeof(B.sf_store_info) == 24
     assert ctypes.sizeof(B.sf_weights_info) == 48
-    assert ctypes.sizeof(B.sf_evict_info) == 48
+    assert ctypes.sizeof(B.sf_evict_info) == 56
 
 
 @pytest.mark.parametrize("lens,news", LENGTHS)
@@ -85,7 +85,7 @@ def test_weights_plan_held_and_positions():
         assert e.value.status == INVALID
 
 
-@pytest.mark.parametrize("lens,keep", [([40, 17, 0, 16], [20, 17, 5, 0]), ([40000, 3], [36000, 9]), ([33], [16]), ([], [])])
+@pytest.mark.parametrize("lens,keep", [([40, 17, 0, 16], [20, 17, 5, 0]), ([3, 40000, 7, 4097, 4096], [9, 36000, 3, 4097, 1]), ([33], [16]), ([], [])])
 def test_evict_plan(lens, keep):
     hkv = 4
     info, work = B.sf_kv_evict_plan(_desc(lens), lens, keep)
@@ -93,6 +93,7 @@ def test_evict_plan(lens, keep):
     assert _rows(work, info, 8) == rows + moved
     assert (info.num_seqs, info.num_moves, info.hole_pages) == (len(lens), len(moved), hole)
     assert info.workspace_bytes == (hole * 8 + 255) // 256 * 256 + tail * 4
+    assert info.num_long == sum(n > 4096 for n in lens)
     assert bool(info.boundary) == any(min(k, n) < n and min(k, n) % 16 for n, k in zip(lens, keep))
 
 
