@@ -113,7 +113,7 @@ sf_status attend(const sf_attn_desc* desc, const sf_plan_info* info, const int32
                  const int32_t* block_table, float* out, float* lse, void* workspace,
                  uint64_t workspace_bytes, void* stream, const AppendArgs* app,
                  const float* k_scale = nullptr, const float* v_scale = nullptr, const RowCopy* copy = nullptr,
-                 void* attn_start = nullptr, void* attn_end = nullptr, bool shared_groups = false) {
+                 void* attn_start = nullptr, void* attn_end = nullptr, bool shared_groups = false, bool fine = false) {
   sf_status st = check_step_args(desc, info, work_dev, q, k_pool, v_pool, block_table, out, lse,
                                  app ? app->k_new : nullptr, app ? app->v_new : nullptr,
                                  app ? app->new_pages : nullptr, k_scale, v_scale);
@@ -156,6 +156,7 @@ sf_status attend(const sf_attn_desc* desc, const sf_plan_info* info, const int32
   a.new_pages = app ? app->new_pages : nullptr;
   a.k_scale = k_scale;
   a.v_scale = v_scale;
+  a.fine = fine;
   const bool copying = copy && copy->ints > 0 && copy->ints <= int64_t(64) * info->num_workers;
   a.copy_src = copying ? copy->src : nullptr;
   a.copy_dst = copying ? copy->dst : nullptr;
@@ -192,9 +193,10 @@ sf_status sf::decode_attn_rows(const sf_attn_desc* desc, const sf_plan_info* inf
                                const void* k_pool, const void* v_pool, const float* k_scale, const float* v_scale,
                                const int32_t* block_table, float* out, float* lse, void* workspace,
                                uint64_t workspace_bytes, void* stream, const RowCopy* copy, void* attn_start,
-                               void* attn_end, bool shared_groups) {
+                               void* attn_end, bool shared_groups, bool fine) {
   sf_status st = attend(desc, info, nullptr, work_dev, q, k_pool, v_pool, block_table, out, lse, workspace,
-                        workspace_bytes, stream, nullptr, k_scale, v_scale, copy, attn_start, attn_end, shared_groups);
+                        workspace_bytes, stream, nullptr, k_scale, v_scale, copy, attn_start, attn_end, shared_groups,
+                        fine);
   if (st != SF_OK) return st;
   if (info->num_workers == 0 || info->num_combine == 0) return st;
   const bool copying = copy && copy->ints > 0 && copy->ints <= int64_t(64) * info->num_workers;

@@ -72,6 +72,13 @@ __device__ __forceinline__ f32x4 mfma_bf16(u32x4 a, u32x4 b, f32x4 c) {
                                                  __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
 
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ f32x4 mfma_f16(u32x4 a, u32x4 b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
+
 __device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
 
 __device__ __forceinline__ uint32_t bf16_bits(float x) {
@@ -207,7 +214,8 @@ struct PageScales {
   float c0, c1, v0, v1;
 };
 
-template <int D, bool kMayBeEmpty = false, bool kScaled = false>
+// kFine: the weights go as two fp16 parts (see attend_segment_fp8).
+template <int D, bool kMayBeEmpty = false, bool kScaled = false, bool kFine = false>
 __device__ __forceinline__ BlockWeights score_block(const KHalf<D>& b, const u32x4* qf, int nvalid, int grp,
                                                     float scale_log2, SoftmaxState<D>& st,
                                                     PageScales scl = PageScales{0.f, 0.f, 0.f, 0.f}) {
@@ -252,6 +260,13 @@ __device__ __forceinline__ BlockWeights score_block(const KHalf<D>& b, const u32
       p0 *= vs;
       p1 *= vs;
     }
+    if constexpr (kFine) {
+      const f16x2 h = __builtin_convertvector(f32x2{p0, p1}, f16x2);
+      const f16x2 l = __builtin_convertvector(f32x2{p0 - float(h[0]), p1 - float(h[1])}, f16x2);
+      hi[i] = __builtin_bit_cast(uint32_t, h);
+      lo[i] = __builtin_bit_cast(uint32_t, l);
+      continue;
+    }
     const uint32_t h0 = bf16_bits(p0), h1 = bf16_bits(p1);
     const uint32_t l0 = bf16_bits(p0 - bf16_value(h0)), l1 = bf16_bits(p1 - bf16_value(h1));
     hi[i] = h0 | (h1 << 16);
@@ -264,7 +279,7 @@ __device__ __forceinline__ BlockWeights score_block(const KHalf<D>& b, const u32
 }
 
 // P.V accumulation for one block.
-template <int D>
+template <int D, bool kFine = false>
 __device__ __forceinline__ void accumulate_block(VHalf<D>& b, const BlockWeights& w, int nvalid, int grp,
                                                  SoftmaxState<D>& st) {
   if (nvalid < 2 * kPage) {
@@ -281,6 +296,11 @@ __device__ __forceinline__ void accumulate_block(VHalf<D>& b, const BlockWeights
 #pragma unroll
   for (int jb = 0; jb < Shape<D>::JB; ++jb) {
     st.o[jb] *= w.alpha;
+    if constexpr (kFine) {
+      st.o[jb] = mfma_f16(b.v[jb], w.phi, st.o[jb]);
+      st.o[jb] = mfma_f16(b.v[jb], w.plo, st.o[jb]);
+      continue;
+    }
     st.o[jb] = mfma_bf16(b.v[jb], w.phi, st.o[jb]);
     st.o[jb] = mfma_bf16(b.v[jb], w.plo, st.o[jb]);
   }
@@ -795,17 +815,33 @@ __device__ __forceinline__ void widen_k(const KHalf8<D>& r, KHalf<D>& b) {
     }
 }
 
-template <int D>
+// The same as two fp16.
+template <bool kHigh>
+__device__ __forceinline__ uint32_t widen2_f16(uint32_t codes4) {
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(codes4, 1.0f, kHigh));
+}
+
+template <int D, bool kFine>
 __device__ __forceinline__ void widen_v(const VHalf8<D>& r, VHalf<D>& b) {
 #pragma unroll
   for (int jb = 0; jb < Shape<D>::JB; ++jb) {
     const uint32_t p0 = r.v[0][jb / 4][jb % 4], p1 = r.v[1][jb / 4][jb % 4];
+    if constexpr (kFine) {
+      b.v[jb] = u32x4{widen2_f16<false>(p0), widen2_f16<true>(p0), widen2_f16<false>(p1), widen2_f16<true>(p1)};
+      continue;
+    }
     b.v[jb] = u32x4{widen2<false>(p0), widen2<true>(p0), widen2<false>(p1), widen2<true>(p1)};
   }
 }
 
 // One segment over an fp8 cache; otherwise as attend_segment.
-template <int D, int R, bool kShared = false>
+// kFine (appending steps): the P.V product on fp16 operands. An E4M3 value is
+// exact in fp16, too, and a weight as two fp16 parts keeps 22 bits where two bf16
+// parts keep 16: out is off by 3e-7 of its size instead of 2.5e-6, for the same
+// matrix work. fp16's range wants the weights near 1, so the pages' value scales
+// enter as ratios to a power of two that is at least the largest one of the
+// segment so far, which O is kept in units of.
+template <int D, int R, bool kShared = false, bool kFine = false>
 __device__ __forceinline__ void attend_segment_fp8(const AttnArgs& a, const Segment& item, WorkerRows& w, int index,
                                                    float* stash) {
   constexpr int KB = Shape<D>::KB;
@@ -863,6 +899,9 @@ __device__ __forceinline__ void attend_segment_fp8(const AttnArgs& a, const Segm
   st.m = -__builtin_inff();
   st.lsum = 0.f;
 
+  float vref = 0x1p-126f;   // kFine: the value reference
+  // 1 / x of a power of two, by its exponent
+  auto over = [](float x) { return __builtin_bit_cast(float, 0x7F000000u - __builtin_bit_cast(uint32_t, x)); };
   // Block at pg from (kc, vc); the block R - 1 ahead loads into (kn, vn).
   auto step = [&](int pg, KHalf8<D>& kc, VHalf8<D>& vc, KHalf8<D>& kn, VHalf8<D>& vn) {
     const bool more = pg + 2 * (R - 1) < pe;
@@ -874,12 +913,25 @@ __device__ __forceinline__ void attend_segment_fp8(const AttnArgs& a, const Segm
     const int nvalid = min(len - pg * kPage, pg + 1 < pe ? 2 * kPage : kPage);
     KHalf<D> kw;
     widen_k(kc, kw);
-    const PageScales scl{a.scale_log2 * kc.ks[0], a.scale_log2 * kc.ks[1], vc.vs[0], vc.vs[1]};
-    const BlockWeights w = score_block<D, false, true>(kw, qf, nvalid, grp, a.scale_log2, st, scl);
+    PageScales scl{a.scale_log2 * kc.ks[0], a.scale_log2 * kc.ks[1], vc.vs[0], vc.vs[1]};
+    float moved = 1.f;   // the old reference over the new one
+    if constexpr (kFine) {
+      const float top = fmaxf(scl.v0, scl.v1);
+      if (top > vref) {   // wave-uniform; scales are at most 2^110
+        const uint32_t b = __builtin_bit_cast(uint32_t, top);
+        const float up = __builtin_bit_cast(float, ((b >> 23) + ((b & 0x7FFFFFu) ? 1u : 0u)) << 23);
+        moved = vref * over(up);
+        vref = up;
+      }
+      scl.v0 *= over(vref);
+      scl.v1 *= over(vref);
+    }
+    BlockWeights w = score_block<D, false, true, kFine>(kw, qf, nvalid, grp, a.scale_log2, st, scl);
+    if constexpr (kFine) w.alpha *= moved;
     if (more) load_v8(c, nxt, vn);
     VHalf<D> vw;
-    widen_v(vc, vw);
-    accumulate_block(vw, w, nvalid, grp, st);
+    widen_v<D, kFine>(vc, vw);
+    accumulate_block<D, kFine>(vw, w, nvalid, grp, st);
   };
   for (int pg = pb; pg < pe; pg += 2 * R) {
 #pragma unroll
@@ -891,7 +943,8 @@ __device__ __forceinline__ void attend_segment_fp8(const AttnArgs& a, const Segm
 
   float lt = st.lsum + __shfl_xor(st.lsum, 16);
   lt += __shfl_xor(lt, 32);
-  const float inv = lt > 0.f ? 1.f / lt : 0.f;
+  float inv = lt > 0.f ? 1.f / lt : 0.f;
+  if constexpr (kFine) inv *= vref;
   f32x4 o[JB];
 #pragma unroll
   for (int jb = 0; jb < JB; ++jb) o[jb] = st.o[jb] * inv;
@@ -908,7 +961,7 @@ __device__ __forceinline__ void attend_segment_fp8(const AttnArgs& a, const Segm
   write_result<D>(a, item, o, l);
 }
 
-template <int D, int kWG, bool kShared>
+template <int D, int kWG, bool kShared, bool kFine>
 __global__ __launch_bounds__(64 * kWG) __attribute__((amdgpu_waves_per_eu(2, 2))) void attn_worker_fp8_kernel(AttnArgs a) {
   // The worker's first result waits in LDS, as in attn_worker_kernel.
   __shared__ float stash_all[kWG][(4 * Shape<D>::JB + 1) * 64];
@@ -917,14 +970,14 @@ __global__ __launch_bounds__(64 * kWG) __attribute__((amdgpu_waves_per_eu(2, 2))
   if (!worker_rows<kWG>(a, rows_lds, w)) return;
   float* stash = stash_all[w.worker - int(blockIdx.x) * kWG];
   if constexpr (kShared) {
-    attend_segment_fp8<D, 3, true>(a, w.head, w, 0, stash);
+    attend_segment_fp8<D, 3, true, kFine>(a, w.head, w, 0, stash);
     merge_group<D, kWG>(a, w.head, stash_all);
     row_copy_store(a, w);
     return;
   }
   Segment sg = w.head;
   for (int i = 0; i < w.count; ++i) {
-    attend_segment_fp8<D, 3>(a, sg, w, i, i == 0 && w.count > 1 ? stash : nullptr);
+    attend_segment_fp8<D, 3, false, kFine>(a, sg, w, i, i == 0 && w.count > 1 ? stash : nullptr);
     if (i + 1 < w.count) sg = worker_item(w, i + 1);
   }
   if (w.count > 1) flush_stash<D>(a, w.head, stash);
@@ -1363,7 +1416,10 @@ __global__ __launch_bounds__(256) void gather_kernel(GatherArgs a) {
 template <int kWG, bool kShared>
 void (*pick_attention(const AttnArgs& a))(AttnArgs) {
   const bool d128 = a.head_dim == 128;
-  if (a.k_scale) return d128 ? attn_worker_fp8_kernel<128, kWG, kShared> : attn_worker_fp8_kernel<64, kWG, kShared>;
+  if (a.k_scale && a.fine)
+    return d128 ? attn_worker_fp8_kernel<128, kWG, kShared, true> : attn_worker_fp8_kernel<64, kWG, kShared, true>;
+  if (a.k_scale)
+    return d128 ? attn_worker_fp8_kernel<128, kWG, kShared, false> : attn_worker_fp8_kernel<64, kWG, kShared, false>;
   if (a.k_new)
     return d128 ? attn_worker_kernel<128, true, kWG, kShared> : attn_worker_kernel<64, true, kWG, kShared>;
   return d128 ? attn_worker_kernel<128, false, kWG, kShared> : attn_worker_kernel<64, false, kWG, kShared>;

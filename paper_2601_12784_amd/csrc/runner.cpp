@@ -458,7 +458,7 @@ extern "C" sf_status sf_runner_step(sf_runner* r, const sf_attn_desc* desc, cons
     if (num_store > 0 && sf::launch_store_fp8(store_args, main) != hipSuccess) return close_slot(r, main, pin, SF_ERR_HIP);
     st = sf::decode_attn_rows(desc, &info, work, q, k_pool, v_pool, fp8 ? extras->k_scale : nullptr,
                               fp8 ? extras->v_scale : nullptr, block_table, out, lse, r->workspace,
-                              r->workspace_bytes, stream, cp, ev0, ev1, shared);
+                              r->workspace_bytes, stream, cp, ev0, ev1, shared, store);
   }
   return close_slot(r, main, pin, st);
 }

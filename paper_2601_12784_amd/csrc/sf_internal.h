@@ -83,6 +83,7 @@ struct AttnArgs {
   // hold E4M3 codes, and these the per-(page, KV head) scales.
   const float* k_scale;
   const float* v_scale;
+  bool fine;                  // fp8: weights as two fp16 parts (the runner's appending steps)
   // Optional side job: copy_ints ints from copy_src (the merge rows in
   // pinned host memory) to copy_dst (device), 64 per worker, so that the
   // launch after this one reads its rows from device memory. NULL dst: none.
@@ -358,7 +359,7 @@ sf_status decode_attn_rows(const sf_attn_desc* desc, const sf_plan_info* info, i
                            const void* k_pool, const void* v_pool, const float* k_scale, const float* v_scale,
                            const int32_t* block_table, float* out, float* lse, void* workspace,
                            uint64_t workspace_bytes, void* stream, const RowCopy* copy, void* attn_start,
-                           void* attn_end, bool shared_groups = false);
+                           void* attn_end, bool shared_groups = false, bool fine = false);
 // done (may be NULL): an event that the call's last launch completes.
 hipError_t launch_extend(const ExtendArgs& a, hipStream_t stream, hipEvent_t done = nullptr);
 

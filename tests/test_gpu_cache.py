@@ -6,7 +6,8 @@ Tolerances, u = 2^-24 (half a step of fp32), Z = max_t scale sum_d |q_d k_td| of
 a score is off by at most (D + 8) u Z (D products in fp32, the scale, the base change),
 which its weight e^z is off by relatively, and so are the weights' sum and lse (the
 hardware's exp2 and log2 are good to 2^-22).
-  append: weights enter P.V as two bf16 parts, off by 2^-16; sums of n terms by n u.
+  append: weights enter P.V as two fp16 parts, off by 2^-22 (a value scale 2^-4 of the largest: 2^-20 of its row's
+    size, parts below 2^-14 being subnormal), in a plain step as two bf16 ones, by 2^-16; sums of n terms by n u.
   extend: weights and values enter P.V as fp16, off by 2^-11 each; a bf16 result by 2^-8.
   key weights: n_rows terms, each off by its score's error, u |lse|, 2^-22, and the sum's n_rows u.
 """
@@ -153,7 +154,7 @@ def reference(c, q, lens, news, scale, kind, out_bf16=False):
             k, v = c.dense(s, h, L)
             o, l, spread, size = R.attention(qd[row:row + e, h * g:(h + 1) * g], k, v, scale, L - e)
             rel = 2 * (c.d + 8) * U * size + 2.0 ** -21 + 2 * L * U
-            part = 2.0 ** -16 if kind == "append" else 2.0 ** -10
+            part = {"fine": 2.0 ** -20, "append": 2.0 ** -16, "extend": 2.0 ** -10}[kind]
             t = (part + rel)[..., None] * spread * 1.0001 + 1e-30
             if out_bf16:
                 t = t + 2.0 ** -8 * (np.abs(o) + t)
@@ -275,16 +276,18 @@ def test_append_step(heads, lens):
     live = np.asarray(lens) > 0
     R.store_fp8(bits(kn).reshape(kn.shape)[live], bits(vn).reshape(vn.shape)[live], lens, news, c.bt, c.k, c.v, c.ks, c.vs, pages)
     c.same("append")
-    ro, rl, to, tl = reference(c, q[torch.from_numpy(live)], lens, news, scale, "append")
+    ro, rl, to, tl = reference(c, q[torch.from_numpy(live)], lens, news, scale, "fine")
+    ts = reference(c, q[torch.from_numpy(live)], lens, news, scale, "append")[2]
     o, l = out.cpu().numpy(), lse.cpu().numpy()
     check(o[live], ro, to, "out")
     check(l[live], rl, tl, "lse")
     assert np.all(o[~live] == 0) and np.all(np.isneginf(l[~live]))
-    # the same without the lse, and a plain step over the stored cache: the same bits
+    # the same without the lse: the same bits; a plain step over the stored cache rounds its weights to 16 bits
     again = attn(q.cuda(), c.g_k, c.g_v, c.g_bt, lens, scale, append=(kn.cuda(), vn.cuda(), pages), fp8=c.g_fp8)
     plain = attn(q.cuda(), c.g_k, c.g_v, c.g_bt, lens, scale, fp8=c.g_fp8)
     c.same("append again")
-    assert torch.equal(again, out) and torch.equal(plain, out)
+    assert torch.equal(again, out)
+    check(plain.cpu().numpy()[live], ro, ts, "plain step")
 
 
 def test_append_step_refusals():
