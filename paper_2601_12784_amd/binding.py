@@ -1387,6 +1387,7 @@ class DecodeLoopRunner:
         self.table = PageTable(k_pool.shape[0], bt_host, lens0)
         self.fp8 = fp8
         self.evicted = np.zeros(self.table.prev.size, dtype=np.int32)   # tokens given up so far, per sequence
+        self.weighed = np.zeros_like(self.evicted)   # cached tokens that have weights
         self.steps = 0
 
     @property
@@ -1415,20 +1416,25 @@ class DecodeLoopRunner:
         return out
 
     def key_weights(self, q, lse, weights, positions, stream=None):
-        """Adds the last step's attention weights (its q and lse) to weights; the tokens that it appended, or before
-        the first one every token, start there and get their positions."""
+        """Adds the last step's attention weights (its q and lse) to weights. Tokens that no call has weighed start
+        there, and get their positions."""
         lens = self.table.prev
-        held = np.where(lens > 0, lens - 1, 0).astype(np.int32) if self.steps > 1 else np.zeros_like(lens)
+        held = np.minimum(self.weighed, lens)
         self.attn.key_weights(q, lse, self.k_pool, self.block_table, lens, (lens > 0).astype(np.int32), self.scale, weights,
                               positions=positions, held_lens=held, first_pos=held + self.evicted,
                               k_scale=None if self.fp8 is None else self.fp8[0], stream=stream)
+        self.weighed = lens.copy()
 
     def evict(self, keep, weights, positions, sinks=0, recent=0, stream=None):
-        """Evicts every running sequence to at most keep tokens and frees the pages behind them. Returns the lengths."""
+        """Evicts every running sequence to at most keep tokens and frees the pages behind them. Returns the lengths.
+        Every cached token must have weights: key_weights comes first."""
         lens = self.table.prev
+        if not np.array_equal(self.weighed, lens):
+            raise ValueError("tokens without weights: call key_weights after the last step")
         kept = np.minimum(lens, keep).astype(np.int32)
         self.attn.evict(self.k_pool, self.v_pool, self.block_table, lens, kept, weights, positions,
                         ends=lens + self.evicted, sinks=sinks, recent=recent, fp8=self.fp8, stream=stream)
         self.table.truncate(kept)
         self.evicted = self.evicted + (lens - kept)
+        self.weighed = kept.copy()
         return kept

@@ -541,19 +541,26 @@ void extend_attn_kernel(ExtendArgs a) {
       }
     }
   };
-  auto factors = [&](int buffer) {
+  // The step's scales are requested ahead of its keys, and looked at after them.
+  auto uniform = [](float x) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, x)));
+  };
+  auto scales = [&](int buffer) {
+    if constexpr (!kFp8) return f32x4{0.f, 0.f, 0.f, 0.f};
+    return *reinterpret_cast<const f32x4*>(lds_scale[buffer]);
+  };
+  auto factors = [&](const f32x4& sc) {
     if constexpr (!kFp8) return PageFactors<kFp8>{c, c};
-    return PageFactors<kFp8>{c * __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, lds_scale[buffer][0]))),
-                             c * __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, lds_scale[buffer][1])))};
+    return PageFactors<kFp8>{c * uniform(sc[0]), c * uniform(sc[1])};
   };
   auto compute = [&](int buffer, int key0) {
     const uint16_t* L = lds[buffer];
+    const f32x4 sc = scales(buffer);
     f32x4 s0[kRowTiles], s1[kRowTiles];
     scores(L, s0, s1);
-    const PageFactors<kFp8> cf = factors(buffer);
+    const PageFactors<kFp8> cf = factors(sc);
     if constexpr (kFp8) {
-      const float v =
-          __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, lds_scale[buffer][2])));
+      const float v = uniform(sc[2]);
       if (v != vref) {
         const float f = vref / v;   // a power of two; O is 0 before the first step
 #pragma unroll
@@ -598,7 +605,7 @@ void extend_attn_kernel(ExtendArgs a) {
   if (begin > 0) {
     f32x4 s0[kRowTiles], s1[kRowTiles];
     scores(lds[1], s0, s1);
-    const PageFactors<kFp8> cf = factors(1);
+    const PageFactors<kFp8> cf = factors(scales(1));
 #pragma unroll
     for (int rt = 0; rt < kRowTiles; ++rt) {
       TileWeights t;

@@ -764,6 +764,8 @@ def test_a_loop_within_a_budget(heads, fp8):
     pos = torch.full((c.n, hkv, PAGE), -1, dtype=torch.int32, device="cuda")
     l1 = torch.empty((3, hq), device="cuda")
     loop.step(q[last].cuda(), prompts, lse=l1)
+    with pytest.raises(ValueError):
+        loop.evict(budget, w, pos)
     loop.key_weights(q[last].cuda(), l1, w, pos)
     lens = loop.evict(budget, w, pos, sinks=2, recent=4)
     assert lens.tolist() == [32, 32, 9]
