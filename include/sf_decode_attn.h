@@ -464,7 +464,8 @@ sf_status sf_key_weights_plan(const sf_attn_desc* desc, const int32_t* seq_lens_
                               const int32_t* held_lens_host, const int32_t* first_pos_host, const sf_plan_opts* opts,
                               int32_t* work_host, uint64_t work_capacity_bytes, sf_weights_info* info);
 
-/* Enqueues the weights pass (one launch, or two where walks are cut). k_pool
+/* Enqueues the weights pass (one launch, or two where walks are cut). Calls that
+ * share a work_dev or workspace must not overlap on the device. k_pool
  * holds bf16 keys if k_scale is NULL, else E4M3 codes with k_scale as for
  * sf_decode_attn_fp8. Arrays 16-byte aligned (lse, k_scale, block_table: 4).
  * Errors as sf_decode_attn. */
@@ -510,15 +511,16 @@ typedef struct sf_evict_info {
  * sinks or recent, L_s > min(16 * block_table_stride, 2^30), end_s < L_s, and
  * n_s < min(L_s, sinks + recent). Work list, int32 rows of 8: num_seqs rows L_s,
  * n_s, first hole page, first tail, end_s, s, 0, 0, those of more than 4096 tokens first; then the moves, runs of one of the
- * first ceil(n_s / 16) pages, or of up to 4 where there are more than 2048 in all: seq, first page,
- * pages, L_s, n_s, first hole page, first tail, 0.
+ * first ceil(n_s / 16) pages, or of up to 4 where there are more than 2048 in all and sum_s
+ * min(n_s, L_s - n_s) is less than 4 per page: seq, first page, pages, L_s, n_s, first hole page, first tail, 0.
  */
 sf_status sf_kv_evict_plan(const sf_attn_desc* desc, const int32_t* seq_lens_host, const int32_t* keep_lens_host,
                            const int32_t* ends_host, int32_t sinks, int32_t recent, int32_t* work_host,
                            uint64_t work_capacity_bytes, sf_evict_info* info);
 
-/* Enqueues the eviction (two launches; three for an fp8 cache with a budget
- * inside a page). Arrays 16-byte aligned (scales, block_table: 4). Errors as
+/* Enqueues the eviction: a selection launch (two where sequences are of both sides
+ * of 4096 tokens), the moves, and for an fp8 cache with a budget inside a page one
+ * more. Calls that share a work_dev or workspace must not overlap on the device. Arrays 16-byte aligned (scales, block_table: 4). Errors as
  * sf_decode_attn. */
 sf_status sf_kv_evict(const sf_attn_desc* desc, const sf_evict_info* info, const int32_t* work_host, int32_t* work_dev,
                       void* k_pool, void* v_pool, float* k_scale, float* v_scale, const int32_t* block_table,
@@ -526,7 +528,8 @@ sf_status sf_kv_evict(const sf_attn_desc* desc, const sf_evict_info* info, const
                       void* workspace, uint64_t workspace_bytes, void* stream);
 
 /* The same three through a runner: planned into its ring, which the kernels
- * read in place, in its workspace, in order with its steps. Arguments as
+ * read in place, in its workspace, in order with its steps (a call that needs more of
+ * either than the runner holds grows it, as a step does). Arguments as
  * the plan's and the call's, lengths and new_pages on the host (new_pages_host
  * may be NULL). SF_ERR_UNSUPPORTED, with nothing launched, on a stream that is
  * being captured into a graph. Other errors as theirs and sf_runner_step. */

@@ -269,7 +269,8 @@ def weights_plan(seq_lens, q_lens, hq, hkv, held=None, first_pos=None, num_cus=2
 
 def evict_plan(seq_lens, keep_lens, hkv, ends=None):
     n = [min(L, k) for L, k in zip(seq_lens, keep_lens)]
-    run = 4 if sum(_pages(x) for x in n) > 2048 else 1
+    pages = sum(_pages(x) for x in n)
+    run = 4 if pages > 2048 and sum(min(x, L - x) for x, L in zip(n, seq_lens)) < 4 * pages else 1
     rows, moved, hole, tail = [], [], 0, 0
     for s, L in enumerate(seq_lens):
         rows.append([L, n[s], hole, tail, L if ends is None else ends[s], s, 0, 0])

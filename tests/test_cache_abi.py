@@ -85,7 +85,7 @@ def test_weights_plan_held_and_positions():
         assert e.value.status == INVALID
 
 
-@pytest.mark.parametrize("lens,keep", [([40, 17, 0, 16], [20, 17, 5, 0]), ([3, 40000, 7, 4097, 4096], [9, 36000, 3, 4097, 1]), ([33], [16]), ([], [])])
+@pytest.mark.parametrize("lens,keep", [([40, 17, 0, 16], [20, 17, 5, 0]), ([3, 40000, 7, 4097, 4096], [9, 36000, 3, 4097, 1]), ([40000, 9000], [33333, 20]), ([33], [16]), ([], [])])
 def test_evict_plan(lens, keep):
     hkv = 4
     info, work = B.sf_kv_evict_plan(_desc(lens), lens, keep)
