@@ -9,15 +9,19 @@
 // cache a token is rounded again only when it moves. The positions array keeps
 // what the slot no longer says.
 //
-// Launch 1, one workgroup per (sequence, KV head), a thread per page: the n-th
+// Selection, one workgroup per (sequence, KV head), a thread per page: the n-th
 // largest key of (weight, lowest slot first) by four passes of 8 bits over the
 // weights' order-preserving integers, then for every page of the first n slots
 // the freed slots' mask and number, and the list of kept slots behind. Bound by
-// latency: the weights and positions come from L2 after the first pass.
-// Launch 2, a wave per (page, KV head, keys or values) of the first n slots:
-// gathers its page's new tokens. Bound by memory; a bf16 value tile is
+// latency: 14 us for 64 sequences of 2112 tokens, 20 + 27 us for the long-tail batch
+// (256 sequences, up to 16384 tokens; four KV heads each). Sixteen copies of the counters
+// took as long.
+// Moves, a wave per (page, KV head, keys or values) of the first n slots:
+// gathers its page's new tokens. Bound by memory at tile granularity; a bf16 value tile is
 // dim-major, so a token's values are 2 bytes of D 32-byte rows, and a page with
-// one freed slot reads and writes its whole tile.
+// one freed slot reads and writes its whole tile: the long-tail batch halved takes
+// 450 us for 2.2 GB of tiles (0.72 GB of tokens), 64 sequences of 2112 fp8 tokens cut to
+// 2048 37 us.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
