@@ -398,8 +398,8 @@ typedef struct sf_store_info {
  * token, L_s, cu_s, 0, 0; each a run of the pages that new tokens land in, of
  * one page, or of up to 4 where there are more than 2048 in all.
  * Lengths: 0 <= E_s <= L_s <= min(16 * block_table_stride, 2^30), T * Hq * D
- * < 2^31. work_host NULL only reports the sizes; SF_ERR_CAPACITY if
- * work_capacity_bytes < info->work_bytes.
+ * < 2^31; SF_ERR_UNSUPPORTED for 2^24 rows or more. work_host NULL only reports
+ * the sizes; SF_ERR_CAPACITY if work_capacity_bytes < info->work_bytes.
  */
 sf_status sf_kv_store_fp8_plan(const sf_attn_desc* desc, const int32_t* seq_lens_host, const int32_t* q_lens_host,
                                int32_t* work_host, uint64_t work_capacity_bytes, sf_store_info* info);
@@ -446,7 +446,7 @@ typedef struct sf_weights_info {
  * num_cus only.
  * Rule. If no sequence has more than 16 query rows per KV head (a decode step):
  * the blocks of four pages (the last of a pair shorter) of the pairs (sequence
- * with E_s > 0, KV head), in that order end to end, are N; W = min(8 num_cus, N)
+ * with E_s > 0, KV head), in that order end to end, are N; W = min(8 num_cus, N, 2^22)
  * waves take the blocks [floor(N w / W), floor(N (w + 1) / W)), cut at pair ends
  * into segments. Rows 0 .. W - 1 are the waves' first segments, the others follow
  * wave by wave; steps = W, and int 12 of a row is that of the wave's next segment, or -1.
@@ -458,7 +458,7 @@ typedef struct sf_weights_info {
  * Work list, int32 rows of 16: num_items rows seq, kv_head, first page, end
  * page, first token, end token, part slot (-1: uncut), L_s, P_s, cu_s, held_s,
  * first_pos_s, next row (0 with steps = 0), 0 ..; then num_merge rows with the first part slot
- * and the number of parts in place of the tokens.
+ * and the number of parts in place of the tokens. SF_ERR_UNSUPPORTED for 2^22 items or more.
  */
 sf_status sf_key_weights_plan(const sf_attn_desc* desc, const int32_t* seq_lens_host, const int32_t* q_lens_host,
                               const int32_t* held_lens_host, const int32_t* first_pos_host, const sf_plan_opts* opts,
@@ -513,6 +513,8 @@ typedef struct sf_evict_info {
  * n_s, first hole page, first tail, end_s, s, 0, 0, those of more than 4096 tokens first; then the moves, runs of one of the
  * first ceil(n_s / 16) pages, or of up to 4 where there are more than 2048 in all and sum_s
  * min(n_s, L_s - n_s) is less than 4 per page: seq, first page, pages, L_s, n_s, first hole page, first tail, 0.
+ * SF_ERR_UNSUPPORTED for 2^22 (sequence, KV head) pairs, 2^24 moves, 2^30 hole pages or
+ * 2^31 tails, or more.
  */
 sf_status sf_kv_evict_plan(const sf_attn_desc* desc, const int32_t* seq_lens_host, const int32_t* keep_lens_host,
                            const int32_t* ends_host, int32_t sinks, int32_t recent, int32_t* work_host,

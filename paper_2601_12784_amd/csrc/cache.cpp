@@ -18,6 +18,7 @@ using namespace sf;
 namespace {
 
 constexpr int32_t kMaxTokens = 1 << 30;   // per sequence: token and page numbers stay far from 2^31
+constexpr int64_t kMaxGroups = 1 << 22;   // workgroups of 1024 threads (4 times as many of 256): 2^32 threads are too many for a launch
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
@@ -63,7 +64,8 @@ extern "C" sf_status sf_kv_store_fp8_plan(const sf_attn_desc* desc, const int32_
   for (int32_t s = 0; s < desc->num_seqs; ++s) pages += touched(s);
   const int32_t run = run_of(pages);
   for (int32_t s = 0; s < desc->num_seqs; ++s) rows += (touched(s) + run - 1) / run;
-  info->num_rows = int32_t(rows);   // at most 16 per token, and T Hq D < 2^31
+  if (rows >= 4 * kMaxGroups) return SF_ERR_UNSUPPORTED;
+  info->num_rows = int32_t(rows);
   info->num_q_rows = int32_t(tokens);
   info->work_bytes = uint64_t(rows) * kItemInts * 4;
   info->desc_key = desc_key(desc);
@@ -242,9 +244,9 @@ extern "C" sf_status sf_key_weights_plan(const sf_attn_desc* desc, const int32_t
   if (blocks == 0) return SF_OK;
 
   if (most <= kStepRows) {
-    const int64_t waves = std::min(kStepWavesPerCu * cus, blocks);
-    if (waves + blocks > INT32_MAX / kWeightInts) return SF_ERR_INVALID_ARG;
+    const int64_t waves = std::min({kStepWavesPerCu * cus, blocks, kMaxGroups});
     const int64_t rows = plan_weight_steps(desc, q, blocks, waves, nullptr);
+    if (rows > INT32_MAX / kWeightInts) return SF_ERR_UNSUPPORTED;
     info->num_items = int32_t(rows);
     info->steps = int32_t(waves);
     info->work_bytes = uint64_t(rows) * kWeightInts * 4;
@@ -264,7 +266,7 @@ extern "C" sf_status sf_key_weights_plan(const sf_attn_desc* desc, const int32_t
     items += parts * hkv;
     if (parts > 1) merges += hkv, slots += parts * hkv;
   });
-  if (items + merges > INT32_MAX / kWeightInts) return SF_ERR_INVALID_ARG;
+  if (std::max(items, merges) >= kMaxGroups) return SF_ERR_UNSUPPORTED;
   info->num_items = int32_t(items);
   info->num_merge = int32_t(merges);
   info->num_slots = int32_t(slots);
@@ -413,9 +415,9 @@ extern "C" sf_status sf_kv_evict_plan(const sf_attn_desc* desc, const int32_t* s
     num_long += seq_lens_host[s] > kEvictLong;
     boundary = boundary || (n < seq_lens_host[s] && n % kPage != 0);
   }
-  if (pages * hkv > INT32_MAX / 2 || tails * hkv > INT32_MAX || int64_t(desc->num_seqs) * hkv > INT32_MAX ||
-      desc->num_seqs + moves > INT32_MAX / kItemInts)
-    return SF_ERR_INVALID_ARG;
+  if (pages * hkv > INT32_MAX / 2 || tails * hkv > INT32_MAX || int64_t(desc->num_seqs) * hkv >= kMaxGroups ||
+      moves >= 4 * kMaxGroups)
+    return SF_ERR_UNSUPPORTED;
   info->num_seqs = desc->num_seqs;
   info->num_moves = int32_t(moves);
   info->sinks = sinks;

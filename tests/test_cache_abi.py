@@ -126,6 +126,24 @@ def test_new_token_plans_reject_bad_lengths(plan):
         plan(_desc([8, 8]), [8], [1])
 
 
+def test_plans_too_large_for_a_launch():
+    lens = [1 << 30] * 2
+    desc = B.make_desc(2, 8, 8, 64, 1 << 26, 1 << 27, 0.1)
+    info = B.sf_weights_info()
+    h, e = np.array(lens, np.int32), np.array([40, 40], np.int32)
+    assert B.lib().sf_key_weights_plan(ctypes.byref(desc), h.ctypes.data, e.ctypes.data, None, None, None, None, 0,
+                                       ctypes.byref(info)) == UNSUPPORTED
+    one = np.array([1, 1], np.int32)          # a decode step over them is planned: a row per segment
+    assert B.lib().sf_key_weights_plan(ctypes.byref(desc), h.ctypes.data, one.ctypes.data, None, None, None, None, 0,
+                                       ctypes.byref(info)) == OK and info.steps == 2048
+    ev = B.sf_evict_info()
+    assert B.lib().sf_kv_evict_plan(ctypes.byref(desc), h.ctypes.data, h.ctypes.data, None, 0, 0, None, 0, ctypes.byref(ev)) == UNSUPPORTED
+    many = np.ones(1 << 24, np.int32)
+    desc = B.make_desc(1 << 24, 1, 1, 64, 1, 1 << 24, 0.1)
+    assert B.lib().sf_kv_store_fp8_plan(ctypes.byref(desc), many.ctypes.data, many.ctypes.data, None, 0,
+                                        ctypes.byref(B.sf_store_info())) == UNSUPPORTED
+
+
 def test_capacity_is_reported_with_the_sizes():
     desc = _desc([400])
     for plan, args, info in ((B.sf_kv_store_fp8_plan, ([400], [400]), B.sf_store_info()),
