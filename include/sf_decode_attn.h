@@ -422,8 +422,8 @@ sf_status sf_kv_store_fp8(const sf_attn_desc* desc, const sf_store_info* info, c
  * slot as the cache (they may be one array). Keys t >= held_s have not been
  * weighed before: what stands in weights for them is not read, and positions
  * (int32 [num_pages][Hkv][16], may be NULL) gets first_pos_s + t - held_s.
- * Rows whose lse is not finite add nothing. Sequences with E_s = 0 are left
- * out, and so is every slot past L_s. All sums are fp32 in an order that does
+ * Rows whose lse is not finite add nothing, whatever their queries hold; cached
+ * keys must be finite. Sequences with E_s = 0 are left out, and so is every slot past L_s. All sums are fp32 in an order that does
  * not change from run to run. No page may be part of two sequences.
  */
 typedef struct sf_weights_info {

@@ -483,6 +483,26 @@ def test_key_weights(heads, fp8, lens, news):
     assert np.array_equal(pos, want_pos)
 
 
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("news", [[2, 1, 0], [40, 17, 3]])   # the list of a decode step and that of items
+def test_key_weights_of_rows_that_hold_no_numbers(fp8, news):
+    """A row whose lse is not finite adds nothing whatever its queries hold: the same bits as with zeros there."""
+    lens, (hq, hkv, d) = [90, 17, 33], (8, 2, 128)
+    c = Cache(lens, hkv, d, fp8, 58, k_mult=1.5)
+    q = new_tokens(sum(news), hq, d, 23)[0]
+    lse = reference(c, q, lens, news, 0.1, "append")[1].astype(np.float32)
+    zeros, bad = q.clone(), q.clone()
+    row = 0
+    for value, dead in ((float("nan"), -np.inf), (float("inf"), np.nan), (-float("inf"), np.inf)):
+        for h in (0, hq - 1):
+            lse[row, h], zeros[row, h], bad[row, h] = dead, 0, value
+        row = (row + news[0] - 1) % sum(news)
+    w0, pos0 = np.ones((c.n, hkv, PAGE), np.float32), np.zeros((c.n, hkv, PAGE), np.int32)
+    held = [L - e for L, e in zip(lens, news)]
+    got = [run_weights(c, x.cuda(), torch.from_numpy(lse).cuda(), lens, news, hq, 0.1, w0, pos0, held, held)[0] for x in (zeros, bad)]
+    assert np.all(np.isfinite(got[0])) and np.array_equal(*got)
+
+
 def test_key_weights_cut_walks_are_the_same_up_to_rounding():
     """A device of one compute unit cuts nothing, one of 4096 cuts every walk to eight tiles."""
     hq, hkv, d, L = 28, 4, 128, 900
