@@ -1413,12 +1413,21 @@ class DecodeLoopRunner:
         out = self.attn(q, self.k_pool, self.v_pool, self.block_table, lens.astype(np.int32), self.scale,
                         out=out, lse=lse, stream=stream, attn_events=attn_events, append=append, fp8=self.fp8)
         self.steps += 1
+        if not lens.all():   # sequences that are not running: one that starts there later has nothing of theirs
+            self.evicted, self.weighed = (np.where(lens > 0, x, 0) for x in (self.evicted, self.weighed))
         return out
 
     def key_weights(self, q, lse, weights, positions, stream=None):
-        """Adds the last step's attention weights (its q and lse) to weights. Tokens that no call has weighed start
-        there, and get their positions."""
+        """Adds the last step's attention weights (its q and lse, or their rows of the running sequences) to weights.
+        Tokens that no call has weighed start there, and get their positions."""
         lens = self.table.prev
+        live = lens > 0
+        if not live.all() and q.shape[0] == lse.shape[0] == lens.size:
+            if not live.any():
+                return
+            edges = np.flatnonzero(np.diff(live, prepend=False, append=False)).reshape(-1, 2).tolist()
+            with torch.cuda.stream(stream):   # where the rows are read
+                q, lse = (torch.cat([x[a:b] for a, b in edges]) for x in (q, lse))
         held = np.minimum(self.weighed, lens)
         self.attn.key_weights(q, lse, self.k_pool, self.block_table, lens, (lens > 0).astype(np.int32), self.scale, weights,
                               positions=positions, held_lens=held, first_pos=held + self.evicted,

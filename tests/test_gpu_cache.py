@@ -845,3 +845,50 @@ def test_a_loop_within_a_budget(heads, fp8):
                     assert sorted(hp[loop.bt_host[s, t // PAGE], h, t % PAGE].tolist()) == want[s, h]
     held = [-(-int(L) // PAGE) for L in loop.table.prev]
     assert loop.pool.available() == c.n - sum(held)
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+def test_loop_whose_sequences_end_and_start(fp8):
+    """Rows of sequences that are not running are left out of the weights, and a sequence that starts in an ended
+    one's place has none of its counts."""
+    hq, hkv, d, scale = 8, 2, 64, 0.125
+    prompts, budget = np.array([40, 24, 9], np.int64), 16
+    c = Cache([64, 64, 64], hkv, d, fp8, 95)
+    loop = B.DecodeLoopRunner(hq, hkv, d, c.g_k, c.g_v, c.g_bt, c.bt, prompts, scale, fp8=c.g_fp8)
+    w = torch.full((c.n, hkv, PAGE), float("nan"), device="cuda")
+    pos = torch.full((c.n, hkv, PAGE), -1, dtype=torch.int32, device="cuda")
+    side = torch.cuda.Stream()
+
+    def step(lens, seed, weigh=True, stream=None):
+        q = new_tokens(3, hq, d, seed)[0].cuda()
+        kn, vn = (x.cuda() for x in new_tokens(3, hkv, d, seed + 1))
+        l1 = torch.empty((3, hq), device="cuda")
+        loop.step(q, np.asarray(lens), kn if loop.steps else None, vn if loop.steps else None, lse=l1)
+        if not weigh:
+            return
+        before = w.clone()
+        torch.cuda.synchronize()
+        live = np.asarray(lens) > 0
+        held = np.minimum(loop.weighed, lens)
+        loop.key_weights(q, l1, w, pos, stream=stream)
+        torch.cuda.synchronize()
+        if live.any():
+            rows = torch.from_numpy(np.flatnonzero(live)).cuda()
+            loop.attn.key_weights(q[rows], l1[rows], c.g_k, c.g_bt, np.asarray(lens), live.astype(np.int32), scale, before,
+                                  held_lens=held, first_pos=held + loop.evicted, k_scale=c.g_fp8[0] if fp8 else None)
+        assert torch.equal(torch.isnan(w), torch.isnan(before)) and torch.equal(w.nan_to_num(), before.nan_to_num())
+
+    step(prompts, 300)
+    assert loop.evict(budget, w, pos).tolist() == [16, 16, 9]
+    step([17, 0, 10], 310)                 # the second ends
+    step([18, 0, 11], 320, stream=side)
+    step([19, 1, 12], 330)                 # another starts in its place
+    torch.cuda.synchronize()
+    first = loop.bt_host[1, 0]
+    assert pos[first, :, 0].tolist() == [0, 0] and loop.evicted.tolist() == [24, 0, 0]
+    step([0, 0, 13], 340, weigh=False)
+    step([1, 0, 14], 350)                  # no call between has weighed
+    assert pos[loop.bt_host[0, 0], :, 0].tolist() == [0, 0] and loop.weighed.tolist() == [1, 0, 14]
+    assert loop.evict(budget, w, pos).tolist() == [1, 0, 14]
+    step([0, 0, 0], 360)
+    assert loop.evicted.tolist() == [0, 0, 0] and loop.weighed.tolist() == [0, 0, 0]
