@@ -522,8 +522,8 @@ sf_status sf_kv_evict_plan(const sf_attn_desc* desc, const int32_t* seq_lens_hos
 
 /* Enqueues the eviction: a selection launch (two where sequences are of both sides
  * of 4096 tokens), the moves, and for an fp8 cache with a budget inside a page one
- * more. Calls that share a work_dev or workspace must not overlap on the device. Arrays 16-byte aligned (scales, block_table: 4). Errors as
- * sf_decode_attn. */
+ * more. Calls that share a work_dev or workspace must not overlap on the device.
+ * Arrays 16-byte aligned (scales, block_table: 4). Errors as sf_decode_attn. */
 sf_status sf_kv_evict(const sf_attn_desc* desc, const sf_evict_info* info, const int32_t* work_host, int32_t* work_dev,
                       void* k_pool, void* v_pool, float* k_scale, float* v_scale, const int32_t* block_table,
                       const float* weights, const int32_t* positions, float* weights_out, int32_t* positions_out,

@@ -400,11 +400,10 @@ sf_status sf::extend_args(const sf_attn_desc* desc, const int32_t* work_dev, con
   return SF_OK;
 }
 
-static sf_status extend_attn(const sf_attn_desc* desc, const sf_extend_info* info,
-                                    const int32_t* work_host, int32_t* work_dev, const void* q,
-                                    const void* k_new, const void* v_new, void* k_pool, void* v_pool,
-                                    const int32_t* block_table, float* out, float* lse, void* stream, const float* k_scale = nullptr,
-                             const float* v_scale = nullptr, bool out_bf16 = false) {
+static sf_status extend_attn(const sf_attn_desc* desc, const sf_extend_info* info, const int32_t* work_host,
+                             int32_t* work_dev, const void* q, const void* k_new, const void* v_new, void* k_pool,
+                             void* v_pool, const int32_t* block_table, float* out, float* lse, void* stream,
+                             const float* k_scale = nullptr, const float* v_scale = nullptr, bool out_bf16 = false) {
   sf_status st = validate_desc(desc);
   if (st != SF_OK) return st;
   if (!info) return SF_ERR_INVALID_ARG;
