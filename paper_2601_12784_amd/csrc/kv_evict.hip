@@ -214,6 +214,58 @@ __global__ __launch_bounds__(kThreads) void evict_select_kernel(EvictArgs a) {
 
 constexpr int kMoveWaves = 4;
 constexpr int kMoveRun = kMaxRun;   // pages of a row, at most
+constexpr int kFewTokens = 2;
+
+// An fp8 tile that takes one or two tokens (set in mask) and keeps its scale: a lane
+// has dims lane and 64 + lane of each token, where the full store has 16 or 32 values of
+// which an eighth or less are new. False, with nothing written, where the scale
+// must change.
+template <int D>
+__device__ __forceinline__ bool move_few_fp8(uint8_t* pool, const float* scales, size_t dst_tile, int hkv, int kvh, bool is_v,
+                                             uint32_t held, uint32_t mask, int src_page, int src_slot, int lane) {
+  constexpr int kPieces = D / 64;
+  const int slots[2] = {__ffs(mask) - 1, 31 - __clz(mask)};   // alike for one token, which is then moved twice
+  // byte of (slot, dim 64 p + lane): 1024 p + of_lane + of_slot (fp8_tile.h)
+  const int of_lane = is_v ? 16 * (lane & 15) + 4 * (lane >> 4) : 256 * ((lane >> 3) & 3) + 8 * (lane >> 5) + (lane & 7);
+  auto of_slot = [&](int s) { return is_v ? 256 * (s >> 2) + (s & 3) : 16 * s; };
+  uint8_t* dst = pool + dst_tile * (kPage * D);
+  uint32_t raw[2][kPieces];
+  float s[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const size_t tile = size_t(__builtin_amdgcn_readlane(src_page, slots[i])) * hkv + kvh;
+    const uint8_t* from = pool + tile * (kPage * D) + of_slot(__builtin_amdgcn_readlane(src_slot, slots[i])) + of_lane;
+    s[i] = scales[tile];
+#pragma unroll
+    for (int p = 0; p < kPieces; ++p) raw[i][p] = from[1024 * p];
+  }
+  tile_u32x4 codes[kPieces];
+#pragma unroll
+  for (int p = 0; p < kPieces; ++p) codes[p] = *reinterpret_cast<const tile_u32x4*>(dst + 1024 * p + 16 * lane);
+  const float scale = scales[dst_tile];
+  uint32_t any = 0;
+#pragma unroll
+  for (int p = 0; p < kPieces; ++p) any |= codes[p][0] | codes[p][1] | codes[p][2] | codes[p][3];
+  any &= fp8_slot_bytes(held, is_v, lane) & 0x7F7F7F7Fu;
+  float x[2][kPieces], top = 0.f;
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int p = 0; p < kPieces; ++p) {
+      x[i][p] = fp8_value(raw[i][p], 0) * s[i];
+      top = fmaxf(top, fabsf(x[i][p]));
+    }
+  // fp8_new_scale's shift is 0 where the quotient rounds to at most 1, which is where top <= 448 scale
+  if (!__any(any != 0) || __any(top > __fmul_rn(448.f, scale))) return false;
+  const float factor = __fdiv_rn(1.f, scale);
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const uint32_t n = fp8_codes(x[i][0] * factor, x[i][kPieces - 1] * factor, 0.f, 0.f);
+#pragma unroll
+    for (int p = 0; p < kPieces; ++p) dst[1024 * p + of_slot(slots[i]) + of_lane] = uint8_t(n >> (8 * p));
+  }
+  return true;
+}
 
 // One tile of page pg (pool page `page`). Lane t (every 16 lanes alike): slot t
 // takes the token of slot `source` of the sequence, in pool page src_page, if its bit is set in mask.
@@ -240,6 +292,10 @@ __device__ __forceinline__ void move_tile(const EvictArgs& a, int pg, int kvh, b
     uint8_t* pool = static_cast<uint8_t*>(is_v ? a.v_pool : a.k_pool);
     float* scales = is_v ? a.v_scale : a.k_scale;
     uint8_t* dst = pool + dst_tile * (kPage * D);
+    const uint32_t live = (1u << min(len - pg * kPage, kPage)) - 1u;
+    if (__popc(mask) <= kFewTokens && live == 0xFFFFu &&
+        move_few_fp8<D>(pool, scales, dst_tile, hkv, kvh, is_v, ~mask, mask, src_page, src_slot, lane))
+      return;
     tile_u32x4 codes[kPieces];
     float x[kPieces][16];
 #pragma unroll
@@ -279,7 +335,6 @@ __device__ __forceinline__ void move_tile(const EvictArgs& a, int pg, int kvh, b
         }
       }
     }
-    const uint32_t live = (1u << min(len - pg * kPage, kPage)) - 1u;
     fp8_store_tile<D>(codes, true, fp8_slot_bytes(live & ~mask, is_v, lane), x, fp8_slot_bytes(mask, is_v, lane),
                       old_scale, dst, scales + dst_tile, lane);
   } else if (!is_v) {
