@@ -481,11 +481,10 @@ sf_status sf::evict_args(const sf_attn_desc* desc, const sf_evict_info* info, co
   return SF_OK;
 }
 
-extern "C" sf_status sf_kv_evict(const sf_attn_desc* desc, const sf_evict_info* info, const int32_t* work_host,
-                                 int32_t* work_dev, void* k_pool, void* v_pool, float* k_scale, float* v_scale,
-                                 const int32_t* block_table, const float* weights, const int32_t* positions,
-                                 float* weights_out, int32_t* positions_out, void* workspace, uint64_t workspace_bytes,
-                                 void* stream) {
+sf_status sf::run_evict(const sf_attn_desc* desc, const sf_evict_info* info, const int32_t* work_host, int32_t* work_dev,
+                        void* k_pool, void* v_pool, float* k_scale, float* v_scale, const int32_t* block_table,
+                        const float* weights, const int32_t* positions, float* weights_out, int32_t* positions_out,
+                        void* workspace, uint64_t workspace_bytes, void* stream, int32_t* late_rows) {
   sf_status st = validate_desc(desc);
   if (st != SF_OK) return st;
   if (!info) return SF_ERR_INVALID_ARG;
@@ -503,5 +502,15 @@ extern "C" sf_status sf_kv_evict(const sf_attn_desc* desc, const sf_evict_info* 
   hipStream_t s = static_cast<hipStream_t>(stream);
   if (work_host && hipMemcpyAsync(work_dev, work_host, info->work_bytes, hipMemcpyHostToDevice, s) != hipSuccess)
     return SF_ERR_HIP;
+  a.late_rows = late_rows;
   return from_hip(launch_evict(a, s));
+}
+
+extern "C" sf_status sf_kv_evict(const sf_attn_desc* desc, const sf_evict_info* info, const int32_t* work_host,
+                                 int32_t* work_dev, void* k_pool, void* v_pool, float* k_scale, float* v_scale,
+                                 const int32_t* block_table, const float* weights, const int32_t* positions,
+                                 float* weights_out, int32_t* positions_out, void* workspace, uint64_t workspace_bytes,
+                                 void* stream) {
+  return run_evict(desc, info, work_host, work_dev, k_pool, v_pool, k_scale, v_scale, block_table, weights, positions,
+                   weights_out, positions_out, workspace, workspace_bytes, stream, nullptr);
 }

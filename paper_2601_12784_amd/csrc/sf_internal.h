@@ -214,6 +214,7 @@ struct EvictArgs {
   // num_seqs rows: L, n, first page of holes, first entry of tails (of KV head 0), next position, seq, 0, 0; then
   // num_moves rows: seq, first page, pages, L, n, first page of holes, first entry of tails, 0
   const int32_t* rows;
+  int32_t* late_rows;         // a device copy of the rows, made by the selection for the launches behind it; NULL: rows
   int32_t num_seqs;
   int32_t num_moves;
   bool boundary;              // some sequence's n ends inside a page
@@ -240,6 +241,11 @@ sf_status evict_args(const sf_attn_desc* desc, const sf_evict_info* info, const 
                      const int32_t* positions, float* weights_out, int32_t* positions_out, void* workspace,
                      EvictArgs* args);
 hipError_t launch_evict(const EvictArgs& a, hipStream_t stream);
+// sf_kv_evict; late_rows: NULL, or info->work_bytes of device memory for rows that lie in host memory.
+sf_status run_evict(const sf_attn_desc* desc, const sf_evict_info* info, const int32_t* work_host, int32_t* work_dev,
+                    void* k_pool, void* v_pool, float* k_scale, float* v_scale, const int32_t* block_table,
+                    const float* weights, const int32_t* positions, float* weights_out, int32_t* positions_out,
+                    void* workspace, uint64_t workspace_bytes, void* stream, int32_t* late_rows);
 
 // Checks the lengths of an extend-like call and counts its query rows.
 sf_status check_extend_lengths(const sf_attn_desc* desc, const int32_t* seq_lens_host, const int32_t* q_lens_host,
