@@ -404,7 +404,7 @@ extern "C" sf_status sf_kv_evict_plan(const sf_attn_desc* desc, const int32_t* s
   }
   // Where most pages take several tokens their moves are the work, and every
   // wave has one tile; runs pay where most pages have little to do (us with runs of 1, 2
-  // and 4: long-tail batch halved 494, 505, 522; 64 x 2112 to 2048 79, 58, 49).
+  // and 4: long-tail batch halved 494, 505, 522; 64 x 2112 to 2048 76, 46, 40).
   const int32_t run = tails >= kBusyPage * pages ? 1 : run_of(pages);
   int64_t moves = 0;
   int32_t num_long = 0;

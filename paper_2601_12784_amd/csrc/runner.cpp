@@ -509,10 +509,10 @@ extern "C" sf_status sf_runner_key_weights(sf_runner* r, const sf_attn_desc* des
 }
 
 // Every workgroup of an eviction's moves begins with a row, which the ring's host
-// memory gives late: the selection, which waits most of its time, copies the list to the device. Up to this size: 8, 64
-// and 200 sequences of 2112 fp8 tokens take 20.4, 39.8 and 96.4 us with the copy (2 to 211 KiB) and
-// 22.8, 44.5 and 104.7 without; the long-tail batch (700 KiB) 507 and 495.
-constexpr uint64_t kLateBytes = 256 << 10;
+// memory gives late: the selection, which waits most of its time, copies the list to the device.
+// Up to this size: 8, 64, 200 and 480 sequences of 2112 fp8 tokens take 20.4, 39.8, 96.4 and 259 us with the
+// copy (32 to 495 KiB) and 22.8, 44.5, 104.7 and 279 without; the long-tail batch (700 KiB) 507 and 495.
+constexpr uint64_t kLateBytes = 512 << 10;
 
 extern "C" sf_status sf_runner_evict(sf_runner* r, const sf_attn_desc* desc, const int32_t* seq_lens_host,
                                      const int32_t* keep_lens_host, const int32_t* ends_host, int32_t sinks,
