@@ -36,7 +36,8 @@ constexpr int kWaves = 4;
 template <int D>
 __global__ __launch_bounds__(64 * kWaves) void kv_store_fp8_kernel(Store8Args a) {
   constexpr int kPieces = D / 64;
-  int i0 = (int(blockIdx.y) * int(gridDim.x) + int(blockIdx.x)) * 64 * kWaves + int(threadIdx.x);
+  // 64 bits: a launch of up to 2^24 rows, times the heads' groups, has more threads than 2^31
+  int64_t i0 = (int64_t(blockIdx.y) * gridDim.x + blockIdx.x) * (64 * kWaves) + int(threadIdx.x);
   const int copied = i0 < a.copy_ints ? a.copy_src[i0] : 0;
   const const_i32_ptr row = as_constant(a.rows) + size_t(blockIdx.x) * kItemInts;
   const int seq = row[0];
@@ -120,7 +121,7 @@ __global__ __launch_bounds__(64 * kWaves) void kv_store_fp8_kernel(Store8Args a)
     if (opened && rem == 0 && lane == 0) a.block_table[entry0 + pg] = page;
   }
   if (i0 < a.copy_ints) a.copy_dst[i0] = copied;
-  const int stride = int(gridDim.x) * int(gridDim.y) * 64 * kWaves;
+  const int64_t stride = int64_t(gridDim.x) * gridDim.y * (64 * kWaves);
   for (i0 += stride; i0 < a.copy_ints; i0 += stride) a.copy_dst[i0] = a.copy_src[i0];
 }
 
