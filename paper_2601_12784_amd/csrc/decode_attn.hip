@@ -72,13 +72,6 @@ __device__ __forceinline__ f32x4 mfma_bf16(u32x4 a, u32x4 b, f32x4 c) {
                                                  __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
 
-typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
-typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
-typedef float f32x2 __attribute__((ext_vector_type(2)));
-__device__ __forceinline__ f32x4 mfma_f16(u32x4 a, u32x4 b, f32x4 c) {
-  return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
-}
-
 __device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
 
 __device__ __forceinline__ uint32_t bf16_bits(float x) {
@@ -198,11 +191,21 @@ struct SoftmaxState {
 };
 
 // Weights of one block as the P^T operand (bf16 hi + lo parts, about 16 bits
-// of each weight) and the factor that rescales earlier accumulations.
+// of each weight; fine: three parts, all 24) and the factor that rescales
+// earlier accumulations.
 struct BlockWeights {
-  u32x4 phi, plo;
+  u32x4 phi, plo, plast;
   float alpha;
 };
+
+// The upper halves of two words (bf16 by truncation), and x less its own: the
+// rest is exact, so that three such parts hold all 24 bits of x.
+__device__ __forceinline__ uint32_t upper_halves(float x0, float x1) {
+  return __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, x1), __builtin_bit_cast(uint32_t, x0), 0x07060302u);
+}
+__device__ __forceinline__ float without_upper_half(float x) {
+  return x - __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, x) & 0xFFFF0000u);
+}
 
 // Scores and online-softmax update for one block.
 // nvalid = tokens of the block (from its first token) inside the sequence.
@@ -214,7 +217,7 @@ struct PageScales {
   float c0, c1, v0, v1;
 };
 
-// kFine: the weights go as two fp16 parts (see attend_segment_fp8).
+// kFine: the weights go as three bf16 parts (see attend_segment_fp8).
 template <int D, bool kMayBeEmpty = false, bool kScaled = false, bool kFine = false>
 __device__ __forceinline__ BlockWeights score_block(const KHalf<D>& b, const u32x4* qf, int nvalid, int grp,
                                                     float scale_log2, SoftmaxState<D>& st,
@@ -248,7 +251,7 @@ __device__ __forceinline__ BlockWeights score_block(const KHalf<D>& b, const u32
   w.alpha = fast_exp2(st.m - mref);
   st.m = mnew;
   float ps = 0.f;
-  uint32_t hi[4], lo[4];
+  uint32_t hi[4], lo[4], last[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     float p0 = fast_exp2(sc[2 * i] - mref);
@@ -261,10 +264,10 @@ __device__ __forceinline__ BlockWeights score_block(const KHalf<D>& b, const u32
       p1 *= vs;
     }
     if constexpr (kFine) {
-      const f16x2 h = __builtin_convertvector(f32x2{p0, p1}, f16x2);
-      const f16x2 l = __builtin_convertvector(f32x2{p0 - float(h[0]), p1 - float(h[1])}, f16x2);
-      hi[i] = __builtin_bit_cast(uint32_t, h);
-      lo[i] = __builtin_bit_cast(uint32_t, l);
+      const float r0 = without_upper_half(p0), r1 = without_upper_half(p1);
+      hi[i] = upper_halves(p0, p1);
+      lo[i] = upper_halves(r0, r1);
+      last[i] = upper_halves(without_upper_half(r0), without_upper_half(r1));
       continue;
     }
     const uint32_t h0 = bf16_bits(p0), h1 = bf16_bits(p1);
@@ -275,6 +278,7 @@ __device__ __forceinline__ BlockWeights score_block(const KHalf<D>& b, const u32
   st.lsum = st.lsum * w.alpha + ps;
   w.phi = u32x4{hi[0], hi[1], hi[2], hi[3]};
   w.plo = u32x4{lo[0], lo[1], lo[2], lo[3]};
+  if constexpr (kFine) w.plast = u32x4{last[0], last[1], last[2], last[3]};
   return w;
 }
 
@@ -296,13 +300,9 @@ __device__ __forceinline__ void accumulate_block(VHalf<D>& b, const BlockWeights
 #pragma unroll
   for (int jb = 0; jb < Shape<D>::JB; ++jb) {
     st.o[jb] *= w.alpha;
-    if constexpr (kFine) {
-      st.o[jb] = mfma_f16(b.v[jb], w.phi, st.o[jb]);
-      st.o[jb] = mfma_f16(b.v[jb], w.plo, st.o[jb]);
-      continue;
-    }
     st.o[jb] = mfma_bf16(b.v[jb], w.phi, st.o[jb]);
     st.o[jb] = mfma_bf16(b.v[jb], w.plo, st.o[jb]);
+    if constexpr (kFine) st.o[jb] = mfma_bf16(b.v[jb], w.plast, st.o[jb]);
   }
 }
 
@@ -815,32 +815,22 @@ __device__ __forceinline__ void widen_k(const KHalf8<D>& r, KHalf<D>& b) {
     }
 }
 
-// The same as two fp16.
-template <bool kHigh>
-__device__ __forceinline__ uint32_t widen2_f16(uint32_t codes4) {
-  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(codes4, 1.0f, kHigh));
-}
-
-template <int D, bool kFine>
+template <int D>
 __device__ __forceinline__ void widen_v(const VHalf8<D>& r, VHalf<D>& b) {
 #pragma unroll
   for (int jb = 0; jb < Shape<D>::JB; ++jb) {
     const uint32_t p0 = r.v[0][jb / 4][jb % 4], p1 = r.v[1][jb / 4][jb % 4];
-    if constexpr (kFine) {
-      b.v[jb] = u32x4{widen2_f16<false>(p0), widen2_f16<true>(p0), widen2_f16<false>(p1), widen2_f16<true>(p1)};
-      continue;
-    }
     b.v[jb] = u32x4{widen2<false>(p0), widen2<true>(p0), widen2<false>(p1), widen2<true>(p1)};
   }
 }
 
 // One segment over an fp8 cache; otherwise as attend_segment.
-// kFine (appending steps): the P.V product on fp16 operands. An E4M3 value is
-// exact in fp16, too, and a weight as two fp16 parts keeps 22 bits where two bf16
-// parts keep 16: out is off by 3e-7 of its size instead of 2.5e-6, for the same
-// matrix work. fp16's range wants the weights near 1, so the pages' value scales
-// enter as ratios to a power of two that is at least the largest one of the
-// segment so far, which O is kept in units of.
+// kFine (appending steps): a weight, times its page's value scale, enters the
+// P.V product as three bf16 parts, all of its 24 bits, where two keep 16: out is off
+// by 1.6e-7 of its size instead of 2.5e-6. bf16 has fp32's exponents, so how unlike
+// the pages' scales are does not matter; fp16 parts over a common reference, no
+// faster (162.7 against 163.6 us for the 842k tokens of 512 sequences), would lose
+// what lies 2^-24 below it, and a page of zero values (scale 1) is enough for that.
 template <int D, int R, bool kShared = false, bool kFine = false>
 __device__ __forceinline__ void attend_segment_fp8(const AttnArgs& a, const Segment& item, WorkerRows& w, int index,
                                                    float* stash) {
@@ -899,9 +889,6 @@ __device__ __forceinline__ void attend_segment_fp8(const AttnArgs& a, const Segm
   st.m = -__builtin_inff();
   st.lsum = 0.f;
 
-  float vref = 0x1p-126f;   // kFine: the value reference
-  // 1 / x of a power of two, by its exponent
-  auto over = [](float x) { return __builtin_bit_cast(float, 0x7F000000u - __builtin_bit_cast(uint32_t, x)); };
   // Block at pg from (kc, vc); the block R - 1 ahead loads into (kn, vn).
   auto step = [&](int pg, KHalf8<D>& kc, VHalf8<D>& vc, KHalf8<D>& kn, VHalf8<D>& vn) {
     const bool more = pg + 2 * (R - 1) < pe;
@@ -913,24 +900,11 @@ __device__ __forceinline__ void attend_segment_fp8(const AttnArgs& a, const Segm
     const int nvalid = min(len - pg * kPage, pg + 1 < pe ? 2 * kPage : kPage);
     KHalf<D> kw;
     widen_k(kc, kw);
-    PageScales scl{a.scale_log2 * kc.ks[0], a.scale_log2 * kc.ks[1], vc.vs[0], vc.vs[1]};
-    float moved = 1.f;   // the old reference over the new one
-    if constexpr (kFine) {
-      const float top = fmaxf(scl.v0, scl.v1);
-      if (top > vref) {   // wave-uniform; scales are at most 2^110
-        const uint32_t b = __builtin_bit_cast(uint32_t, top);
-        const float up = __builtin_bit_cast(float, ((b >> 23) + ((b & 0x7FFFFFu) ? 1u : 0u)) << 23);
-        moved = vref * over(up);
-        vref = up;
-      }
-      scl.v0 *= over(vref);
-      scl.v1 *= over(vref);
-    }
-    BlockWeights w = score_block<D, false, true, kFine>(kw, qf, nvalid, grp, a.scale_log2, st, scl);
-    if constexpr (kFine) w.alpha *= moved;
+    const PageScales scl{a.scale_log2 * kc.ks[0], a.scale_log2 * kc.ks[1], vc.vs[0], vc.vs[1]};
+    const BlockWeights w = score_block<D, false, true, kFine>(kw, qf, nvalid, grp, a.scale_log2, st, scl);
     if (more) load_v8(c, nxt, vn);
     VHalf<D> vw;
-    widen_v<D, kFine>(vc, vw);
+    widen_v(vc, vw);
     accumulate_block<D, kFine>(vw, w, nvalid, grp, st);
   };
   for (int pg = pb; pg < pe; pg += 2 * R) {
@@ -943,8 +917,7 @@ __device__ __forceinline__ void attend_segment_fp8(const AttnArgs& a, const Segm
 
   float lt = st.lsum + __shfl_xor(st.lsum, 16);
   lt += __shfl_xor(lt, 32);
-  float inv = lt > 0.f ? 1.f / lt : 0.f;
-  if constexpr (kFine) inv *= vref;
+  const float inv = lt > 0.f ? 1.f / lt : 0.f;
   f32x4 o[JB];
 #pragma unroll
   for (int jb = 0; jb < JB; ++jb) o[jb] = st.o[jb] * inv;

@@ -83,7 +83,7 @@ struct AttnArgs {
   // hold E4M3 codes, and these the per-(page, KV head) scales.
   const float* k_scale;
   const float* v_scale;
-  bool fine;                  // fp8: weights as two fp16 parts (the runner's appending steps)
+  bool fine;                  // fp8: weights as three bf16 parts (the runner's appending steps)
   // Optional side job: copy_ints ints from copy_src (the merge rows in
   // pinned host memory) to copy_dst (device), 64 per worker, so that the
   // launch after this one reads its rows from device memory. NULL dst: none.
