@@ -248,8 +248,10 @@ sf_status sf_decode_attn_append(const sf_attn_desc* desc, const sf_plan_info* in
  * buffers, the split-K workspace and a few events, one recorded after every
  * 16th step: a buffer is rewritten only after the step that read it has
  * ended, so the host plans ahead while the kernels of earlier steps run. One runner serves one device (the current one at
- * creation) and one caller stream at a time; steps on different streams, or
- * calls that overlap, are not supported.
+ * creation), and its calls must not overlap on the host. A step (or a store, a
+ * weights pass or an eviction, below) on another stream than the last one waits on the
+ * device for the runner's calls so far, as they share the workspace; not where either
+ * stream is being captured into a graph: there the caller orders them.
  */
 typedef struct sf_runner sf_runner;
 

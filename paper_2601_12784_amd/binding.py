@@ -1101,7 +1101,8 @@ class DecodeAttention:
     """Plan + attention + combine for successive decode steps, through the
     library's native runner (sf_runner_create / sf_runner_step): one call per
     step plans into the runner's pinned, device-mapped ring and launches the
-    kernels, which read that work list in place, on the caller's stream. Tensor checks run once per
+    kernels, which read that work list in place, on the caller's stream (a call on another stream than
+    the last one waits there for the calls before it: they share a workspace). Tensor checks run once per
     distinct set of tensors (the last 64 sets are remembered)."""
 
     def __init__(self, num_q_heads, num_kv_heads, head_dim, device=None, num_cus=None,

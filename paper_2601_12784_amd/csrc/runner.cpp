@@ -92,6 +92,7 @@ struct sf_runner {
   uint64_t num_marks = 0;  // marks recorded so far (the next one reuses marks[num_marks % kMarks])
   uint64_t unmarked = 0;   // steps [unmarked, steps) have no mark yet
   hipStream_t last_stream = nullptr;
+  hipEvent_t order = nullptr;   // on the last stream, for a call on another
   void* workspace = nullptr;
   uint64_t workspace_bytes = 0;
   Lent lent;
@@ -180,14 +181,38 @@ bool same_shape(const sf_runner* r, const sf_attn_desc* desc) {
          desc->head_dim == r->shape.head_dim && desc->page_size == r->shape.page_size;
 }
 
+bool capturing(hipStream_t stream) {
+  hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
+  return hipStreamIsCapturing(stream, &status) == hipSuccess && status != hipStreamCaptureStatusNone;
+}
+
+// A call on another stream than the last one comes after the runner's calls so
+// far on the device, too: all of them share the workspace, and an eviction's lists
+// there are indexes. Where either stream is being captured the wait would tie the
+// graph to work outside of it, or that work to the graph.
+sf_status follow_last_stream(sf_runner* r, hipStream_t main) {
+  if (r->steps == 0 || main == r->last_stream) return SF_OK;
+  if (capturing(main) || capturing(r->last_stream)) return mark_steps(r);   // a mark stands for steps of one stream
+  // an event of its own: unlike the marks' it publishes what the calls wrote
+  if (mark_steps(r) == SF_OK && hipEventRecord(r->order, r->last_stream) == hipSuccess &&
+      hipStreamWaitEvent(main, r->order, 0) == hipSuccess)
+    return SF_OK;
+  // the caller may have destroyed the last stream: the device is waited for
+  (void)hipGetLastError();
+  if (hipDeviceSynchronize() != hipSuccess) return SF_ERR_HIP;
+  for (auto& p : r->ring) p.used = false;
+  r->unmarked = r->steps;
+  return SF_OK;
+}
+
 // Takes the next ring slot for a call on `main`: after the step that last read
-// it has ended. A mark stands for steps of one stream: a new stream closes the run.
+// it has ended.
 sf_status open_slot(sf_runner* r, hipStream_t main, Pinned** slot) {
   Pinned& pin = r->ring[r->steps % kRing];
   sf_status st = pin.used ? wait_step(r, pin.last_step) : SF_OK;
   if (st != SF_OK) return st;
   pin.used = false;
-  if (r->unmarked < r->steps && main != r->last_stream && (st = mark_steps(r)) != SF_OK) return st;
+  if ((st = follow_last_stream(r, main)) != SF_OK) return st;
   *slot = &pin;
   return SF_OK;
 }
@@ -212,9 +237,9 @@ sf_status close_slot(sf_runner* r, hipStream_t main, Pinned& pin, sf_status st) 
 
 // Slots are reused by waiting on the host, which a graph's replays would not.
 sf_status not_capturing(hipStream_t main) {
-  hipStreamCaptureStatus capturing = hipStreamCaptureStatusNone;
-  if (hipStreamIsCapturing(main, &capturing) != hipSuccess) return SF_ERR_HIP;
-  return capturing == hipStreamCaptureStatusNone ? SF_OK : SF_ERR_UNSUPPORTED;
+  hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
+  if (hipStreamIsCapturing(main, &status) != hipSuccess) return SF_ERR_HIP;
+  return status == hipStreamCaptureStatusNone ? SF_OK : SF_ERR_UNSUPPORTED;
 }
 
 // Makes the runner's device current for a call, and the caller's again after it.
@@ -306,6 +331,7 @@ extern "C" sf_status sf_runner_create(const sf_attn_desc* shape, const sf_plan_o
   for (auto& m : r->marks)
     if (hipEventCreateWithFlags(&m.ev, hipEventDisableTiming | hipEventDisableSystemFence) != hipSuccess)
       st = SF_ERR_HIP;
+  if (hipEventCreateWithFlags(&r->order, hipEventDisableTiming) != hipSuccess) st = SF_ERR_HIP;
   if (st != SF_OK) {
     sf_runner_destroy(r);
     return st;
@@ -328,6 +354,7 @@ extern "C" void sf_runner_destroy(sf_runner* r) {
     if (m.ev && m.valid) (void)hipEventSynchronize(m.ev);
     if (m.ev) (void)hipEventDestroy(m.ev);
   }
+  if (r->order) (void)hipEventDestroy(r->order);
   (void)wait_lent(r->lent);
   for (auto ev : r->lent.done)
     if (ev) (void)hipEventDestroy(ev);
@@ -552,13 +579,11 @@ static sf_status runner_extend(sf_runner* r, const sf_attn_desc* desc, const int
   hipStream_t main = static_cast<hipStream_t>(stream);
   // Slots are reused by waiting for events on the host, which a graph's
   // replays would not: a capturing stream is left to sf_extend_attn.
-  hipStreamCaptureStatus capturing = hipStreamCaptureStatusNone;
-  if (hipStreamIsCapturing(main, &capturing) != hipSuccess) return SF_ERR_HIP;
-  if (capturing != hipStreamCaptureStatusNone) return SF_ERR_UNSUPPORTED;
+  sf_status st = not_capturing(main);
+  if (st != SF_OK) return st;
 
   // Other memory than the last call's: nothing may still use either.
   const bool per_call = memory->device_per_call == 1;
-  sf_status st = SF_OK;
   Lent& lent = r->lent;
   const uint64_t slot_bytes = memory->slots > 0 ? memory->pinned_bytes / memory->slots / 32 * 32 : 0;
   if (!per_call && (lent.device != memory->device || lent.device_bytes != memory->device_bytes)) {
