@@ -594,7 +594,8 @@ typedef struct sf_extend_info {
  * Work list, int32 rows of 8: seq, kv_head, t0, nt, P_s, cu_s, steps, 0.
  * Lengths must satisfy 0 <= E_s <= L_s <= 16 * block_table_stride.
  * work_host NULL only reports the sizes in *info; SF_ERR_CAPACITY if
- * work_capacity_bytes < info->work_bytes.
+ * work_capacity_bytes < info->work_bytes; SF_ERR_UNSUPPORTED for more than
+ * floor((2^32 - 1) / 768) items.
  */
 sf_status sf_extend_attn_plan(const sf_attn_desc* desc, const int32_t* seq_lens_host,
                               const int32_t* q_lens_host, int32_t* work_host,

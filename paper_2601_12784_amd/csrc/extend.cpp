@@ -65,6 +65,9 @@ extern "C" sf_status sf_extend_attn_plan(const sf_attn_desc* desc, const int32_t
   if (!info) return SF_ERR_INVALID_ARG;
   if ((st = check_extend_lengths(desc, seq_lens_host, q_lens_host, &rows)) != SF_OK) return st;
   const int32_t per_item = kExtendRows / (desc->num_q_heads / desc->num_kv_heads);
+  int64_t count = 0;
+  for (int32_t s = 0; s < desc->num_seqs; ++s) count += (int64_t(q_lens_host[s]) + per_item - 1) / per_item * desc->num_kv_heads;
+  if (count > kExtendMaxItems) return SF_ERR_UNSUPPORTED;
 
   std::vector<Item> items;
   int32_t qrow0 = 0;
@@ -317,6 +320,7 @@ sf_status sf::extend_plan_parts(const sf_attn_desc* desc, const int32_t* seq_len
   if (store)
     for (int32_t s = 0; s < desc->num_seqs; ++s)
       if (news[s] > 0) stores += (pages_of(lens[s]) - (lens[s] - news[s]) / kPage + run - 1) / run;
+  if (parts > kExtendMaxItems) return SF_ERR_UNSUPPORTED;
   if (parts + merges + stores > INT32_MAX / kItemInts) return SF_ERR_INVALID_ARG;
   plan->rows = rows;
   plan->num_parts = int32_t(parts);

@@ -312,6 +312,7 @@ struct ExtendArgs {
 // of sf_extend_attn_plan, and of the small items that sf_runner_extend's plan
 // takes where the large ones would leave compute units idle.
 constexpr int kExtendRows = 384;
+constexpr int64_t kExtendMaxItems = ((int64_t(1) << 32) - 1) / 768;   // workgroups of 768 threads: 2^32 threads are too many for a launch
 constexpr int kExtendSmallRows = 128;
 
 // The plan of sf_runner_extend: rows of kItemInts ints, in this order.
