@@ -633,10 +633,13 @@ sf_status sf_extend_attn(const sf_attn_desc* desc, const sf_extend_info* info, c
  * token, too, as stored. out is fp32 [T][Hq][D], or bf16 if out_bf16 is 1 (rounded once,
  * to nearest even). Numerics: scores from bf16 q and the codes, exact in bf16,
  * with fp32 accumulation, the page's key scale applied in fp32; softmax weights
- * and values enter the P.V product as fp16, values as code * scale over a power of
- * two that is at least the largest value scale that the walk has met. Within
- * 2^-14 of that largest scale, the error is at most 2^-10 times sum_t p_t |V_t| /
- * sum_t p_t plus fp32 rounding; lse is fp32 throughout. Errors as
+ * and values enter the P.V product as fp16, values as code * scale over the least power
+ * of two that none of the value scales met by the walk exceeds. With p_t = exp(z_t - max z), P =
+ * sum_t p_t and S the largest value scale of the pages that a sequence's rows read,
+ *   |err| <= 2^-10 sum_t p_t |V_t| / P + 2^-24 S + 2^-25 sum_t |V_t| / P
+ * (t = 0 .. P_s + j) plus fp32 rounding, and a bf16 out's own. The second term is that of values far
+ * below the largest scale: pages of small scale behind one of a large one, and dims that are
+ * small in their tile; lse is fp32 throughout. Errors as
  * sf_decode_attn_fp8, and SF_ERR_INVALID_ARG for another out_bf16 than 0 and 1.
  */
 sf_status sf_extend_attn_fp8(const sf_attn_desc* desc, const sf_extend_info* info, const int32_t* work_host,

@@ -288,8 +288,8 @@ __device__ __forceinline__ u32x4 settle(TileWeights& t, PageFactors<kFp8> c, flo
 // way into LDS: keys to bf16, exact, with the page's scale left to the factor of
 // its scores; values to fp16 times their page's scale over a reference, one
 // rounding. The reference is a power of two, at least the largest value scale of
-// the walk so far (so no product leaves fp16's range, and pages of any smaller
-// scale keep their precision down to 2^-14 of it); it goes with the step's key scales
+// the walk so far (so no product leaves fp16's range; values keep their 11 bits down
+// to 2^-14 of it, and what is smaller is off by 2^-25 of it at most); it goes with the step's key scales
 // through LDS, and a wave rescales its O where it has moved, which the scales'
 // spread makes rare. The pool's 16-byte pieces are half as many, so the staging
 // waves take one each at D = 128, and four waves are enough at D = 64. Bound as

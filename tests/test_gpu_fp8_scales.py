@@ -14,8 +14,9 @@ import pytest
 import torch
 
 from oracle import cache_ref as R
+from oracle import fp8_ref
 from paper_2601_12784_amd import binding as B
-from test_gpu_cache import Cache, bits, check, new_tokens, reference
+from test_gpu_cache import Cache, _give_pages, bits, check, new_tokens, reference, wide
 
 pytestmark = pytest.mark.gpu
 
@@ -82,3 +83,53 @@ def test_append_step_over_unlike_scales(heads, kind, size, lens):
     check(lse.cpu().numpy(), wl, tl, "lse")
     plain = attn(q.cuda(), c.g_k, c.g_v, c.g_bt, lens, scale, fp8=c.g_fp8)
     check(plain.cpu().numpy(), want, reference(c, q, lens, news, scale, "append")[2], "plain step")
+
+
+@pytest.mark.parametrize("heads", [(4, 1, 64), (28, 4, 128)])
+@pytest.mark.parametrize("lens,news", [([900, 60], [70, 60]), ([6000], [40])])   # whole walks, and walks cut into parts
+@pytest.mark.parametrize("lift,small", [(0, 9), (13, 9), (20, 0), (-6, 5)])
+def test_extend_bound_over_unlike_scales(heads, lens, news, lift, small):
+    """The header's bound, with each of its terms the largest somewhere: the first page's value scale is 2^lift times the
+    others' (lift > 0: for dim 0, its only one), and half of every tile's dims are 2^-small of the others. p_t = exp(z_t - max z), P its sum, S the
+    largest value scale: 2^-10 sum p|V| / P + 2^-24 S + 2^-25 sum |V| / P, and fp32's part as in test_gpu_cache.py."""
+    hq, hkv, d = heads
+    g = hq // hkv
+    held = [L - e for L, e in zip(lens, news)]
+    c = Cache(held, hkv, d, True, 111 + d, spare=20, stride_extra=8, spread=0.5, k_mult=2.0)
+    for s, L in enumerate(held):
+        for p in c.bt[s, : -(-L // 16)]:
+            for h in range(hkv):
+                codes = R.tile_codes(c.v, p, h, d, True)
+                value = fp8_ref.values()[codes[:, d // 2:]] * 2.0 ** -small
+                codes[:, d // 2:] = fp8_ref.encode(np.where(np.isnan(value), 0, value).astype(np.float32))
+                if lift > 0 and p == c.bt[s, 0]:
+                    codes[:, 1:] = 0
+                R.put_tile_codes(c.v, p, h, d, True, codes)
+        if L:
+            c.vs[c.bt[s, 0]] *= np.float32(2.0 ** lift)
+    c.g_v.copy_(torch.from_numpy(c.v))
+    c.g_fp8[1].copy_(torch.from_numpy(c.vs))
+    _give_pages(c, held, lens)
+    T, scale = sum(news), 1.0 / np.sqrt(d)
+    kn, vn = new_tokens(T, hkv, d, 52)
+    q = new_tokens(T, hq, d, 53)[0]
+    out = torch.empty((T, hq, d), device="cuda")
+    B.ExtendAttention(hq, hkv, d)(q.cuda(), c.g_k, c.g_v, c.g_bt, lens, news, scale, out=out, k_new=kn.cuda(), v_new=vn.cuda(),
+                                  fp8=c.g_fp8)
+    R.store_fp8(bits(kn).reshape(kn.shape), bits(vn).reshape(vn.shape), lens, news, c.bt, c.k, c.v, c.ks, c.vs)
+    c.same("extend")
+    want, _, tol, _ = reference(c, q, lens, news, scale, "extend")
+    print("of the first term alone:", float((np.abs(out.cpu().numpy() - want) / tol).max()))
+    qd, row = wide(q), 0
+    for s, (L, e) in enumerate(zip(lens, news)):
+        largest = float(c.vs[c.bt[s, : -(-L // 16)]].max())
+        for h in range(hkv):
+            k, v = c.dense(s, h, L)
+            z = scale * np.einsum("egd,td->egt", qd[row:row + e, h * g:(h + 1) * g], k)
+            seen = np.arange(L)[None, :] <= L - e + np.arange(e)[:, None]
+            z = np.where(seen[:, None, :], z, -np.inf)
+            total = np.exp(z - z.max(axis=2, keepdims=True)).sum(axis=2)
+            every = np.einsum("et,td->ed", seen.astype(float), np.abs(v))
+            tol[row:row + e, h * g:(h + 1) * g] += 2.0 ** -24 * largest + 2.0 ** -25 * every[:, None, :] / total[..., None]
+        row += e
+    check(out.cpu().numpy(), want, tol, "extend")
