@@ -12,6 +12,7 @@ import ctypes
 import os
 import re
 import threading
+import weakref
 
 import numpy as np
 import torch
@@ -290,6 +291,8 @@ def _check(where, st):
 
 
 def _dev(t: torch.Tensor, name: str, dtype, shape=None):
+    if isinstance(t, torch.Tensor) and t.is_cuda and t.dtype is dtype and t.is_contiguous() and (shape is None or t.shape == shape):
+        return t
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
     if not t.is_cuda:
@@ -298,9 +301,7 @@ def _dev(t: torch.Tensor, name: str, dtype, shape=None):
         raise ValueError(f"{name} must be {dtype} (got {t.dtype})")
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
-    if shape is not None and t.shape != shape:
-        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
-    return t
+    raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
 
 
 # ----------------------------------------------------------------------------
@@ -1102,8 +1103,8 @@ class DecodeAttention:
     library's native runner (sf_runner_create / sf_runner_step): one call per
     step plans into the runner's pinned, device-mapped ring and launches the
     kernels, which read that work list in place, on the caller's stream (a call on another stream than
-    the last one waits there for the calls before it: they share a workspace). Tensor checks run once per
-    distinct set of tensors (the last 64 sets are remembered)."""
+    the last one waits there for the calls before it: they share a workspace). A cache's
+    tensors are checked once (the last 64 caches are remembered)."""
 
     def __init__(self, num_q_heads, num_kv_heads, head_dim, device=None, num_cus=None,
                  opts: sf_plan_opts | None = None):
@@ -1117,11 +1118,13 @@ class DecodeAttention:
         self.L = lib()
         self._runners = {}
         self._info = sf_plan_info()
-        self._extras = sf_runner_extras()
+        self._info_ref = ctypes.byref(self._info)
+        self._extras, self._fp8_only = sf_runner_extras(), sf_runner_extras()
+        self._extras_ref, self._fp8_only_ref = ctypes.byref(self._extras), ctypes.byref(self._fp8_only)
         self._checked = {}
         self._desc_key = None
-        self._desc = None
-        self.last_info = None
+        self._desc = self._desc_ref = None
+        self._stepped = False
         self._lse = None
         self._host_checked = False   # set by a caller that checked its own host copy
 
@@ -1140,29 +1143,29 @@ class DecodeAttention:
         return r
 
     def _check_tensors(self, q, k_pool, v_pool, block_table, out, lse, fp8=None):
-        key = (q.data_ptr(), k_pool.data_ptr(), v_pool.data_ptr(), block_table.data_ptr(),
-               out.data_ptr(), None if lse is None else lse.data_ptr(), q.shape,
-               k_pool.shape, v_pool.shape, block_table.shape,
-               None if fp8 is None else (fp8[0].data_ptr(), fp8[1].data_ptr()))
-        if key in self._checked:
-            return
-        b, hkv, d = q.shape[0], self.hkv, self.d
+        hkv, d, b = self.hkv, self.d, q.shape[0]
         _dev(q, "q", torch.bfloat16, (b, self.hq, d))
+        _dev(out, "out", torch.float32, (b, self.hq, d))
+        if lse is not None:
+            _dev(lse, "lse", torch.float32, (b, self.hq))
+        ks, vs = (None, None) if fp8 is None else fp8
+        key = (b, id(k_pool), id(v_pool), id(block_table), id(ks), id(vs))
+        known = self._checked.get(key)
+        if known is not None and known[0]() is k_pool and known[1]() is v_pool and known[2]() is block_table and \
+                (fp8 is None or (known[3]() is ks and known[4]() is vs)):
+            return
         if fp8 is None:
             _dev(k_pool, "k_pool", torch.bfloat16, (k_pool.shape[0], hkv, d // 8, PAGE, 8))
             _dev(v_pool, "v_pool", torch.bfloat16, (k_pool.shape[0], hkv, d, PAGE))
         else:
-            _dev(k_pool, "k_pool8", torch.uint8, (k_pool.shape[0], hkv, PAGE * d))
-            _dev(v_pool, "v_pool8", torch.uint8, (k_pool.shape[0], hkv, PAGE * d))
-            _dev(fp8[0], "k_scale", torch.float32, (k_pool.shape[0], hkv))
-            _dev(fp8[1], "v_scale", torch.float32, (k_pool.shape[0], hkv))
+            _dev(k_pool, "k_pool", torch.uint8, (k_pool.shape[0], hkv, PAGE * d))
+            _dev(v_pool, "v_pool", torch.uint8, (k_pool.shape[0], hkv, PAGE * d))
+            _dev(ks, "k_scale", torch.float32, (k_pool.shape[0], hkv))
+            _dev(vs, "v_scale", torch.float32, (k_pool.shape[0], hkv))
         _dev(block_table, "block_table", torch.int32, (b, block_table.shape[1]))
-        _dev(out, "out", torch.float32, (b, self.hq, d))
-        if lse is not None:
-            _dev(lse, "lse", torch.float32, (b, self.hq))
-        if len(self._checked) >= 64:      # a few tensor sets in rotation stay checked
+        if len(self._checked) >= 64:      # a few caches in rotation stay checked
             self._checked.clear()
-        self._checked[key] = True
+        self._checked[key] = [weakref.ref(t) for t in (k_pool, v_pool, block_table, ks, vs) if t is not None]
 
     def reserve(self, seq_lens, num_pages, block_table_stride, chunk_pages=None, fp8=False, stream=None):
         """Sizes the native runner's workspace and work-list ring for a step
@@ -1204,6 +1207,7 @@ class DecodeAttention:
         dkey = (b, block_table.shape[1], k_pool.shape[0], float(scale))
         if dkey != self._desc_key:
             self._desc = make_desc(b, self.hq, self.hkv, self.d, block_table.shape[1], k_pool.shape[0], scale)
+            self._desc_ref = ctypes.byref(self._desc)
             self._desc_key = dkey
         if isinstance(seq_lens, torch.Tensor):
             seq_lens = seq_lens.cpu().numpy()
@@ -1211,8 +1215,13 @@ class DecodeAttention:
                             and seq_lens.flags.c_contiguous) else np.ascontiguousarray(seq_lens, np.int32)
         if lens.shape != (b,):
             raise ValueError("seq_lens must have one entry per sequence")
-        ex = self._extras
-        ex.k_new = ex.v_new = ex.new_pages_host = ex.k_scale = ex.v_scale = ex.attn_start = ex.attn_end = None
+        # A plain step has no extras, one over an fp8 cache only the scales.
+        extras = None
+        if append is not None or attn_events is not None:
+            ex, extras = self._extras, self._extras_ref
+            ex.k_new = ex.v_new = ex.new_pages_host = ex.k_scale = ex.v_scale = ex.attn_start = ex.attn_end = None
+        elif fp8 is not None:
+            ex, extras = self._fp8_only, self._fp8_only_ref
         pages = None
         if append is not None:
             k_new, v_new, new_pages = append
@@ -1239,13 +1248,17 @@ class DecodeAttention:
             timed = stream or torch.cuda.current_stream(self.device)
             ex.attn_start = kernel_event(attn_events[0], timed)
             ex.attn_end = kernel_event(attn_events[1], timed)
-        info = self._info
         _check("sf_runner_step", self.L.sf_runner_step(
-            self._runner(chunk_pages), ctypes.byref(self._desc), _host_addr(lens), q.data_ptr(), k_pool.data_ptr(),
+            self._runner(chunk_pages), self._desc_ref, _host_addr(lens), q.data_ptr(), k_pool.data_ptr(),
             v_pool.data_ptr(), block_table.data_ptr(), out.data_ptr(), None if lse is None else lse.data_ptr(),
-            ctypes.byref(ex), main, ctypes.byref(info)))
-        self.last_info = sf_plan_info.from_buffer_copy(info)
+            extras, main, self._info_ref))
+        self._stepped = True
         return out
+
+    @property
+    def last_info(self):
+        """A copy of the last step's plan; None before the first."""
+        return sf_plan_info.from_buffer_copy(self._info) if self._stepped else None
 
     def _call_desc(self, k_pool, block_table, seq_lens, scale):
         """(desc, lengths) of a call besides the steps."""
