@@ -135,10 +135,13 @@ __device__ __forceinline__ bool row_counts(float lse, bool there) {
 // weights that the keys had come with them, so one segment runs into the next. Wave
 // w starts with row w; a row names the one that follows it, which is requested with the
 // segment's first keys: the list may lie in host memory. The results wait in LDS
-// and are stored once the wave has no more keys (or 24 blocks of them): stored as they
+// and are stored once the wave has no more keys or LDS is full: stored as they
 // come, 64 bytes here and there in the middle of the read stream, they cost 21 us of the
-// long-tail batch's 133 (0.72 GB of keys, 11 MB of weights).
-constexpr int kStash = 24;   // blocks
+// long-tail batch's 133 (0.72 GB of keys, 11 MB of weights). The stash is as large as two
+// workgroups per CU allow, 39 blocks per wave: batches of 22 and 26 blocks per wave
+// take the same with 24 (125 and 151 us), one of 65 takes 375 us against 384 (fp8 211, 218).
+constexpr int kStashBlockBytes = kWaves * (64 * 8 + 4);   // a sum and a page per lane, a KV head
+constexpr int kStash = (160 << 10) / 2 / kStashBlockBytes;
 
 template <int D, bool kFp8>
 __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 2))) void key_weights_step_kernel(WeightArgs a) {
