@@ -21,8 +21,8 @@
 // dim-major, so a token's values are 2 bytes of D 32-byte rows, and a page with
 // one freed slot reads and writes its whole tile: the long-tail batch halved takes
 // 450 us for 2.2 GB of tiles (0.72 GB of tokens); 64 sequences of 2112 fp8 tokens cut to
-// 2048, at one or two tokens per tile and most of them with none, 27 us, of which waves wait two thirds
-// (full stores of their tiles 33).
+// 2048, at one or two tokens per tile and most of them with none, 27 us, of which waves wait more than
+// half (full stores of their tiles 33).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 

@@ -15,8 +15,8 @@
 // go out as 1 KiB per wave store. Values of new tokens are read two
 // bytes at a time (16 lanes, 32 contiguous bytes per token), which is not what
 // bounds it: memory is. 95,330 tokens of 32 prompts (28/4 heads, D = 128; 195 MB in,
-// 98 MB out) take 58 us = 5.0 TB/s, more than a 4 GiB device copy's 4.8; one token of
-// 512 sequences 9 us, latency. With the reads of a lane's four slots behind branches
+// 98 MB out) take 62 us (56 at best) = 4.7 TB/s, a 4 GiB device copy's rate; one token of
+// 512 sequences 10 us, latency. With the reads of a lane's four slots behind branches
 // the prompts took 68 us.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
