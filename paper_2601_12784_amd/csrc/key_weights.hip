@@ -19,8 +19,8 @@
 // the keys (long-tail batch, 704k tokens, 28/4 heads, D = 128, bf16: 124 us = 6.0 TB/s of
 // a plain read's 6.85; fp8 73 us = 5.2 TB/s). Prompts, or their last rows, are bound by matrix and
 // vector work: key_weights_rows_kernel holds the keys and streams the rows through LDS (every row of
-// 32 long-tail prompts, 2.27 TFLOP: 2.36 ms = 0.96 PFLOP/s; the last 32 rows of 16
-// prompts, fp8: 69 us). Counted per SIMD, 16 rows and 64 keys take 536 cycles: 16 MFMAs
+// 32 long-tail prompts, 2.27 TFLOP: 2.44 ms = 0.93 PFLOP/s; the last 32 rows of 16
+// prompts, fp8: 72 us). Counted per SIMD, 16 rows and 64 keys take 536 cycles: 16 MFMAs
 // (256) and 63 vector instructions, 16 of them exponentials of two issue slots (316). The
 // two hardly overlap. Work items, and the parts that long walks are cut into, are the host
 // plan's; key_weights_merge_kernel adds the parts of a cut item in order.
