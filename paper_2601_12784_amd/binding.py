@@ -1104,7 +1104,7 @@ class DecodeAttention:
     step plans into the runner's pinned, device-mapped ring and launches the
     kernels, which read that work list in place, on the caller's stream (a call on another stream than
     the last one waits there for the calls before it: they share a workspace). A cache's
-    tensors are checked once (the last 64 caches are remembered)."""
+    tensors are checked once (the first 256 sets are remembered while they live)."""
 
     def __init__(self, num_q_heads, num_kv_heads, head_dim, device=None, num_cus=None,
                  opts: sf_plan_opts | None = None):
@@ -1122,6 +1122,7 @@ class DecodeAttention:
         self._extras, self._fp8_only = sf_runner_extras(), sf_runner_extras()
         self._extras_ref, self._fp8_only_ref = ctypes.byref(self._extras), ctypes.byref(self._fp8_only)
         self._checked = {}
+        self._checks_left = 256   # views made anew for every call are never known: then nothing is remembered
         self._desc_key = None
         self._desc = self._desc_ref = None
         self._stepped = False
@@ -1149,23 +1150,26 @@ class DecodeAttention:
         if lse is not None:
             _dev(lse, "lse", torch.float32, (b, self.hq))
         ks, vs = (None, None) if fp8 is None else fp8
-        key = (b, id(k_pool), id(v_pool), id(block_table), id(ks), id(vs))
-        known = self._checked.get(key)
-        if known is not None and known[0]() is k_pool and known[1]() is v_pool and known[2]() is block_table and \
-                (fp8 is None or (known[3]() is ks and known[4]() is vs)):
-            return
+        remember = self._checks_left > 0
+        if remember:
+            key = (b, id(k_pool), id(v_pool), id(block_table), id(ks), id(vs))
+            known = self._checked.get(key)
+            if known is not None and known[0]() is k_pool and known[1]() is v_pool and known[2]() is block_table and \
+                    (fp8 is None or (known[3]() is ks and known[4]() is vs)):
+                return
+        n = k_pool.shape[0]
         if fp8 is None:
-            _dev(k_pool, "k_pool", torch.bfloat16, (k_pool.shape[0], hkv, d // 8, PAGE, 8))
-            _dev(v_pool, "v_pool", torch.bfloat16, (k_pool.shape[0], hkv, d, PAGE))
+            _dev(k_pool, "k_pool", torch.bfloat16, (n, hkv, d // 8, PAGE, 8))
+            _dev(v_pool, "v_pool", torch.bfloat16, (n, hkv, d, PAGE))
         else:
-            _dev(k_pool, "k_pool", torch.uint8, (k_pool.shape[0], hkv, PAGE * d))
-            _dev(v_pool, "v_pool", torch.uint8, (k_pool.shape[0], hkv, PAGE * d))
-            _dev(ks, "k_scale", torch.float32, (k_pool.shape[0], hkv))
-            _dev(vs, "v_scale", torch.float32, (k_pool.shape[0], hkv))
+            _dev(k_pool, "k_pool", torch.uint8, (n, hkv, PAGE * d))
+            _dev(v_pool, "v_pool", torch.uint8, (n, hkv, PAGE * d))
+            _dev(ks, "k_scale", torch.float32, (n, hkv))
+            _dev(vs, "v_scale", torch.float32, (n, hkv))
         _dev(block_table, "block_table", torch.int32, (b, block_table.shape[1]))
-        if len(self._checked) >= 64:      # a few caches in rotation stay checked
-            self._checked.clear()
-        self._checked[key] = [weakref.ref(t) for t in (k_pool, v_pool, block_table, ks, vs) if t is not None]
+        if remember:
+            self._checks_left -= 1
+            self._checked[key] = [weakref.ref(t) for t in (k_pool, v_pool, block_table, ks, vs) if t is not None]
 
     def reserve(self, seq_lens, num_pages, block_table_stride, chunk_pages=None, fp8=False, stream=None):
         """Sizes the native runner's workspace and work-list ring for a step

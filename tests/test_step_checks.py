@@ -35,9 +35,10 @@ def strided(t):
 
 @pytest.mark.parametrize("fp8", [False, True])
 @pytest.mark.parametrize("change", [other_type, shorter, strided])
-def test_another_tensor_at_a_remembered_address_is_checked(fp8, change):
+@pytest.mark.parametrize("remembered", [256, 4, 0])
+def test_another_tensor_at_a_remembered_address_is_checked(fp8, change, remembered):
     attn = B.DecodeAttention.__new__(B.DecodeAttention)
-    attn.hq, attn.hkv, attn.d, attn._checked = 4, 2, 64, {}
+    attn.hq, attn.hkv, attn.d, attn._checked, attn._checks_left = 4, 2, 64, {}, remembered
 
     def check(x):
         attn._check_tensors(x["q"], x["k_pool"], x["v_pool"], x["block_table"], x["out"], x["lse"],
