@@ -1162,8 +1162,8 @@ class DecodeAttention:
             _dev(k_pool, "k_pool", torch.bfloat16, (n, hkv, d // 8, PAGE, 8))
             _dev(v_pool, "v_pool", torch.bfloat16, (n, hkv, d, PAGE))
         else:
-            _dev(k_pool, "k_pool", torch.uint8, (n, hkv, PAGE * d))
-            _dev(v_pool, "v_pool", torch.uint8, (n, hkv, PAGE * d))
+            _dev(k_pool, "k_pool8", torch.uint8, (n, hkv, PAGE * d))
+            _dev(v_pool, "v_pool8", torch.uint8, (n, hkv, PAGE * d))
             _dev(ks, "k_scale", torch.float32, (n, hkv))
             _dev(vs, "v_scale", torch.float32, (n, hkv))
         _dev(block_table, "block_table", torch.int32, (b, block_table.shape[1]))
