@@ -842,6 +842,161 @@ sf_status sf_route(const sf_cost_model* model, double mu, int32_t min_initial_ve
                    int32_t num_trajs, int32_t* target, int32_t* num_routed);
 
 /*
+ * A decode step of groups that share their first tokens. Several trajectories sampled from one prompt hold the same pages
+ * first: sequences group_offsets[i] .. group_offsets[i+1] - 1 of the batch are group i, and its shared_lens[i] first
+ * tokens are the same for all members. The result is sf_decode_attn's (out and lse over each sequence's L_s tokens),
+ * but the pages that are whole within the shared tokens are read once for the group, from the block-table row of its
+ * first member with L_s > 0, and the members' queries meet them together:
+ * shared_lens[i] / 16 entries of the other members' rows are not read. Tokens behind those pages, the rest of the
+ * shared ones among them, come from each member's own row. Groups lie one behind the other and cover the batch
+ * (group_offsets[0] = 0, group_offsets[num_groups] = num_seqs); shared_lens[i] is at most L_s of every member with
+ * L_s > 0. Members with L_s = 0 get out = 0, lse = -inf.
+ *
+ * Plan (host only). A prompt's rows, members times g, are taken in blocks of at most 64 (4 tiles of 16), 1, 2 or a multiple of 4 blocks,
+ * which walk the same pages side by side; the pages of all prompts with one number of blocks, and those that
+ * sequences have to themselves, are each cut into equal runs, one per wave, as many runs as their share of the work.
+ * Results of runs that end inside a prompt or sequence, and of all prompts, go to the workspace and are joined by a
+ * second launch. Of opts, num_cus and min_chunk_pages (default 4) count.
+ */
+typedef struct sf_shared_info {
+  int32_t num_workers;       /* waves */
+  int32_t num_work;          /* segments */
+  int32_t num_merge;         /* (sequence, KV head) pairs that the second launch writes */
+  int32_t num_rows;          /* rows of partial results */
+  int32_t workers_per_group; /* waves per workgroup: 1 or 4 */
+  int32_t reserved;
+  uint64_t work_bytes;       /* bytes of the work list */
+  uint64_t workspace_bytes;
+  uint64_t desc_key;
+} sf_shared_info;
+sf_status sf_shared_attn_plan(const sf_attn_desc* desc, const int32_t* seq_lens_host, int32_t num_groups,
+                              const int32_t* group_offsets_host, const int32_t* shared_lens_host,
+                              const sf_plan_opts* opts, int32_t* work_host, uint64_t work_capacity_bytes,
+                              sf_shared_info* info);
+/* Enqueues the step: two launches (the second where info->num_merge > 0). Arguments as for sf_decode_attn; k_scale and
+ * v_scale: both NULL, or an fp8 cache's (sf_decode_attn_fp8). out: fp32, or with out_bf16 = 1 bf16 [B][Hq][D]. */
+sf_status sf_shared_attn(const sf_attn_desc* desc, const sf_shared_info* info, const int32_t* work_host,
+                         int32_t* work_dev, const void* q, const void* k_pool, const void* v_pool,
+                         const float* k_scale, const float* v_scale, const int32_t* block_table, void* out,
+                         int32_t out_bf16, float* lse, void* workspace, uint64_t workspace_bytes, void* stream);
+/* Both through a runner (its options' num_cus and min_chunk_pages), as sf_runner_step. */
+sf_status sf_runner_shared(sf_runner* runner, const sf_attn_desc* desc, const int32_t* seq_lens_host,
+                           int32_t num_groups, const int32_t* group_offsets_host, const int32_t* shared_lens_host,
+                           const void* q, const void* k_pool, const void* v_pool, const float* k_scale,
+                           const float* v_scale, const int32_t* block_table, void* out, int32_t out_bf16, float* lse,
+                           void* stream);
+
+/*
+ * Rotary positions. A model's queries and keys are turned by their positions before they meet: pair i of a head's first
+ * R = rotary_dim dims, i < R/2, is (x[i], x[i + R/2]) (interleaved = 0) or (x[2i], x[2i+1]) (interleaved = 1), and at
+ * position t it becomes
+ *   (a cos - b sin, b cos + a sin) * magnitude,   of the angle t f_i;
+ * dims R .. D-1 stay as they are. Queries and keys are bf16, the products are formed in fp32 and rounded once.
+ * Frequencies enter as turns: f_i / (2 pi), less whole turns, in units of 2^-64, so t times it, modulo 2^64, is the
+ * angle's fraction of a turn, off by at most |t| 2^-65 turns whatever t is.
+ * Negative positions turn backwards (which also is the gradient's way through a rotation).
+ */
+typedef struct sf_rotary_desc {
+  int32_t head_dim;      /* D: 64 or 128 */
+  int32_t rotary_dim;    /* R: a multiple of 16, 16 .. D */
+  int32_t interleaved;   /* 0: pairs half of R apart; 1: neighbours */
+  float magnitude;       /* multiplies what is turned (1 unless the scaling asks for more); finite */
+} sf_rotary_desc;
+
+/* Frequencies of longer contexts than a model was trained on: with r_i = trained_length f_i / (2 pi) turns in the
+ * trained length and s = clamp((r_i - low_turns) / (high_turns - low_turns), 0, 1), f_i becomes
+ * s f_i + (1 - s) f_i / factor. trained_length = 0: f_i / factor. */
+typedef struct sf_rotary_scaling {
+  double factor;           /* > 0 */
+  double trained_length;   /* >= 0 */
+  double low_turns;        /* low_turns < high_turns (unless trained_length is 0) */
+  double high_turns;
+} sf_rotary_scaling;
+
+/* freq_host[i] = base^(-2i / R), i < R/2, scaled (scaling may be NULL). base > 0. Host only. */
+sf_status sf_rotary_frequencies(int32_t rotary_dim, double base, const sf_rotary_scaling* scaling, double* freq_host);
+/* turns_host[i] for n finite frequencies (radians per position). Host only. */
+sf_status sf_rotary_turns(const double* freq_host, int32_t n, uint64_t* turns_host);
+
+/*
+ * Turns the queries and keys of num_tokens tokens, token i by positions[i] (device int32). turns: device, R/2 of them.
+ * q, k (bf16, either may be NULL: not turned): head h of token i starts at q + i * q_stride + h * D, in elements, so
+ * both may be parts of a wider tensor; outputs likewise. An output may be its own input (same pointer and stride);
+ * otherwise it must not overlap an input. Pointers are 16-byte aligned, strides a multiple of 8 and at least the heads'
+ * num_q_heads * D (num_kv_heads * D). One launch on the stream; nothing is allocated, so it can be captured.
+ */
+sf_status sf_rotary(const sf_rotary_desc* rotary, int32_t num_tokens, int32_t num_q_heads, int32_t num_kv_heads,
+                    const uint64_t* turns, const int32_t* positions, const void* q, int64_t q_stride, void* q_out,
+                    int64_t q_out_stride, const void* k, int64_t k_stride, void* k_out, int64_t k_out_stride,
+                    void* stream);
+
+/*
+ * The same for new tokens, whose turned keys and whose values go straight into the pages of a bf16 cache. The last
+ * q_lens_host[s] of sequence s' seq_lens_host[s] tokens are new; rows of q [T][Hq][D], k_new and v_new [T][Hkv][D] are
+ * theirs, sequence after sequence, with token strides as for sf_rotary. The first new one is at position
+ * first_pos_host[s] (NULL: at its index in the cache; a cache that has given up tokens counts on).
+ * sf_rotary_store_plan (host only) makes the work list, sf_rotary_store enqueues the call: one launch. new_pages and the
+ * block table are sf_kv_store_fp8's: with new_pages[s] >= 0 (device int32 [num_seqs], or NULL) the page of s' last token
+ * is new, and the call writes it to the block table. q may be NULL (keys and values only). Slots without a new
+ * token are left as they were. SF_ERR_PLAN_MISMATCH for the plan of another kind of call.
+ */
+sf_status sf_rotary_store_plan(const sf_attn_desc* desc, const int32_t* seq_lens_host, const int32_t* q_lens_host,
+                               const int32_t* first_pos_host, int32_t* work_host, uint64_t work_capacity_bytes,
+                               sf_store_info* info);
+sf_status sf_rotary_store(const sf_attn_desc* desc, const sf_rotary_desc* rotary, const sf_store_info* info,
+                          const int32_t* work_host, int32_t* work_dev, const uint64_t* turns, const void* q,
+                          int64_t q_stride, void* q_out, int64_t q_out_stride, const void* k_new, int64_t k_stride,
+                          const void* v_new, int64_t v_stride, const int32_t* new_pages, void* k_pool, void* v_pool,
+                          int32_t* block_table, void* stream);
+/* sf_rotary_store through a runner, as sf_runner_store_fp8. */
+sf_status sf_runner_rotary_store(sf_runner* runner, const sf_attn_desc* desc, const sf_rotary_desc* rotary,
+                                 const int32_t* seq_lens_host, const int32_t* q_lens_host,
+                                 const int32_t* first_pos_host, const uint64_t* turns, const void* q, int64_t q_stride,
+                                 void* q_out, int64_t q_out_stride, const void* k_new, int64_t k_stride,
+                                 const void* v_new, int64_t v_stride, const int32_t* new_pages_host, void* k_pool,
+                                 void* v_pool, int32_t* block_table, void* stream);
+
+/*
+ * Sampling: the token that every running trajectory goes on with, and its log-probability (what training on a rollout
+ * needs of it). Row i of the logits has V entries l_v, a temperature T, a top-k number k, a top-p share p, a min-p share m
+ * and a uniform number u. With w_v = exp((l_v - max l) / T):
+ *   in the order of falling logits, equal ones by rising index, the first k entries stay (k <= 0 or k >= V: all);
+ *   of these, in that order, every entry before which less than p of their sum of w lies (p >= 1 or NaN: all; the
+ *   first always);
+ *   of these, the ones with w_v >= m (m <= 0 or NaN: all; the first always);
+ *   token   = the first index v at which the sum of the weights that stayed, over indexes 0 .. v, exceeds u times
+ *             their whole sum (u is taken into [0, 1 - 2^-24]; NaN: 0);
+ *   logprob = ln(w_token / sum of all w), of the whole softmax at T;
+ *   kept    = the sum of what stayed over the sum of all w (ln(w / what stayed) is logprob - ln(kept)).
+ * T = 0 (or less, or NaN) takes the largest logit, the lowest index of equal ones, and reports as for T = 1. A NaN
+ * logit counts as -inf; +inf shares all weight among the +inf entries. A row with nothing but -inf has no token: -1, logprob
+ * -inf, kept 0. Weights enter the sums as multiples of 2^-44, off by half of one, so that a sum has one value in whatever order it is
+ * formed; of the draws of a row at most V 2^-43 or so fall to a neighbour of the exact token, and equal inputs give equal
+ * tokens on every run.
+ */
+typedef struct sf_sample_desc {
+  int32_t num_rows;      /* >= 0 */
+  int32_t vocab;         /* V: 1 .. SF_SAMPLE_MAX_VOCAB */
+  int64_t row_stride;    /* elements from a row's logits to the next's, >= V */
+  int32_t dtype;         /* 0: fp32, 1: bf16, 2: fp16 */
+  int32_t reserved;      /* 0 */
+} sf_sample_desc;
+#define SF_SAMPLE_MAX_VOCAB (1 << 19)
+
+/* Device scratch that sf_sample needs. */
+sf_status sf_sample_workspace(const sf_sample_desc* desc, uint64_t* bytes);
+/*
+ * Enqueues the draw of a token per row. All pointers are device memory, logits aligned to their elements, workspace to 16
+ * bytes, the others to 4: temperature, top_p, min_p (fp32 [num_rows]) and top_k (int32 [num_rows]) may be NULL (T = 1, no
+ * cut), logprob and kept (fp32 [num_rows]) too; uniform fp32 and token int32 [num_rows]. Two launches on the stream,
+ * nothing is allocated or kept, so the call can be captured. Calls that share a workspace must not overlap.
+ * SF_ERR_CAPACITY for a workspace smaller than sf_sample_workspace says.
+ */
+sf_status sf_sample(const sf_sample_desc* desc, const void* logits, const float* temperature, const int32_t* top_k,
+                    const float* top_p, const float* min_p, const float* uniform, int32_t* token, float* logprob,
+                    float* kept, void* workspace, uint64_t workspace_bytes, void* stream);
+
+/*
  * Test support: bytes[0] of device memory and bytes[1] per ring slot that
  * sf_runner_reserve (total_pages < 0) or sf_runner_reserve_batch (0 bytes, and
  * the pages of all pairs) sees to for a runner of that shape and options; host

@@ -80,6 +80,27 @@ class sf_evict_info(ctypes.Structure):
                [(n, ctypes.c_uint64) for n in ("work_bytes", "workspace_bytes", "desc_key")]
 
 
+class sf_shared_info(ctypes.Structure):
+    _fields_ = [("num_workers", ctypes.c_int32), ("num_work", ctypes.c_int32), ("num_merge", ctypes.c_int32),
+                ("num_rows", ctypes.c_int32), ("workers_per_group", ctypes.c_int32), ("reserved", ctypes.c_int32),
+                ("work_bytes", ctypes.c_uint64), ("workspace_bytes", ctypes.c_uint64), ("desc_key", ctypes.c_uint64)]
+
+
+class sf_rotary_desc(ctypes.Structure):
+    _fields_ = [("head_dim", ctypes.c_int32), ("rotary_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32),
+                ("magnitude", ctypes.c_float)]
+
+
+class sf_rotary_scaling(ctypes.Structure):
+    _fields_ = [("factor", ctypes.c_double), ("trained_length", ctypes.c_double), ("low_turns", ctypes.c_double),
+                ("high_turns", ctypes.c_double)]
+
+
+class sf_sample_desc(ctypes.Structure):
+    _fields_ = [("num_rows", ctypes.c_int32), ("vocab", ctypes.c_int32), ("row_stride", ctypes.c_int64),
+                ("dtype", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
 class sf_runner_extras(ctypes.Structure):
     _fields_ = [("k_new", ctypes.c_void_p), ("v_new", ctypes.c_void_p), ("new_pages_host", ctypes.c_void_p),
                 ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p), ("attn_start", ctypes.c_void_p),
@@ -171,6 +192,18 @@ def lib():
     L.sf_runner_evict.argtypes = [vp, desc, vp, vp, vp, i32, i32] + [vp] * 10
     L.sf_extend_attn_fp8.argtypes = [desc, P(sf_extend_info)] + [vp] * 9 + [i32, vp, vp]
     L.sf_runner_extend_fp8.argtypes = [vp, desc] + [vp] * 10 + [P(sf_runner_memory), vp, P(sf_extend_info), vp, vp, i32]
+    i64, rope = ctypes.c_int64, P(sf_rotary_desc)
+    L.sf_shared_attn_plan.argtypes = [desc, vp, i32, vp, vp, P(sf_plan_opts), vp, u64, P(sf_shared_info)]
+    L.sf_shared_attn.argtypes = [desc, P(sf_shared_info)] + [vp] * 9 + [i32, vp, vp, u64, vp]
+    L.sf_runner_shared.argtypes = [vp, desc, vp, i32] + [vp] * 9 + [i32, vp, vp]
+    L.sf_rotary_frequencies.argtypes = [i32, ctypes.c_double, P(sf_rotary_scaling), vp]
+    L.sf_rotary_turns.argtypes = [vp, i32, vp]
+    L.sf_rotary.argtypes = [rope, i32, i32, i32, vp, vp] + [vp, i64] * 4 + [vp]
+    L.sf_rotary_store_plan.argtypes = [desc, vp, vp, vp, vp, u64, P(sf_store_info)]
+    L.sf_rotary_store.argtypes = [desc, rope, P(sf_store_info), vp, vp, vp] + [vp, i64] * 4 + [vp] * 5
+    L.sf_runner_rotary_store.argtypes = [vp, desc, rope, vp, vp, vp, vp] + [vp, i64] * 4 + [vp] * 5
+    L.sf_sample_workspace.argtypes = [P(sf_sample_desc), P(u64)]
+    L.sf_sample.argtypes = [P(sf_sample_desc)] + [vp] * 10 + [u64, vp]
     L.sf_page_table_truncate.argtypes = [vp, vp, i32, i32, vp, vp]
     L.sf_page_table_step.argtypes = [vp, vp, ctypes.c_int32, ctypes.c_int32, vp, vp, ctypes.c_int32, vp]
     L.sf_cost_throughput.argtypes = [P(sf_cost_model), P(sf_instance_state)]
@@ -190,7 +223,9 @@ def lib():
                "sf_debug_runner_reserve", "sf_runner_reserve_batch", "sf_debug_stream_read", "sf_decode_attn_scratch",
                "sf_kv_store_fp8_plan", "sf_kv_store_fp8", "sf_key_weights_plan", "sf_key_weights", "sf_kv_evict_plan",
                "sf_kv_evict", "sf_runner_store_fp8", "sf_runner_key_weights", "sf_runner_evict",
-               "sf_page_table_truncate", "sf_extend_attn_fp8", "sf_runner_extend_fp8"):
+               "sf_page_table_truncate", "sf_extend_attn_fp8", "sf_runner_extend_fp8", "sf_shared_attn_plan", "sf_shared_attn",
+               "sf_runner_shared", "sf_rotary_frequencies", "sf_rotary_turns", "sf_rotary", "sf_rotary_store_plan",
+               "sf_rotary_store", "sf_runner_rotary_store", "sf_sample_workspace", "sf_sample"):
         getattr(L, fn).restype = ctypes.c_int
     L.sf_status_string.argtypes = [ctypes.c_int]
     L.sf_status_string.restype = ctypes.c_char_p
@@ -632,6 +667,105 @@ def sf_extend_attn_fp8(desc, info, work_host, work_dev, q, k_pool8, v_pool8, k_s
         ctypes.byref(desc), ctypes.byref(info), _addr(work_host), _addr(work_dev), _addr(q), _addr(k_pool8),
         _addr(v_pool8), _addr(k_scale), _addr(v_scale), _addr(block_table), _addr(out),
         int(out.dtype is torch.bfloat16), _addr(lse), _stream(stream)))
+
+
+def sf_shared_attn_plan(desc, seq_lens, group_offsets, shared_lens, opts=None, work_host=None):
+    """Plans a decode step of groups that share their first tokens: sequences group_offsets[i] .. group_offsets[i+1] - 1
+    have shared_lens[i] of them in common. Returns (info, work_host)."""
+    lens, offsets, shared = _host_groups(desc.num_seqs, seq_lens, group_offsets, shared_lens)
+    info = sf_shared_info()
+    return _planned("sf_shared_attn_plan", info, lambda w, cap: lib().sf_shared_attn_plan(
+        ctypes.byref(desc), _host_addr(lens), shared.size, _host_addr(offsets), _host_addr(shared),
+        None if opts is None else ctypes.byref(opts), w, cap, ctypes.byref(info)), work_host)
+
+
+def _host_groups(n, seq_lens, group_offsets, shared_lens):
+    lens = _host_i32(seq_lens, "seq_lens", n)
+    shared = np.ascontiguousarray(shared_lens, dtype=np.int32)
+    if shared.ndim != 1:
+        raise ValueError("shared_lens must have one entry per group")
+    return lens, _host_i32(group_offsets, "group_offsets", shared.size + 1), shared
+
+
+def _check_step(desc, q, k_pool, v_pool, block_table, out, lse, fp8):
+    b, hq, d = desc.num_seqs, desc.num_q_heads, desc.head_dim
+    _dev(q, "q", torch.bfloat16, (b, hq, d))
+    _dev(out, "out", torch.bfloat16 if out.dtype is torch.bfloat16 else torch.float32, (b, hq, d))
+    if lse is not None:
+        _dev(lse, "lse", torch.float32, (b, hq))
+    _check_pools(desc.num_pages, desc.num_kv_heads, d, k_pool, v_pool, block_table, b, fp8)
+
+
+def sf_shared_attn(desc, info, work_host, work_dev, q, k_pool, v_pool, block_table, out, lse=None, fp8=None,
+                   workspace=None, stream=None):
+    """Enqueues a decode step of groups that share their first tokens. out: fp32 or bf16 [B, Hq, D]; fp8: (k_scale,
+    v_scale) of an fp8 cache."""
+    _check_step(desc, q, k_pool, v_pool, block_table, out, lse, fp8)
+    ws_bytes = _check_work(info, work_dev, workspace)
+    k_scale, v_scale = fp8 if fp8 is not None else (None, None)
+    _check("sf_shared_attn", lib().sf_shared_attn(
+        ctypes.byref(desc), ctypes.byref(info), _addr(work_host), _addr(work_dev), _addr(q), _addr(k_pool), _addr(v_pool),
+        _addr(k_scale), _addr(v_scale), _addr(block_table), _addr(out), int(out.dtype is torch.bfloat16), _addr(lse),
+        _addr(workspace), ws_bytes, _stream(stream)))
+
+
+def sf_rotary_frequencies(rotary_dim, base, scaling=None) -> np.ndarray:
+    """The rotation's frequencies, radians per position (float64 [rotary_dim / 2]). scaling: a sf_rotary_scaling."""
+    freq = np.empty(max(0, int(rotary_dim)) // 2, dtype=np.float64)
+    _check("sf_rotary_frequencies", lib().sf_rotary_frequencies(
+        int(rotary_dim), float(base), None if scaling is None else ctypes.byref(scaling), _host_addr(freq)))
+    return freq
+
+
+def sf_rotary_turns(freq) -> np.ndarray:
+    """Frequencies as turns per position in units of 2^-64, whole turns left out (uint64)."""
+    freq = np.ascontiguousarray(freq, dtype=np.float64)
+    turns = np.empty(freq.shape, dtype=np.uint64)
+    _check("sf_rotary_turns", lib().sf_rotary_turns(_host_addr(freq), freq.size, _host_addr(turns)))
+    return turns
+
+
+def _rows(t, name, shape):
+    """Checks a bf16 tensor [T, H, D] whose tokens may lie apart; returns its token stride."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must live on the GPU (got {t.device})")
+    if t.dtype is not torch.bfloat16:
+        raise ValueError(f"{name} must be torch.bfloat16 (got {t.dtype})")
+    if t.shape != shape:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    _, heads, d = shape
+    if shape[0] > 1 and t.stride(0) < heads * d or t.stride(2) != 1 or (heads > 1 and t.stride(1) != d):
+        raise ValueError(f"{name}: a token's heads must be contiguous, and tokens must not overlap")
+    return t.stride(0) if shape[0] > 1 else heads * d
+
+
+def _extent(t):
+    """First byte of a tensor's elements and the one behind the last."""
+    at = t.data_ptr()
+    return at, at + (sum((n - 1) * s for n, s in zip(t.shape, t.stride())) + 1) * t.element_size() if t.numel() else at
+
+
+def _check_turned(x, x_out, name, others):
+    """An output is its input's own place, or overlaps none."""
+    if x_out.data_ptr() == x.data_ptr() and x_out.stride() == x.stride():
+        others = [t for t in others if t is not x]
+    a, b = _extent(x_out)
+    for t in others:
+        c, e = _extent(t)
+        if a < e and c < b and not _interleaved(x_out, t):
+            raise ValueError(f"{name} overlaps an input")
+
+
+def _interleaved(a, b):
+    """Whether two tensors [T, H, D] of one token stride lie in separate columns of the same rows."""
+    if a.shape[0] <= 1 or a.stride(0) != b.stride(0):
+        return False
+    stride = a.stride(0)
+    off = (b.data_ptr() - a.data_ptr()) // 2 % stride   # b's first column from a's
+    nx, ny = a.shape[1] * a.shape[2], b.shape[1] * b.shape[2]
+    return off >= nx and off + ny <= stride
 
 
 _cus = {}
@@ -1330,12 +1464,202 @@ class DecodeAttention:
             positions.data_ptr(), weights_out.data_ptr(), positions_out.data_ptr(),
             stream.cuda_stream if stream else _current_stream(self.device)))
 
+    def shared(self, q, k_pool, v_pool, block_table, seq_lens, group_offsets, shared_lens, scale, out=None, lse=None,
+               fp8=None, stream=None):
+        """One decode step of groups that share their first tokens (sf_shared_attn, through the runner): sequences
+        group_offsets[i] .. group_offsets[i+1] - 1 hold shared_lens[i] common tokens in the pages that their block tables
+        start with (host int32 arrays). The result is the plain step's over each sequence's seq_lens[s] tokens. out: fp32
+        (default) or bf16 [B, Hq, D]; fp8 = (k_scale, v_scale) of an fp8 cache."""
+        if out is None:
+            out = torch.empty((q.shape[0], self.hq, self.d), dtype=torch.float32, device=self.device)
+        desc, lens = self._call_desc(k_pool, block_table, seq_lens, scale)
+        lens, offsets, shared = _host_groups(lens.size, lens, group_offsets, shared_lens)
+        _check_step(desc, q, k_pool, v_pool, block_table, out, lse, fp8)
+        if DEBUG_CHECKS and not self._host_checked:
+            check_block_table(desc, block_table, lens)
+        self._host_checked = False
+        k_scale, v_scale = fp8 if fp8 is not None else (None, None)
+        _check("sf_runner_shared", self.L.sf_runner_shared(
+            self._runner(None), ctypes.byref(desc), _host_addr(lens), shared.size, _host_addr(offsets), _host_addr(shared),
+            q.data_ptr(), k_pool.data_ptr(), v_pool.data_ptr(), _addr(k_scale), _addr(v_scale), block_table.data_ptr(),
+            out.data_ptr(), int(out.dtype is torch.bfloat16), _addr(lse),
+            stream.cuda_stream if stream else _current_stream(self.device)))
+        return out
+
+    def rotate_store(self, rotary, q, k_new, v_new, k_pool, v_pool, block_table, seq_lens, q_lens, first_pos=None,
+                     new_pages=None, q_out=None, stream=None):
+        """Turns the queries and keys of the last q_lens[s] of seq_lens[s] tokens by their positions and stores the turned
+        keys and the values into the pages of a bf16 cache (sf_rotary_store, through the runner). rotary: a Rotary; q,
+        k_new, v_new: bf16 [T, H, D], parts of wider rows allowed (q may be None); first_pos: host int32 [B], the first new
+        token's position (default: its index in the cache); new_pages as in store_fp8. Returns the turned queries: q_out
+        (may be q), by default a new tensor."""
+        desc, lens = self._call_desc(k_pool, block_table, seq_lens, 1.0)
+        n = lens.size
+        qls, first, pages = (_host_i32(x, name, n) for x, name in ((q_lens, "q_lens"), (first_pos, "first_pos"),
+                                                                   (new_pages, "new_pages")))
+        if rotary.head_dim != self.d:
+            raise ValueError(f"rotary turns heads of {rotary.head_dim} dims, not {self.d}")
+        rows = int(qls.sum(dtype=np.int64))
+        sk, sv = _rows(k_new, "k_new", (rows, self.hkv, self.d)), _rows(v_new, "v_new", (rows, self.hkv, self.d))
+        sq = so = 0
+        if q is not None:
+            sq = _rows(q, "q", (rows, self.hq, self.d))
+            if q_out is None:
+                with torch.cuda.stream(stream):   # the stream that it is written on
+                    q_out = torch.empty((rows, self.hq, self.d), dtype=torch.bfloat16, device=q.device)
+            so = _rows(q_out, "q_out", (rows, self.hq, self.d))
+            _check_turned(q, q_out, "q_out", [q, k_new, v_new])
+        elif q_out is not None:
+            raise ValueError("q_out without q")
+        _check_pools(desc.num_pages, self.hkv, self.d, k_pool, v_pool, block_table, n, None)
+        if DEBUG_CHECKS:
+            named = np.zeros(n, bool) if pages is None else pages >= 0
+            check_block_table(desc, block_table, np.where(qls > 0, lens - named, 0))
+            if pages is not None and np.any((pages < -1) | (pages >= desc.num_pages)):
+                raise ValueError("new_pages holds a page id outside the pool")
+        _check("sf_runner_rotary_store", self.L.sf_runner_rotary_store(
+            self._runner(None), ctypes.byref(desc), ctypes.byref(rotary.desc), _host_addr(lens), _host_addr(qls), _addr(first),
+            rotary.turns_on(k_pool.device).data_ptr(), _addr(q), sq, _addr(q_out), so, k_new.data_ptr(), sk, v_new.data_ptr(), sv,
+            _addr(pages), k_pool.data_ptr(), v_pool.data_ptr(), block_table.data_ptr(),
+            stream.cuda_stream if stream else _current_stream(self.device)))
+        return q_out
+
     def __del__(self):
         L = getattr(self, "L", None)
         for r in getattr(self, "_runners", {}).values():
             if L is not None and r.value:
                 L.sf_runner_destroy(r)
         self._runners = {}
+
+
+class Rotary:
+    """Rotary positions: turns queries and keys by their positions (sf_rotary). The first rotary_dim dims of a head
+    (default: all) turn, in pairs half of rotary_dim apart (layout "half") or of neighbours ("interleaved"), by
+    angles of position * freq[i]; freq (radians per position, float64 [rotary_dim / 2]) defaults to base^(-2i / rotary_dim).
+    scaling: a dict for contexts longer than the trained one, with factor and, for frequencies that keep their turns in it,
+    original (tokens), low, high (turns; sf_rotary_scaling); its magnitude (default 1) multiplies what is turned."""
+
+    def __init__(self, head_dim, rotary_dim=None, base=10000.0, layout="half", scaling=None, freq=None, device=None):
+        self.head_dim = int(head_dim)
+        self.rotary_dim = self.head_dim if rotary_dim is None else int(rotary_dim)
+        if layout not in ("half", "interleaved"):
+            raise ValueError('layout must be "half" or "interleaved"')
+        scaling = dict(scaling or {})
+        magnitude = float(scaling.pop("magnitude", 1.0))
+        if freq is None:
+            c = None
+            if scaling:
+                c = sf_rotary_scaling(float(scaling.pop("factor")), float(scaling.pop("original", 0.0)),
+                                      float(scaling.pop("low", 1.0)), float(scaling.pop("high", 4.0)))
+            freq = sf_rotary_frequencies(self.rotary_dim, base, c)
+        if scaling:
+            raise ValueError(f"unknown scaling: {sorted(scaling)}")
+        self.freq = np.ascontiguousarray(freq, dtype=np.float64)
+        if self.freq.shape != (self.rotary_dim // 2,):
+            raise ValueError("freq must have rotary_dim / 2 entries")
+        self.desc = sf_rotary_desc(self.head_dim, self.rotary_dim, int(layout == "interleaved"), magnitude)
+        self._turns = torch.from_numpy(sf_rotary_turns(self.freq).view(np.int64))
+        self._on = {}
+        # an error of the arguments, if any, here and not at the first call
+        _check("sf_rotary", lib().sf_rotary(ctypes.byref(self.desc), 0, 0, 0, None, None, None, 0, None, 0, None, 0, None, 0, None))
+        if device is not None:
+            self.turns_on(torch.device(device))
+
+    def turns_on(self, device):
+        """The turns per position as a tensor on the device (uploaded at the first call there)."""
+        t = self._on.get(device.index)
+        if t is None:
+            if torch.cuda.is_current_stream_capturing():
+                raise RuntimeError("a Rotary's first call on a device uploads its frequencies: make it before the capture")
+            t = self._on[device.index] = self._turns.to(device)
+            torch.cuda.current_stream(device).synchronize()   # other streams may be the next to read it
+        return t
+
+    def __call__(self, q, k, positions, q_out=None, k_out=None, stream=None):
+        """Turns q and k (bf16 [T, Hq, D] and [T, Hkv, D], parts of wider rows allowed; either may be None) by
+        positions (int32 [T]). Returns (q_out, k_out), by default new tensors; an output may be its input."""
+        given = q if q is not None else k
+        if given is None:
+            return None, None
+        t = given.shape[0]
+        _dev(positions, "positions", torch.int32, (t,))
+        ins = [x for x in (q, k) if x is not None]
+        args, outs = [], []
+        for x, out, name in ((q, q_out, "q"), (k, k_out, "k")):
+            if x is None:
+                if out is not None:
+                    raise ValueError(f"{name}_out without {name}")
+                args += [None, 0, None, 0]
+                outs.append(None)
+                continue
+            if x.dim() != 3:
+                raise ValueError(f"{name} must be [tokens, heads, head_dim]")
+            shape = (t, x.shape[1], self.head_dim)
+            stride = _rows(x, name, shape)
+            if out is None:
+                with torch.cuda.stream(stream):   # the stream that it is written on
+                    out = torch.empty(shape, dtype=torch.bfloat16, device=x.device)
+            out_stride = _rows(out, name + "_out", shape)
+            _check_turned(x, out, name + "_out", ins)
+            args += [x.data_ptr(), stride, out.data_ptr(), out_stride]
+            outs.append(out)
+        if q_out is not None and k_out is not None:
+            _check_turned(q_out, k_out, "k_out", [q_out])
+        device = given.device
+        with torch.cuda.device(device):
+            _check("sf_rotary", lib().sf_rotary(
+                ctypes.byref(self.desc), t, 0 if q is None else q.shape[1], 0 if k is None else k.shape[1],
+                self.turns_on(device).data_ptr(), positions.data_ptr(), *args,
+                stream.cuda_stream if stream else _current_stream(device)))
+        return tuple(outs)
+
+
+class Sampler:
+    """Draws tokens from logits by given uniform numbers, with temperature, top-k, top-p and min-p (sf_sample, whose rules
+    these are). Its scratch memory comes from torch's allocator at every call, in the stream's order, so calls on any
+    stream may overlap and be captured."""
+    DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+
+    def __init__(self, device=None):
+        self.device = torch.device("cuda" if device is None else device)
+        self._L = lib()
+        self._desc, self._bytes, self._key = sf_sample_desc(), ctypes.c_uint64(), None
+
+    def __call__(self, logits, uniform, temperature=None, top_k=None, top_p=None, min_p=None, token=None, logprob=None,
+                 kept=None, stream=None):
+        """logits: fp32, bf16 or fp16 [B, V], rows may lie apart; uniform: fp32 [B] in [0, 1); temperature, top_p,
+        min_p: fp32 [B] or None (1, no cut), top_k: int32 [B] or None. Returns (token int32, logprob fp32, kept fp32),
+        each [B], into the tensors given."""
+        if not isinstance(logits, torch.Tensor) or logits.dim() != 2 or not logits.is_cuda:
+            raise ValueError("logits must be a GPU tensor [rows, vocab]")
+        code = self.DTYPES.get(logits.dtype)
+        if code is None:
+            raise ValueError(f"logits must be float32, bfloat16 or float16 (got {logits.dtype})")
+        b, v = logits.shape
+        stride = logits.stride(0) if b > 1 else v
+        if (v > 1 and logits.stride(1) != 1) or stride < v:
+            raise ValueError("a row's logits must be contiguous, and rows must not overlap")
+        _dev(uniform, "uniform", torch.float32, (b,))
+        for t, name, dtype in ((temperature, "temperature", torch.float32), (top_k, "top_k", torch.int32),
+                               (top_p, "top_p", torch.float32), (min_p, "min_p", torch.float32)):
+            if t is not None:
+                _dev(t, name, dtype, (b,))
+        key = (b, v, stride, code)
+        desc = self._desc
+        if key != self._key:
+            desc.num_rows, desc.vocab, desc.row_stride, desc.dtype = key
+            _check("sf_sample_workspace", self._L.sf_sample_workspace(ctypes.byref(desc), ctypes.byref(self._bytes)))
+            self._key = key
+        with torch.cuda.device(logits.device), torch.cuda.stream(stream):
+            made = []
+            for t, name, dtype in ((token, "token", torch.int32), (logprob, "logprob", torch.float32), (kept, "kept", torch.float32)):
+                made.append(torch.empty((b,), dtype=dtype, device=logits.device) if t is None else _dev(t, name, dtype, (b,)))
+            workspace = torch.empty((max(16, self._bytes.value),), dtype=torch.uint8, device=logits.device)
+            _check("sf_sample", self._L.sf_sample(
+                ctypes.byref(desc), logits.data_ptr(), _addr(temperature), _addr(top_k), _addr(top_p), _addr(min_p),
+                uniform.data_ptr(), made[0].data_ptr(), made[1].data_ptr(), made[2].data_ptr(), workspace.data_ptr(),
+                self._bytes.value, stream.cuda_stream if stream else _current_stream(logits.device)))
+        return tuple(made)
 
 
 class PageTable:

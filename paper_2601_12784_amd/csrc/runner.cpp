@@ -515,6 +515,58 @@ extern "C" sf_status sf_runner_store_fp8(sf_runner* r, const sf_attn_desc* desc,
       });
 }
 
+extern "C" sf_status sf_runner_shared(sf_runner* r, const sf_attn_desc* desc, const int32_t* seq_lens_host,
+                                      int32_t num_groups, const int32_t* group_offsets_host,
+                                      const int32_t* shared_lens_host, const void* q, const void* k_pool,
+                                      const void* v_pool, const float* k_scale, const float* v_scale,
+                                      const int32_t* block_table, void* out, int32_t out_bf16, float* lse, void* stream) {
+  if (!r || !desc || !same_shape(r, desc)) return SF_ERR_INVALID_ARG;
+  sf_shared_info info = {};
+  auto merge_bytes = [&] { return uint64_t(info.num_merge) * sf::kSharedMergeInts * 4; };
+  return run_in_slot(
+      r, static_cast<hipStream_t>(stream),
+      [&](int32_t* work, uint64_t bytes) {
+        return sf_shared_attn_plan(desc, seq_lens_host, num_groups, group_offsets_host, shared_lens_host, &r->opts, work,
+                                   bytes, &info);
+      },
+      [&] { return info.work_bytes; },
+      // the merge rows' device copy lies behind the call's own workspace
+      [&] { return sf::align256(info.workspace_bytes) + merge_bytes(); },
+      [&](int32_t*, const int32_t* dev) {
+        char* rows = static_cast<char*>(r->workspace) + sf::align256(info.workspace_bytes);
+        return sf::run_shared(desc, &info, nullptr, const_cast<int32_t*>(dev), q, k_pool, v_pool, k_scale, v_scale,
+                              block_table, out, out_bf16, lse, r->workspace, r->workspace_bytes, stream,
+                              info.num_workers > 0 ? reinterpret_cast<int32_t*>(rows) : nullptr);
+      });
+}
+
+extern "C" sf_status sf_runner_rotary_store(sf_runner* r, const sf_attn_desc* desc, const sf_rotary_desc* rotary,
+                                            const int32_t* seq_lens_host, const int32_t* q_lens_host,
+                                            const int32_t* first_pos_host, const uint64_t* turns, const void* q,
+                                            int64_t q_stride, void* q_out, int64_t q_out_stride, const void* k_new,
+                                            int64_t k_stride, const void* v_new, int64_t v_stride,
+                                            const int32_t* new_pages_host, void* k_pool, void* v_pool,
+                                            int32_t* block_table, void* stream) {
+  if (!r || !desc || !same_shape(r, desc)) return SF_ERR_INVALID_ARG;
+  sf_store_info info = {};
+  const uint64_t pages_bytes = new_pages_host && desc->num_seqs > 0 ? (uint64_t(desc->num_seqs) * 4 + 31) / 32 * 32 : 0;
+  return run_in_slot(
+      r, static_cast<hipStream_t>(stream),
+      [&](int32_t* work, uint64_t bytes) {
+        return sf_rotary_store_plan(desc, seq_lens_host, q_lens_host, first_pos_host, work, bytes, &info);
+      },
+      [&] { return info.num_rows > 0 ? info.work_bytes + pages_bytes : 0; }, [] { return uint64_t(0); },
+      [&](int32_t* host, const int32_t* dev) {
+        const int32_t* pages = nullptr;
+        if (pages_bytes) {
+          std::memcpy(host + info.work_bytes / 4, new_pages_host, uint64_t(desc->num_seqs) * 4);
+          pages = dev + info.work_bytes / 4;
+        }
+        return sf_rotary_store(desc, rotary, &info, nullptr, const_cast<int32_t*>(dev), turns, q, q_stride, q_out,
+                               q_out_stride, k_new, k_stride, v_new, v_stride, pages, k_pool, v_pool, block_table, stream);
+      });
+}
+
 extern "C" sf_status sf_runner_key_weights(sf_runner* r, const sf_attn_desc* desc, const int32_t* seq_lens_host,
                                            const int32_t* q_lens_host, const int32_t* held_lens_host,
                                            const int32_t* first_pos_host, const void* q, const float* lse,

@@ -173,6 +173,110 @@ sf_status store8_args(const sf_attn_desc* desc, const int32_t* work_dev, const v
                       int32_t* block_table, Store8Args* args);
 hipError_t launch_store_fp8(const Store8Args& a, hipStream_t stream);
 
+// A decode step of groups with shared first tokens (sf_shared_attn).
+constexpr int kSharedInts = 16;       // int32 fields of a worker's or a segment's row
+constexpr int kSharedMergeInts = 8;
+constexpr int kSharedTiles = 4;       // 16-row tiles of a block
+struct SharedArgs {
+  // num_workers rows: first segment, segments, then the first segment's fields; num_work rows with the fields from int 2
+  // on: first sequence of the rows, block-table row, kv_head, first page, end page, end token, partial row (-1: written
+  // out), first row, rows
+  const int32_t* workers;
+  const int32_t* items;
+  int32_t num_workers;
+  int32_t workers_per_group;
+  const int32_t* merge_rows;  // seq, kv_head, own partial row, own parts, prompt's partial row, its parts, rows between them, 0
+  int32_t num_merge;
+  const int32_t* copy_src;    // optional side job of the first launch: the merge rows from pinned host memory to the device
+  int32_t* copy_dst;
+  int32_t copy_ints;
+  const uint16_t* q;
+  const uint16_t* k_pool;
+  const uint16_t* v_pool;
+  const float* k_scale;       // fp8 cache, else NULL
+  const float* v_scale;
+  const int32_t* block_table;
+  void* out;
+  bool out_bf16;
+  float* lse;                 // or NULL
+  float* part_o;              // [rows][D]
+  float* part_lse;            // [rows], log2 units
+  int32_t num_q_heads;
+  int32_t num_kv_heads;
+  int32_t group;
+  int32_t head_dim;
+  int32_t bt_stride;
+  float scale_log2;
+};
+hipError_t launch_shared(const SharedArgs& a, hipStream_t stream);
+// sf_shared_attn; late_rows: NULL, or device memory for merge rows that lie in host memory.
+sf_status run_shared(const sf_attn_desc* desc, const sf_shared_info* info, const int32_t* work_host, int32_t* work_dev,
+                     const void* q, const void* k_pool, const void* v_pool, const float* k_scale, const float* v_scale,
+                     const int32_t* block_table, void* out, int32_t out_bf16, float* lse, void* workspace,
+                     uint64_t workspace_bytes, void* stream, int32_t* late_rows);
+
+// Rotary positions (sf_rotary; with rows: sf_rotary_store).
+struct RotaryArgs {
+  int32_t head_dim;
+  int32_t rotary_dim;
+  bool interleaved;
+  float magnitude;
+  const uint64_t* turns;      // [rotary_dim / 2], units of 2^-64 turns per position
+  int32_t num_tokens;
+  int32_t num_q_heads;        // 0: no queries
+  int32_t num_kv_heads;       // 0: no keys
+  const uint16_t* q;
+  int64_t q_stride;           // elements per token
+  uint16_t* q_out;
+  int64_t q_out_stride;
+  const uint16_t* k;
+  int64_t k_stride;
+  // sf_rotary
+  uint16_t* k_out;
+  int64_t k_out_stride;
+  const int32_t* positions;   // [num_tokens]
+  // sf_rotary_store: seq, first page, pages, first new index, L, query row of the first, its position, 0
+  const int32_t* rows;
+  int32_t num_rows;
+  const uint16_t* v;
+  int64_t v_stride;
+  const int32_t* new_pages;   // [B] or NULL
+  uint16_t* k_pool;
+  uint16_t* v_pool;
+  int32_t* block_table;
+  int32_t bt_stride;
+};
+hipError_t launch_rotary(const RotaryArgs& a, hipStream_t stream);
+
+// Sampling (sf_sample).
+constexpr int kSampleChunk = 8192;        // logits that a workgroup of the first launch reads
+constexpr int kSampleSmallChunk = 2048;
+struct SampleChunk {
+  float top;       // the chunk's largest logit
+  int32_t at;      // its first index
+  uint64_t sum;    // sum of the weights relative to it, in units of 2^-44
+};
+struct SampleArgs {
+  const void* logits;
+  int32_t num_rows;
+  int32_t vocab;
+  int64_t row_stride;         // elements
+  const float* temperature;   // [num_rows] or NULL, as the next three
+  const int32_t* top_k;
+  const float* top_p;
+  const float* min_p;
+  const float* uniform;
+  int32_t* token;
+  float* logprob;             // or NULL
+  float* kept;                // or NULL
+  int32_t chunk;
+  int32_t num_chunks;         // per row
+  SampleChunk* chunks;        // [num_rows][num_chunks]
+};
+int32_t sample_chunk(const sf_sample_desc& d);
+int32_t sample_chunks(const sf_sample_desc& d);
+hipError_t launch_sample(const SampleArgs& a, int32_t dtype, hipStream_t stream);
+
 // Attention weights of cached keys (sf_key_weights).
 constexpr int kWeightInts = 16;   // int32 fields per work-list row
 constexpr int kWeightPages = 4;   // pages a wave holds at a time (64 keys)

@@ -1,0 +1,469 @@
+// gfx950 kernels of a decode step whose sequences share their first tokens in
+// groups: several trajectories sampled from one prompt.
+//
+// A prompt's pages are read once for all members. Their query rows (members times
+// the g query heads of a KV head) fill tiles of 16 matrix-core columns, up to four
+// per wave, so a K or V operand that a wave has loaded meets up to 64 rows; a prompt with
+// more rows has several waves walk the same pages side by side, each with its own 64. What a sequence
+// has to itself is a walk with the g rows of one sequence. Per block of two pages (32 keys) and tile,
+//
+//   S^T[16 keys][16 rows] = K Q^T per page   (D/32) v_mfma_f32_16x16x32_bf16 each
+//   weights 2^(z - m), the row's reference m moved only when a block's weights grow past 2^kHeadroom
+//   O^T[D][16 rows]      += V^T P^T           (D/16) x 2 MFMAs, P as two bf16 parts (16 bits of each weight)
+//
+// Operands come straight from memory to registers (the page layouts are the
+// operands' own), one wave per SIMD with the next block's loads in flight. A wave
+// (worker) walks an equal share of the pages; its results are rows of normalized
+// output with their log-sum-exp, which a second launch joins per (sequence, KV head).
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <type_traits>
+
+#include "sf_internal.h"
+
+namespace sf {
+namespace {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef __attribute__((address_space(4))) const int32_t* const_i32_ptr;
+typedef __attribute__((address_space(4))) const float* const_f32_ptr;
+
+constexpr float kLn2 = 0.69314718055994530942f;
+constexpr float kHeadroom = 1024.f;   // most that a lane's eight weights of a block may sum to
+
+__device__ __forceinline__ const_i32_ptr as_constant(const int32_t* p) { return (const_i32_ptr)(p); }
+
+__device__ __forceinline__ f32x4 mfma_bf16(u32x4 a, u32x4 b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, bf16x2));
+}
+__device__ __forceinline__ float low_bf16(uint32_t w) { return __builtin_bit_cast(float, w << 16); }
+__device__ __forceinline__ float high_bf16(uint32_t w) { return __builtin_bit_cast(float, w & 0xFFFF0000u); }
+template <bool kHigh>
+__device__ __forceinline__ uint32_t widen2(uint32_t codes4) {
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes4, 1.0f, kHigh));
+}
+
+struct Item {
+  int seq0, source, kvh, pb, pe, end, slot, row0, rows;
+};
+
+// Lane's position in the MFMA layouts.
+struct Lane {
+  int col, grp;
+  __device__ __forceinline__ Lane() : col(int(threadIdx.x) & 15), grp((int(threadIdx.x) & 63) >> 4) {}
+};
+
+// Keys and values of a block of two pages as they come from memory: bf16
+// operands, or fp8 codes with their scales.
+template <int D, bool kFp8>
+struct Keys;
+template <int D, bool kFp8>
+struct Values;
+template <int D>
+struct Keys<D, false> {
+  u32x4 k[2][D / 32];
+};
+template <int D>
+struct Values<D, false> {
+  u32x4 v[D / 16];
+};
+template <int D>
+struct Keys<D, true> {
+  u32x4 k[2][D / 64];
+  float scale[2];
+};
+template <int D>
+struct Values<D, true> {
+  u32x4 v[2][D / 64];
+  float scale[2];
+};
+
+template <int D, bool kFp8>
+struct Source {
+  const char* k_pool;
+  const char* v_pool;
+  const_f32_ptr k_scale, v_scale;
+  const_i32_ptr bt;
+  int hkv, kvh, pe;
+  int k_off, v_off;   // this lane's bytes inside a tile
+
+  __device__ __forceinline__ Source(const SharedArgs& a, const Item& it, const Lane& l) {
+    k_pool = reinterpret_cast<const char*>(a.k_pool);
+    v_pool = reinterpret_cast<const char*>(a.v_pool);
+    k_scale = (const_f32_ptr)a.k_scale;
+    v_scale = (const_f32_ptr)a.v_scale;
+    bt = as_constant(a.block_table) + size_t(it.source) * a.bt_stride;
+    hkv = a.num_kv_heads;
+    kvh = it.kvh;
+    pe = it.pe;
+    k_off = kFp8 ? (l.grp * kPage + l.col) * 16 : (l.grp * kPage + l.col) * 16;
+    v_off = kFp8 ? (l.grp * kPage + l.col) * 16 : (l.col * kPage + 4 * l.grp) * 2;
+  }
+  __device__ __forceinline__ size_t tile(int page) const {
+    return (size_t(page) * hkv + kvh) * size_t(kPage * D * (kFp8 ? 1 : 2));
+  }
+};
+
+struct Pages {
+  int p0, p1;
+};
+template <int D, bool kFp8>
+__device__ __forceinline__ Pages pages_at(const Source<D, kFp8>& s, int pg) {
+  Pages p;
+  p.p0 = s.bt[pg];
+  p.p1 = pg + 1 < s.pe ? s.bt[pg + 1] : p.p0;   // masked
+  return p;
+}
+
+// kOnce: no other wave reads these bytes.
+template <bool kOnce, class T>
+__device__ __forceinline__ T load(const char* p) {
+  if constexpr (kOnce) return __builtin_nontemporal_load(reinterpret_cast<const T*>(p));
+  return *reinterpret_cast<const T*>(p);
+}
+
+template <bool kOnce, int D, bool kFp8>
+__device__ __forceinline__ void load_keys(const Source<D, kFp8>& s, Pages p, Keys<D, kFp8>& b) {
+  const char* k0 = s.k_pool + s.tile(p.p0) + s.k_off;
+  const char* k1 = s.k_pool + s.tile(p.p1) + s.k_off;
+  constexpr int kN = kFp8 ? D / 64 : D / 32;
+#pragma unroll
+  for (int i = 0; i < kN; ++i) {
+    b.k[0][i] = load<kOnce, u32x4>(k0 + 1024 * i);
+    b.k[1][i] = load<kOnce, u32x4>(k1 + 1024 * i);
+  }
+  if constexpr (kFp8) {
+    b.scale[0] = s.k_scale[size_t(p.p0) * s.hkv + s.kvh];
+    b.scale[1] = s.k_scale[size_t(p.p1) * s.hkv + s.kvh];
+  }
+}
+
+template <bool kOnce, int D, bool kFp8>
+__device__ __forceinline__ void load_values(const Source<D, kFp8>& s, Pages p, Values<D, kFp8>& b) {
+  const char* v0 = s.v_pool + s.tile(p.p0) + s.v_off;
+  const char* v1 = s.v_pool + s.tile(p.p1) + s.v_off;
+  if constexpr (kFp8) {
+#pragma unroll
+    for (int i = 0; i < D / 64; ++i) {
+      b.v[0][i] = load<kOnce, u32x4>(v0 + 1024 * i);
+      b.v[1][i] = load<kOnce, u32x4>(v1 + 1024 * i);
+    }
+    b.scale[0] = s.v_scale[size_t(p.p0) * s.hkv + s.kvh];
+    b.scale[1] = s.v_scale[size_t(p.p1) * s.hkv + s.kvh];
+  } else {
+#pragma unroll
+    for (int j = 0; j < D / 16; ++j) {
+      const u32x2 x = load<kOnce, u32x2>(v0 + 512 * j);
+      const u32x2 y = load<kOnce, u32x2>(v1 + 512 * j);
+      b.v[j] = u32x4{x[0], x[1], y[0], y[1]};
+    }
+  }
+}
+
+// K operand of page h for dims 32 kb ..; V^T operand for dims 16 jb .. (fp8: widened, exact).
+template <int D, bool kFp8>
+__device__ __forceinline__ u32x4 key_operand(const Keys<D, kFp8>& b, int h, int kb) {
+  if constexpr (!kFp8) return b.k[h][kb];
+  else {
+    const u32x4 w = b.k[h][kb / 2];
+    const uint32_t lo = w[2 * (kb % 2)], hi = w[2 * (kb % 2) + 1];
+    return u32x4{widen2<false>(lo), widen2<true>(lo), widen2<false>(hi), widen2<true>(hi)};
+  }
+}
+template <int D, bool kFp8>
+__device__ __forceinline__ u32x4 value_operand(const Values<D, kFp8>& b, int jb) {
+  if constexpr (!kFp8) return b.v[jb];
+  else {
+    const uint32_t p0 = b.v[0][jb / 4][jb % 4], p1 = b.v[1][jb / 4][jb % 4];
+    return u32x4{widen2<false>(p0), widen2<true>(p0), widen2<false>(p1), widen2<true>(p1)};
+  }
+}
+
+// Key of a block that a lane's weight e belongs to: 0 .. 3 are slots 4 grp + e
+// of the first page, 4 .. 7 of the second.
+__device__ __forceinline__ int key_at(int grp, int e) { return (e < 4 ? 0 : kPage - 4) + 4 * grp + e; }
+
+// A tile's weights of one block: the P^T operand as two bf16 parts.
+struct Weights {
+  u32x4 hi, lo;
+};
+
+template <int D>
+struct Tile {
+  f32x4 o[D / 16];   // O[row col][16 jb + 4 grp + i]
+  float m;           // reference, log2 units
+  float sum;         // this lane's share of the weights' sum
+};
+
+__device__ __forceinline__ float sum8(const float* p) {
+  return ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
+}
+
+// c0, c1: factors of the two pages' scores in log2 units; v0, v1: value scales (fp8).
+// A lane's sum of weights bounds each of them; until one passes the headroom (the first
+// block's does: m is -inf) lanes of a row need not agree on its maximum, and nothing is exchanged.
+template <int D, bool kFp8, bool kMasked>
+__device__ __forceinline__ Weights weigh(Tile<D>& t, const f32x4& s0, const f32x4& s1, float c0, float c1, float v0, float v1,
+                                         int valid, int grp) {
+  float z[8], p[8];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    z[e] = s0[e] * c0;
+    z[4 + e] = s1[e] * c1;
+  }
+  if constexpr (kMasked) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) z[e] = key_at(grp, e) < valid ? z[e] : -__builtin_inff();
+  }
+#pragma unroll
+  for (int e = 0; e < 8; ++e) p[e] = exp2_fast(z[e] - t.m);
+  float part = sum8(p);
+  if (__any(!(part <= kHeadroom))) {
+    float top = fmaxf(fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3])), fmaxf(fmaxf(z[4], z[5]), fmaxf(z[6], z[7])));
+    top = fmaxf(top, __shfl_xor(top, 16));
+    top = fmaxf(top, __shfl_xor(top, 32));
+    const float m = fmaxf(t.m, top);
+    const float ref = m == -__builtin_inff() ? 0.f : m;   // no key with a finite score so far
+    const float keep = exp2_fast(t.m - ref);
+    t.m = m;
+    t.sum *= keep;
+#pragma unroll
+    for (int j = 0; j < D / 16; ++j) t.o[j] *= keep;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) p[e] = exp2_fast(z[e] - ref);
+    part = sum8(p);
+  }
+  t.sum += part;
+  Weights w;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float a = p[2 * i], b = p[2 * i + 1];
+    if constexpr (kFp8) {
+      a *= i < 2 ? v0 : v1;
+      b *= i < 2 ? v0 : v1;
+    }
+    const uint32_t hi = pack_bf16(a, b);
+    w.hi[i] = hi;
+    w.lo[i] = pack_bf16(a - low_bf16(hi), b - high_bf16(hi));
+  }
+  return w;
+}
+
+// One segment with kTiles tiles of rows.
+template <int D, int kTiles, bool kFp8>
+__device__ __forceinline__ void walk(const SharedArgs& a, const Item& it) {
+  constexpr int KB = D / 32, JB = D / 16;
+  constexpr int kBufs = kFp8 ? 3 : 2;   // codes are half the bytes: two blocks ahead
+  constexpr bool kOnce = kTiles == 1;
+  const Lane l;
+  const Source<D, kFp8> src(a, it, l);
+  Keys<D, kFp8> kb_[kBufs];
+  Values<D, kFp8> vb_[kBufs];
+#pragma unroll
+  for (int j = 0; j < kBufs - 1; ++j) {
+    if (it.pb + 2 * j >= it.pe) break;
+    const Pages p = pages_at(src, it.pb + 2 * j);
+    load_keys<kOnce>(src, p, kb_[j]);
+    load_values<kOnce>(src, p, vb_[j]);
+  }
+  u32x4 qf[kTiles][KB];
+  Tile<D> tile[kTiles];
+#pragma unroll
+  for (int t = 0; t < kTiles; ++t) {
+    const int r = 16 * t + l.col;
+    const bool ok = r < it.rows;
+    const int row = it.row0 + (ok ? r : 0);
+    const int member = row / a.group, head = row - member * a.group;
+    const uint16_t* q = a.q + (size_t(it.seq0 + member) * a.num_q_heads + it.kvh * a.group + head) * D + 8 * l.grp;
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) {
+      const u32x4 x = *reinterpret_cast<const u32x4*>(q + 32 * kb);
+      qf[t][kb] = ok ? x : u32x4{0u, 0u, 0u, 0u};
+    }
+#pragma unroll
+    for (int j = 0; j < JB; ++j) tile[t].o[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    tile[t].m = -__builtin_inff();
+    tile[t].sum = 0.f;
+  }
+
+  // Block at pg from kc, vc; the one kBufs - 1 ahead loads into kn, vn. Only a
+  // segment's last block may lack keys.
+  auto step = [&](auto masked, int pg, Keys<D, kFp8>& kc, Values<D, kFp8>& vc, Keys<D, kFp8>& kn, Values<D, kFp8>& vn) {
+    constexpr bool kMasked = decltype(masked)::value;
+    const bool more = !kMasked && pg + 2 * (kBufs - 1) < it.pe;
+    Pages next = {0, 0};
+    if (more) {
+      next = pages_at(src, pg + 2 * (kBufs - 1));
+      load_keys<kOnce>(src, next, kn);
+    }
+    f32x4 s0[kTiles], s1[kTiles];
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) s0[t] = s1[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) {
+      const u32x4 k0 = key_operand(kc, 0, kb), k1 = key_operand(kc, 1, kb);
+#pragma unroll
+      for (int t = 0; t < kTiles; ++t) {
+        s0[t] = mfma_bf16(k0, qf[t][kb], s0[t]);
+        s1[t] = mfma_bf16(k1, qf[t][kb], s1[t]);
+      }
+    }
+    float c0 = a.scale_log2, c1 = a.scale_log2, v0 = 1.f, v1 = 1.f;
+    if constexpr (kFp8) {
+      c0 *= kc.scale[0];
+      c1 *= kc.scale[1];
+      v0 = vc.scale[0];
+      v1 = vc.scale[1];
+    }
+    if (more) load_values<kOnce>(src, next, vn);
+    // Slots past the end may hold anything (a zero weight times NaN is NaN): their values are zeroed.
+    u32x4 mask;
+    int valid = 2 * kPage;
+    if constexpr (kMasked) {
+      valid = min(it.end - pg * kPage, pg + 1 < it.pe ? 2 * kPage : kPage);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        mask[i] = (key_at(l.grp, 2 * i) < valid ? 0x0000FFFFu : 0u) | (key_at(l.grp, 2 * i + 1) < valid ? 0xFFFF0000u : 0u);
+    }
+    Weights w[kTiles];
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) w[t] = weigh<D, kFp8, kMasked>(tile[t], s0[t], s1[t], c0, c1, v0, v1, valid, l.grp);
+#pragma unroll
+    for (int j = 0; j < JB; ++j) {
+      u32x4 v = value_operand(vc, j);
+      if constexpr (kMasked) v &= mask;
+#pragma unroll
+      for (int t = 0; t < kTiles; ++t) {
+        tile[t].o[j] = mfma_bf16(v, w[t].hi, tile[t].o[j]);
+        tile[t].o[j] = mfma_bf16(v, w[t].lo, tile[t].o[j]);
+      }
+    }
+  };
+  const int full = it.pb + (min(it.pe, it.end / kPage) - it.pb) / 2 * 2;   // blocks before it lack nothing
+  for (int pg = it.pb; pg < full; pg += 2) {
+    step(std::false_type{}, pg, kb_[0], vb_[0], kb_[kBufs - 1], vb_[kBufs - 1]);
+#pragma unroll
+    for (int b = 0; b + 1 < kBufs; ++b) {
+      kb_[b] = kb_[b + 1];
+      vb_[b] = vb_[b + 1];
+    }
+  }
+  if (full < it.pe) step(std::true_type{}, full, kb_[0], vb_[0], kb_[1], vb_[1]);
+
+#pragma unroll
+  for (int t = 0; t < kTiles; ++t) {
+    float total = tile[t].sum + __shfl_xor(tile[t].sum, 16);
+    total += __shfl_xor(total, 32);
+    const float inv = total > 0.f ? 1.f / total : 0.f;
+    const float lse = total > 0.f ? tile[t].m + __log2f(total) : -__builtin_inff();
+    const int r = 16 * t + l.col;
+    if (r >= it.rows) continue;
+    if (it.slot >= 0) {
+      float* dst = a.part_o + size_t(it.slot + r) * D + 4 * l.grp;
+#pragma unroll
+      for (int j = 0; j < JB; ++j) *reinterpret_cast<f32x4*>(dst + 16 * j) = tile[t].o[j] * inv;
+      if (l.grp == 0) a.part_lse[it.slot + r] = lse;
+      continue;
+    }
+    // a sequence's only segment: its rows are the heads
+    const size_t row = size_t(it.seq0) * a.num_q_heads + it.kvh * a.group + r;
+#pragma unroll
+    for (int j = 0; j < JB; ++j) {
+      const f32x4 o = tile[t].o[j] * inv;
+      const size_t at = row * D + 16 * j + 4 * l.grp;
+      if (a.out_bf16)
+        *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.out) + at) = u32x2{pack_bf16(o[0], o[1]), pack_bf16(o[2], o[3])};
+      else
+        *reinterpret_cast<f32x4*>(static_cast<float*>(a.out) + at) = o;
+    }
+    if (a.lse && l.grp == 0) a.lse[row] = lse * kLn2;
+  }
+}
+
+__device__ __forceinline__ Item item_at(const_i32_ptr row) {
+  return {row[2], row[3], row[4], row[5], row[6], row[7], row[8], row[9], row[10]};
+}
+
+template <int D, bool kFp8, int kWG>
+__global__ __launch_bounds__(64 * kWG) __attribute__((amdgpu_waves_per_eu(1, 1))) void shared_attn_kernel(SharedArgs a) {
+  const int wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
+  const int worker = int(blockIdx.x) * kWG + wave;
+  // the side job: merge rows to the device
+  for (int64_t i = int64_t(blockIdx.x) * (64 * kWG) + int(threadIdx.x); i < a.copy_ints; i += int64_t(gridDim.x) * (64 * kWG))
+    a.copy_dst[i] = a.copy_src[i];
+  if (worker >= a.num_workers) return;
+  const const_i32_ptr head = as_constant(a.workers) + size_t(worker) * kSharedInts;
+  const int first = head[0], count = head[1];
+  for (int i = 0; i < count; ++i) {
+    const Item it = item_at(i == 0 ? head : as_constant(a.items) + size_t(first + i) * kSharedInts);
+    if (it.rows <= 16) walk<D, 1, kFp8>(a, it);
+    else if (it.rows <= 32) walk<D, 2, kFp8>(a, it);
+    else walk<D, 4, kFp8>(a, it);
+  }
+}
+
+// One workgroup per (sequence, KV head): its parts and those of its prompt.
+__global__ __launch_bounds__(256) void shared_merge_kernel(SharedArgs a) {
+  const const_i32_ptr row = as_constant(a.merge_rows) + size_t(blockIdx.x) * kSharedMergeInts;
+  const int seq = row[0], kvh = row[1], own = row[2], own_parts = row[3], pre = row[4], pre_parts = row[5], stride = row[6];
+  const int g = a.group, d4n = a.head_dim / 4;
+  for (int i = int(threadIdx.x); i < g * d4n; i += int(blockDim.x)) {
+    const int h = i / d4n, d4 = i - h * d4n;
+    float top = -__builtin_inff(), sum = 0.f;
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    auto add = [&](size_t at) {
+      const float lse = a.part_lse[at];
+      const f32x4 o = *reinterpret_cast<const f32x4*>(a.part_o + at * a.head_dim + 4 * d4);
+      const float m = fmaxf(top, lse);
+      const float ref = m == -__builtin_inff() ? 0.f : m;
+      const float keep = exp2_fast(top - ref), w = exp2_fast(lse - ref);
+      acc = acc * keep + o * w;
+      sum = sum * keep + w;
+      top = m;
+    };
+#pragma unroll 4
+    for (int c = 0; c < pre_parts; ++c) add(size_t(pre) + size_t(c) * stride + h);
+#pragma unroll 4
+    for (int c = 0; c < own_parts; ++c) add(size_t(own) + size_t(c) * g + h);
+    const f32x4 o = acc * (sum > 0.f ? 1.f / sum : 0.f);
+    const size_t r = size_t(seq) * a.num_q_heads + kvh * g + h;
+    if (a.out_bf16)
+      *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.out) + r * a.head_dim + 4 * d4) =
+          u32x2{pack_bf16(o[0], o[1]), pack_bf16(o[2], o[3])};
+    else
+      *reinterpret_cast<f32x4*>(static_cast<float*>(a.out) + r * a.head_dim + 4 * d4) = o;
+    if (a.lse && d4 == 0) a.lse[r] = sum > 0.f ? (top + __log2f(sum)) * kLn2 : -__builtin_inff();
+  }
+}
+
+template <int D, bool kFp8>
+void launch_walks(const SharedArgs& a, hipStream_t stream) {
+  if (a.workers_per_group == 4)
+    hipLaunchKernelGGL((shared_attn_kernel<D, kFp8, 4>), dim3((a.num_workers + 3) / 4), dim3(256), 0, stream, a);
+  else
+    hipLaunchKernelGGL((shared_attn_kernel<D, kFp8, 1>), dim3(a.num_workers), dim3(64), 0, stream, a);
+}
+
+}  // namespace
+
+hipError_t launch_shared(const SharedArgs& a, hipStream_t stream) {
+  if (a.num_workers > 0) {
+    if (a.head_dim == 128) a.k_scale ? launch_walks<128, true>(a, stream) : launch_walks<128, false>(a, stream);
+    else a.k_scale ? launch_walks<64, true>(a, stream) : launch_walks<64, false>(a, stream);
+  }
+  if (a.num_merge > 0) hipLaunchKernelGGL(shared_merge_kernel, dim3(a.num_merge), dim3(256), 0, stream, a);
+  return hipGetLastError();
+}
+
+}  // namespace sf
