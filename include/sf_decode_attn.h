@@ -728,8 +728,15 @@ sf_status sf_page_pool_claim(sf_page_pool* pool, const int32_t* pages, int32_t n
 /* Takes n pages into pages[0..n) (host), in hand-out order; SF_ERR_CAPACITY
  * if fewer than n are free. */
 sf_status sf_page_pool_alloc(sf_page_pool* pool, int32_t n, int32_t* pages);
+/* Each of the n pages in use gets one more holder per time it is listed (a
+ * page that several sequences start with is claimed or taken for the first of
+ * them and shared for every other). SF_ERR_INVALID_ARG if one is out of range
+ * or free; nothing changes then. */
+sf_status sf_page_pool_share(sf_page_pool* pool, const int32_t* pages, int32_t n);
 /* Returns n pages in use, in the given order (the last one is handed out
- * next). SF_ERR_INVALID_ARG if one is out of range, repeated or not in use. */
+ * next); a page with several holders is free once every one has returned it.
+ * SF_ERR_INVALID_ARG if one is out of range, not in use or listed more often
+ * than it has holders. */
 sf_status sf_page_pool_release(sf_page_pool* pool, const int32_t* pages, int32_t n);
 
 /*

@@ -180,6 +180,7 @@ def lib():
     for fn in ("sf_page_pool_claim", "sf_page_pool_release"):
         getattr(L, fn).argtypes = [vp, vp, ctypes.c_int32]
     L.sf_page_pool_alloc.argtypes = [vp, ctypes.c_int32, vp]
+    L.sf_page_pool_share.argtypes = [vp, vp, ctypes.c_int32]
     i32, u64, desc = ctypes.c_int32, ctypes.c_uint64, P(sf_attn_desc)
     L.sf_kv_store_fp8_plan.argtypes = [desc, vp, vp, vp, u64, P(sf_store_info)]
     L.sf_kv_store_fp8.argtypes = [desc, P(sf_store_info)] + [vp] * 11
@@ -225,7 +226,7 @@ def lib():
                "sf_kv_evict", "sf_runner_store_fp8", "sf_runner_key_weights", "sf_runner_evict",
                "sf_page_table_truncate", "sf_extend_attn_fp8", "sf_runner_extend_fp8", "sf_shared_attn_plan", "sf_shared_attn",
                "sf_runner_shared", "sf_rotary_frequencies", "sf_rotary_turns", "sf_rotary", "sf_rotary_store_plan",
-               "sf_rotary_store", "sf_runner_rotary_store", "sf_sample_workspace", "sf_sample"):
+               "sf_rotary_store", "sf_runner_rotary_store", "sf_sample_workspace", "sf_sample", "sf_page_pool_share"):
         getattr(L, fn).restype = ctypes.c_int
     L.sf_status_string.argtypes = [ctypes.c_int]
     L.sf_status_string.restype = ctypes.c_char_p
@@ -768,6 +769,53 @@ def _interleaved(a, b):
     return off >= nx and off + ny <= stride
 
 
+def sf_rotary(rotary, turns, positions, q, k, q_out, k_out, stream=None):
+    """Enqueues the turn of q and k (bf16 [T, H, D], parts of wider rows allowed, either may be None with its output) by
+    positions (device int32 [T]). rotary: a sf_rotary_desc; turns: device int64 [rotary_dim / 2]."""
+    t = positions.numel()
+    _dev(positions, "positions", torch.int32, (t,))
+    _dev(turns, "turns", torch.int64, (rotary.rotary_dim // 2,))
+    args, heads = [], []
+    for x, out, name in ((q, q_out, "q"), (k, k_out, "k")):
+        if x is None:
+            args += [None, 0, None, 0]
+            heads.append(0)
+            continue
+        shape = (t, x.shape[1], rotary.head_dim)
+        args += [x.data_ptr(), _rows(x, name, shape), out.data_ptr(), _rows(out, name + "_out", shape)]
+        heads.append(x.shape[1])
+    _check("sf_rotary", lib().sf_rotary(ctypes.byref(rotary), t, *heads, _addr(turns), _addr(positions), *args, _stream(stream)))
+
+
+def sf_rotary_store_plan(desc, seq_lens, q_lens=None, first_pos=None, work_host=None):
+    """Plans the turn and store of the last q_lens[s] of seq_lens[s] tokens (None: a decode step). Returns (info, work_host)."""
+    n = desc.num_seqs
+    lens, qls, first = (_host_i32(x, name, n) for x, name in ((seq_lens, "seq_lens"), (q_lens, "q_lens"), (first_pos, "first_pos")))
+    info = sf_store_info()
+    return _planned("sf_rotary_store_plan", info, lambda w, cap: lib().sf_rotary_store_plan(
+        ctypes.byref(desc), _host_addr(lens), _addr(qls), _addr(first), w, cap, ctypes.byref(info)), work_host)
+
+
+def sf_rotary_store(desc, rotary, info, work_host, work_dev, turns, q, q_out, k_new, v_new, new_pages, k_pool, v_pool,
+                    block_table, stream=None):
+    """Enqueues the turn of queries and keys and the store of keys and values into a bf16 cache. rotary: a sf_rotary_desc or
+    None; q and q_out may be None; new_pages: device int32 [B] or None."""
+    hq, hkv, d = desc.num_q_heads, desc.num_kv_heads, desc.head_dim
+    rows = info.num_q_rows
+    sk, sv = _rows(k_new, "k_new", (rows, hkv, d)), _rows(v_new, "v_new", (rows, hkv, d))
+    sq, so = (0, 0) if q is None else (_rows(q, "q", (rows, hq, d)), _rows(q_out, "q_out", (rows, hq, d)))
+    if new_pages is not None:
+        _dev(new_pages, "new_pages", torch.int32, (desc.num_seqs,))
+    if rotary is not None:
+        _dev(turns, "turns", torch.int64, (rotary.rotary_dim // 2,))
+    _check_pools(desc.num_pages, hkv, d, k_pool, v_pool, block_table, desc.num_seqs, None)
+    _check_work(info, work_dev)
+    _check("sf_rotary_store", lib().sf_rotary_store(
+        ctypes.byref(desc), None if rotary is None else ctypes.byref(rotary), ctypes.byref(info), _addr(work_host),
+        _addr(work_dev), _addr(turns), _addr(q), sq, _addr(q_out), so, _addr(k_new), sk, _addr(v_new), sv, _addr(new_pages),
+        _addr(k_pool), _addr(v_pool), _addr(block_table), _stream(stream)))
+
+
 _cus = {}
 
 
@@ -1106,6 +1154,11 @@ class PagePool:
         out = np.empty(max(0, int(n)), dtype=np.int32)
         _check("sf_page_pool_alloc", self._L.sf_page_pool_alloc(self._p, int(n), out.ctypes.data))
         return out
+
+    def share(self, pages) -> None:
+        """One more holder for every page listed."""
+        a = np.ascontiguousarray(pages, dtype=np.int32)
+        _check("sf_page_pool_share", self._L.sf_page_pool_share(self._p, a.ctypes.data, a.size))
 
     def release(self, pages) -> None:
         a = np.ascontiguousarray(pages, dtype=np.int32)
@@ -1486,20 +1539,24 @@ class DecodeAttention:
             stream.cuda_stream if stream else _current_stream(self.device)))
         return out
 
-    def rotate_store(self, rotary, q, k_new, v_new, k_pool, v_pool, block_table, seq_lens, q_lens, first_pos=None,
+    def rotate_store(self, rotary, q, k_new, v_new, k_pool, v_pool, block_table, seq_lens, q_lens=None, first_pos=None,
                      new_pages=None, q_out=None, stream=None):
         """Turns the queries and keys of the last q_lens[s] of seq_lens[s] tokens by their positions and stores the turned
-        keys and the values into the pages of a bf16 cache (sf_rotary_store, through the runner). rotary: a Rotary; q,
-        k_new, v_new: bf16 [T, H, D], parts of wider rows allowed (q may be None); first_pos: host int32 [B], the first new
-        token's position (default: its index in the cache); new_pages as in store_fp8. Returns the turned queries: q_out
-        (may be q), by default a new tensor."""
+        keys and the values into the pages of a bf16 cache (sf_rotary_store, through the runner). rotary: a Rotary, or
+        None (nothing turns); q, k_new, v_new: bf16 [T, H, D], parts of wider rows allowed (q may be None). q_lens None is
+        a decode step: a row per sequence, of which the running ones' (seq_lens[s] > 0) last token is new. first_pos: host
+        int32 [B], the first new token's position (default: its index in the cache); new_pages as in store_fp8. Returns the
+        turned queries: q_out (may be q), by default a new tensor."""
         desc, lens = self._call_desc(k_pool, block_table, seq_lens, 1.0)
         n = lens.size
         qls, first, pages = (_host_i32(x, name, n) for x, name in ((q_lens, "q_lens"), (first_pos, "first_pos"),
                                                                    (new_pages, "new_pages")))
-        if rotary.head_dim != self.d:
-            raise ValueError(f"rotary turns heads of {rotary.head_dim} dims, not {self.d}")
-        rows = int(qls.sum(dtype=np.int64))
+        rope, turns = None, None
+        if rotary is not None:
+            if rotary.head_dim != self.d:
+                raise ValueError(f"rotary turns heads of {rotary.head_dim} dims, not {self.d}")
+            rope, turns = rotary.desc_ref, rotary.turns_on(k_pool.device).data_ptr()
+        rows = n if qls is None else int(qls.sum(dtype=np.int64))
         sk, sv = _rows(k_new, "k_new", (rows, self.hkv, self.d)), _rows(v_new, "v_new", (rows, self.hkv, self.d))
         sq = so = 0
         if q is not None:
@@ -1512,16 +1569,16 @@ class DecodeAttention:
         elif q_out is not None:
             raise ValueError("q_out without q")
         _check_pools(desc.num_pages, self.hkv, self.d, k_pool, v_pool, block_table, n, None)
-        if DEBUG_CHECKS:
+        if DEBUG_CHECKS and not self._host_checked:
             named = np.zeros(n, bool) if pages is None else pages >= 0
-            check_block_table(desc, block_table, np.where(qls > 0, lens - named, 0))
+            check_block_table(desc, block_table, np.where((lens if qls is None else qls) > 0, lens - named, 0))
             if pages is not None and np.any((pages < -1) | (pages >= desc.num_pages)):
                 raise ValueError("new_pages holds a page id outside the pool")
+        self._host_checked = False
         _check("sf_runner_rotary_store", self.L.sf_runner_rotary_store(
-            self._runner(None), ctypes.byref(desc), ctypes.byref(rotary.desc), _host_addr(lens), _host_addr(qls), _addr(first),
-            rotary.turns_on(k_pool.device).data_ptr(), _addr(q), sq, _addr(q_out), so, k_new.data_ptr(), sk, v_new.data_ptr(), sv,
-            _addr(pages), k_pool.data_ptr(), v_pool.data_ptr(), block_table.data_ptr(),
-            stream.cuda_stream if stream else _current_stream(self.device)))
+            self._runner(None), ctypes.byref(desc), rope, _host_addr(lens), _addr(qls), _addr(first), turns, _addr(q), sq,
+            _addr(q_out), so, k_new.data_ptr(), sk, v_new.data_ptr(), sv, _addr(pages), k_pool.data_ptr(),
+            v_pool.data_ptr(), block_table.data_ptr(), stream.cuda_stream if stream else _current_stream(self.device)))
         return q_out
 
     def __del__(self):
@@ -1558,10 +1615,11 @@ class Rotary:
         if self.freq.shape != (self.rotary_dim // 2,):
             raise ValueError("freq must have rotary_dim / 2 entries")
         self.desc = sf_rotary_desc(self.head_dim, self.rotary_dim, int(layout == "interleaved"), magnitude)
+        self.desc_ref = ctypes.byref(self.desc)
         self._turns = torch.from_numpy(sf_rotary_turns(self.freq).view(np.int64))
         self._on = {}
         # an error of the arguments, if any, here and not at the first call
-        _check("sf_rotary", lib().sf_rotary(ctypes.byref(self.desc), 0, 0, 0, None, None, None, 0, None, 0, None, 0, None, 0, None))
+        _check("sf_rotary", lib().sf_rotary(self.desc_ref, 0, 0, 0, None, None, None, 0, None, 0, None, 0, None, 0, None))
         if device is not None:
             self.turns_on(torch.device(device))
 
@@ -1608,7 +1666,7 @@ class Rotary:
         device = given.device
         with torch.cuda.device(device):
             _check("sf_rotary", lib().sf_rotary(
-                ctypes.byref(self.desc), t, 0 if q is None else q.shape[1], 0 if k is None else k.shape[1],
+                self.desc_ref, t, 0 if q is None else q.shape[1], 0 if k is None else k.shape[1],
                 self.turns_on(device).data_ptr(), positions.data_ptr(), *args,
                 stream.cuda_stream if stream else _current_stream(device)))
         return tuple(outs)
@@ -1676,15 +1734,35 @@ class PageTable:
          records it in the host block table.
     It returns the int32 [B] new-page array the append kernel takes (-1 where
     the token lands in a page the sequence already holds).
+
+    groups = (group_offsets, shared_lens): sequences group_offsets[i] .. group_offsets[i+1] - 1 start with the same
+    shared_lens[i] // 16 pages, which are free once the last of them has left.
     """
 
-    def __init__(self, num_pages, bt_host, lens0):
+    def __init__(self, num_pages, bt_host, lens0, groups=None):
         self.bt = np.array(bt_host, dtype=np.int32, order="C", copy=True)
         lens0 = np.asarray(lens0, dtype=np.int64)
         self.pool = PagePool(num_pages)
         npg = (lens0 + PAGE - 1) // PAGE
-        held = [self.bt[s, : npg[s]] for s in range(lens0.size)]
+        common = np.zeros(lens0.size, dtype=np.int64)   # pages whose first holder is an earlier member
+        shared = []
+        if groups is not None:
+            _, offsets, counts = _host_groups(lens0.size, lens0, *groups)
+            if offsets[0] != 0 or offsets[-1] != lens0.size or np.any(np.diff(offsets) < 0) or np.any(counts < 0):
+                raise ValueError("groups must cover the sequences one behind the other")
+            for a, b, tokens in zip(offsets[:-1].tolist(), offsets[1:].tolist(), counts.tolist()):
+                live = [s for s in range(a, b) if lens0[s] > 0]
+                if any(lens0[s] < tokens for s in live):
+                    raise ValueError("a member is shorter than its group's shared tokens")
+                for s in live[1:]:
+                    common[s] = tokens // PAGE
+                    if not np.array_equal(self.bt[s, : common[s]], self.bt[live[0], : common[s]]):
+                        raise ValueError("members of a group must start with the same pages")
+                    shared.append(self.bt[s, : common[s]])
+        held = [self.bt[s, common[s]: npg[s]] for s in range(lens0.size)]
         self.pool.claim(np.concatenate(held) if held else np.zeros(0, np.int32))
+        if shared:
+            self.pool.share(np.concatenate(shared))
         self.prev = np.ascontiguousarray(lens0, dtype=np.int32)
         self.new_pages = np.empty(lens0.size, dtype=np.int32)
 
@@ -1716,18 +1794,25 @@ class DecodeLoopRunner:
     block_table is the device table the kernels read and extend. With fp8 =
     (k_scale, v_scale) the pools are an fp8 cache. A loop with a budget calls
     key_weights after its steps and evict every so many of them; the lengths of
-    the step after an eviction go on from the kept tokens."""
+    the step after an eviction go on from the kept tokens.
+
+    rotary (a Rotary): q and k_new come as the projections give them, and are turned by their positions
+    (the keys of the cache at the start are turned already). groups = (group_offsets, shared_lens): trajectories sampled
+    from common prompts, as for DecodeAttention.shared and PageTable; such a loop neither evicts nor weighs keys (a
+    page that several sequences hold has no weights of one's own), and a sequence that has left does not
+    start again. With either, new tokens are stored before the attention (and over bf16 pools attended to as stored)."""
 
     def __init__(self, num_q_heads, num_kv_heads, head_dim, k_pool, v_pool, block_table, bt_host, lens0,
-                 scale, device=None, num_cus=None, attn=None, fp8=None):
+                 scale, device=None, num_cus=None, attn=None, fp8=None, rotary=None, groups=None):
         """attn: an existing DecodeAttention of the same head geometry to reuse
         (its native runner keeps its pinned ring and workspace across loops)."""
         if attn is not None and (attn.hq, attn.hkv, attn.d) != (int(num_q_heads), int(num_kv_heads), int(head_dim)):
             raise ValueError("attn was made for another head geometry")
         self.attn = attn or DecodeAttention(num_q_heads, num_kv_heads, head_dim, device=device, num_cus=num_cus)
         self.k_pool, self.v_pool, self.block_table, self.scale = k_pool, v_pool, block_table, float(scale)
-        self.table = PageTable(k_pool.shape[0], bt_host, lens0)
-        self.fp8 = fp8
+        self.table = PageTable(k_pool.shape[0], bt_host, lens0, groups)
+        self.fp8, self.rotary = fp8, rotary
+        self.groups = None if groups is None else _host_groups(len(lens0), lens0, *groups)[1:]
         self.evicted = np.zeros(self.table.prev.size, dtype=np.int32)   # tokens given up so far, per sequence
         self.weighed = np.zeros_like(self.evicted)   # cached tokens that have weights
         self.steps = 0
@@ -1745,6 +1830,8 @@ class DecodeLoopRunner:
         appending = self.steps > 0
         if appending and (k_new is None or v_new is None):
             raise ValueError("every step after the first appends a token: pass k_new and v_new")
+        if self.groups is not None and np.any((lens > 0) & (self.table.prev == 0)):
+            raise ValueError("a sequence of a group that has left does not start again")
         new_pages = self.table.advance(lens, appending)
         if DEBUG_CHECKS:
             desc = make_desc(lens.size, self.attn.hq, self.attn.hkv, self.attn.d, self.table.bt.shape[1],
@@ -1752,16 +1839,55 @@ class DecodeLoopRunner:
             check_block_table(desc, self.table.bt, lens)
             self.attn._host_checked = True
         append = (k_new, v_new, new_pages) if appending else None
-        out = self.attn(q, self.k_pool, self.v_pool, self.block_table, lens.astype(np.int32), self.scale,
-                        out=out, lse=lse, stream=stream, attn_events=attn_events, append=append, fp8=self.fp8)
+        if self.rotary is None and self.groups is None:
+            out = self.attn(q, self.k_pool, self.v_pool, self.block_table, lens.astype(np.int32), self.scale,
+                            out=out, lse=lse, stream=stream, attn_events=attn_events, append=append, fp8=self.fp8)
+        else:
+            out = self._step_stored(q, lens.astype(np.int32), append, out, lse, stream, attn_events)
         self.steps += 1
         if not lens.all():   # sequences that are not running: one that starts there later has nothing of theirs
             self.evicted, self.weighed = (np.where(lens > 0, x, 0) for x in (self.evicted, self.weighed))
         return out
 
+    def _step_stored(self, q, lens, append, out, lse, stream, attn_events):
+        """A step of a loop with rotary positions or groups: what is new is turned and stored, then attended to."""
+        attn, checked = self.attn, self.attn._host_checked
+        if self.groups is not None and attn_events is not None:
+            raise ValueError("a step over groups takes no attn_events")
+        if self.rotary is not None and (append is None or self.fp8 is not None):
+            with torch.cuda.stream(stream):
+                at = torch.from_numpy(np.maximum(lens - 1 + self.evicted, 0).astype(np.int32)).to(q.device)
+                q, k = self.rotary(q, None if append is None else append[0], at, stream=stream)
+            if append is not None:
+                append = (k, *append[1:])
+        if append is not None and self.fp8 is None:
+            first = np.maximum(lens - 1 + self.evicted, 0).astype(np.int32)
+            turned = attn.rotate_store(self.rotary, q if self.rotary is not None else None, append[0], append[1], self.k_pool,
+                                       self.v_pool, self.block_table, lens, first_pos=first, new_pages=append[2], stream=stream)
+            q, append = q if turned is None else turned, None
+        elif append is not None and self.groups is not None:
+            rows = np.flatnonzero(lens > 0)
+            k, v = append[0], append[1]
+            if rows.size < lens.size:   # the store takes the running sequences' rows
+                with torch.cuda.stream(stream):
+                    at = torch.from_numpy(rows).to(q.device)
+                    k, v = k[at], v[at]
+            attn._host_checked = checked
+            attn.store_fp8(k, v, self.k_pool, self.v_pool, self.fp8, self.block_table, lens, (lens > 0).astype(np.int32),
+                           new_pages=append[2], stream=stream)
+            append = None
+        attn._host_checked = checked
+        if self.groups is None:
+            return attn(q, self.k_pool, self.v_pool, self.block_table, lens, self.scale, out=out, lse=lse, stream=stream,
+                        attn_events=attn_events, append=append, fp8=self.fp8)
+        return attn.shared(q, self.k_pool, self.v_pool, self.block_table, lens, *self.groups, self.scale, out=out, lse=lse,
+                           fp8=self.fp8, stream=stream)
+
     def key_weights(self, q, lse, weights, positions, stream=None):
         """Adds the last step's attention weights (its q and lse, or their rows of the running sequences) to weights.
         Tokens that no call has weighed start there, and get their positions."""
+        if self.groups is not None:
+            raise ValueError("a loop over groups weighs no keys")
         lens = self.table.prev
         live = lens > 0
         if not live.all() and q.shape[0] == lse.shape[0] == lens.size:
@@ -1779,6 +1905,8 @@ class DecodeLoopRunner:
     def evict(self, keep, weights, positions, sinks=0, recent=0, stream=None):
         """Evicts every running sequence to at most keep tokens and frees the pages behind them. Returns the lengths.
         Every cached token must have weights: key_weights comes first."""
+        if self.groups is not None:
+            raise ValueError("a loop over groups does not evict")
         lens = self.table.prev
         if not np.array_equal(self.weighed, lens):
             raise ValueError("tokens without weights: call key_weights after the last step")

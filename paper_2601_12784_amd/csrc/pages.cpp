@@ -8,6 +8,7 @@
 // tiles are the most likely to still sit in a cache); a new pool hands pages
 // out in increasing id order. Every call checks all of its arguments before
 // it changes anything.
+#include <climits>
 #include <cstdint>
 #include <new>
 #include <vector>
@@ -17,26 +18,40 @@
 struct sf_page_pool {
   int32_t num_pages;
   std::vector<int32_t> stack;   // free pages; the top is the back
-  std::vector<uint8_t> in_use;  // per page
-  std::vector<uint8_t> mark;    // scratch for duplicate checks, all zero between calls
+  std::vector<int32_t> in_use;  // per page: its holders (0: free)
+  std::vector<int32_t> mark;    // scratch for duplicate checks, all zero between calls
 };
 
 namespace {
 
-// True if pages[0..n) are distinct, in range and each has in_use == want.
-bool check_pages(sf_page_pool* p, const int32_t* pages, int32_t n, uint8_t want) {
+// True if pages[0..n) are in range and, of want = 0, distinct and free, of want = 1,
+// each listed at most as often as it has holders. *freed: pages that lose their last one.
+bool check_pages(sf_page_pool* p, const int32_t* pages, int32_t n, int32_t want, int64_t* freed = nullptr) {
   bool ok = true;
+  int64_t last = 0;
   int32_t i = 0;
   for (; i < n; ++i) {
     const int32_t pg = pages[i];
-    if (pg < 0 || pg >= p->num_pages || p->in_use[size_t(pg)] != want || p->mark[size_t(pg)]) {
+    if (pg < 0 || pg >= p->num_pages) {
       ok = false;
       break;
     }
-    p->mark[size_t(pg)] = 1;
+    const int32_t holders = p->in_use[size_t(pg)], listed = ++p->mark[size_t(pg)];
+    if (want ? listed > holders : holders != 0 || listed > 1) {
+      p->mark[size_t(pg)] = 0;
+      ok = false;
+      break;
+    }
+    last += want && listed == holders;
   }
   for (int32_t j = 0; j < i; ++j) p->mark[size_t(pages[j])] = 0;
+  if (freed) *freed = last;
   return ok;
+}
+
+// One holder of a page in use less; the last one frees it.
+void give_back(sf_page_pool* p, int32_t page) {
+  if (--p->in_use[size_t(page)] == 0) p->stack.push_back(page);
 }
 
 }  // namespace
@@ -92,10 +107,18 @@ extern "C" sf_status sf_page_pool_alloc(sf_page_pool* pool, int32_t n, int32_t* 
 extern "C" sf_status sf_page_pool_release(sf_page_pool* pool, const int32_t* pages, int32_t n) {
   if (!pool || n < 0 || (n > 0 && !pages)) return SF_ERR_INVALID_ARG;
   if (!check_pages(pool, pages, n, 1)) return SF_ERR_INVALID_ARG;
+  for (int32_t i = 0; i < n; ++i) give_back(pool, pages[i]);
+  return SF_OK;
+}
+
+extern "C" sf_status sf_page_pool_share(sf_page_pool* pool, const int32_t* pages, int32_t n) {
+  if (!pool || n < 0 || (n > 0 && !pages)) return SF_ERR_INVALID_ARG;
   for (int32_t i = 0; i < n; ++i) {
-    pool->in_use[size_t(pages[i])] = 0;
-    pool->stack.push_back(pages[i]);
+    if (pages[i] < 0 || pages[i] >= pool->num_pages) return SF_ERR_INVALID_ARG;
+    const int32_t holders = pool->in_use[size_t(pages[i])];
+    if (holders == 0 || holders > INT32_MAX - n) return SF_ERR_INVALID_ARG;
   }
+  for (int32_t i = 0; i < n; ++i) ++pool->in_use[size_t(pages[i])];
   return SF_OK;
 }
 
@@ -119,12 +142,10 @@ extern "C" sf_status sf_page_table_step(sf_page_pool* pool, int32_t* block_table
     }
     if (appending && len > 0 && (len - 1) % kPage == 0) ++opens;
   }
-  if (!check_pages(pool, gone.data(), int32_t(gone.size()), 1)) return SF_ERR_INVALID_ARG;
-  if (opens > int64_t(pool->stack.size() + gone.size())) return SF_ERR_CAPACITY;
-  for (int32_t pg : gone) {
-    pool->in_use[size_t(pg)] = 0;
-    pool->stack.push_back(pg);
-  }
+  int64_t freed = 0;
+  if (!check_pages(pool, gone.data(), int32_t(gone.size()), 1, &freed)) return SF_ERR_INVALID_ARG;
+  if (opens > int64_t(pool->stack.size()) + freed) return SF_ERR_CAPACITY;
+  for (int32_t pg : gone) give_back(pool, pg);
   for (int32_t s = 0; s < num_seqs; ++s) {
     const int32_t len = lens[s];
     int32_t page = -1;

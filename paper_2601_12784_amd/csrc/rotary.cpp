@@ -130,17 +130,23 @@ extern "C" sf_status sf_rotary_store_plan(const sf_attn_desc* desc, const int32_
                                           const int32_t* q_lens_host, const int32_t* first_pos_host, int32_t* work_host,
                                           uint64_t work_capacity_bytes, sf_store_info* info) {
   if (!info) return SF_ERR_INVALID_ARG;
-  int64_t tokens = 0;
-  const sf_status st = check_extend_lengths(desc, seq_lens_host, q_lens_host, &tokens);
+  const sf_status st = validate_desc(desc);
   if (st != SF_OK) return st;
   const int32_t n = desc->num_seqs;
+  if (n > 0 && !seq_lens_host) return SF_ERR_INVALID_ARG;
+  auto news = [&](int32_t s) { return q_lens_host ? q_lens_host[s] : int32_t(seq_lens_host[s] > 0); };
   auto touched = [&](int32_t s) {
-    return q_lens_host[s] == 0 ? 0 : pages_of(seq_lens_host[s]) - (seq_lens_host[s] - q_lens_host[s]) / kPage;
+    return news(s) == 0 ? 0 : pages_of(seq_lens_host[s]) - (seq_lens_host[s] - news(s)) / kPage;
   };
-  int64_t pages = 0, rows = 0;
+  int64_t pages = 0, rows = 0, tokens = 0;
   for (int32_t s = 0; s < n; ++s) {
-    if (seq_lens_host[s] > kMaxTokens) return SF_ERR_INVALID_ARG;
-    if (first_pos_host && (first_pos_host[s] < 0 || first_pos_host[s] > INT32_MAX - q_lens_host[s])) return SF_ERR_INVALID_ARG;
+    const int32_t L = seq_lens_host[s], e = news(s);
+    if (L < 0 || e < 0 || L < e || L > kMaxTokens || int64_t(L) > int64_t(kPage) * desc->block_table_stride)
+      return SF_ERR_INVALID_ARG;
+    if (L > 0 && desc->num_pages == 0) return SF_ERR_INVALID_ARG;
+    tokens += q_lens_host ? e : 1;
+    if (tokens > INT32_MAX) return SF_ERR_INVALID_ARG;
+    if (first_pos_host && (first_pos_host[s] < 0 || first_pos_host[s] > INT32_MAX - news(s))) return SF_ERR_INVALID_ARG;
     pages += touched(s);
   }
   const int32_t run = pages > kSinglePages ? kMaxRun : 1;
@@ -153,8 +159,8 @@ extern "C" sf_status sf_rotary_store_plan(const sf_attn_desc* desc, const int32_
   if (!work_host) return SF_OK;
   if (work_capacity_bytes < info->work_bytes) return SF_ERR_CAPACITY;
   int32_t qrow = 0;
-  for (int32_t s = 0; s < n; qrow += q_lens_host[s++]) {
-    const int32_t first = seq_lens_host[s] - q_lens_host[s], begin = first / kPage, end = begin + touched(s);
+  for (int32_t s = 0; s < n; qrow += q_lens_host ? q_lens_host[s] : 1, ++s) {
+    const int32_t first = seq_lens_host[s] - news(s), begin = first / kPage, end = begin + touched(s);
     for (int32_t p = begin; p < end; p += run) {
       const int32_t row[kItemInts] = {s,    p, std::min(run, end - p), first, seq_lens_host[s], qrow,
                                       first_pos_host ? first_pos_host[s] : first, 0};
@@ -171,15 +177,17 @@ extern "C" sf_status sf_rotary_store(const sf_attn_desc* desc, const sf_rotary_d
                                      int64_t k_stride, const void* v_new, int64_t v_stride, const int32_t* new_pages,
                                      void* k_pool, void* v_pool, int32_t* block_table, void* stream) {
   sf_status st = validate_desc(desc);
-  if (st != SF_OK || (st = check_rotary(rotary)) != SF_OK) return st;
+  if (st != SF_OK || (rotary && (st = check_rotary(rotary)) != SF_OK)) return st;
+  const sf_rotary_desc none = {desc->head_dim, 0, 0, 1.f};
+  if (!rotary) rotary = &none;
   if (!info || rotary->head_dim != desc->head_dim) return SF_ERR_INVALID_ARG;
   if (info->desc_key != (desc_key(desc) ^ kRotaryKey) || info->num_rows < 0 || info->num_q_rows < 0 ||
       info->work_bytes != uint64_t(info->num_rows) * kItemInts * 4)
     return SF_ERR_PLAN_MISMATCH;
   if (info->num_rows == 0) return SF_OK;
   const int32_t hq = desc->num_q_heads, hkv = desc->num_kv_heads, d = desc->head_dim;
-  if (!work_dev || !turns || !k_pool || !v_pool || !block_table) return SF_ERR_INVALID_ARG;
-  if (!aligned16(work_dev) || !aligned8(turns) || !aligned16(k_pool) || !aligned16(v_pool) || !aligned4(block_table) ||
+  if (!work_dev || (rotary->rotary_dim && (!turns || !aligned8(turns))) || !k_pool || !v_pool || !block_table) return SF_ERR_INVALID_ARG;
+  if (!aligned16(work_dev) || !aligned16(k_pool) || !aligned16(v_pool) || !aligned4(block_table) ||
       (new_pages && !aligned4(new_pages)))
     return SF_ERR_INVALID_ARG;
   if (!good_rows(k_new, k_stride, hkv, d) || !good_rows(v_new, v_stride, hkv, d)) return SF_ERR_INVALID_ARG;
