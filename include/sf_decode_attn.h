@@ -859,25 +859,26 @@ sf_status sf_route(const sf_cost_model* model, double mu, int32_t min_initial_ve
  * (group_offsets[0] = 0, group_offsets[num_groups] = num_seqs); shared_lens[i] is at most L_s of every member with
  * L_s > 0. Members with L_s = 0 get out = 0, lse = -inf.
  *
- * Plan (host only). A prompt's rows, members times g, are taken in blocks of at most 64 (4 tiles of 16), 1, 2 or a multiple of 4 blocks,
+ * Plan (host only). A prompt's rows, members times g, are taken in blocks of at most 32 (2 tiles of 16), 1 (up to 16 rows), 2, 4 or a multiple of 8 blocks,
  * which walk the same pages side by side; the pages of all prompts with one number of blocks, and those that
  * sequences have to themselves, are each cut into equal runs, one per wave, as many runs as their share of the work.
  * Results of runs that end inside a prompt or sequence, and of all prompts, go to the workspace and are joined by a
- * second launch. Of opts, num_cus and min_chunk_pages (default 4) count.
+ * second launch. fp8 = 1: for an fp8 cache, whose pages are half the bytes at the same arithmetic (only the shares go by
+ * it: the plan runs over either). Of opts, num_cus and min_chunk_pages (default 4) count.
  */
 typedef struct sf_shared_info {
   int32_t num_workers;       /* waves */
   int32_t num_work;          /* segments */
   int32_t num_merge;         /* (sequence, KV head) pairs that the second launch writes */
   int32_t num_rows;          /* rows of partial results */
-  int32_t workers_per_group; /* waves per workgroup: 1 or 4 */
+  int32_t workers_per_group; /* waves per workgroup: 1 or 8 */
   int32_t reserved;
   uint64_t work_bytes;       /* bytes of the work list */
   uint64_t workspace_bytes;
   uint64_t desc_key;
 } sf_shared_info;
 sf_status sf_shared_attn_plan(const sf_attn_desc* desc, const int32_t* seq_lens_host, int32_t num_groups,
-                              const int32_t* group_offsets_host, const int32_t* shared_lens_host,
+                              const int32_t* group_offsets_host, const int32_t* shared_lens_host, int32_t fp8,
                               const sf_plan_opts* opts, int32_t* work_host, uint64_t work_capacity_bytes,
                               sf_shared_info* info);
 /* Enqueues the step: two launches (the second where info->num_merge > 0). Arguments as for sf_decode_attn; k_scale and

@@ -194,7 +194,7 @@ def lib():
     L.sf_extend_attn_fp8.argtypes = [desc, P(sf_extend_info)] + [vp] * 9 + [i32, vp, vp]
     L.sf_runner_extend_fp8.argtypes = [vp, desc] + [vp] * 10 + [P(sf_runner_memory), vp, P(sf_extend_info), vp, vp, i32]
     i64, rope = ctypes.c_int64, P(sf_rotary_desc)
-    L.sf_shared_attn_plan.argtypes = [desc, vp, i32, vp, vp, P(sf_plan_opts), vp, u64, P(sf_shared_info)]
+    L.sf_shared_attn_plan.argtypes = [desc, vp, i32, vp, vp, i32, P(sf_plan_opts), vp, u64, P(sf_shared_info)]
     L.sf_shared_attn.argtypes = [desc, P(sf_shared_info)] + [vp] * 9 + [i32, vp, vp, u64, vp]
     L.sf_runner_shared.argtypes = [vp, desc, vp, i32] + [vp] * 9 + [i32, vp, vp]
     L.sf_rotary_frequencies.argtypes = [i32, ctypes.c_double, P(sf_rotary_scaling), vp]
@@ -670,13 +670,13 @@ def sf_extend_attn_fp8(desc, info, work_host, work_dev, q, k_pool8, v_pool8, k_s
         int(out.dtype is torch.bfloat16), _addr(lse), _stream(stream)))
 
 
-def sf_shared_attn_plan(desc, seq_lens, group_offsets, shared_lens, opts=None, work_host=None):
+def sf_shared_attn_plan(desc, seq_lens, group_offsets, shared_lens, opts=None, work_host=None, fp8=False):
     """Plans a decode step of groups that share their first tokens: sequences group_offsets[i] .. group_offsets[i+1] - 1
     have shared_lens[i] of them in common. Returns (info, work_host)."""
     lens, offsets, shared = _host_groups(desc.num_seqs, seq_lens, group_offsets, shared_lens)
     info = sf_shared_info()
     return _planned("sf_shared_attn_plan", info, lambda w, cap: lib().sf_shared_attn_plan(
-        ctypes.byref(desc), _host_addr(lens), shared.size, _host_addr(offsets), _host_addr(shared),
+        ctypes.byref(desc), _host_addr(lens), shared.size, _host_addr(offsets), _host_addr(shared), int(fp8),
         None if opts is None else ctypes.byref(opts), w, cap, ctypes.byref(info)), work_host)
 
 

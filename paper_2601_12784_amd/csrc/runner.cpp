@@ -526,8 +526,8 @@ extern "C" sf_status sf_runner_shared(sf_runner* r, const sf_attn_desc* desc, co
   return run_in_slot(
       r, static_cast<hipStream_t>(stream),
       [&](int32_t* work, uint64_t bytes) {
-        return sf_shared_attn_plan(desc, seq_lens_host, num_groups, group_offsets_host, shared_lens_host, &r->opts, work,
-                                   bytes, &info);
+        return sf_shared_attn_plan(desc, seq_lens_host, num_groups, group_offsets_host, shared_lens_host, k_scale != nullptr,
+                                   &r->opts, work, bytes, &info);
       },
       [&] { return info.work_bytes; },
       // the merge rows' device copy lies behind the call's own workspace

@@ -176,7 +176,8 @@ hipError_t launch_store_fp8(const Store8Args& a, hipStream_t stream);
 // A decode step of groups with shared first tokens (sf_shared_attn).
 constexpr int kSharedInts = 16;       // int32 fields of a worker's or a segment's row
 constexpr int kSharedMergeInts = 8;
-constexpr int kSharedTiles = 4;       // 16-row tiles of a block
+constexpr int kSharedTiles = 2;       // 16-row tiles of a block
+constexpr int kSharedWaves = 8;       // waves of a workgroup, two per SIMD
 struct SharedArgs {
   // num_workers rows: first segment, segments, then the first segment's fields; num_work rows with the fields from int 2
   // on: first sequence of the rows, block-table row, kv_head, first page, end page, end token, partial row (-1: written

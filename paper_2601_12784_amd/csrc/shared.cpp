@@ -16,6 +16,7 @@ using namespace sf;
 namespace {
 
 constexpr int32_t kMinChunk = 4;   // pages per wave, at least
+constexpr int64_t kSegmentPages = 2;   // what a segment's start costs, in pages
 constexpr uint64_t kSharedKey = 0x536861726564ull;
 constexpr int64_t kMaxMerge = int64_t(1) << 23;   // workgroups of 256 threads: 2^32 threads are too many for a launch
 
@@ -23,10 +24,17 @@ bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) ==
 bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 int32_t pages_of(int32_t tokens) { return (tokens + kPage - 1) / kPage; }
 
-// Cost of a page for a wave, per mille of one that only this wave reads: memory
-// gives a page to all of a prompt's blocks at once, and each of a block's tiles takes
-// its own time on the matrix cores.
-int64_t page_cost(int32_t blocks, int32_t tiles) { return std::max<int64_t>(1000 / blocks, 110 * tiles); }
+// Waves of a workgroup that hold a prompt's rows together, of `blocks` in all, and
+// the sets of them that take its key blocks in turns.
+int32_t blocks_together(int32_t blocks) { return std::min(blocks, kSharedWaves); }
+int32_t splits_of(int32_t blocks) { return blocks == 1 ? 1 : kSharedWaves / blocks_together(blocks); }
+
+// Cost of a prompt's page, per mille of one that a wave reads for itself: memory
+// gives it once, and a block of rows takes its time on the matrix cores, which in pages
+// of half the bytes is twice as many. Measured, us at 250, 320, 400 and 500 per block: 16 prompts of 2048
+// tokens with 16 members (28/4 heads) 147, 128, 116, 119; one of 32760 with 64 (32/8) 101, 90, 95, 97; one of 4000
+// with 256 200, 181, 179, 182; 8 of 8000 with 8 (40/8, fp8) at 500, 640, 800 and 1000 98, 90, 85, 81.
+int64_t page_cost(int32_t blocks, bool fp8) { return std::max<int64_t>(1000, (fp8 ? 1000 : 400) * int64_t(blocks)); }
 
 // A group whose prompt is read once.
 struct Prompt {
@@ -45,7 +53,7 @@ struct Track {
   int32_t blocks;
   int64_t pages = 0;
   int64_t cost = 0;
-  int64_t columns = 0;
+  int64_t columns = 0;     // runs; blocks > 1: of workgroups
   std::vector<int32_t> prompts;
 };
 
@@ -72,13 +80,14 @@ struct Scratch {
 };
 
 void put_fields(int32_t* row, int32_t seq0, int32_t source, int32_t kvh, int32_t pb, int32_t pe, int32_t end, int32_t slot,
-                int32_t row0, int32_t rows) {
-  const int32_t f[kSharedInts] = {0, 0, seq0, source, kvh, pb, pe, end, slot, row0, rows, 0, 0, 0, 0, 0};
+                int32_t row0, int32_t rows, int32_t together = 0, int32_t split = 0) {
+  const int32_t f[kSharedInts] = {0, 0, seq0, source, kvh, pb, pe, end, slot, row0, rows, together, split, 0, 0, 0};
   std::memcpy(row, f, sizeof f);
 }
 
 sf_status plan(const sf_attn_desc* desc, const int32_t* lens, int32_t num_groups, const int32_t* offsets,
-               const int32_t* shared, const sf_plan_opts* opts, int32_t* work, uint64_t capacity, sf_shared_info* info) {
+               const int32_t* shared, bool fp8, const sf_plan_opts* opts, int32_t* work, uint64_t capacity,
+               sf_shared_info* info) {
   sf_status st = validate_desc(desc);
   if (st != SF_OK) return st;
   const int32_t n = desc->num_seqs, hkv = desc->num_kv_heads, g = desc->num_q_heads / hkv;
@@ -123,7 +132,8 @@ sf_status plan(const sf_attn_desc* desc, const int32_t* lens, int32_t num_groups
     p.rows = (last - first + 1) * g;
     p.tiles = (p.rows + 15) / 16;
     p.blocks = (p.tiles + kSharedTiles - 1) / kSharedTiles;
-    if (p.blocks > 2) p.blocks = (p.blocks + 3) / 4 * 4;
+    if (p.tiles > 1) p.blocks = std::max(p.blocks, 2);
+    p.blocks = p.blocks > 4 ? (p.blocks + kSharedWaves - 1) / kSharedWaves * kSharedWaves : p.blocks > 2 ? 4 : p.blocks;
     p.unit = num_units;
     num_units += hkv;
     for (int32_t s = first; s <= last; ++s)
@@ -136,7 +146,7 @@ sf_status plan(const sf_attn_desc* desc, const int32_t* lens, int32_t num_groups
     }
     p.start = track->pages;
     track->pages += int64_t(pages) * hkv;
-    track->cost += int64_t(pages) * hkv * p.blocks * page_cost(p.blocks, (p.tiles + p.blocks - 1) / p.blocks);
+    track->cost += int64_t(pages) * hkv * page_cost(p.blocks, fp8);
     track->prompts.push_back(int32_t(t.prompts.size()));
     t.prompts.push_back(p);
   }
@@ -147,18 +157,30 @@ sf_status plan(const sf_attn_desc* desc, const int32_t* lens, int32_t num_groups
     t.start[s] = own_pages;
     own_pages += int64_t(pages_of(lens[s]) - (t.prompt_of[s] >= 0 ? t.prompts[t.prompt_of[s]].pages : 0)) * hkv;
   }
-  cost = own_pages * 1000;
+  cost = (own_pages + kSegmentPages * int64_t(n) * hkv) * 1000;
   for (const Track& x : t.tracks) cost += x.cost;
-  // waves: one per SIMD, fewer rather than thinner runs
-  const int64_t waves = std::max<int64_t>(1, std::min<int64_t>(4 * int64_t(cus), cost / 1000 / least));
-  int64_t workers = 0;
+  // waves: two per SIMD, fewer rather than thinner runs
+  const int64_t waves = std::max<int64_t>(1, std::min<int64_t>(int64_t(kSharedWaves) * cus, cost / 1000 / least));
+  // Prompts of several blocks take whole workgroups, the first ones; the other
+  // waves (prompts of one block, then the sequences' own pages) are spread over the rest.
+  int64_t groups = 0, alone = 0;
   for (Track& x : t.tracks) {
-    x.columns = std::max<int64_t>(1, std::min(x.pages, int64_t(double(waves) * double(x.cost) / double(cost)) / x.blocks));
-    workers += x.columns * x.blocks;
+    const double share = double(waves) * double(x.cost) / double(cost);
+    if (x.blocks == 1) {
+      x.columns = std::max<int64_t>(1, std::min<int64_t>(x.pages, int64_t(share)));
+      alone += x.columns;
+    } else {
+      const int32_t each = (x.blocks + kSharedWaves - 1) / kSharedWaves;
+      x.columns = std::max<int64_t>(1, std::min<int64_t>(x.pages, int64_t(share / kSharedWaves / each)));
+      groups += x.columns * each;
+    }
   }
-  const int64_t own_columns = own_pages == 0 ? 0 : std::max<int64_t>(1, std::min(own_pages, waves - workers));
-  const int64_t own_first = workers;
-  workers += own_columns;
+  const int64_t own_columns =
+      own_pages == 0 ? 0 : std::max<int64_t>(1, std::min(own_pages, waves - groups * kSharedWaves - alone));
+  alone += own_columns;
+  const bool whole = groups > 0 || alone > cus;
+  const int64_t alone_groups = std::max((alone + kSharedWaves - 1) / kSharedWaves, std::min(alone, std::max<int64_t>(0, cus - groups)));
+  const int64_t workers = whole ? (groups + alone_groups) * kSharedWaves : alone;
 
   // parts and partial rows
   int64_t rows = 0, items = 0, merges = 0;
@@ -170,9 +192,10 @@ sf_status plan(const sf_attn_desc* desc, const int32_t* lens, int32_t num_groups
       for (int32_t h = 0; h < hkv; ++h) {
         const int64_t begin = p.start + int64_t(h) * p.pages;
         const int32_t parts = runs.parts(begin, begin + p.pages);
-        t.units[size_t(p.unit + h)] = {int32_t(std::min<int64_t>(rows, INT32_MAX)), parts};
-        rows += int64_t(parts) * p.rows;
-        items += int64_t(parts) * p.blocks;
+        const int32_t splits = splits_of(x.blocks);
+        t.units[size_t(p.unit + h)] = {int32_t(std::min<int64_t>(rows, INT32_MAX)), parts * splits};
+        rows += int64_t(parts) * splits * p.rows;
+        items += int64_t(parts) * splits * p.blocks;
       }
     }
   }
@@ -198,7 +221,7 @@ sf_status plan(const sf_attn_desc* desc, const int32_t* lens, int32_t num_groups
   info->num_work = int32_t(items);
   info->num_merge = int32_t(merges);
   info->num_rows = int32_t(rows);
-  info->workers_per_group = workers > cus ? 4 : 1;
+  info->workers_per_group = whole ? kSharedWaves : 1;
   info->reserved = 0;
   info->work_bytes = uint64_t(workers + items) * kSharedInts * 4 + uint64_t(merges) * kSharedMergeInts * 4;
   info->workspace_bytes = rows ? align256(uint64_t(rows) * desc->head_dim * 4) + uint64_t(rows) * 4 : 0;
@@ -221,12 +244,19 @@ sf_status plan(const sf_attn_desc* desc, const int32_t* lens, int32_t num_groups
     row[1] = item - first;
     ++worker;
   };
+  // Waves alone go to every workgroup of theirs in turn, as many as fit one behind the other.
+  const int64_t per_group = whole && alone_groups ? (alone + alone_groups - 1) / alone_groups : 1;
+  int64_t lonely = 0;
+  auto next_alone = [&] {
+    if (whole && ++lonely == per_group) {
+      for (; worker % kSharedWaves; lonely = 0) close_worker(item);
+      lonely = 0;
+    }
+  };
   for (const Track& x : t.tracks) {
     const Runs runs = {x.pages, x.columns};
-    // Workgroups go round the eight XCDs: a column of several workgroups takes every eighth,
-    // so that its waves find each other's pages in one L2.
-    const int32_t groups = x.blocks / 4;
-    auto emit = [&](int64_t col, int32_t block) {
+    const int32_t together = x.blocks == 1 ? 0 : blocks_together(x.blocks), splits = splits_of(x.blocks);
+    auto emit = [&](int64_t col, int32_t block, int32_t split) {
       const int32_t first = item;
       int64_t page = runs.at(col);
       const int64_t end = runs.at(col + 1);
@@ -238,31 +268,34 @@ sf_status plan(const sf_attn_desc* desc, const int32_t* lens, int32_t num_groups
       }
       for (; page < end; ++lo) {
         const Prompt& p = t.prompts[x.prompts[lo]];
+        const int32_t row0 = int32_t(int64_t(p.tiles) * block / p.blocks) * 16;
+        const int32_t row1 = std::min(p.rows, int32_t(int64_t(p.tiles) * (block + 1) / p.blocks) * 16);
         while (page < end && page < p.start + int64_t(p.pages) * hkv) {
           const int32_t h = int32_t((page - p.start) / p.pages);
           const int64_t begin = p.start + int64_t(h) * p.pages;
           const int64_t stop = std::min(end, begin + p.pages);
-          const Unit& u = t.units[size_t(p.unit + h)];
-          const int32_t part = int32_t(col - runs.of(begin));
-          const int32_t row0 = int32_t(int64_t(p.tiles) * block / p.blocks) * 16;
-          const int32_t row1 = std::min(p.rows, int32_t(int64_t(p.tiles) * (block + 1) / p.blocks) * 16);
-          if (row1 > row0)
-            put_fields(list + int64_t(item++) * kSharedInts, p.first, p.source, h, int32_t(page - begin), int32_t(stop - begin),
-                       p.pages * kPage, u.base + part * p.rows + row0, row0, row1 - row0);
+          const int32_t part = int32_t(col - runs.of(begin)) * splits + split;
+          put_fields(list + int64_t(item++) * kSharedInts, p.first, p.source, h, int32_t(page - begin), int32_t(stop - begin),
+                     p.pages * kPage, t.units[size_t(p.unit + h)].base + part * p.rows + row0, row0, row1 - row0, together, split);
           page = stop;
         }
       }
       close_worker(first);
     };
-    if (groups <= 1) {
-      for (int64_t c = 0; c < x.columns; ++c)
-        for (int32_t b = 0; b < x.blocks; ++b) emit(c, b);
-    } else {
-      for (int64_t c0 = 0; c0 < x.columns; c0 += 8)
-        for (int32_t k = 0; k < groups; ++k)
-          for (int64_t c = c0; c < std::min(x.columns, c0 + 8); ++c)
-            for (int32_t b = 4 * k; b < 4 * k + 4; ++b) emit(c, b);
+    if (x.blocks == 1) {
+      for (int64_t c = 0; c < x.columns; ++c) {
+        emit(c, 0, 0);
+        next_alone();
+      }
+      continue;
     }
+    // Workgroups go round the eight XCDs: a run of several workgroups takes every eighth,
+    // so that they find each other's pages in one L2.
+    const int32_t each = (x.blocks + kSharedWaves - 1) / kSharedWaves;
+    for (int64_t c0 = 0; c0 < x.columns; c0 += 8)
+      for (int32_t k = 0; k < each; ++k)
+        for (int64_t c = c0; c < std::min(x.columns, c0 + 8); ++c)
+          for (int32_t w = 0; w < kSharedWaves; ++w) emit(c, k * kSharedWaves + w % together, w / together);
   }
   if (own_columns > 0) {
     int64_t page = 0, col = 0;
@@ -280,6 +313,7 @@ sf_status plan(const sf_attn_desc* desc, const int32_t* lens, int32_t num_groups
           page = stop;
           if (page == own_runs.at(col + 1)) {
             close_worker(first);
+            next_alone();
             first = item;
             ++col;
           }
@@ -287,7 +321,7 @@ sf_status plan(const sf_attn_desc* desc, const int32_t* lens, int32_t num_groups
       }
     }
   }
-  (void)own_first;
+  while (worker < workers) close_worker(item);
   for (int32_t s = 0; s < n; ++s) {
     const Prompt* p = t.prompt_of[s] >= 0 ? &t.prompts[t.prompt_of[s]] : nullptr;
     for (int32_t h = 0; h < hkv; ++h) {
@@ -306,11 +340,13 @@ sf_status plan(const sf_attn_desc* desc, const int32_t* lens, int32_t num_groups
 }  // namespace
 
 extern "C" sf_status sf_shared_attn_plan(const sf_attn_desc* desc, const int32_t* seq_lens_host, int32_t num_groups,
-                                         const int32_t* group_offsets_host, const int32_t* shared_lens_host,
+                                         const int32_t* group_offsets_host, const int32_t* shared_lens_host, int32_t fp8,
                                          const sf_plan_opts* opts, int32_t* work_host, uint64_t work_capacity_bytes,
                                          sf_shared_info* info) {
+  if ((fp8 | 1) != 1) return SF_ERR_INVALID_ARG;
   try {
-    return plan(desc, seq_lens_host, num_groups, group_offsets_host, shared_lens_host, opts, work_host, work_capacity_bytes, info);
+    return plan(desc, seq_lens_host, num_groups, group_offsets_host, shared_lens_host, fp8 != 0, opts, work_host,
+                work_capacity_bytes, info);
   } catch (const std::bad_alloc&) {
     return SF_ERR_HIP;
   }
@@ -324,7 +360,7 @@ sf_status sf::run_shared(const sf_attn_desc* desc, const sf_shared_info* info, c
   if (st != SF_OK) return st;
   if (!info || (out_bf16 | 1) != 1) return SF_ERR_INVALID_ARG;
   if (info->desc_key != (desc_key(desc) ^ kSharedKey) || info->num_workers < 0 || info->num_work < 0 || info->num_merge < 0 ||
-      info->num_rows < 0 || (info->workers_per_group != 1 && info->workers_per_group != 4) ||
+      info->num_rows < 0 || (info->workers_per_group != 1 && info->workers_per_group != kSharedWaves) ||
       info->work_bytes != (uint64_t(info->num_workers) + uint64_t(info->num_work)) * kSharedInts * 4 +
                               uint64_t(info->num_merge) * kSharedMergeInts * 4 ||
       info->workspace_bytes !=

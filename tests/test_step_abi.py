@@ -214,20 +214,28 @@ def test_shared_plan_covers_everything_once(seed):
     g = hq // hkv
     opts = B.make_opts(num_cus=int(rng.choice([1, 3, 256])), min_chunk_pages=int(rng.choice([0, 1, 50])))
     desc = _desc(lens, hq, hkv)
-    info, work = B.sf_shared_attn_plan(desc, lens, offsets, shared, opts)
+    info, work = B.sf_shared_attn_plan(desc, lens, offsets, shared, opts, fp8=bool(seed % 3))
     table, items, merges = _shared_rows(info, work)
     assert [r[0] for r in table] == np.cumsum([0] + [r[1] for r in table])[:-1].tolist() and sum(r[1] for r in table) == len(items)
     for r in table:
         if r[1]:
             assert r[2:] == items[r[0]][2:]
+    if info.workers_per_group == 8:     # a workgroup that walks a prompt together does the same in all waves
+        for i in range(0, len(table), 8):
+            walks = [[it[2:8] + [it[11]] for it in items[r[0]: r[0] + r[1]]] for r in table[i: i + 8]]
+            if any(it[-1] for w in walks for it in w):
+                assert all(w == walks[0] for w in walks) and all(it[-1] in (2, 4, 8) for it in walks[0])
+    else:
+        assert info.workers_per_group == 1 and not any(it[11] for it in items)
     source = {}
     for i in range(len(shared)):
         live = [s for s in range(offsets[i], offsets[i + 1]) if lens[s] > 0]
         if len(live) > 1 and shared[i] >= 16:
             source.update({s: (live[0], shared[i] // 16) for s in live})
     seen, parts, used = set(), {}, set()
-    for _, _, seq0, src, kvh, pb, pe, end, slot, row0, rows, *_ in items:
-        assert 0 <= pb < pe and 1 <= rows <= 64 and row0 % 16 == 0
+    for _, _, seq0, src, kvh, pb, pe, end, slot, row0, rows, together, split, *_ in items:
+        pages = [p for p in range(pb, pe) if not together or (p - pb) // 2 % (8 // together) == split]
+        assert 0 <= pb < pe and 1 <= rows <= 32 and row0 % 16 == 0
         for r in range(rows):
             s, h = seq0 + (row0 + r) // g, (row0 + r) % g
             if slot >= 0:
@@ -236,7 +244,7 @@ def test_shared_plan_covers_everything_once(seed):
                 parts.setdefault((s, kvh, h), []).append(slot + r)
             else:
                 assert src == s and (pb, pe) == (0, -(-lens[s] // 16))
-            for p in range(pb, pe):
+            for p in pages:
                 assert (s, kvh, h, p) not in seen
                 seen.add((s, kvh, h, p))
             if lens[s] == 0:
@@ -267,7 +275,8 @@ def test_shared_plan_uses_the_whole_gpu():
     for members, common, own in ((16, 2048, 2000), (64, 32760, 300), (256, 4000, 1000), (2, 100000, 1)):
         lens = [common + own] * members
         info, work = B.sf_shared_attn_plan(_desc(lens), lens, [0, members], [common])
-        assert 900 <= info.num_workers <= 1030, (members, info.num_workers)
+        busy = sum(r[1] > 0 for r in _shared_rows(info, work)[0])
+        assert 1800 <= busy <= 2048 and info.num_workers <= 2064, (members, busy, info.num_workers)
 
 
 @pytest.mark.parametrize("want,lens,offsets,shared", [
@@ -277,7 +286,7 @@ def test_shared_plan_uses_the_whole_gpu():
 def test_shared_plan_refusals(want, lens, offsets, shared):
     a = [np.array(x, np.int32) for x in (lens, offsets, shared)]
     desc, info = _desc([max(n, 0) for n in lens]), B.sf_shared_info()
-    st = B.lib().sf_shared_attn_plan(ctypes.byref(desc), a[0].ctypes.data, len(shared), a[1].ctypes.data, a[2].ctypes.data, None, None, 0,
+    st = B.lib().sf_shared_attn_plan(ctypes.byref(desc), a[0].ctypes.data, len(shared), a[1].ctypes.data, a[2].ctypes.data, 0, None, None, 0,
                                      ctypes.byref(info))
     assert st == want
 
@@ -287,12 +296,12 @@ def test_shared_plan_more_refusals():
     lens, off, sh = (np.array(x, np.int32) for x in ([40, 40], [0, 2], [32]))
     desc = _desc([40, 40])
 
-    def call(desc=desc, lens=lens.ctypes.data, n=1, off=off.ctypes.data, sh=sh.ctypes.data, opts=None, work=None, cap=0, info=info):
-        return L.sf_shared_attn_plan(None if desc is None else ctypes.byref(desc), lens, n, off, sh, None if opts is None else ctypes.byref(opts),
+    def call(desc=desc, lens=lens.ctypes.data, n=1, off=off.ctypes.data, sh=sh.ctypes.data, fp8=0, opts=None, work=None, cap=0, info=info):
+        return L.sf_shared_attn_plan(None if desc is None else ctypes.byref(desc), lens, n, off, sh, fp8, None if opts is None else ctypes.byref(opts),
                                      work, cap, None if info is None else ctypes.byref(info))
 
     assert call() == OK
-    for bad in (dict(desc=None), dict(lens=None), dict(n=-1), dict(n=0), dict(off=None), dict(sh=None), dict(info=None),
+    for bad in (dict(desc=None), dict(lens=None), dict(n=-1), dict(n=0), dict(off=None), dict(sh=None), dict(info=None), dict(fp8=2),
                 dict(opts=B.make_opts(num_cus=-1)), dict(opts=B.make_opts(min_chunk_pages=-1)), dict(desc=_desc([40, 40], stride=2)),
                 dict(desc=_desc([40, 40], pages=0))):
         assert call(**bad) == INVALID, bad
