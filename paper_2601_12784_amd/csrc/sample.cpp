@@ -38,7 +38,8 @@ extern "C" sf_status sf_sample_workspace(const sf_sample_desc* desc, uint64_t* b
   const sf_status st = check_sample(desc);
   if (st != SF_OK) return st;
   if (!bytes) return SF_ERR_INVALID_ARG;
-  *bytes = uint64_t(desc->num_rows) * uint64_t(sample_chunks(*desc)) * sizeof(SampleChunk);
+  *bytes = uint64_t(desc->num_rows) * uint64_t(sample_chunks(*desc)) *
+           (sizeof(SampleChunk) + uint64_t(sample_chunk(*desc) / kSampleGroup) * 4);
   return SF_OK;
 }
 
@@ -72,5 +73,6 @@ extern "C" sf_status sf_sample(const sf_sample_desc* desc, const void* logits, c
   a.chunk = sample_chunk(*desc);
   a.num_chunks = sample_chunks(*desc);
   a.chunks = static_cast<SampleChunk*>(workspace);
+  if (top_k || top_p || min_p) a.groups = reinterpret_cast<float*>(a.chunks + int64_t(a.num_rows) * a.num_chunks);
   return launch_sample(a, desc->dtype, static_cast<hipStream_t>(stream)) == hipSuccess ? SF_OK : SF_ERR_HIP;
 }

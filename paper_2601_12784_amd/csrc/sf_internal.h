@@ -252,6 +252,7 @@ hipError_t launch_rotary(const RotaryArgs& a, hipStream_t stream);
 // Sampling (sf_sample).
 constexpr int kSampleChunk = 8192;        // logits that a workgroup of the first launch reads
 constexpr int kSampleSmallChunk = 2048;
+constexpr int kSampleGroup = 64;          // logits whose largest one the first launch keeps
 struct SampleChunk {
   float top;       // the chunk's largest logit
   int32_t at;      // its first index
@@ -273,6 +274,7 @@ struct SampleArgs {
   int32_t chunk;
   int32_t num_chunks;         // per row
   SampleChunk* chunks;        // [num_rows][num_chunks]
+  float* groups;              // [num_rows][num_chunks][chunk / 64]; NULL: no cuts
 };
 int32_t sample_chunk(const sf_sample_desc& d);
 int32_t sample_chunks(const sf_sample_desc& d);
