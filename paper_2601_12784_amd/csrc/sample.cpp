@@ -34,12 +34,28 @@ int32_t sf::sample_chunks(const sf_sample_desc& d) {
   return (pieces + chunk - 1) / chunk;
 }
 
+namespace {
+
+// The workspace: chunks, rows, bins and lists, groups.
+struct Layout {
+  uint64_t rows, bins, lists, groups, bytes;
+  explicit Layout(const sf_sample_desc& d) {
+    const uint64_t n = uint64_t(d.num_rows), chunks = n * uint64_t(sample_chunks(d));
+    rows = align256(chunks * sizeof(SampleChunk));
+    bins = align256(rows + n * sizeof(SampleRow));
+    lists = bins + n * kSampleBins * 8;
+    groups = lists + n * kSampleList * 8;
+    bytes = groups + chunks * uint64_t(sample_chunk(d) / kSampleGroup) * 4;
+  }
+};
+
+}  // namespace
+
 extern "C" sf_status sf_sample_workspace(const sf_sample_desc* desc, uint64_t* bytes) {
   const sf_status st = check_sample(desc);
   if (st != SF_OK) return st;
   if (!bytes) return SF_ERR_INVALID_ARG;
-  *bytes = uint64_t(desc->num_rows) * uint64_t(sample_chunks(*desc)) *
-           (sizeof(SampleChunk) + uint64_t(sample_chunk(*desc) / kSampleGroup) * 4);
+  *bytes = Layout(*desc).bytes;
   return SF_OK;
 }
 
@@ -72,7 +88,14 @@ extern "C" sf_status sf_sample(const sf_sample_desc* desc, const void* logits, c
   a.kept = kept;
   a.chunk = sample_chunk(*desc);
   a.num_chunks = sample_chunks(*desc);
-  a.chunks = static_cast<SampleChunk*>(workspace);
-  if (top_k || top_p || min_p) a.groups = reinterpret_cast<float*>(a.chunks + int64_t(a.num_rows) * a.num_chunks);
+  char* ws = static_cast<char*>(workspace);
+  const Layout at(*desc);
+  a.chunks = reinterpret_cast<SampleChunk*>(ws);
+  if (top_k || top_p || min_p) {
+    a.rows = reinterpret_cast<SampleRow*>(ws + at.rows);
+    a.bins = reinterpret_cast<uint64_t*>(ws + at.bins);
+    a.lists = reinterpret_cast<uint64_t*>(ws + at.lists);
+    a.groups = reinterpret_cast<float*>(ws + at.groups);
+  }
   return launch_sample(a, desc->dtype, static_cast<hipStream_t>(stream)) == hipSuccess ? SF_OK : SF_ERR_HIP;
 }

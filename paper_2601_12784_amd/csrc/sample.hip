@@ -5,17 +5,19 @@
 // multiples of 2^-44 of the largest (fp64 arithmetic, whose fma runs at the rate of an unpacked fp32 one
 // here) and added as integers, by atomics too.
 //
-// Two launches. The first reads the logits once, a chunk per workgroup: the
-// chunk's largest logit, the sum of its weights relative to it and, where there are cuts, the
-// largest logit of every 64. The second, a workgroup per row, joins the chunks'
-// sums. Without cuts it then knows the chunk of the drawn index, and reads that again.
+// The first launch reads the logits once, a chunk per workgroup: the chunk's largest
+// logit, the sum of its weights relative to it and, where there are cuts, the largest
+// logit of every 64. The second, a workgroup per row, joins the chunks' sums. Without cuts it
+// then knows the chunk of the drawn index, and reads that again.
+//
 // With cuts, the kept entries are the first ones in the order of falling logits, and
 // the groups' largest logits bound where that order can end (Bound below): if
 // no more than 4096 entries lie above the bound, only their groups are read again, the
-// entries are sorted in LDS and every cut is a position there. Else the row is read
-// again: one pass for counts and sums by 2048 equal steps of the logit, one that
-// sorts the entries of the step in which the cut falls, one for the sums of what stays by runs of the row and
-// one over the run of the draw.
+// entries are sorted in LDS and every cut is a position there. A row left open by
+// that takes one of two ways. A top-p of everything is found by all of the row's chunks at once, in two
+// launches: sums by 2048 equal steps of the logit, then the entries of the step in which the share is
+// reached, which a third one sorts. The rest (a top-k of thousands) is read whole by the third's workgroup.
+// Rows that are done cost those launches a workgroup each that ends at once.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -30,13 +32,12 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kChunkThreads = 256;
 constexpr int kDrawThreads = 256;
-constexpr int kRowThreads = 512;    // two waves per SIMD: nothing may spill (below)
-constexpr int kRowWaves = kRowThreads / 64;
-constexpr int kBins = 2048;
+constexpr int kCutThreads = 512;   // two waves per SIMD
+constexpr int kRowThreads = 512;
+constexpr int kBins = kSampleBins;
 constexpr int kUnitBits = 44;
 constexpr double kUnit = 0x1p-44;
-constexpr int kList = 4096;        // entries that are sorted
-constexpr int kPos = kList / kRowThreads;   // neighbouring ones of a thread
+constexpr int kList = kSampleList;   // entries that are sorted
 constexpr int kGroup = kSampleGroup;
 constexpr float kNone = -__builtin_inff();
 
@@ -49,7 +50,7 @@ struct Elem {
 };
 
 // A NaN counts as no entry, and -0 as 0 (equal logits have equal keys).
-__device__ __forceinline__ float clean(float x) { return x == x ? x + 0.f : kNone; }
+__device__ __forceinline__ float clean(float x) { return fmaxf(x, kNone) + 0.f; }
 
 // (A bit cast of a vector's element itself takes the vector's first.)
 __device__ __forceinline__ float value32(uint32_t bits) { return __builtin_bit_cast(float, bits); }
@@ -108,40 +109,50 @@ struct Row {
   }
 };
 
-// 2^f, |f| <= 1/2: the Taylor series to f^11 (the next term is below 2^-47).
-__device__ __forceinline__ double exp2_part(double f) {
-  double p = 4.4455382718708114976e-10;
-  p = __builtin_fma(p, f, 7.0549116208011233299e-9);
-  p = __builtin_fma(p, f, 1.0178086009239699728e-7);
-  p = __builtin_fma(p, f, 1.3215486790144309488e-6);
-  p = __builtin_fma(p, f, 1.5252733804059840280e-5);
-  p = __builtin_fma(p, f, 0.00015403530393381610);
-  p = __builtin_fma(p, f, 0.00133335581464284434);
+// 2^(i / 32), i < 32, in LDS: 64 lanes read it without a conflict.
+struct Powers {
+  double at[32];
+};
+__constant__ const double kPowers[32] = {
+    0x1.0000000000000p+0, 0x1.059b0d3158574p+0, 0x1.0b5586cf9890fp+0, 0x1.11301d0125b51p+0,
+    0x1.172b83c7d517bp+0, 0x1.1d4873168b9aap+0, 0x1.2387a6e756238p+0, 0x1.29e9df51fdee1p+0,
+    0x1.306fe0a31b715p+0, 0x1.371a7373aa9cbp+0, 0x1.3dea64c123422p+0, 0x1.44e086061892dp+0,
+    0x1.4bfdad5362a27p+0, 0x1.5342b569d4f82p+0, 0x1.5ab07dd485429p+0, 0x1.6247eb03a5585p+0,
+    0x1.6a09e667f3bcdp+0, 0x1.71f75e8ec5f74p+0, 0x1.7a11473eb0187p+0, 0x1.82589994cce13p+0,
+    0x1.8ace5422aa0dbp+0, 0x1.93737b0cdc5e5p+0, 0x1.9c49182a3f090p+0, 0x1.a5503b23e255dp+0,
+    0x1.ae89f995ad3adp+0, 0x1.b7f76f2fb5e47p+0, 0x1.c199bdd85529cp+0, 0x1.cb720dcef9069p+0,
+    0x1.d5818dcfba487p+0, 0x1.dfc97337b9b5fp+0, 0x1.ea4afa2a490dap+0, 0x1.f50765b6e4540p+0,
+};
+__device__ __forceinline__ void make_powers(Powers& t) {
+  if (threadIdx.x < 32) t.at[threadIdx.x] = kPowers[threadIdx.x];
+}
+
+// 2^(y + shift), -1000 < y + shift: the nearest multiple of 1/32 comes off by adding
+// 1.5 2^47, its whole part goes back as an addition to the exponent, and what is left,
+// within 1/64, enters the Taylor series to f^5 (the next term is below 2^-48).
+__device__ __forceinline__ double exp2_of(const Powers& t, double y, int shift) {
+  const double m = y + 0x1.8p47;
+  const int n = int(uint32_t(__builtin_bit_cast(uint64_t, m)));
+  const double f = y - (m - 0x1.8p47);
+  double p = 0.00133335581464284434;
   p = __builtin_fma(p, f, 0.00961812910762847716);
   p = __builtin_fma(p, f, 0.05550410866482157995);
   p = __builtin_fma(p, f, 0.24022650695910071233);
   p = __builtin_fma(p, f, 0.69314718055994530942);
-  return __builtin_fma(p, f, 1.0);
-}
-
-// 2^(y + shift) for -1000 < y + shift: the nearest whole number comes off by adding
-// 1.5 2^52, and goes back as an addition to the exponent.
-__device__ __forceinline__ double exp2_of(double y, int shift) {
-  const double t = y + 0x1.8p52;
-  const int n = int(uint32_t(__builtin_bit_cast(uint64_t, t))) + shift;
-  const double p = exp2_part(y - (t - 0x1.8p52));
-  return __builtin_bit_cast(double, __builtin_bit_cast(uint64_t, p) + (uint64_t(uint32_t(n << 20)) << 32));
+  p = __builtin_fma(p, f, 1.0) * t.at[n & 31];
+  return __builtin_bit_cast(double, __builtin_bit_cast(uint64_t, p) + (uint64_t(uint32_t((n >> 5) + shift) << 20) << 32));
 }
 
 // Weights of logits relative to a largest one: exp((l - top) / T), 1 / (T ln 2) in rate.
 struct Scale {
+  const Powers& powers;
   float top;
   double rate;
+  __device__ __forceinline__ Scale(const Powers& t, float largest, double r) : powers(t), top(largest), rate(r) {}
   __device__ __forceinline__ double exponent(float l) const { return (double(l) - double(top)) * rate; }
   // In units of 2^-44, rounded, with the bits of 2^52 above them. (max takes its other operand for the NaN of -inf * 0.)
   __device__ __forceinline__ uint64_t raw_units(float l) const {
-    const double y = fmax(exponent(l), -62.0);
-    return __builtin_bit_cast(uint64_t, exp2_of(y, kUnitBits) + 0x1p52);   // the sum's last bit is one unit
+    return __builtin_bit_cast(uint64_t, exp2_of(powers, fmax(exponent(l), -62.0), kUnitBits) + 0x1p52);   // the sum's last bit is one unit
   }
   static constexpr uint64_t kRaw = 0x4330000000000000ull;
   __device__ __forceinline__ uint64_t units(float l) const {
@@ -150,8 +161,9 @@ struct Scale {
   }
   __device__ __forceinline__ double weight(float l) const {
     if (top == __builtin_inff()) return l == top ? 1.0 : 0.0;
+    if (l == kNone) return 0.0;
     const double y = exponent(l);
-    return y > -1000.0 ? exp2_of(y, 0) : 0.0;
+    return y > -1000.0 ? exp2_of(powers, y, 0) : 0.0;
   }
 };
 
@@ -235,6 +247,7 @@ __global__ __launch_bounds__(kChunkThreads) void sample_chunk_kernel(SampleArgs 
   __shared__ float tops[kWaves];
   __shared__ int ats[kWaves];
   __shared__ uint64_t sums[kWaves];
+  __shared__ Powers powers;
   const int row = int(blockIdx.x) / a.num_chunks, chunk = int(blockIdx.x) % a.num_chunks;
   const Row<kType> r(a, row);
   const int tid = int(threadIdx.x), lane = tid & 63, wave = tid >> 6;
@@ -242,6 +255,7 @@ __global__ __launch_bounds__(kChunkThreads) void sample_chunk_kernel(SampleArgs 
   float x[kPieces][kPer];
 #pragma unroll
   for (int j = 0; j < kPieces; ++j) r.load(p0 + j * kChunkThreads, x[j]);
+  make_powers(powers);
   float top = kNone;
 #pragma unroll
   for (int j = 0; j < kPieces; ++j) {
@@ -260,7 +274,7 @@ __global__ __launch_bounds__(kChunkThreads) void sample_chunk_kernel(SampleArgs 
 #pragma unroll
   for (int w = 0; w < kWaves; ++w) top = fmaxf(top, tops[w]);
   const float t = temperature_of(a, row);
-  const Scale s = {top, rate_of(t)};
+  const Scale s(powers, top, rate_of(t));
   uint64_t sum = 0;
   if (top == __builtin_inff()) {
 #pragma unroll
@@ -309,7 +323,7 @@ struct Whole {
   double before[kPerLane];     // of the chunks before it
   double part[kPerLane];       // its own
 };
-__device__ __forceinline__ Whole join_chunks(const SampleArgs& a, int row, double rate) {
+__device__ __forceinline__ Whole join_chunks(const SampleArgs& a, int row, double rate, const Powers& powers) {
   const SampleChunk* chunks = a.chunks + int64_t(row) * a.num_chunks;
   const int lane = int(threadIdx.x) & 63;
   SampleChunk c[kPerLane];
@@ -321,7 +335,7 @@ __device__ __forceinline__ Whole join_chunks(const SampleArgs& a, int row, doubl
     w.top = fmaxf(w.top, c[i].top);
   }
   w.top = wave_max(w.top);
-  const Scale s = {w.top, rate};
+  const Scale s(powers, w.top, rate);
   w.total = 0.0;
 #pragma unroll
   for (int i = 0; i < kPerLane; ++i) {
@@ -361,6 +375,7 @@ struct Drawn {
   float top, chunk_top;
   double total, want;
   uint64_t waves[kRowThreads / 64];
+  Powers powers;
 };
 template <int kType, int kThreads>
 __device__ __forceinline__ void draw_row(const SampleArgs& a, int row, Drawn& sh) {
@@ -370,8 +385,10 @@ __device__ __forceinline__ void draw_row(const SampleArgs& a, int row, Drawn& sh
   const float t = temperature_of(a, row);
   const double rate = rate_of(t);
   const SampleChunk* chunks = a.chunks + int64_t(row) * a.num_chunks;
+  make_powers(sh.powers);
+  __syncthreads();
   if (wave == 0) {
-    const Whole w = join_chunks(a, row, rate);
+    const Whole w = join_chunks(a, row, rate, sh.powers);
     int chunk = -1;
     if (w.top == kNone) {
       if (lane == 0) finish(a, row, w.top, 1.0, -1, 0.f, 0.0);
@@ -397,7 +414,7 @@ __device__ __forceinline__ void draw_row(const SampleArgs& a, int row, Drawn& sh
       for (int m = 1; m < 64; m *= 2) last = max(last, __shfl_xor(last, m));
       if (chunk == last) {
         const SampleChunk c = chunks[chunk];
-        const Scale s = {w.top, rate};
+        const Scale s(sh.powers, w.top, rate);
         sh.top = w.top;
         sh.chunk_top = c.top;
         sh.total = w.total;
@@ -410,7 +427,7 @@ __device__ __forceinline__ void draw_row(const SampleArgs& a, int row, Drawn& sh
   __syncthreads();
   const int chunk = sh.chunk;
   if (chunk < 0) return;
-  const Scale cs = {sh.chunk_top, rate};
+  const Scale cs(sh.powers, sh.chunk_top, rate);
   const double want = sh.want;
   // thread by thread in index order
   constexpr int kRun = kSampleChunk / kPer / kThreads;
@@ -451,8 +468,10 @@ __global__ __launch_bounds__(kDrawThreads) void sample_draw_kernel(SampleArgs a)
   draw_row<kType, kDrawThreads>(a, int(blockIdx.x), sh);
 }
 
-// What a workgroup that looks for a threshold shares.
+// What a workgroup that looks for a threshold shares. kThreads: its threads.
+template <int kThreads>
 struct Shared {
+  static constexpr int kWaves = kThreads / 64;
   union {
     Drawn drawn;
     struct {
@@ -461,8 +480,9 @@ struct Shared {
     };
   };
   uint64_t list[kList];          // entries: key, then the complement of the index (falling order is the ranks')
-  uint64_t wave_mass[kRowWaves];
-  uint32_t wave_count[kRowWaves];
+  uint64_t wave_mass[64];
+  uint32_t wave_count[64];
+  Powers powers;
   float top;
   double total;
   // found by one thread
@@ -484,8 +504,10 @@ __device__ __forceinline__ uint64_t entry_of(uint32_t key, int index) { return j
 __device__ __forceinline__ int index_of(uint64_t entry) { return int(~uint32_t(entry)); }
 __device__ __forceinline__ uint32_t key_of(uint64_t entry) { return uint32_t(entry >> 32); }
 
-// Sum and count of the threads before this one in the workgroup (exclusive).
-__device__ __forceinline__ void block_scan(Shared& sh, uint64_t mass, uint32_t count, uint64_t* mass_before, uint32_t* count_before) {
+// Sum and count of the threads before this one in the workgroup (exclusive); *all_*: of all of them.
+template <int kThreads>
+__device__ __forceinline__ void block_scan(Shared<kThreads>& sh, uint64_t mass, uint32_t count, uint64_t* mass_before,
+                                           uint32_t* count_before, uint64_t* all_mass, uint32_t* all_count) {
   const int lane = int(threadIdx.x) & 63, wave = int(threadIdx.x) >> 6;
   const uint64_t m = wave_scan(mass);
   const uint32_t c = wave_scan(count);
@@ -495,26 +517,32 @@ __device__ __forceinline__ void block_scan(Shared& sh, uint64_t mass, uint32_t c
     sh.wave_count[wave] = c;
   }
   __syncthreads();
-  uint64_t mb = m - mass;
-  uint32_t cb = c - count;
-  for (int w = 0; w < wave; ++w) {
-    mb += sh.wave_mass[w];
-    cb += sh.wave_count[w];
+  uint64_t mb = m - mass, ma = 0;
+  uint32_t cb = c - count, ca = 0;
+#pragma unroll
+  for (int w = 0; w < kThreads / 64; ++w) {
+    mb += w < wave ? sh.wave_mass[w] : 0;
+    cb += w < wave ? sh.wave_count[w] : 0;
+    ma += sh.wave_mass[w];
+    ca += sh.wave_count[w];
   }
   *mass_before = mb;
   *count_before = cb;
+  *all_mass = ma;
+  *all_count = ca;
 }
 
 // Sorts list[0 .. n) into falling order (n <= kList; behind it, up to the next power of two, zeros). All threads.
+template <int kThreads>
 __device__ __forceinline__ void sort_list(uint64_t* list, int n) {
   const int tid = int(threadIdx.x);
   int size = 64;
   while (size < n) size *= 2;
-  for (int i = n + tid; i < size; i += kRowThreads) list[i] = 0;
+  for (int i = n + tid; i < size; i += kThreads) list[i] = 0;
   __syncthreads();
   for (int k = 2; k <= size; k *= 2)
     for (int j = k / 2; j > 0; j /= 2) {
-      for (int p = tid; p < size / 2; p += kRowThreads) {
+      for (int p = tid; p < size / 2; p += kThreads) {
         const int lo = 2 * p - (p & (j - 1)), hi = lo + j;
         const uint64_t x = list[lo], y = list[hi];
         const bool falling = (lo & k) == 0;
@@ -527,53 +555,26 @@ __device__ __forceinline__ void sort_list(uint64_t* list, int n) {
     }
 }
 
-// Calls use(logit, index) for every entry of the row, from the thread that holds it: the waves take runs of the row.
-template <int kType>
-struct Runs {
-  int begin, end;
-  __device__ __forceinline__ explicit Runs(const Row<kType>& r) {
-    const int wave = int(threadIdx.x) >> 6, per = (r.pieces + kRowWaves - 1) / kRowWaves;
-    begin = wave * per;
-    end = min(r.pieces, begin + per);
-  }
-};
-template <int kType, class Use>
-__device__ __forceinline__ void for_each(const Row<kType>& r, Use use) {
-  constexpr int kPer = Elem<kType>::kPer, kDeep = 4;
-  const Runs<kType> run(r);
-  for (int p = run.begin + (int(threadIdx.x) & 63); p < run.end; p += 64 * kDeep) {
-    float x[kDeep][kPer];
-#pragma unroll
-    for (int d = 0; d < kDeep; ++d) {
-      if (p + 64 * d < run.end) r.load(p + 64 * d, x[d]);
-    }
-#pragma unroll
-    for (int d = 0; d < kDeep; ++d) {
-      if (p + 64 * d >= run.end) break;
-#pragma unroll
-      for (int i = 0; i < kPer; ++i) use(x[d][i], r.first(p + 64 * d) + i);
-    }
-  }
-}
-
-// Counts and sums by 2048 ranges of keys from lo on, each 2^shift wide.
-template <int kType>
-__device__ __forceinline__ void clear_bins(Shared& sh) {
-  for (int b = int(threadIdx.x); b < kBins; b += kRowThreads) {
+// Counts and sums by ranges of keys or steps of the logit, in falling order.
+template <int kThreads>
+__device__ __forceinline__ void clear_bins(Shared<kThreads>& sh) {
+  for (int b = int(threadIdx.x); b < kBins; b += kThreads) {
     sh.mass[b] = 0;
     sh.count[b] = 0;
   }
-  if (threadIdx.x == 0) sh.bin = -1;
   __syncthreads();
 }
-__device__ __forceinline__ void add_to_bin(Shared& sh, int b, uint64_t units) {
+template <int kThreads>
+__device__ __forceinline__ void add_to_bin(Shared<kThreads>& sh, int b, uint64_t units) {
   atomicAdd(&sh.count[b], 1u);
   atomicAdd(reinterpret_cast<unsigned long long*>(&sh.mass[b]), (unsigned long long)(units));
 }
-// The bin, bins in falling order of logits, that completes the first `most` entries (most > 0), or at which the
+// The bin that completes the first `most` entries (most > 0), or at which the
 // sum reaches `share` (most = 0); -1: none. above_*: of what lies before it.
-__device__ __forceinline__ int crossing_bin(Shared& sh, uint32_t most, double share, uint32_t* above_count, uint64_t* above) {
-  constexpr int kMine = kBins / kRowThreads;
+template <int kThreads>
+__device__ __forceinline__ int crossing_bin(Shared<kThreads>& sh, uint32_t most, double share, uint32_t* above_count, uint64_t* above) {
+  constexpr int kMine = kBins / kThreads;
+  if (threadIdx.x == 0) sh.bin = -1;
   __syncthreads();
   const int b0 = kMine * int(threadIdx.x);
   uint64_t m[kMine], mass = 0;
@@ -583,9 +584,9 @@ __device__ __forceinline__ int crossing_bin(Shared& sh, uint32_t most, double sh
     mass += m[i] = sh.mass[b0 + i];
     count += c[i] = sh.count[b0 + i];
   }
-  uint64_t mb;
-  uint32_t cb;
-  block_scan(sh, mass, count, &mb, &cb);
+  uint64_t mb, unused64;
+  uint32_t cb, unused;
+  block_scan(sh, mass, count, &mb, &cb, &unused64, &unused);
   mb += *above;
   cb += *above_count;
 #pragma unroll
@@ -606,130 +607,19 @@ __device__ __forceinline__ int crossing_bin(Shared& sh, uint32_t most, double sh
     *above_count = sh.above_count;
     *above = sh.above_mass;
   }
+  __syncthreads();
   return bin;
 }
 
-// The cut by repeated refinement of key ranges (three times for 32 bits): for steps
-// of the logit that hold more entries than the list.
-template <int kType>
-__device__ __forceinline__ Cut refine(Shared& sh, const Row<kType>& r, const Scale& s, uint32_t top_key, Cut within, uint32_t most, double share) {
-  uint32_t lo = max(within.key, 1u), hi = top_key, above_count = 0;
-  uint64_t above = 0;
-  for (;;) {
-    const uint32_t range = hi - lo;
-    const int bits = range ? 32 - __builtin_clz(range) : 0;
-    const int shift = max(0, bits - 11);
-    clear_bins<kType>(sh);
-    for_each(r, [&](float l, int) {
-      const uint32_t key = key_of(l);
-      if (key >= lo && key <= hi) add_to_bin(sh, int((hi - key) >> shift), s.units(l));
-    });
-    const int bin = crossing_bin(sh, most, share, &above_count, &above);
-    if (bin < 0) {
-      __syncthreads();
-      return within;
-    }
-    const uint64_t mass = sh.mass[bin];
-    const uint32_t count = sh.count[bin];
-    __syncthreads();
-    hi -= uint32_t(bin) << shift;
-    if (shift == 0) {
-      const uint64_t w = mass / count;
-      uint32_t ties = count;
-      if (most)
-        ties = most - above_count;
-      else if (w > 0)
-        ties = uint32_t(fmin(double(count), ceil((share - double(above)) / double(w))));
-      if (hi == within.key) ties = min(ties, within.ties);
-      return {hi, ties, above + ties * w};
-    }
-    lo = hi - lo >= (1u << shift) ? hi - ((1u << shift) - 1u) : lo;
-  }
-}
-
-// Steps of the logit from the row's largest down to the bound: rounding keeps the order.
-struct Steps {
-  float top, per;
-  __device__ __forceinline__ int of(float l) const { return int(fminf((top - l) * per, float(kBins - 1))); }
-};
-
-// The cut by equal steps of the logit; the bins hold the row's counts and sums.
-// The step in which it falls is sorted. *spoiled: the bins are gone.
-template <int kType>
-__device__ __forceinline__ Cut select(Shared& sh, const Row<kType>& r, const Scale& s, const Steps& steps, uint32_t top_key, float bound, Cut within,
-                      uint32_t most, double share, bool* spoiled) {
-  uint32_t above_count = 0;
-  uint64_t above = 0;
-  if (threadIdx.x == 0) {
-    sh.bin = -1;
-    sh.listed = 0;
-    sh.found = -1;
-  }
-  const int bin = crossing_bin(sh, most, share, &above_count, &above);
-  if (bin < 0) {
-    __syncthreads();
-    return within;
-  }
-  const uint32_t count = sh.count[bin];
-  __syncthreads();
-  if (count > kList) {
-    *spoiled = true;
-    return refine(sh, r, s, top_key, within, most, share);
-  }
-  for_each(r, [&](float l, int index) {
-    if (l >= bound && l != kNone && steps.of(l) == bin) sh.list[atomicAdd(&sh.listed, 1u)] = entry_of(key_of(l), index);
-  });
-  __syncthreads();
-  sort_list(sh.list, int(count));
-  // positions of the list
-  const int n = int(count), p0 = kPos * int(threadIdx.x);
-  uint64_t w[kPos], sum = 0;
-#pragma unroll
-  for (int i = 0; i < kPos; ++i) {
-    w[i] = p0 + i < n ? s.units(logit_of(key_of(sh.list[p0 + i]))) : 0;
-    sum += w[i];
-  }
-  uint64_t before;
-  uint32_t unused;
-  block_scan(sh, sum, 0, &before, &unused);
-  before += above;
-#pragma unroll
-  for (int i = 0; i < kPos; ++i) {
-    const int p = p0 + i;
-    const bool last = p < n && (most ? above_count + uint32_t(p) + 1 == most
-                                     : double(before) < share && (double(before + w[i]) >= share || p + 1 == n));
-    before += w[i];
-    if (last && (most || atomicMax(&sh.found, p) < p)) {
-      sh.found = p;
-      sh.above_mass = before;
-    }
-  }
-  __syncthreads();
-  // entries equal to the last one that stays
-  const int at = sh.found;
-  const uint32_t key = key_of(sh.list[at]);
-  uint32_t ties = 0;
-#pragma unroll
-  for (int i = 0; i < kPos; ++i) ties += p0 + i <= at && key_of(sh.list[p0 + i]) == key;
-  uint64_t unused64;
-  const uint64_t mass = sh.above_mass;
-  block_scan(sh, 0, ties, &unused64, &unused);
-  ties = 0;
-  for (int v = 0; v < kRowWaves; ++v) ties += sh.wave_count[v];
-  __syncthreads();
-  return {key, ties, mass};
-}
-
-// (With 1024 threads, and so 128 registers, values that outlive a divergent block were
-// stored to memory before its end, by the lanes still active alone.)
 // One row with cuts. Bound: no entry below it stays, and none below it enters the sums that say which do.
 //   top-k: the k-th largest of the groups' largest logits (k entries at least are no smaller);
 //   top-p of everything: entries with less than (1 - p) of the whole's mean weight sum to less than (1 - p) of the whole;
 //   min-p: its own limit, where no top-k has to sum what lies below.
 template <int kType>
-__global__ __launch_bounds__(kRowThreads) void sample_cut_kernel(SampleArgs a) {
+__global__ __launch_bounds__(kCutThreads) void sample_cut_kernel(SampleArgs a) {
   constexpr int kPer = Elem<kType>::kPer;
-  __shared__ Shared sh;
+  __shared__ Shared<kCutThreads> sh;
+  constexpr int kPos = kList / kCutThreads;   // neighbouring positions of a thread
   const int row = int(blockIdx.x), tid = int(threadIdx.x), lane = tid & 63, wave = tid >> 6;
   const float t = temperature_of(a, row);
   const int k = a.top_k ? a.top_k[row] : 0;
@@ -737,13 +627,17 @@ __global__ __launch_bounds__(kRowThreads) void sample_cut_kernel(SampleArgs a) {
   const double low = a.min_p && a.min_p[row] > 0.f ? fmin(double(a.min_p[row]), 1.0) : 0.0;
   const bool cut_k = k > 0 && k < a.vocab, cut_p = p < 1.f;
   if (greedy(t) || (!cut_k && !cut_p && low == 0.0)) {
-    draw_row<kType, kRowThreads>(a, row, sh.drawn);
+    if (tid == 0) a.rows[row].open = 0;
+    draw_row<kType, kCutThreads>(a, row, sh.drawn);
     return;
   }
   const Row<kType> r(a, row);
   const double rate = rate_of(t);
+  make_powers(sh.powers);
+  if (tid == 0) a.rows[row].open = 0;
+  __syncthreads();
   if (wave == 0) {
-    const Whole w = join_chunks(a, row, rate);
+    const Whole w = join_chunks(a, row, rate, sh.powers);
     if (lane == 0) {
       sh.top = w.top;
       sh.total = w.total;
@@ -757,7 +651,7 @@ __global__ __launch_bounds__(kRowThreads) void sample_cut_kernel(SampleArgs a) {
     if (tid == 0) finish(a, row, top, 1.0, -1, 0.f, 0.0);
     return;
   }
-  const Scale s = {top, rate};
+  const Scale s(sh.powers, top, rate);
   const uint32_t top_key = key_of(top);
   const float* groups = a.groups + size_t(row) * a.num_chunks * (a.chunk / kGroup);
   const int num_groups = (r.pieces * kPer + kGroup - 1) / kGroup;
@@ -778,13 +672,12 @@ __global__ __launch_bounds__(kRowThreads) void sample_cut_kernel(SampleArgs a) {
       const uint32_t range = hi - lo;
       const int bits = range ? 32 - __builtin_clz(range) : 0;
       const int shift = max(0, bits - 11);
-      clear_bins<kType>(sh);
-      for (int g = tid; g < num_groups; g += kRowThreads) {
+      clear_bins(sh);
+      for (int g = tid; g < num_groups; g += kCutThreads) {
         const uint32_t key = key_of(groups[g]);
         if (key >= lo && key <= hi) atomicAdd(&sh.count[(hi - key) >> shift], 1u);
       }
       const int bin = crossing_bin(sh, uint32_t(k), 0.0, &above_count, &above);
-      __syncthreads();
       if (bin < 0) break;
       hi -= uint32_t(bin) << shift;
       lo = hi - lo >= (1u << shift) ? hi - ((1u << shift) - 1u) : lo;
@@ -800,34 +693,44 @@ __global__ __launch_bounds__(kRowThreads) void sample_cut_kernel(SampleArgs a) {
 
   // the entries above it, if the list holds them
   uint32_t near = 0;
-  for (int g = tid; g < num_groups; g += kRowThreads) near += groups[g] >= bound;
-  uint64_t unused64;
-  uint32_t near_before;
-  block_scan(sh, 0, near, &unused64, &near_before);
-  uint32_t num_near = 0;
-  for (int w = 0; w < kRowWaves; ++w) num_near += sh.wave_count[w];
-  __syncthreads();
+  for (int g = tid; g < num_groups; g += kCutThreads) near += groups[g] >= bound;
+  uint64_t unused64, unused_sum;
+  uint32_t near_before, num_near;
+  block_scan(sh, 0, near, &unused64, &near_before, &unused_sum, &num_near);
   if (num_near <= kBins) {
     uint32_t* const ids = sh.count;
-    for (int g = tid; g < num_groups; g += kRowThreads)
+    for (int g = tid; g < num_groups; g += kCutThreads)
       if (groups[g] >= bound) ids[near_before++] = uint32_t(g);
     __syncthreads();
     constexpr int kPieces = kGroup / kPer;
-    for (uint32_t i = uint32_t(tid); i < num_near * kPieces; i += kRowThreads) {
-      const int piece = int(ids[i / kPieces]) * kPieces + int(i % kPieces);
-      float x[kPer];
-      r.load(piece, x);
+    constexpr int kDeep = kType == kF32 ? 8 : 4;   // loads in flight
+    for (uint32_t i0 = uint32_t(tid); i0 < num_near * kPieces; i0 += kCutThreads * kDeep) {
+      float x[kDeep][kPer];
+      int piece[kDeep];
 #pragma unroll
-      for (int j = 0; j < kPer; ++j)
-        if (x[j] >= bound && x[j] != kNone) {
-          const uint32_t at = atomicAdd(&sh.listed, 1u);
-          if (at < kList) sh.list[at] = entry_of(key_of(x[j]), r.first(piece) + j);
-        }
+      for (int d = 0; d < kDeep; ++d) {
+        const uint32_t i = i0 + uint32_t(d) * kCutThreads;
+        piece[d] = i < num_near * kPieces ? int(ids[i / kPieces]) * kPieces + int(i % kPieces) : r.pieces;
+        r.load(piece[d], x[d]);   // (nothing behind the last)
+      }
+#pragma unroll
+      for (int d = 0; d < kDeep; ++d) {
+        float most = x[d][0];
+#pragma unroll
+        for (int j = 1; j < kPer; ++j) most = fmaxf(most, x[d][j]);
+        if (!(most >= bound)) continue;
+#pragma unroll
+        for (int j = 0; j < kPer; ++j)
+          if (x[d][j] >= bound && x[d][j] != kNone) {
+            const uint32_t at = atomicAdd(&sh.listed, 1u);
+            if (at < kList) sh.list[at] = entry_of(key_of(x[d][j]), r.first(piece[d]) + j);
+          }
+      }
     }
     __syncthreads();
     const int n = int(sh.listed);
     if (n <= kList) {
-      sort_list(sh.list, n);
+      sort_list<kCutThreads>(sh.list, n);
       const int p0 = kPos * tid;
       uint64_t w[kPos], sum = 0;
       uint32_t heavy = 0;   // entries of at least the least weight, the first ones
@@ -841,15 +744,10 @@ __global__ __launch_bounds__(kRowThreads) void sample_cut_kernel(SampleArgs a) {
         }
         sum += w[i];
       }
-      uint64_t before;
-      uint32_t heavy_before;
-      block_scan(sh, sum, heavy, &before, &heavy_before);
-      int stays = 0;
-      uint64_t list_sum = 0;
-      for (int v = 0; v < kRowWaves; ++v) {
-        stays += int(sh.wave_count[v]);
-        list_sum += sh.wave_mass[v];
-      }
+      uint64_t before, list_sum;
+      uint32_t heavy_before, all_heavy;
+      block_scan(sh, sum, heavy, &before, &heavy_before, &list_sum, &all_heavy);
+      int stays = int(all_heavy);
       if (cut_k) stays = min(stays, k);
       if (tid == 0) {
         sh.above_mass = list_sum;
@@ -890,17 +788,16 @@ __global__ __launch_bounds__(kRowThreads) void sample_cut_kernel(SampleArgs a) {
       for (int i = 0; i < kPos; ++i)
         if (p0 + i < stays) sh.list[p0 + i] = join(key_of(entry[i]), ~uint32_t(index_of(entry[i])));   // falling: index rising
       __syncthreads();
-      sort_list(sh.list, stays);
+      sort_list<kCutThreads>(sh.list, stays);
       sum = 0;
 #pragma unroll
       for (int i = 0; i < kPos; ++i) {
         w[i] = p0 + i < stays ? s.units(logit_of(uint32_t(sh.list[p0 + i]))) : 0;
         sum += w[i];
       }
-      uint32_t unused;
-      block_scan(sh, sum, 0, &before, &unused);
-      uint64_t kept = 0;
-      for (int v = 0; v < kRowWaves; ++v) kept += sh.wave_mass[v];
+      uint64_t kept;
+      uint32_t unused, unused_count;
+      block_scan(sh, sum, 0, &before, &unused, &kept, &unused_count);
       const double target = uniform_of(a, row) * double(kept);
 #pragma unroll
       for (int i = 0; i < kPos; ++i) {
@@ -915,94 +812,220 @@ __global__ __launch_bounds__(kRowThreads) void sample_cut_kernel(SampleArgs a) {
     }
   }
 
-  // the whole row again
+  // left to the launches behind this one
+  const bool spread = cut_p && !cut_k;
+  if (tid == 0) a.rows[row] = SampleRow{total, 0, top, bound, spread ? 1 : 2, 0};
+  if (spread)
+    for (int b = tid; b < kBins; b += kCutThreads) a.bins[size_t(row) * kBins + b] = 0;
+}
+
+// The slow way, of a row with a top-k of more entries than the list holds, or with as many near
+// a cut: read whole by one workgroup, in 64 runs, once per cut and twice for the draw.
+constexpr int kRuns = 64;
+constexpr int kWaveRuns = kRuns / (kRowThreads / 64);
+template <int kType>
+__device__ __forceinline__ int run_begin(const Row<kType>& r, int run) {
+  const int per = (r.pieces + kRuns - 1) / kRuns;
+  return min(r.pieces, run * per);
+}
+// Calls use(logit, index) for every entry of a run, in the wave that takes it.
+template <int kType, class Use>
+__device__ __forceinline__ void for_run(const Row<kType>& r, int run, Use use) {
+  constexpr int kPer = Elem<kType>::kPer, kDeep = 4;   // loads in flight
+  const int end = run_begin(r, run + 1);
+  for (int p = run_begin(r, run) + (int(threadIdx.x) & 63); p < end; p += 64 * kDeep) {
+    float x[kDeep][kPer];
+#pragma unroll
+    for (int d = 0; d < kDeep; ++d) r.load(p + 64 * d < end ? p + 64 * d : r.pieces, x[d]);   // (nothing behind the last)
+#pragma unroll
+    for (int d = 0; d < kDeep; ++d)
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) use(x[d][i], r.first(p + 64 * d) + i);
+  }
+}
+template <int kType, class Use>
+__device__ __forceinline__ void for_each(const Row<kType>& r, Use use) {
+  const int wave = int(threadIdx.x) >> 6;
+#pragma nounroll
+  for (int i = 0; i < kWaveRuns; ++i) for_run(r, kWaveRuns * wave + i, use);
+}
+
+// Steps of the logit from the row's largest down to the bound: rounding keeps the order.
+struct Steps {
+  float top, per;
+  __device__ __forceinline__ int of(float l) const { return int(fminf((top - l) * per, float(kBins - 1))); }
+};
+
+template <int kType>
+__device__ __forceinline__ void whole_row(const SampleArgs& a, int row, const SampleRow& st, Shared<kRowThreads>& sh) {
+  constexpr int kPer = Elem<kType>::kPer;
+  constexpr int kPos = kList / kRowThreads;
+  const int tid = int(threadIdx.x), lane = tid & 63, wave = tid >> 6;
+  const float t = temperature_of(a, row);
+  const int k = a.top_k ? a.top_k[row] : 0;
+  const float p = a.top_p ? a.top_p[row] : 1.f;
+  const double low = a.min_p && a.min_p[row] > 0.f ? fmin(double(a.min_p[row]), 1.0) : 0.0;
+  const bool cut_k = k > 0 && k < a.vocab, cut_p = p < 1.f;
+  const Row<kType> r(a, row);
+  const double rate = rate_of(t);
+  make_powers(sh.powers);
+  __syncthreads();
+  const float top = st.top, bound = st.bound;   // (the chunks' sums may be those of what stays by now)
+  const Scale s(sh.powers, top, rate);
+  const float span = top - bound;
+  const Steps steps = {top, span > 0.f && span < __builtin_inff() ? float(kBins) / span : 0.f};
+
   Cut cut = {0, 0, 0};   // nothing is cut: every key is above 0
-  if (cut_k || cut_p) {
-    const float span = top - bound;
-    const Steps steps = {top, span > 0.f && span < __builtin_inff() ? float(kBins) / span : 0.f};
-    auto fill = [&] {
-      clear_bins<kType>(sh);
+  double whole = st.total;
+  // Top-k, then top-p of what it leaves. Ranges: equal steps of the logit first; the one in
+  // which the cut falls is sorted, or, of more entries than the list, refined by keys (three times for 32 bits).
+  for (int by_p = cut_k ? 0 : 1; by_p < (cut_p ? 2 : 1); ++by_p) {
+    const uint32_t most = by_p ? 0u : uint32_t(k);
+    // no share lies before the first, so it always stays; entries behind the k-th do not reach the share
+    const double share = by_p ? fmax(double(p) * whole, 1.0) : 0.0;
+    uint32_t above_count = 0, lo = max(cut.key, 1u), hi = key_of(top);
+    uint64_t above = 0;
+    int shift = -1;        // by steps
+    bool found = false;
+    Cut next = cut;
+#pragma nounroll
+    for (;;) {
+      clear_bins(sh);
       for_each(r, [&](float l, int) {
-        if (l >= bound && l != kNone) add_to_bin(sh, steps.of(l), s.units(l));
+        const uint32_t key = key_of(l);
+        if (l >= bound && key >= lo && key <= hi) add_to_bin(sh, shift < 0 ? steps.of(l) : int((hi - key) >> shift), s.units(l));
       });
-      __syncthreads();
-    };
-    double whole = total;
-    bool filled = false;
-    for (int by_p = cut_k ? 0 : 1; by_p < (cut_p ? 2 : 1); ++by_p) {   // top-k, then top-p of what it leaves
-      if (!filled) fill();
-      filled = true;
-      // no share lies before the first, so it always stays; entries behind the k-th do not reach the share
-      bool spoiled = false;
-      Cut next = select(sh, r, s, steps, top_key, bound, cut, by_p ? 0u : uint32_t(k), by_p ? fmax(double(p) * whole, 1.0) : 0.0, &spoiled);
-      filled = !spoiled;
-      if (next.key == cut.key) next.ties = min(next.ties, cut.ties);
-      if (next.key) {
-        cut = next;
-        whole = double(cut.mass);
+      const int bin = crossing_bin(sh, most, share, &above_count, &above);
+      if (bin < 0) break;
+      const uint32_t count = sh.count[bin];
+      const uint64_t mass = sh.mass[bin];
+      if (shift == 0) {    // one key
+        const uint64_t w = mass / count;
+        next.key = hi - uint32_t(bin);
+        next.ties = most ? most - above_count : w ? uint32_t(fmin(double(count), ceil((share - double(above)) / double(w)))) : count;
+        next.mass = above + next.ties * w;
+        found = true;
+        break;
       }
+      if (count <= kList) {
+        if (tid == 0) {
+          sh.listed = 0;
+          sh.found = -1;
+        }
+        __syncthreads();
+        for_each(r, [&](float l, int index) {
+          const uint32_t key = key_of(l);
+          if (l >= bound && key >= lo && key <= hi && (shift < 0 ? steps.of(l) : int((hi - key) >> shift)) == bin)
+            sh.list[atomicAdd(&sh.listed, 1u)] = entry_of(key, index);
+        });
+        __syncthreads();
+        sort_list<kRowThreads>(sh.list, int(count));
+        const int n = int(count), p0 = kPos * tid;
+        uint64_t sum = 0;
+#pragma unroll
+        for (int i = 0; i < kPos; ++i) sum += p0 + i < n ? s.units(logit_of(key_of(sh.list[p0 + i]))) : 0;
+        uint64_t before, unused64;
+        uint32_t unused, unused2;
+        block_scan(sh, sum, 0, &before, &unused, &unused64, &unused2);
+        before += above;
+#pragma unroll
+        for (int i = 0; i < kPos; ++i) {
+          const int q = p0 + i;
+          const uint64_t w = q < n ? s.units(logit_of(key_of(sh.list[q]))) : 0;
+          const bool last = q < n && (most ? above_count + uint32_t(q) + 1 == most
+                                           : double(before) < share && (double(before + w) >= share || q + 1 == n));
+          before += w;
+          if (last) {
+            sh.found = q;
+            sh.above_mass = before;
+          }
+        }
+        __syncthreads();
+        // entries equal to the last one that stays
+        const int at = sh.found;
+        next.key = key_of(sh.list[at]);
+        next.mass = sh.above_mass;
+        uint32_t ties = 0;
+#pragma unroll
+        for (int i = 0; i < kPos; ++i) ties += p0 + i <= at && key_of(sh.list[p0 + i]) == next.key;
+        block_scan(sh, 0, ties, &unused64, &unused, &before, &next.ties);
+        found = true;
+        break;
+      }
+      // by keys from here on, all of them the first time
+      if (shift < 0) {
+        above_count = 0;
+        above = 0;
+      } else {
+        hi -= uint32_t(bin) << shift;
+        lo = hi - lo >= (1u << shift) ? hi - ((1u << shift) - 1u) : lo;
+      }
+      shift = max(0, (hi > lo ? 32 - __builtin_clz(hi - lo) : 0) - 11);
+      __syncthreads();
+    }
+    __syncthreads();
+    if (found) {
+      if (next.key == cut.key) next.ties = min(next.ties, cut.ties);
+      cut = next;
+      whole = double(cut.mass);
     }
   }
-  // what stays, wave by wave
-  const Runs<kType> run(r);
-  uint64_t sum = 0, tie_units = 0;
-  uint32_t ties = 0;
-  for_each(r, [&](float l, int) {
-    const uint32_t key = key_of(l);
-    if (key < cut.key || key == 0 || (low > 0.0 && s.weight(l) < low)) return;
-    const uint64_t w = s.units(l);
-    if (key > cut.key) {
-      sum += w;
-    } else {
-      ++ties;
-      tie_units = w;
+
+  // what stays, run by run
+  uint64_t tie_units = 0;
+#pragma nounroll
+  for (int i = 0; i < kWaveRuns; ++i) {
+    uint64_t sum = 0;
+    uint32_t ties = 0;
+    for_run(r, kWaveRuns * wave + i, [&](float l, int) {
+      const uint32_t key = key_of(l);
+      if (l < bound || key < cut.key || key == 0 || (low > 0.0 && s.weight(l) < low)) return;
+      const uint64_t w = s.units(l);
+      if (key > cut.key) {
+        sum += w;
+      } else {
+        ++ties;
+        tie_units = w;
+      }
+    });
+    sum = wave_sum(sum);
+    ties = wave_sum(ties);
+    if (lane == 0) {
+      sh.wave_mass[kWaveRuns * wave + i] = sum;
+      sh.wave_count[kWaveRuns * wave + i] = ties;
     }
-  });
-  sum = wave_sum(sum);
-  const uint32_t wave_ties = wave_sum(ties);
+  }
 #pragma unroll
   for (int m = 1; m < 64; m *= 2) {
     const uint64_t y = shuffle_xor(tie_units, m);
     tie_units = tie_units > y ? tie_units : y;
   }
+  if (lane == 0) sh.mass[wave] = tie_units;
   __syncthreads();
-  if (lane == 0) {
-    sh.wave_mass[wave] = sum;
-    sh.wave_count[wave] = wave_ties;
-    sh.mass[wave] = tie_units;
-  }
-  __syncthreads();
-  for (int w = 0; w < kRowWaves; ++w) tie_units = tie_units > sh.mass[w] ? tie_units : sh.mass[w];
-  uint64_t kept = 0, before_me = 0, in_me = 0;
-  uint32_t seen = 0, ties_before = 0;
-  for (int w = 0; w < kRowWaves; ++w) {
-    const uint32_t left = cut.ties > seen ? cut.ties - seen : 0;
-    const uint64_t here = sh.wave_mass[w] + uint64_t(min(left, sh.wave_count[w])) * tie_units;
-    if (w == wave) {
-      before_me = kept;
-      ties_before = seen;
-      in_me = here;
-    }
-    kept += here;
-    seen += sh.wave_count[w];
-  }
+  for (int w = 0; w < kRowThreads / 64; ++w) tie_units = tie_units > sh.mass[w] ? tie_units : sh.mass[w];
+  // lane i of every wave: run i
+  const uint32_t seen = wave_scan(sh.wave_count[lane]) - sh.wave_count[lane];
+  const uint32_t left = cut.ties > seen ? cut.ties - seen : 0;
+  const uint64_t in_run = sh.wave_mass[lane] + uint64_t(min(left, sh.wave_count[lane])) * tie_units;
+  const uint64_t upto = wave_scan(in_run), kept = shuffle(upto, 63);
   const double target = uniform_of(a, row) * double(kept);
-  if (!(double(before_me) <= target && target < double(before_me + in_me))) return;
-  // this wave's run holds the draw
-  uint64_t cum = before_me;
-  uint32_t tie = ties_before;
-  for (int q0 = run.begin; q0 < run.end; q0 += 64) {
+  const uint64_t holds = __ballot(double(upto - in_run) <= target && target < double(upto));
+  const int run = __builtin_ctzll(holds);   // (some run does: target < kept)
+  if (wave != 0) return;
+  // the run that holds the draw
+  uint64_t cum = shuffle(upto - in_run, run);
+  uint32_t tie = uint32_t(__shfl(int(seen), run));
+  const int end = run_begin(r, run + 1);
+  for (int q0 = run_begin(r, run); q0 < end; q0 += 64) {
     float x[kPer];
-    uint64_t w[kPer];
+    uint64_t w[kPer], lane_sum = 0;
     uint32_t is_tie = 0, mine_ties = 0;
     const int q = q0 + lane;
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) x[i] = kNone;
-    if (q < run.end) r.load(q, x);
+    r.load(q < end ? q : r.pieces, x);
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
       const uint32_t key = key_of(x[i]);
-      const bool in = key >= cut.key && key != 0 && !(low > 0.0 && s.weight(x[i]) < low);
+      const bool in = x[i] >= bound && key >= cut.key && key != 0 && !(low > 0.0 && s.weight(x[i]) < low);
       w[i] = in ? s.units(x[i]) : 0;
       if (in && key == cut.key) {
         is_tie |= 1u << i;
@@ -1010,7 +1033,6 @@ __global__ __launch_bounds__(kRowThreads) void sample_cut_kernel(SampleArgs a) {
       }
     }
     uint32_t rank = tie + wave_scan(mine_ties) - mine_ties;
-    uint64_t lane_sum = 0;
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
       if (is_tie >> i & 1) {
@@ -1026,13 +1048,219 @@ __global__ __launch_bounds__(kRowThreads) void sample_cut_kernel(SampleArgs a) {
       for (int i = 0; i < kPer; ++i) {
         const bool was = double(at) > target;
         at += w[i];
-        if (!was && double(at) > target) finish(a, row, top, total, r.first(q) + i, x[i], double(kept));
+        if (!was && double(at) > target) finish(a, row, top, st.total, r.first(q) + i, x[i], double(kept));
       }
     }
     cum += shuffle(scan, 63);
     tie += wave_sum(mine_ties);
     if (double(cum) > target) return;
   }
+}
+
+// Top-p rows whose nucleus may be more than the list holds, by three launches over all of the row's chunks:
+// sums by equal steps of the logit; the step in which the share is reached, whose entries are
+// listed, with the sums of what lies above it by chunk; the order of the listed ones, which is the cut, and the draw.
+struct Crossing {
+  int bin;          // kBins: nowhere
+  uint64_t above;   // the sum before it
+};
+__device__ __forceinline__ double share_of(const SampleArgs& a, int row, double whole) {
+  return fmax(double(a.top_p[row]) * whole, 1.0);   // no share lies before the first, so it always stays
+}
+__device__ __forceinline__ double least_of(const SampleArgs& a, int row) {
+  return a.min_p && a.min_p[row] > 0.f ? fmin(double(a.min_p[row]), 1.0) : 0.0;
+}
+__device__ __forceinline__ Steps steps_of(const SampleRow& st) {
+  const float span = st.top - st.bound;
+  return {st.top, span > 0.f && span < __builtin_inff() ? float(kBins) / span : 0.f};
+}
+
+template <int kType, int kChunk>
+__global__ __launch_bounds__(kChunkThreads) void sample_bins_kernel(SampleArgs a) {
+  constexpr int kPer = Elem<kType>::kPer;
+  constexpr int kPieces = kChunk / kPer / kChunkThreads;
+  __shared__ uint64_t mass[kBins];
+  __shared__ Powers powers;
+  const int row = int(blockIdx.x) / a.num_chunks, chunk = int(blockIdx.x) % a.num_chunks, tid = int(threadIdx.x);
+  const SampleRow st = a.rows[row];
+  if (st.open != 1) return;
+  const Row<kType> r(a, row);
+  float x[kPieces][kPer];
+#pragma unroll
+  for (int j = 0; j < kPieces; ++j) r.load(chunk * (kChunk / kPer) + tid + j * kChunkThreads, x[j]);
+  make_powers(powers);
+  for (int b = tid; b < kBins; b += kChunkThreads) mass[b] = 0;
+  __syncthreads();
+  const Scale s(powers, st.top, rate_of(temperature_of(a, row)));
+  const Steps steps = steps_of(st);
+#pragma unroll
+  for (int j = 0; j < kPieces; ++j)
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const uint64_t w = s.units(x[j][i]);
+      if (x[j][i] >= st.bound && w) atomicAdd(reinterpret_cast<unsigned long long*>(&mass[steps.of(x[j][i])]), (unsigned long long)(w));
+    }
+  __syncthreads();
+  for (int b = tid; b < kBins; b += kChunkThreads)
+    if (mass[b]) atomicAdd(reinterpret_cast<unsigned long long*>(a.bins + size_t(row) * kBins + b), (unsigned long long)(mass[b]));
+}
+
+template <int kType, int kChunk>
+__global__ __launch_bounds__(kChunkThreads) void sample_collect_kernel(SampleArgs a) {
+  constexpr int kPer = Elem<kType>::kPer;
+  constexpr int kPieces = kChunk / kPer / kChunkThreads;
+  constexpr int kWaves = kChunkThreads / 64, kMine = kBins / kChunkThreads;
+  __shared__ uint64_t sums[kWaves];
+  __shared__ Crossing found;
+  __shared__ Powers powers;
+  const int row = int(blockIdx.x) / a.num_chunks, chunk = int(blockIdx.x) % a.num_chunks;
+  const int tid = int(threadIdx.x), lane = tid & 63, wave = tid >> 6;
+  const SampleRow st = a.rows[row];
+  if (st.open != 1) return;
+  const Row<kType> r(a, row);
+  float x[kPieces][kPer];
+#pragma unroll
+  for (int j = 0; j < kPieces; ++j) r.load(chunk * (kChunk / kPer) + tid + j * kChunkThreads, x[j]);
+  // the crossing, by every chunk for itself
+  const uint64_t* bins = a.bins + size_t(row) * kBins + kMine * tid;
+  uint64_t m[kMine], mine = 0;
+#pragma unroll
+  for (int i = 0; i < kMine; ++i) mine += m[i] = bins[i];
+  const uint64_t scan = wave_scan(mine);
+  if (lane == 63) sums[wave] = scan;
+  if (tid == 0) found.bin = kBins;
+  make_powers(powers);
+  __syncthreads();
+  uint64_t before = scan - mine;
+  for (int w = 0; w < wave; ++w) before += sums[w];
+  const double share = share_of(a, row, st.total);
+#pragma unroll
+  for (int i = 0; i < kMine; ++i) {
+    if (double(before) < share && double(before + m[i]) >= share) {
+      found.bin = kMine * tid + i;
+      found.above = before;
+      if (chunk == 0) a.rows[row].above = before;
+    }
+    before += m[i];
+  }
+  __syncthreads();
+  const int bin = found.bin;
+  const Scale s(powers, st.top, rate_of(temperature_of(a, row)));
+  const Steps steps = steps_of(st);
+  const double low = least_of(a, row);
+  uint64_t sum = 0;
+#pragma unroll
+  for (int j = 0; j < kPieces; ++j)
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const float l = x[j][i];
+      const uint64_t w = s.units(l);
+      const bool in = l >= st.bound && w;
+      const int b = steps.of(l);
+      if (in && b < bin && (low == 0.0 || s.weight(l) >= low)) sum += w;
+      if (in && b == bin) {
+        const uint32_t at = atomicAdd(&a.rows[row].listed, 1u);
+        if (at < kList) a.lists[size_t(row) * kList + at] = entry_of(key_of(l), r.first(chunk * (kChunk / kPer) + tid + j * kChunkThreads) + i);
+      }
+    }
+  sum = wave_sum(sum);
+  __syncthreads();
+  if (lane == 0) sums[wave] = sum;
+  __syncthreads();
+  if (tid == 0) {
+    for (int w = 1; w < kWaves; ++w) sum += sums[w];
+    a.chunks[blockIdx.x].sum = sum;   // what stays of the chunk for certain
+  }
+}
+
+template <int kType>
+__global__ __launch_bounds__(kRowThreads) void sample_finish_kernel(SampleArgs a) {
+  constexpr int kPer = Elem<kType>::kPer;
+  constexpr int kPos = kList / kRowThreads;
+  __shared__ Shared<kRowThreads> sh;
+  const int row = int(blockIdx.x), tid = int(threadIdx.x);
+  const SampleRow st = a.rows[row];
+  if (st.open == 0) return;
+  if (st.open == 2 || st.listed > kList) {
+    whole_row<kType>(a, row, st, sh);
+    return;
+  }
+  const Row<kType> r(a, row);
+  const float top = st.top;
+  make_powers(sh.powers);
+  const int n = int(st.listed), p0 = kPos * tid;
+  for (int i = tid; i < n; i += kRowThreads) sh.list[i] = a.lists[size_t(row) * kList + i];
+  // sums of what stays by chunk, joined below by the listed entries'
+  uint64_t* const by_chunk = sh.mass;
+  for (int c = tid; c < kMaxChunks; c += kRowThreads) by_chunk[c] = c < a.num_chunks ? a.chunks[size_t(row) * a.num_chunks + c].sum : 0;
+  __syncthreads();
+  sort_list<kRowThreads>(sh.list, n);
+  const Scale s(sh.powers, top, rate_of(temperature_of(a, row)));
+  const double low = least_of(a, row), share = share_of(a, row, st.total);
+  uint64_t w[kPos], sum = 0;
+#pragma unroll
+  for (int i = 0; i < kPos; ++i) {
+    w[i] = p0 + i < n ? s.units(logit_of(key_of(sh.list[p0 + i]))) : 0;
+    sum += w[i];
+  }
+  uint64_t before, all;
+  uint32_t unused, unused2;
+  if (tid == 0) sh.found = -1;
+  block_scan(sh, sum, 0, &before, &unused, &all, &unused2);
+  before += st.above;
+#pragma unroll
+  for (int i = 0; i < kPos; ++i) {
+    if (p0 + i < n && double(before) < share) {
+      atomicMax(&sh.found, p0 + i);
+      const float l = logit_of(key_of(sh.list[p0 + i]));
+      if (low == 0.0 || s.weight(l) >= low)
+        atomicAdd(reinterpret_cast<unsigned long long*>(&by_chunk[(index_of(sh.list[p0 + i]) + r.lead) / a.chunk]), (unsigned long long)(w[i]));
+    }
+    before += w[i];
+  }
+  __syncthreads();
+  const uint64_t last = n > 0 ? sh.list[sh.found] : 0;   // entries from it on stay
+  // the chunk that holds the draw
+  const uint64_t mine = tid < kMaxChunks ? by_chunk[tid] : 0;
+  uint64_t kept;
+  block_scan(sh, mine, 0, &before, &unused, &kept, &unused2);
+  const double target = uniform_of(a, row) * double(kept);
+  if (double(before) <= target && target < double(before + mine)) {
+    sh.bin = tid;
+    sh.above_mass = before;
+  }
+  __syncthreads();
+  const int chunk = sh.bin;
+  const uint64_t base = sh.above_mass;
+  const int pieces = a.chunk / kPer, run = (pieces + kRowThreads - 1) / kRowThreads;
+  constexpr int kRun = kSampleChunk / kPer / kRowThreads;
+  float x[kRun][kPer];
+  uint64_t units[kRun][kPer];
+  sum = 0;
+#pragma unroll
+  for (int j = 0; j < kRun; ++j) {
+    const int q = tid * run + j;
+    const int piece = j < run && q < pieces ? chunk * pieces + q : r.pieces;   // (nothing behind the last)
+    r.load(piece, x[j]);
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const float l = x[j][i];
+      const bool in = l >= st.bound && l != kNone && entry_of(key_of(l), r.first(piece) + i) >= last && (low == 0.0 || s.weight(l) >= low);
+      units[j][i] = in ? s.units(l) : 0;
+      sum += units[j][i];
+    }
+  }
+  block_scan(sh, sum, 0, &before, &unused, &all, &unused2);
+  before += base;
+  if (!(double(before) <= target && target < double(before + sum))) return;
+#pragma unroll
+  for (int j = 0; j < kRun; ++j)
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const bool was = double(before) > target;
+      before += units[j][i];
+      if (!was && double(before) > target) finish(a, row, top, st.total, r.first(chunk * pieces + tid * run + j) + i, x[j][i], double(kept));
+    }
 }
 
 template <int kType, int kChunk>
@@ -1044,6 +1272,17 @@ void launch_chunks(const SampleArgs& a, hipStream_t stream) {
     hipLaunchKernelGGL((sample_chunk_kernel<kType, kChunk, false>), grid, dim3(kChunkThreads), 0, stream, a);
 }
 
+// The rows that the sorted list did not do.
+template <int kType, int kChunk>
+void launch_open(const SampleArgs& a, hipStream_t stream) {
+  const dim3 grid{uint32_t(a.num_rows) * uint32_t(a.num_chunks), 1, 1};
+  if (a.top_p) {
+    hipLaunchKernelGGL((sample_bins_kernel<kType, kChunk>), grid, dim3(kChunkThreads), 0, stream, a);
+    hipLaunchKernelGGL((sample_collect_kernel<kType, kChunk>), grid, dim3(kChunkThreads), 0, stream, a);
+  }
+  hipLaunchKernelGGL(sample_finish_kernel<kType>, dim3(uint32_t(a.num_rows)), dim3(kRowThreads), 0, stream, a);
+}
+
 template <int kType>
 hipError_t launch(const SampleArgs& a, hipStream_t stream) {
   if (a.chunk == kSampleChunk)
@@ -1051,9 +1290,15 @@ hipError_t launch(const SampleArgs& a, hipStream_t stream) {
   else
     launch_chunks<kType, kSampleSmallChunk>(a, stream);
   if (a.groups)
-    hipLaunchKernelGGL(sample_cut_kernel<kType>, dim3(uint32_t(a.num_rows)), dim3(kRowThreads), 0, stream, a);
+    hipLaunchKernelGGL(sample_cut_kernel<kType>, dim3(uint32_t(a.num_rows)), dim3(kCutThreads), 0, stream, a);
   else
     hipLaunchKernelGGL(sample_draw_kernel<kType>, dim3(uint32_t(a.num_rows)), dim3(kDrawThreads), 0, stream, a);
+  if (a.groups) {
+    if (a.chunk == kSampleChunk)
+      launch_open<kType, kSampleChunk>(a, stream);
+    else
+      launch_open<kType, kSampleSmallChunk>(a, stream);
+  }
   return hipGetLastError();
 }
 

@@ -252,11 +252,22 @@ hipError_t launch_rotary(const RotaryArgs& a, hipStream_t stream);
 // Sampling (sf_sample).
 constexpr int kSampleChunk = 8192;        // logits that a workgroup of the first launch reads
 constexpr int kSampleSmallChunk = 2048;
+constexpr int kSampleBins = 2048;
+constexpr int kSampleList = 4096;
 constexpr int kSampleGroup = 64;          // logits whose largest one the first launch keeps
 struct SampleChunk {
   float top;       // the chunk's largest logit
   int32_t at;      // its first index
   uint64_t sum;    // sum of the weights relative to it, in units of 2^-44
+};
+// A row with cuts between the launches.
+struct SampleRow {
+  double total;      // sum of all weights, in units of 2^-44
+  uint64_t above;    // sum of those before the step in which the share is reached
+  float top;         // the row's largest logit
+  float bound;       // no entry below it stays
+  int32_t open;      // 0: done; 1: a top-p to be found over the whole row; 2: any cuts, by one workgroup
+  uint32_t listed;   // entries of that step
 };
 struct SampleArgs {
   const void* logits;
@@ -275,6 +286,10 @@ struct SampleArgs {
   int32_t num_chunks;         // per row
   SampleChunk* chunks;        // [num_rows][num_chunks]
   float* groups;              // [num_rows][num_chunks][chunk / 64]; NULL: no cuts
+  // with cuts, for rows that one workgroup's list does not do:
+  SampleRow* rows;            // [num_rows]
+  uint64_t* bins;             // [num_rows][2048]
+  uint64_t* lists;            // [num_rows][4096]
 };
 int32_t sample_chunk(const sf_sample_desc& d);
 int32_t sample_chunks(const sf_sample_desc& d);
