@@ -35,6 +35,8 @@ constexpr int kDrawThreads = 256;
 constexpr int kCutThreads = 512;   // two waves per SIMD
 constexpr int kRowThreads = 512;
 constexpr int kBins = kSampleBins;
+constexpr int kBinBits = 11;
+static_assert(kBins == 1 << kBinBits, "bins");
 constexpr int kUnitBits = 44;
 constexpr double kUnit = 0x1p-44;
 constexpr int kList = kSampleList;   // entries that are sorted
@@ -480,6 +482,7 @@ struct Shared {
     };
   };
   uint64_t list[kList];          // entries: key, then the complement of the index (falling order is the ranks')
+  uint64_t spare[kList];
   uint64_t wave_mass[64];
   uint32_t wave_count[64];
   Powers powers;
@@ -532,27 +535,103 @@ __device__ __forceinline__ void block_scan(Shared<kThreads>& sh, uint64_t mass, 
   *all_count = ca;
 }
 
-// Sorts list[0 .. n) into falling order (n <= kList; behind it, up to the next power of two, zeros). All threads.
-template <int kThreads>
-__device__ __forceinline__ void sort_list(uint64_t* list, int n) {
+// Sorts list[0 .. n) into falling order (n <= kList, no two alike). All threads. bin_of(entry), below kBins, does not
+// fall from an entry to a smaller one: a count by bins places each entry to within its bin, whose others say the rest
+// (4096 entries: 6 us, where the network below takes 50). Few entries are their own bin, and a bin of
+// more than kCrowd, say of equal logits, leaves all to a sorting network.
+constexpr int kCrowd = 256;
+template <int kThreads, class BinOf>
+__device__ __forceinline__ void sort_list(Shared<kThreads>& sh, int n, BinOf bin_of) {
+  constexpr int kMine = kBins / kThreads, kPos = kList / kThreads;
   const int tid = int(threadIdx.x);
+  __syncthreads();
+  if (n <= kCrowd) {
+    const uint64_t e = sh.list[tid < n ? tid : 0];
+    int rank = 0;
+    if ((tid & ~63) < n)
+      for (int i = 0; i < n; ++i) rank += sh.list[i] > e;
+    __syncthreads();
+    if (tid < n) sh.list[rank] = e;
+    __syncthreads();
+    return;
+  }
+  for (int b = tid; b < kBins; b += kThreads) sh.count[b] = 0;
+  if (tid == 0) sh.bin = 0;
+  __syncthreads();
+  uint32_t slot[kPos];
+#pragma unroll
+  for (int j = 0; j < kPos; ++j)
+    if (tid + j * kThreads < n) slot[j] = atomicAdd(&sh.count[bin_of(sh.list[tid + j * kThreads])], 1u);
+  __syncthreads();
+  uint32_t c[kMine], mine = 0, most = 0;
+#pragma unroll
+  for (int i = 0; i < kMine; ++i) {
+    mine += c[i] = sh.count[kMine * tid + i];
+    most = max(most, c[i]);
+  }
+  uint32_t before, all;
+  uint64_t unused, unused2;
+  if (most > kCrowd) sh.bin = 1;
+  block_scan(sh, 0, mine, &unused, &before, &unused2, &all);
+  if (sh.bin == 0) {
+#pragma unroll
+    for (int i = 0; i < kMine; ++i) {
+      sh.count[kMine * tid + i] = before;   // the bin's first place
+      before += c[i];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < kPos; ++j)
+      if (tid + j * kThreads < n) {
+        const uint64_t e = sh.list[tid + j * kThreads];
+        sh.spare[sh.count[bin_of(e)] + slot[j]] = e;
+      }
+    __syncthreads();
+    for (int i = tid; i < n; i += kThreads) {
+      const uint64_t e = sh.spare[i];
+      const int b = bin_of(e), first = int(sh.count[b]), end = b + 1 < kBins ? int(sh.count[b + 1]) : n;
+      int rank = first;
+      for (int q = first; q < end; ++q) rank += sh.spare[q] > e;
+      sh.list[rank] = e;
+    }
+    __syncthreads();
+    return;
+  }
   int size = 64;
   while (size < n) size *= 2;
-  for (int i = n + tid; i < size; i += kThreads) list[i] = 0;
+  for (int i = n + tid; i < size; i += kThreads) sh.list[i] = 0;
   __syncthreads();
   for (int k = 2; k <= size; k *= 2)
     for (int j = k / 2; j > 0; j /= 2) {
       for (int p = tid; p < size / 2; p += kThreads) {
         const int lo = 2 * p - (p & (j - 1)), hi = lo + j;
-        const uint64_t x = list[lo], y = list[hi];
+        const uint64_t x = sh.list[lo], y = sh.list[hi];
         const bool falling = (lo & k) == 0;
         if (falling ? x < y : x > y) {
-          list[lo] = y;
-          list[hi] = x;
+          sh.list[lo] = y;
+          sh.list[hi] = x;
         }
       }
       __syncthreads();
     }
+}
+
+// Steps of the logit from the row's largest down to the bound: rounding keeps the order.
+struct Steps {
+  float top, per;
+  __device__ __forceinline__ Steps(float largest, float bound)
+      : top(largest), per(largest - bound > 0.f && largest - bound < __builtin_inff() ? float(kBins) / (largest - bound) : 0.f) {}
+  __device__ __forceinline__ int of(float l) const { return int(fminf((top - l) * per, float(kBins - 1))); }
+};
+
+// Entries that lie in one step, mostly: by 2048 steps of that.
+template <int kThreads>
+__device__ __forceinline__ void sort_step(Shared<kThreads>& sh, int n, const Steps& steps) {
+  const float first = n > 0 ? float(steps.of(logit_of(key_of(sh.list[0])))) : 0.f;
+  sort_list(sh, n, [&](uint64_t e) {
+    const float part = (steps.top - logit_of(key_of(e))) * steps.per - first;
+    return int(fminf(fmaxf(part * float(kBins), 0.f), float(kBins - 1)));
+  });
 }
 
 // Counts and sums by ranges of keys or steps of the logit, in falling order.
@@ -704,7 +783,8 @@ __global__ __launch_bounds__(kCutThreads) void sample_cut_kernel(SampleArgs a) {
     __syncthreads();
     constexpr int kPieces = kGroup / kPer;
     constexpr int kDeep = kType == kF32 ? 8 : 4;   // loads in flight
-    for (uint32_t i0 = uint32_t(tid); i0 < num_near * kPieces; i0 += kCutThreads * kDeep) {
+    for (uint32_t w0 = 0; w0 < num_near * kPieces; w0 += kCutThreads * kDeep) {
+      const uint32_t i0 = w0 + uint32_t(tid);
       float x[kDeep][kPer];
       int piece[kDeep];
 #pragma unroll
@@ -713,24 +793,30 @@ __global__ __launch_bounds__(kCutThreads) void sample_cut_kernel(SampleArgs a) {
         piece[d] = i < num_near * kPieces ? int(ids[i / kPieces]) * kPieces + int(i % kPieces) : r.pieces;
         r.load(piece[d], x[d]);   // (nothing behind the last)
       }
+      uint32_t mine = 0;
 #pragma unroll
-      for (int d = 0; d < kDeep; ++d) {
-        float most = x[d][0];
+      for (int d = 0; d < kDeep; ++d)
 #pragma unroll
-        for (int j = 1; j < kPer; ++j) most = fmaxf(most, x[d][j]);
-        if (!(most >= bound)) continue;
+        for (int j = 0; j < kPer; ++j) mine += x[d][j] >= bound;
+      const uint32_t upto = wave_scan(mine);
+      uint32_t at = 0;
+      if (lane == 63) at = atomicAdd(&sh.listed, upto);
+      at = uint32_t(__shfl(int(at), 63)) + upto - mine;
+      if (mine == 0) continue;
+#pragma unroll
+      for (int d = 0; d < kDeep; ++d)
 #pragma unroll
         for (int j = 0; j < kPer; ++j)
-          if (x[d][j] >= bound && x[d][j] != kNone) {
-            const uint32_t at = atomicAdd(&sh.listed, 1u);
+          if (x[d][j] >= bound) {
             if (at < kList) sh.list[at] = entry_of(key_of(x[d][j]), r.first(piece[d]) + j);
+            ++at;
           }
-      }
     }
     __syncthreads();
     const int n = int(sh.listed);
     if (n <= kList) {
-      sort_list<kCutThreads>(sh.list, n);
+      const Steps steps(top, bound);
+      sort_list(sh, n, [&](uint64_t e) { return steps.of(logit_of(key_of(e))); });
       const int p0 = kPos * tid;
       uint64_t w[kPos], sum = 0;
       uint32_t heavy = 0;   // entries of at least the least weight, the first ones
@@ -788,7 +874,8 @@ __global__ __launch_bounds__(kCutThreads) void sample_cut_kernel(SampleArgs a) {
       for (int i = 0; i < kPos; ++i)
         if (p0 + i < stays) sh.list[p0 + i] = join(key_of(entry[i]), ~uint32_t(index_of(entry[i])));   // falling: index rising
       __syncthreads();
-      sort_list<kCutThreads>(sh.list, stays);
+      const int shift = max(0, 32 - __builtin_clz(uint32_t(a.vocab)) - kBinBits);
+      sort_list(sh, stays, [&](uint64_t e) { return int(~uint32_t(e >> 32) >> shift); });
       sum = 0;
 #pragma unroll
       for (int i = 0; i < kPos; ++i) {
@@ -850,12 +937,6 @@ __device__ __forceinline__ void for_each(const Row<kType>& r, Use use) {
   for (int i = 0; i < kWaveRuns; ++i) for_run(r, kWaveRuns * wave + i, use);
 }
 
-// Steps of the logit from the row's largest down to the bound: rounding keeps the order.
-struct Steps {
-  float top, per;
-  __device__ __forceinline__ int of(float l) const { return int(fminf((top - l) * per, float(kBins - 1))); }
-};
-
 template <int kType>
 __device__ __forceinline__ void whole_row(const SampleArgs& a, int row, const SampleRow& st, Shared<kRowThreads>& sh) {
   constexpr int kPer = Elem<kType>::kPer;
@@ -872,8 +953,7 @@ __device__ __forceinline__ void whole_row(const SampleArgs& a, int row, const Sa
   __syncthreads();
   const float top = st.top, bound = st.bound;   // (the chunks' sums may be those of what stays by now)
   const Scale s(sh.powers, top, rate);
-  const float span = top - bound;
-  const Steps steps = {top, span > 0.f && span < __builtin_inff() ? float(kBins) / span : 0.f};
+  const Steps steps(top, bound);
 
   Cut cut = {0, 0, 0};   // nothing is cut: every key is above 0
   double whole = st.total;
@@ -919,7 +999,7 @@ __device__ __forceinline__ void whole_row(const SampleArgs& a, int row, const Sa
             sh.list[atomicAdd(&sh.listed, 1u)] = entry_of(key, index);
         });
         __syncthreads();
-        sort_list<kRowThreads>(sh.list, int(count));
+        sort_step(sh, int(count), steps);
         const int n = int(count), p0 = kPos * tid;
         uint64_t sum = 0;
 #pragma unroll
@@ -1070,11 +1150,6 @@ __device__ __forceinline__ double share_of(const SampleArgs& a, int row, double 
 __device__ __forceinline__ double least_of(const SampleArgs& a, int row) {
   return a.min_p && a.min_p[row] > 0.f ? fmin(double(a.min_p[row]), 1.0) : 0.0;
 }
-__device__ __forceinline__ Steps steps_of(const SampleRow& st) {
-  const float span = st.top - st.bound;
-  return {st.top, span > 0.f && span < __builtin_inff() ? float(kBins) / span : 0.f};
-}
-
 template <int kType, int kChunk>
 __global__ __launch_bounds__(kChunkThreads) void sample_bins_kernel(SampleArgs a) {
   constexpr int kPer = Elem<kType>::kPer;
@@ -1092,7 +1167,7 @@ __global__ __launch_bounds__(kChunkThreads) void sample_bins_kernel(SampleArgs a
   for (int b = tid; b < kBins; b += kChunkThreads) mass[b] = 0;
   __syncthreads();
   const Scale s(powers, st.top, rate_of(temperature_of(a, row)));
-  const Steps steps = steps_of(st);
+  const Steps steps(st.top, st.bound);
 #pragma unroll
   for (int j = 0; j < kPieces; ++j)
 #pragma unroll
@@ -1146,7 +1221,7 @@ __global__ __launch_bounds__(kChunkThreads) void sample_collect_kernel(SampleArg
   __syncthreads();
   const int bin = found.bin;
   const Scale s(powers, st.top, rate_of(temperature_of(a, row)));
-  const Steps steps = steps_of(st);
+  const Steps steps(st.top, st.bound);
   const double low = least_of(a, row);
   uint64_t sum = 0;
 #pragma unroll
@@ -1194,7 +1269,7 @@ __global__ __launch_bounds__(kRowThreads) void sample_finish_kernel(SampleArgs a
   uint64_t* const by_chunk = sh.mass;
   for (int c = tid; c < kMaxChunks; c += kRowThreads) by_chunk[c] = c < a.num_chunks ? a.chunks[size_t(row) * a.num_chunks + c].sum : 0;
   __syncthreads();
-  sort_list<kRowThreads>(sh.list, n);
+  sort_step(sh, n, Steps(top, st.bound));
   const Scale s(sh.powers, top, rate_of(temperature_of(a, row)));
   const double low = least_of(a, row), share = share_of(a, row, st.total);
   uint64_t w[kPos], sum = 0;
