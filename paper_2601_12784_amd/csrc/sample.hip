@@ -51,8 +51,8 @@ struct Elem {
   static constexpr int kPer = 16 / kBytes;   // logits of a 16-byte piece
 };
 
-// A NaN counts as no entry, and -0 as 0 (equal logits have equal keys).
-__device__ __forceinline__ float clean(float x) { return fmaxf(x, kNone) + 0.f; }
+// A NaN counts as no entry.
+__device__ __forceinline__ float clean(float x) { return fmaxf(x, kNone); }
 
 // (A bit cast of a vector's element itself takes the vector's first.)
 __device__ __forceinline__ float value32(uint32_t bits) { return __builtin_bit_cast(float, bits); }
@@ -142,7 +142,10 @@ __device__ __forceinline__ double exp2_of(const Powers& t, double y, int shift) 
   p = __builtin_fma(p, f, 0.24022650695910071233);
   p = __builtin_fma(p, f, 0.69314718055994530942);
   p = __builtin_fma(p, f, 1.0) * t.at[n & 31];
-  return __builtin_bit_cast(double, __builtin_bit_cast(uint64_t, p) + (uint64_t(uint32_t((n >> 5) + shift) << 20) << 32));
+  typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+  u32x2 bits = __builtin_bit_cast(u32x2, p);
+  bits.y += (uint32_t(n) << 15 & 0xFFF00000u) + (uint32_t(shift) << 20);
+  return __builtin_bit_cast(double, bits);
 }
 
 // Weights of logits relative to a largest one: exp((l - top) / T), 1 / (T ln 2) in rate.
@@ -173,9 +176,9 @@ __device__ __forceinline__ bool greedy(float t) { return !(t > 0.f); }
 __device__ __forceinline__ float temperature_of(const SampleArgs& a, int row) { return a.temperature ? a.temperature[row] : 1.f; }
 __device__ __forceinline__ double rate_of(float t) { return 1.44269504088896340736 / (greedy(t) ? 1.0 : double(t)); }
 
-// Rising keys for rising logits, above 0 for every finite one and +inf.
+// Rising keys for rising logits, above 0 for every finite one and +inf; -0 is 0 (equal logits have equal keys).
 __device__ __forceinline__ uint32_t key_of(float x) {
-  const uint32_t b = __builtin_bit_cast(uint32_t, x);
+  const uint32_t b = __builtin_bit_cast(uint32_t, x + 0.f);
   return x == kNone ? 0u : b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 __device__ __forceinline__ float logit_of(uint32_t key) {
