@@ -62,11 +62,33 @@ __device__ __forceinline__ float value16(uint32_t bits) {
   return float(__builtin_bit_cast(_Float16, uint16_t(bits)));
 }
 
+template <int kType>
+__device__ __forceinline__ void values(u32x4 w, float* x) {
+#pragma unroll
+  for (int i = 0; i < Elem<kType>::kPer; ++i) {
+    if constexpr (kType == kF32)
+      x[i] = clean(value32(w[i]));
+    else
+      x[i] = clean(value16<kType>(i & 1 ? w[i / 2] >> 16 : w[i / 2] & 0xFFFFu));
+  }
+}
+
+// Some pieces of a row: all loads first, so that they are in flight together.
+template <int kCount, class Row, class At>
+__device__ __forceinline__ void load_all(const Row& r, float (&x)[kCount][Row::kPer], At at) {
+  u32x4 w[kCount];
+#pragma unroll
+  for (int j = 0; j < kCount; ++j) w[j] = r.raw(at(j));
+#pragma unroll
+  for (int j = 0; j < kCount; ++j) values<Row::kElem>(w[j], x[j]);
+}
+
 // A row of logits as 16-byte pieces at 16-byte addresses: piece p holds
 // entries p * kPer - lead .. + kPer - 1, of which the first and the last pieces
 // may lack some.
 template <int kType>
 struct Row {
+  static constexpr int kElem = kType, kPer = Elem<kType>::kPer;
   const char* base;
   int lead;
   int vocab;
@@ -82,33 +104,29 @@ struct Row {
     pieces = (vocab + lead + kPer - 1) / kPer;
   }
   __device__ __forceinline__ int first(int p) const { return p * Elem<kType>::kPer - lead; }
-  // Entries that a piece lacks, or past the last piece, are -inf.
-  __device__ __forceinline__ void load(int p, float* x) const {
+  // A piece as it lies in memory; entries that it lacks, or past the last piece, are -inf.
+  __device__ __forceinline__ u32x4 raw(int p) const {
     constexpr int kPer = Elem<kType>::kPer, kBytes = Elem<kType>::kBytes;
+    constexpr uint32_t kLeast = kType == kF32 ? 0xFF800000u : kType == kBF16 ? 0xFF80FF80u : 0xFC00FC00u;
     const int lo = first(p);
+    u32x4 w = {kLeast, kLeast, kLeast, kLeast};
     if (lo >= 0 && lo + kPer <= vocab) {
-      const u32x4 w = *reinterpret_cast<const u32x4*>(base + int64_t(p) * 16);
+      w = *reinterpret_cast<const u32x4*>(base + int64_t(p) * 16);
+    } else if (p < pieces) {
 #pragma unroll
-      for (int i = 0; i < kPer; ++i) {
-        if constexpr (kType == kF32)
-          x[i] = clean(value32(w[i]));
-        else
-          x[i] = clean(value16<kType>(i & 1 ? w[i / 2] >> 16 : w[i / 2] & 0xFFFFu));
-      }
-      return;
+      for (int i = 0; i < kPer; ++i)
+        if (lo + i >= 0 && lo + i < vocab) {
+          const char* at = base + int64_t(p) * 16 + i * kBytes;
+          if constexpr (kType == kF32)
+            w[i] = *reinterpret_cast<const uint32_t*>(at);
+          else
+            w[i / 2] = i & 1 ? (w[i / 2] & 0xFFFFu) | uint32_t(*reinterpret_cast<const uint16_t*>(at)) << 16
+                             : (w[i / 2] & 0xFFFF0000u) | *reinterpret_cast<const uint16_t*>(at);
+        }
     }
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      x[i] = kNone;
-      if (lo + i >= 0 && lo + i < vocab) {
-        const char* at = base + int64_t(p) * 16 + i * kBytes;
-        if constexpr (kType == kF32)
-          x[i] = clean(*reinterpret_cast<const float*>(at));
-        else
-          x[i] = clean(value16<kType>(*reinterpret_cast<const uint16_t*>(at)));
-      }
-    }
+    return w;
   }
+  __device__ __forceinline__ void load(int p, float* x) const { values<kType>(raw(p), x); }
 };
 
 // 2^(i / 32), i < 32, in LDS: 64 lanes read it without a conflict.
@@ -258,8 +276,7 @@ __global__ __launch_bounds__(kChunkThreads) void sample_chunk_kernel(SampleArgs 
   const int tid = int(threadIdx.x), lane = tid & 63, wave = tid >> 6;
   const int p0 = chunk * (kChunk / kPer) + tid;
   float x[kPieces][kPer];
-#pragma unroll
-  for (int j = 0; j < kPieces; ++j) r.load(p0 + j * kChunkThreads, x[j]);
+  load_all(r, x, [&](int j) { return p0 + j * kChunkThreads; });
   make_powers(powers);
   float top = kNone;
 #pragma unroll
@@ -438,15 +455,12 @@ __device__ __forceinline__ void draw_row(const SampleArgs& a, int row, Drawn& sh
   constexpr int kRun = kSampleChunk / kPer / kThreads;
   const int n = a.chunk / kPer, run = (n + kThreads - 1) / kThreads;
   uint64_t sum = 0;
+  float x[kRun][kPer];
+  load_all(r, x, [&](int j) { return j < run && tid * run + j < n ? chunk * n + tid * run + j : r.pieces; });   // (nothing behind the last)
 #pragma unroll
-  for (int j = 0; j < kRun; ++j) {
-    const int q = tid * run + j;
-    if (j >= run || q >= n) break;
-    float x[kPer];
-    r.load(chunk * n + q, x);
+  for (int j = 0; j < kRun; ++j)
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) sum += cs.units(x[i]);
-  }
+    for (int i = 0; i < kPer; ++i) sum += cs.units(x[j][i]);
   const uint64_t scan = wave_scan(sum);
   if (lane == 63) sh.waves[wave] = scan;
   __syncthreads();
@@ -793,9 +807,9 @@ __global__ __launch_bounds__(kCutThreads) void sample_cut_kernel(SampleArgs a) {
 #pragma unroll
       for (int d = 0; d < kDeep; ++d) {
         const uint32_t i = i0 + uint32_t(d) * kCutThreads;
-        piece[d] = i < num_near * kPieces ? int(ids[i / kPieces]) * kPieces + int(i % kPieces) : r.pieces;
-        r.load(piece[d], x[d]);   // (nothing behind the last)
+        piece[d] = i < num_near * kPieces ? int(ids[i / kPieces]) * kPieces + int(i % kPieces) : r.pieces;   // (nothing behind the last)
       }
+      load_all(r, x, [&](int d) { return piece[d]; });
       uint32_t mine = 0;
 #pragma unroll
       for (int d = 0; d < kDeep; ++d)
@@ -925,8 +939,7 @@ __device__ __forceinline__ void for_run(const Row<kType>& r, int run, Use use) {
   const int end = run_begin(r, run + 1);
   for (int p = run_begin(r, run) + (int(threadIdx.x) & 63); p < end; p += 64 * kDeep) {
     float x[kDeep][kPer];
-#pragma unroll
-    for (int d = 0; d < kDeep; ++d) r.load(p + 64 * d < end ? p + 64 * d : r.pieces, x[d]);   // (nothing behind the last)
+    load_all(r, x, [&](int d) { return p + 64 * d < end ? p + 64 * d : r.pieces; });   // (nothing behind the last)
 #pragma unroll
     for (int d = 0; d < kDeep; ++d)
 #pragma unroll
@@ -1164,8 +1177,7 @@ __global__ __launch_bounds__(kChunkThreads) void sample_bins_kernel(SampleArgs a
   if (st.open != 1) return;
   const Row<kType> r(a, row);
   float x[kPieces][kPer];
-#pragma unroll
-  for (int j = 0; j < kPieces; ++j) r.load(chunk * (kChunk / kPer) + tid + j * kChunkThreads, x[j]);
+  load_all(r, x, [&](int j) { return chunk * (kChunk / kPer) + tid + j * kChunkThreads; });
   make_powers(powers);
   for (int b = tid; b < kBins; b += kChunkThreads) mass[b] = 0;
   __syncthreads();
@@ -1197,8 +1209,7 @@ __global__ __launch_bounds__(kChunkThreads) void sample_collect_kernel(SampleArg
   if (st.open != 1) return;
   const Row<kType> r(a, row);
   float x[kPieces][kPer];
-#pragma unroll
-  for (int j = 0; j < kPieces; ++j) r.load(chunk * (kChunk / kPer) + tid + j * kChunkThreads, x[j]);
+  load_all(r, x, [&](int j) { return chunk * (kChunk / kPer) + tid + j * kChunkThreads; });
   // the crossing, by every chunk for itself
   const uint64_t* bins = a.bins + size_t(row) * kBins + kMine * tid;
   uint64_t m[kMine], mine = 0;
@@ -1315,11 +1326,14 @@ __global__ __launch_bounds__(kRowThreads) void sample_finish_kernel(SampleArgs a
   float x[kRun][kPer];
   uint64_t units[kRun][kPer];
   sum = 0;
+  auto piece_of = [&](int j) {
+    const int q = tid * run + j;
+    return j < run && q < pieces ? chunk * pieces + q : r.pieces;   // (nothing behind the last)
+  };
+  load_all(r, x, piece_of);
 #pragma unroll
   for (int j = 0; j < kRun; ++j) {
-    const int q = tid * run + j;
-    const int piece = j < run && q < pieces ? chunk * pieces + q : r.pieces;   // (nothing behind the last)
-    r.load(piece, x[j]);
+    const int piece = piece_of(j);
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
       const float l = x[j][i];

@@ -477,6 +477,20 @@ def test_sample_equal_logits():
         check_samples(x, u, S(x, u, **p), **p)
 
 
+@pytest.mark.parametrize("dtype, bits, view", [(torch.float32, 0x7F800001, torch.int32), (torch.bfloat16, 0x7F81, torch.int16),
+                                               (torch.float16, 0x7C01, torch.int16)])
+def test_sample_signalling_nan_is_no_entry(dtype, bits, view):
+    rng = np.random.default_rng(1)
+    x = torch.from_numpy(rng.standard_normal((3, 9001)).astype(np.float32)).to(dtype)
+    x.view(view)[0, ::2] = bits
+    x.view(view)[1, 1:] = bits
+    x.view(view)[2, [0, 9000]] = bits
+    x, u, S = x.cuda(), cuda([0.3, 0.6, 0.9], torch.float32), B.Sampler()
+    for params in (dict(), dict(top_p=cuda([0.7] * 3, torch.float32)), dict(top_k=cuda([5000] * 3, torch.int32)),
+                   dict(temperature=cuda([0.0] * 3, torch.float32))):
+        check_samples(x, u, S(x, u, **params), **params)
+
+
 def test_sample_masked_and_broken_logits():
     rng = np.random.default_rng(0)
     inf, nan = math.inf, math.nan
