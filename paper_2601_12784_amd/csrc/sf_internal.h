@@ -181,7 +181,7 @@ constexpr int kSharedWaves = 8;       // waves of a workgroup, two per SIMD
 struct SharedArgs {
   // num_workers rows: first segment, segments, then the first segment's fields; num_work rows with the fields from int 2
   // on: first sequence of the rows, block-table row, kv_head, first page, end page, end token, partial row (-1: written
-  // out), first row, rows
+  // out), first row, rows, waves together, share of the blocks, the first row's sequence, its place among the sequence's
   const int32_t* workers;
   const int32_t* items;
   int32_t num_workers;
@@ -205,6 +205,7 @@ struct SharedArgs {
   int32_t num_q_heads;
   int32_t num_kv_heads;
   int32_t group;
+  int32_t group_inverse;      // x * group_inverse >> 16 is x / group for x < 4096
   int32_t head_dim;
   int32_t bt_stride;
   float scale_log2;

@@ -80,8 +80,9 @@ struct Scratch {
 };
 
 void put_fields(int32_t* row, int32_t seq0, int32_t source, int32_t kvh, int32_t pb, int32_t pe, int32_t end, int32_t slot,
-                int32_t row0, int32_t rows, int32_t together = 0, int32_t split = 0) {
-  const int32_t f[kSharedInts] = {0, 0, seq0, source, kvh, pb, pe, end, slot, row0, rows, together, split, 0, 0, 0};
+                int32_t row0, int32_t rows, int32_t group, int32_t together = 0, int32_t split = 0) {
+  const int32_t f[kSharedInts] = {0, 0, seq0, source, kvh, pb, pe, end, slot, row0, rows, together, split,
+                                  seq0 + row0 / group, row0 % group, 0};
   std::memcpy(row, f, sizeof f);
 }
 
@@ -276,7 +277,8 @@ sf_status plan(const sf_attn_desc* desc, const int32_t* lens, int32_t num_groups
           const int64_t stop = std::min(end, begin + p.pages);
           const int32_t part = int32_t(col - runs.of(begin)) * splits + split;
           put_fields(list + int64_t(item++) * kSharedInts, p.first, p.source, h, int32_t(page - begin), int32_t(stop - begin),
-                     p.pages * kPage, t.units[size_t(p.unit + h)].base + part * p.rows + row0, row0, row1 - row0, together, split);
+                     p.pages * kPage, t.units[size_t(p.unit + h)].base + part * p.rows + row0, row0, row1 - row0, g,
+                     together, split);
           page = stop;
         }
       }
@@ -309,7 +311,7 @@ sf_status plan(const sf_attn_desc* desc, const int32_t* lens, int32_t num_groups
         for (int32_t part = 0; page < end; ++part) {
           const int64_t stop = std::min(end, own_runs.at(col + 1));
           put_fields(list + int64_t(item++) * kSharedInts, s, s, h, skip + int32_t(page - begin), skip + int32_t(stop - begin),
-                     lens[s], u.base < 0 ? -1 : u.base + part * g, 0, g);
+                     lens[s], u.base < 0 ? -1 : u.base + part * g, 0, g, g);
           page = stop;
           if (page == own_runs.at(col + 1)) {
             close_worker(first);
@@ -400,6 +402,7 @@ sf_status sf::run_shared(const sf_attn_desc* desc, const sf_shared_info* info, c
   a.num_q_heads = desc->num_q_heads;
   a.num_kv_heads = desc->num_kv_heads;
   a.group = desc->num_q_heads / desc->num_kv_heads;
+  a.group_inverse = 65536 / a.group + 1;
   a.head_dim = desc->head_dim;
   a.bt_stride = desc->block_table_stride;
   a.scale_log2 = float(double(desc->softmax_scale) * 1.4426950408889634074);

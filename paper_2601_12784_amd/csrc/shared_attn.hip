@@ -55,13 +55,25 @@ __device__ __forceinline__ uint32_t widen2(uint32_t codes4) {
 }
 
 struct Item {
-  int seq0, source, kvh, pb, pe, end, slot, row0, rows, blocks, split;
+  int seq0, source, kvh, pb, pe, end, slot, row0, rows, blocks, split, member, within;
 };
 
 // Lane's position in the MFMA layouts.
 struct Lane {
   int col, grp;
-  __device__ __forceinline__ Lane() : col(int(threadIdx.x) & 15), grp((int(threadIdx.x) & 63) >> 4) {}
+  int lane;
+  // Hidden from the compiler, which else forms every address part of every kind of item before the first
+  // one and keeps them all (35 registers more than there are).
+  __device__ __forceinline__ Lane() {
+    lane = int(__builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u)));
+    asm volatile("" : "+v"(lane));
+    col = lane & 15;
+    grp = lane >> 4;
+  }
+  // x of the lane with another bit of its number
+  __device__ __forceinline__ float across(float x, int bit) const {
+    return __builtin_bit_cast(float, __builtin_amdgcn_ds_bpermute((lane ^ bit) << 2, __builtin_bit_cast(int, x)));
+  }
 };
 
 // Keys and values of a block of two pages as they come from memory: bf16
@@ -249,7 +261,7 @@ __device__ __forceinline__ float sum8(const float* p) {
 // block's does: m is -inf) lanes of a row need not agree on its maximum, and nothing is exchanged.
 template <int D, bool kFp8>
 __device__ __forceinline__ Weights weigh(Tile<D>& t, const f32x4& s0, const f32x4& s1, float c0, float c1, float v0, float v1,
-                                         int valid, int grp) {
+                                         int valid, const Lane& l) {
   float z[8], p[8];
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
@@ -258,15 +270,15 @@ __device__ __forceinline__ Weights weigh(Tile<D>& t, const f32x4& s0, const f32x
   }
   if (valid < 2 * kPage) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) z[e] = key_at(grp, e) < valid ? z[e] : -__builtin_inff();
+    for (int e = 0; e < 8; ++e) z[e] = key_at(l.grp, e) < valid ? z[e] : -__builtin_inff();
   }
 #pragma unroll
   for (int e = 0; e < 8; ++e) p[e] = exp2_fast(z[e] - t.m);
   float part = sum8(p);
   if (__any(!(part <= kHeadroom))) {
     float top = fmaxf(fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3])), fmaxf(fmaxf(z[4], z[5]), fmaxf(z[6], z[7])));
-    top = fmaxf(top, __shfl_xor(top, 16));
-    top = fmaxf(top, __shfl_xor(top, 32));
+    top = fmaxf(top, l.across(top, 16));
+    top = fmaxf(top, l.across(top, 32));
     const float m = fmaxf(t.m, top);
     const float ref = m == -__builtin_inff() ? 0.f : m;   // no key with a finite score so far
     const float keep = exp2_fast(t.m - ref);
@@ -305,9 +317,9 @@ struct Rows {
     for (int t = 0; t < kTiles; ++t) {
       const int r = 16 * t + l.col;
       const bool ok = r < it.rows;
-      const int row = it.row0 + (ok ? r : 0);
-      const int member = row / a.group, head = row - member * a.group;
-      const uint16_t* src = a.q + (size_t(it.seq0 + member) * a.num_q_heads + it.kvh * a.group + head) * D + 8 * l.grp;
+      const int row = it.within + (ok ? r : 0);   // below 16 + 32
+      const int member = row * a.group_inverse >> 16, head = row - member * a.group;
+      const uint16_t* src = a.q + (size_t(it.member + member) * a.num_q_heads + it.kvh * a.group + head) * D + 8 * l.grp;
 #pragma unroll
       for (int kb = 0; kb < D / 32; ++kb) {
         const u32x4 x = *reinterpret_cast<const u32x4*>(src + 32 * kb);
@@ -323,8 +335,8 @@ struct Rows {
   __device__ __forceinline__ void finish(const SharedArgs& a, const Item& it, const Lane& l) const {
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) {
-      float total = tile[t].sum + __shfl_xor(tile[t].sum, 16);
-      total += __shfl_xor(total, 32);
+      float total = tile[t].sum + l.across(tile[t].sum, 16);
+      total += l.across(total, 32);
       const float inv = total > 0.f ? 1.f / total : 0.f;
       const float lse = total > 0.f ? tile[t].m + __log2f(total) : -__builtin_inff();
       const int r = 16 * t + l.col;
@@ -431,7 +443,7 @@ __device__ __forceinline__ void walk(const SharedArgs& a, const Item& it) {
     }
     Weights w[kTiles];
 #pragma unroll
-    for (int t = 0; t < kTiles; ++t) w[t] = weigh<D, kFp8>(rows.tile[t], s0[t], s1[t], c0, c1, v0, v1, valid, l.grp);
+    for (int t = 0; t < kTiles; ++t) w[t] = weigh<D, kFp8>(rows.tile[t], s0[t], s1[t], c0, c1, v0, v1, valid, l);
     accumulate(rows, w, [&](int j) { return value_operand(vc, j); });
     if constexpr (kBufs == 1) {
       __builtin_amdgcn_sched_barrier(0);
@@ -463,15 +475,14 @@ struct Stage {
 __device__ __forceinline__ int v_swizzle(int d) { return (d >> 1) & 3; }
 
 template <int D, bool kFp8, int kSplits>
-__device__ __forceinline__ void walk_together(const SharedArgs& a, const Item& it, uint16_t* lds, f32x4* lds_scale) {
+__device__ __forceinline__ void walk_together(const SharedArgs& a, const Item& it, int wave, uint16_t* lds, f32x4* lds_scale) {
   constexpr int kTiles = kSharedTiles;
   constexpr int kAhead = 4 / kSplits;               // steps in registers
   constexpr int kTile = Stage<D>::kTile;
   constexpr int kChunks = kTile * (kFp8 ? 1 : 2) / 1024;   // of 1 KiB in a page's K or V
   constexpr int kMine = kChunks > 1 ? kChunks / 2 : 1;     // of a wave
   const Lane l;
-  const int lane = int(threadIdx.x) & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
+  const int lane = l.lane;
   const Source<D, kFp8> src(a, it, l);
   const int blocks = (it.pe - it.pb + 1) / 2, steps = (blocks + kSplits - 1) / kSplits;
 
@@ -506,6 +517,9 @@ __device__ __forceinline__ void walk_together(const SharedArgs& a, const Item& i
   };
   auto put = [&](const Staged& s, int step) {
     if (!stager) return;
+    // (a ring of 128 KiB is more than an address reaches: the parts' addresses are formed anew rather than all kept)
+    int lane = l.lane;
+    if constexpr (kSplits == 4) asm volatile("" : "+v"(lane));
 #pragma unroll
     for (int b = 0; b < kSplits; ++b) {
       const int slot = (step & 1) * kSplits + b;
@@ -572,7 +586,7 @@ __device__ __forceinline__ void walk_together(const SharedArgs& a, const Item& i
     }
     Weights w[kTiles];
 #pragma unroll
-    for (int t = 0; t < kTiles; ++t) w[t] = weigh<D, kFp8>(rows.tile[t], s0[t], s1[t], c0, c1, v0, v1, valid, l.grp);
+    for (int t = 0; t < kTiles; ++t) w[t] = weigh<D, kFp8>(rows.tile[t], s0[t], s1[t], c0, c1, v0, v1, valid, l);
     const int vat = 2 * kTile + l.col * 32 + (l.grp ^ v_swizzle(l.col)) * 8;
     accumulate(rows, w, [&](int j) { return *reinterpret_cast<const u32x4*>(L + vat + j * 16 * 32); });
   };
@@ -599,7 +613,7 @@ __device__ __forceinline__ void walk_together(const SharedArgs& a, const Item& i
 }
 
 __device__ __forceinline__ Item item_at(const_i32_ptr row) {
-  return {row[2], row[3], row[4], row[5], row[6], row[7], row[8], row[9], row[10], row[11], row[12]};
+  return {row[2], row[3], row[4], row[5], row[6], row[7], row[8], row[9], row[10], row[11], row[12], row[13], row[14]};
 }
 
 template <int D, bool kFp8, int kWG>
@@ -619,9 +633,9 @@ __global__ __launch_bounds__(64 * kWG) __attribute__((amdgpu_waves_per_eu(2, 2))
       if (it.blocks) {
         __shared__ __attribute__((aligned(16))) uint16_t lds[Stage<D>::kRing];
         __shared__ f32x4 lds_scale[8];
-        if (it.blocks == 8) walk_together<D, kFp8, 1>(a, it, lds, lds_scale);
-        else if (it.blocks == 4) walk_together<D, kFp8, 2>(a, it, lds, lds_scale);
-        else walk_together<D, kFp8, 4>(a, it, lds, lds_scale);
+        if (it.blocks == 8) walk_together<D, kFp8, 1>(a, it, wave, lds, lds_scale);
+        else if (it.blocks == 4) walk_together<D, kFp8, 2>(a, it, wave, lds, lds_scale);
+        else walk_together<D, kFp8, 4>(a, it, wave, lds, lds_scale);
         continue;
       }
     }
