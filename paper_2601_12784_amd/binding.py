@@ -313,6 +313,16 @@ def _current_stream(device=None) -> int:
     return _raw_stream(_current_device() if index is None else index)
 
 
+_HERE = contextlib.nullcontext()
+
+
+def _on_device(device):
+    """torch.cuda.device(device), which costs 2 us, or nothing if that is the current one."""
+    if _current_device is not None and torch.cuda.is_initialized() and _current_device() == device.index:
+        return _HERE
+    return torch.cuda.device(device)
+
+
 def _stream(stream) -> int | None:
     if stream is None:
         return _current_stream()
@@ -1664,7 +1674,7 @@ class Rotary:
         if q_out is not None and k_out is not None:
             _check_turned(q_out, k_out, "k_out", [q_out])
         device = given.device
-        with torch.cuda.device(device):
+        with _on_device(device):
             _check("sf_rotary", lib().sf_rotary(
                 self.desc_ref, t, 0 if q is None else q.shape[1], 0 if k is None else k.shape[1],
                 self.turns_on(device).data_ptr(), positions.data_ptr(), *args,
@@ -1708,7 +1718,7 @@ class Sampler:
             desc.num_rows, desc.vocab, desc.row_stride, desc.dtype = key
             _check("sf_sample_workspace", self._L.sf_sample_workspace(ctypes.byref(desc), ctypes.byref(self._bytes)))
             self._key = key
-        with torch.cuda.device(logits.device), torch.cuda.stream(stream):
+        with _on_device(logits.device), torch.cuda.stream(stream) if stream else _HERE:
             made = []
             for t, name, dtype in ((token, "token", torch.int32), (logprob, "logprob", torch.float32), (kept, "kept", torch.float32)):
                 made.append(torch.empty((b,), dtype=dtype, device=logits.device) if t is None else _dev(t, name, dtype, (b,)))
