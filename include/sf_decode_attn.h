@@ -859,8 +859,8 @@ sf_status sf_route(const sf_cost_model* model, double mu, int32_t min_initial_ve
  * (group_offsets[0] = 0, group_offsets[num_groups] = num_seqs); shared_lens[i] is at most L_s of every member with
  * L_s > 0. Members with L_s = 0 get out = 0, lse = -inf.
  *
- * Plan (host only). A prompt's rows, members times g, are taken in blocks of at most 32 (2 tiles of 16), 1 (up to 16 rows), 2, 4 or a multiple of 8 blocks,
- * which walk the same pages side by side; the pages of all prompts with one number of blocks, and those that
+ * Plan (host only). A prompt's rows, members times g, are taken in blocks of at most 32 (2 tiles of 16): 1 (up to 16 rows),
+ * 2, 4 or a multiple of 8 blocks, which walk the same pages side by side; the pages of all prompts with one number of blocks, and those that
  * sequences have to themselves, are each cut into equal runs, one per wave, as many runs as their share of the work.
  * Results of runs that end inside a prompt or sequence, and of all prompts, go to the workspace and are joined by a
  * second launch. fp8 = 1: for an fp8 cache, whose pages are half the bytes at the same arithmetic (only the shares go by
@@ -942,7 +942,9 @@ sf_status sf_rotary(const sf_rotary_desc* rotary, int32_t num_tokens, int32_t nu
  * The same for new tokens, whose turned keys and whose values go straight into the pages of a bf16 cache. The last
  * q_lens_host[s] of sequence s' seq_lens_host[s] tokens are new; rows of q [T][Hq][D], k_new and v_new [T][Hkv][D] are
  * theirs, sequence after sequence, with token strides as for sf_rotary. The first new one is at position
- * first_pos_host[s] (NULL: at its index in the cache; a cache that has given up tokens counts on).
+ * first_pos_host[s] (NULL: at its index in the cache; a cache that has given up tokens counts on). q_lens_host NULL is a
+ * decode step: there is a row per sequence, and the last token of each with seq_lens_host[s] > 0 is new; rows of the others
+ * are not read, and theirs of q_out stay as they were. rotary NULL: nothing turns, q is copied.
  * sf_rotary_store_plan (host only) makes the work list, sf_rotary_store enqueues the call: one launch. new_pages and the
  * block table are sf_kv_store_fp8's: with new_pages[s] >= 0 (device int32 [num_seqs], or NULL) the page of s' last token
  * is new, and the call writes it to the block table. q may be NULL (keys and values only). Slots without a new
@@ -978,9 +980,9 @@ sf_status sf_runner_rotary_store(sf_runner* runner, const sf_attn_desc* desc, co
  *   kept    = the sum of what stayed over the sum of all w (ln(w / what stayed) is logprob - ln(kept)).
  * T = 0 (or less, or NaN) takes the largest logit, the lowest index of equal ones, and reports as for T = 1. A NaN
  * logit counts as -inf; +inf shares all weight among the +inf entries. A row with nothing but -inf has no token: -1, logprob
- * -inf, kept 0. Weights enter the sums as multiples of 2^-44, off by half of one, so that a sum has one value in whatever order it is
- * formed; of the draws of a row at most V 2^-43 or so fall to a neighbour of the exact token, and equal inputs give equal
- * tokens on every run.
+ * -inf, kept 0. Weights enter the sums as multiples of 2^-44, off by half of one, so that a sum has one value in whatever
+ * order it is formed; of the draws of a row at most V 2^-43 or so fall to a neighbour of the exact token, and equal calls
+ * give equal tokens on every run.
  */
 typedef struct sf_sample_desc {
   int32_t num_rows;      /* >= 0 */
@@ -996,8 +998,8 @@ sf_status sf_sample_workspace(const sf_sample_desc* desc, uint64_t* bytes);
 /*
  * Enqueues the draw of a token per row. All pointers are device memory, logits aligned to their elements, workspace to 16
  * bytes, the others to 4: temperature, top_p, min_p (fp32 [num_rows]) and top_k (int32 [num_rows]) may be NULL (T = 1, no
- * cut), logprob and kept (fp32 [num_rows]) too; uniform fp32 and token int32 [num_rows]. Two launches on the stream (three with cuts, five with top_p),
- * nothing is allocated or kept, so the call can be captured. Calls that share a workspace must not overlap.
+ * cut), logprob and kept (fp32 [num_rows]) too; uniform fp32 and token int32 [num_rows]. Two launches on the stream, three
+ * with top_k or min_p, five with top_p; nothing is allocated or kept, so the call can be captured. Calls that share a workspace must not overlap.
  * SF_ERR_CAPACITY for a workspace smaller than sf_sample_workspace says.
  */
 sf_status sf_sample(const sf_sample_desc* desc, const void* logits, const float* temperature, const int32_t* top_k,

@@ -14,6 +14,8 @@ Modules:
   extend_ref   extend (re-prefill) attention and the new-token store
   cost_ref     throughput cost model and routing
   fp8_ref      FP8 E4M3 encoding and the per-page quantizer of the KV cache
+  cache_ref    the bounded cache: growing fp8 tiles, key weights, eviction
+  step_ref     a group rollout's step: rotary positions, shared prompts, sampling
 """
 from __future__ import annotations
 

@@ -1554,7 +1554,8 @@ class DecodeAttention:
         """Turns the queries and keys of the last q_lens[s] of seq_lens[s] tokens by their positions and stores the turned
         keys and the values into the pages of a bf16 cache (sf_rotary_store, through the runner). rotary: a Rotary, or
         None (nothing turns); q, k_new, v_new: bf16 [T, H, D], parts of wider rows allowed (q may be None). q_lens None is
-        a decode step: a row per sequence, of which the running ones' (seq_lens[s] > 0) last token is new. first_pos: host
+        a decode step: a row per sequence, of which the running ones' (seq_lens[s] > 0) last token is new (the others' rows
+        of q_out are not written). first_pos: host
         int32 [B], the first new token's position (default: its index in the cache); new_pages as in store_fp8. Returns the
         turned queries: q_out (may be q), by default a new tensor."""
         desc, lens = self._call_desc(k_pool, block_table, seq_lens, 1.0)

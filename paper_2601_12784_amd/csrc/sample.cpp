@@ -1,4 +1,5 @@
 // Sampling: entry points. The rules are stated in sf_decode_attn.h.
+#include <algorithm>
 #include <cstdint>
 
 #include "sf_internal.h"
@@ -36,15 +37,18 @@ int32_t sf::sample_chunks(const sf_sample_desc& d) {
 
 namespace {
 
-// The workspace: chunks, rows, bins and lists, groups.
+// The workspace: chunks, rows, a counter, bins and lists, groups.
 struct Layout {
-  uint64_t rows, bins, lists, groups, bytes;
+  uint64_t rows, taken, bins, lists, groups, bytes;
+  int32_t places;
   explicit Layout(const sf_sample_desc& d) {
     const uint64_t n = uint64_t(d.num_rows), chunks = n * uint64_t(sample_chunks(d));
     rows = align256(chunks * sizeof(SampleChunk));
-    bins = align256(rows + n * sizeof(SampleRow));
-    lists = bins + n * kSampleBins * 8;
-    groups = lists + n * kSampleList * 8;
+    taken = align256(rows + n * sizeof(SampleRow));
+    bins = taken + 256;
+    places = std::min(d.num_rows, kSamplePlaces);
+    lists = bins + uint64_t(places) * kSampleBins * 8;
+    groups = lists + uint64_t(places) * kSampleList * 8;
     bytes = groups + chunks * uint64_t(sample_chunk(d) / kSampleGroup) * 4;
   }
 };
@@ -93,6 +97,8 @@ extern "C" sf_status sf_sample(const sf_sample_desc* desc, const void* logits, c
   a.chunks = reinterpret_cast<SampleChunk*>(ws);
   if (top_k || top_p || min_p) {
     a.rows = reinterpret_cast<SampleRow*>(ws + at.rows);
+    a.places = at.places;
+    a.taken = reinterpret_cast<uint32_t*>(ws + at.taken);
     a.bins = reinterpret_cast<uint64_t*>(ws + at.bins);
     a.lists = reinterpret_cast<uint64_t*>(ws + at.lists);
     a.groups = reinterpret_cast<float*>(ws + at.groups);

@@ -18,6 +18,12 @@
 // launches: sums by 2048 equal steps of the logit, then the entries of the step in which the share is
 // reached, which a third one sorts. The rest (a top-k of thousands) is read whole by the third's workgroup.
 // Rows that are done cost those launches a workgroup each that ends at once.
+//
+// Measured: 256 rows of 131072 bf16 without cuts 34 + 11 us, where reading them takes 15: an entry
+// costs the first launch some thirty vector instructions (13 of them fp64), which is 25 us of that
+// work alone. 192 rows of 200003 fp32 with mixed cuts (33 us to read): 50 + 58 + 19 + 20 + 23, the second bound by its
+// slowest workgroup (thousands of entries near a cut, read again and sorted). The step forms of the
+// flat rows by one workgroup each instead took 460 us, sorting networks for the lists 120 more.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -278,6 +284,9 @@ __global__ __launch_bounds__(kChunkThreads) void sample_chunk_kernel(SampleArgs 
   float x[kPieces][kPer];
   load_all(r, x, [&](int j) { return p0 + j * kChunkThreads; });
   make_powers(powers);
+  if constexpr (kGroups) {
+    if (blockIdx.x == 0 && tid == 0) *a.taken = 0;
+  }
   float top = kNone;
 #pragma unroll
   for (int j = 0; j < kPieces; ++j) {
@@ -457,27 +466,36 @@ __device__ __forceinline__ void draw_row(const SampleArgs& a, int row, Drawn& sh
   uint64_t sum = 0;
   float x[kRun][kPer];
   load_all(r, x, [&](int j) { return j < run && tid * run + j < n ? chunk * n + tid * run + j : r.pieces; });   // (nothing behind the last)
+  uint64_t part[kRun];   // a piece's
 #pragma unroll
-  for (int j = 0; j < kRun; ++j)
+  for (int j = 0; j < kRun; ++j) {
+    part[j] = 0;
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) sum += cs.units(x[j][i]);
+    for (int i = 0; i < kPer; ++i) part[j] += cs.units(x[j][i]);
+    sum += part[j];
+  }
   const uint64_t scan = wave_scan(sum);
   if (lane == 63) sh.waves[wave] = scan;
   __syncthreads();
   uint64_t at = scan - sum;
   for (int w = 0; w < wave; ++w) at += sh.waves[w];
-  if (double(at) <= want && want < double(at + sum)) {
-    for (int j = 0; j < run; ++j) {
-      float x[kPer];
-      r.load(chunk * n + tid * run + j, x);
-      for (int i = 0; i < kPer; ++i) {
-        at += cs.units(x[i]);
-        if (double(at) > want) {
-          finish(a, row, sh.top, sh.total, r.first(chunk * n + tid * run + j) + i, x[i], sh.total);
-          return;
-        }
-      }
+  if (!(double(at) <= want && want < double(at + sum))) return;
+  float y[kPer];   // the piece that holds the draw
+  int piece = -1;
+#pragma unroll
+  for (int j = 0; j < kRun; ++j) {
+    if (piece < 0 && double(at + part[j]) > want) {
+      piece = j;
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) y[i] = x[j][i];
     }
+    if (piece < 0) at += part[j];
+  }
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    const bool was = double(at) > want;
+    at += cs.units(y[i]);
+    if (!was && double(at) > want) finish(a, row, sh.top, sh.total, r.first(chunk * n + tid * run + piece) + i, y[i], sh.total);
   }
 }
 
@@ -917,10 +935,16 @@ __global__ __launch_bounds__(kCutThreads) void sample_cut_kernel(SampleArgs a) {
   }
 
   // left to the launches behind this one
-  const bool spread = cut_p && !cut_k;
-  if (tid == 0) a.rows[row] = SampleRow{total, 0, top, bound, spread ? 1 : 2, 0};
-  if (spread)
-    for (int b = tid; b < kBins; b += kCutThreads) a.bins[size_t(row) * kBins + b] = 0;
+  // (which rows get a place may differ from run to run; what they give does not)
+  if (tid == 0) {
+    const uint32_t place = cut_p && !cut_k ? atomicAdd(a.taken, 1u) : uint32_t(a.places);
+    sh.found = place < uint32_t(a.places) ? int(place) + 1 : -1;
+    a.rows[row] = SampleRow{total, 0, top, bound, sh.found, 0};
+  }
+  __syncthreads();
+  const int open = sh.found;
+  if (open > 0)
+    for (int b = tid; b < kBins; b += kCutThreads) a.bins[size_t(open - 1) * kBins + b] = 0;
 }
 
 // The slow way, of a row with a top-k of more entries than the list holds, or with as many near
@@ -1174,7 +1198,7 @@ __global__ __launch_bounds__(kChunkThreads) void sample_bins_kernel(SampleArgs a
   __shared__ Powers powers;
   const int row = int(blockIdx.x) / a.num_chunks, chunk = int(blockIdx.x) % a.num_chunks, tid = int(threadIdx.x);
   const SampleRow st = a.rows[row];
-  if (st.open != 1) return;
+  if (st.open <= 0) return;
   const Row<kType> r(a, row);
   float x[kPieces][kPer];
   load_all(r, x, [&](int j) { return chunk * (kChunk / kPer) + tid + j * kChunkThreads; });
@@ -1192,7 +1216,7 @@ __global__ __launch_bounds__(kChunkThreads) void sample_bins_kernel(SampleArgs a
     }
   __syncthreads();
   for (int b = tid; b < kBins; b += kChunkThreads)
-    if (mass[b]) atomicAdd(reinterpret_cast<unsigned long long*>(a.bins + size_t(row) * kBins + b), (unsigned long long)(mass[b]));
+    if (mass[b]) atomicAdd(reinterpret_cast<unsigned long long*>(a.bins + size_t(st.open - 1) * kBins + b), (unsigned long long)(mass[b]));
 }
 
 template <int kType, int kChunk>
@@ -1206,12 +1230,12 @@ __global__ __launch_bounds__(kChunkThreads) void sample_collect_kernel(SampleArg
   const int row = int(blockIdx.x) / a.num_chunks, chunk = int(blockIdx.x) % a.num_chunks;
   const int tid = int(threadIdx.x), lane = tid & 63, wave = tid >> 6;
   const SampleRow st = a.rows[row];
-  if (st.open != 1) return;
+  if (st.open <= 0) return;
   const Row<kType> r(a, row);
   float x[kPieces][kPer];
   load_all(r, x, [&](int j) { return chunk * (kChunk / kPer) + tid + j * kChunkThreads; });
   // the crossing, by every chunk for itself
-  const uint64_t* bins = a.bins + size_t(row) * kBins + kMine * tid;
+  const uint64_t* bins = a.bins + size_t(st.open - 1) * kBins + kMine * tid;
   uint64_t m[kMine], mine = 0;
 #pragma unroll
   for (int i = 0; i < kMine; ++i) mine += m[i] = bins[i];
@@ -1249,7 +1273,7 @@ __global__ __launch_bounds__(kChunkThreads) void sample_collect_kernel(SampleArg
       if (in && b < bin && (low == 0.0 || s.weight(l) >= low)) sum += w;
       if (in && b == bin) {
         const uint32_t at = atomicAdd(&a.rows[row].listed, 1u);
-        if (at < kList) a.lists[size_t(row) * kList + at] = entry_of(key_of(l), r.first(chunk * (kChunk / kPer) + tid + j * kChunkThreads) + i);
+        if (at < kList) a.lists[size_t(st.open - 1) * kList + at] = entry_of(key_of(l), r.first(chunk * (kChunk / kPer) + tid + j * kChunkThreads) + i);
       }
     }
   sum = wave_sum(sum);
@@ -1270,7 +1294,7 @@ __global__ __launch_bounds__(kRowThreads) void sample_finish_kernel(SampleArgs a
   const int row = int(blockIdx.x), tid = int(threadIdx.x);
   const SampleRow st = a.rows[row];
   if (st.open == 0) return;
-  if (st.open == 2 || st.listed > kList) {
+  if (st.open < 0 || st.listed > kList) {
     whole_row<kType>(a, row, st, sh);
     return;
   }
@@ -1278,7 +1302,7 @@ __global__ __launch_bounds__(kRowThreads) void sample_finish_kernel(SampleArgs a
   const float top = st.top;
   make_powers(sh.powers);
   const int n = int(st.listed), p0 = kPos * tid;
-  for (int i = tid; i < n; i += kRowThreads) sh.list[i] = a.lists[size_t(row) * kList + i];
+  for (int i = tid; i < n; i += kRowThreads) sh.list[i] = a.lists[size_t(st.open - 1) * kList + i];
   // sums of what stays by chunk, joined below by the listed entries'
   uint64_t* const by_chunk = sh.mass;
   for (int c = tid; c < kMaxChunks; c += kRowThreads) by_chunk[c] = c < a.num_chunks ? a.chunks[size_t(row) * a.num_chunks + c].sum : 0;

@@ -255,6 +255,7 @@ constexpr int kSampleChunk = 8192;        // logits that a workgroup of the firs
 constexpr int kSampleSmallChunk = 2048;
 constexpr int kSampleBins = 2048;
 constexpr int kSampleList = 4096;
+constexpr int kSamplePlaces = 1024;   // (48 KiB each; more rows than that fill the card with a workgroup each)
 constexpr int kSampleGroup = 64;          // logits whose largest one the first launch keeps
 struct SampleChunk {
   float top;       // the chunk's largest logit
@@ -267,7 +268,7 @@ struct SampleRow {
   uint64_t above;    // sum of those before the step in which the share is reached
   float top;         // the row's largest logit
   float bound;       // no entry below it stays
-  int32_t open;      // 0: done; 1: a top-p to be found over the whole row; 2: any cuts, by one workgroup
+  int32_t open;      // 0: done; 1 + its place: a top-p to be found by all chunks; -1: any cuts, by one workgroup
   uint32_t listed;   // entries of that step
 };
 struct SampleArgs {
@@ -289,8 +290,10 @@ struct SampleArgs {
   float* groups;              // [num_rows][num_chunks][chunk / 64]; NULL: no cuts
   // with cuts, for rows that one workgroup's list does not do:
   SampleRow* rows;            // [num_rows]
-  uint64_t* bins;             // [num_rows][2048]
-  uint64_t* lists;            // [num_rows][4096]
+  int32_t places;             // such rows that all of their chunks work on
+  uint32_t* taken;            // of the places
+  uint64_t* bins;             // [places][2048]
+  uint64_t* lists;            // [places][4096]
 };
 int32_t sample_chunk(const sf_sample_desc& d);
 int32_t sample_chunks(const sf_sample_desc& d);

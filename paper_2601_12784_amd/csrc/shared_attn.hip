@@ -11,10 +11,15 @@
 //   weights 2^(z - m), the row's reference m moved only when a block's weights grow past 2^kHeadroom
 //   O^T[D][16 rows]      += V^T P^T           (D/16) x 2 MFMAs, P as two bf16 parts (16 bits of each weight)
 //
-// Operands come straight from memory to registers (the page layouts are the
-// operands' own), two waves per SIMD. A wave
+// A sequence's own operands come straight from memory to registers (the page layouts are the
+// operands' own), a prompt's through LDS, which all waves of its workgroup read; two waves per SIMD. A wave
 // (worker) walks an equal share of the pages; its results are rows of normalized
 // output with their log-sum-exp, which a second launch joins per (sequence, KV head).
+//
+// What bounds it: own pages memory (16 prompts of 2048 tokens with 16 samples each, 484 MB in all: 110 us, of which
+// the merge is 6), prompts with hundreds of rows the matrix and the vector work of their blocks, which hardly
+// overlap (32760 tokens under 64 samples of 8 x 4 heads: 93 us; their products alone are 31). Without LDS, every
+// wave reading the prompt's pages for itself, these took 210 and 165 us.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 

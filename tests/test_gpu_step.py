@@ -772,3 +772,14 @@ def test_grouped_loop_refuses_what_it_cannot_do():
         attn.rotate_store(B.Rotary(128), None, k, k, cache.g_k, cache.g_v, args[5], [40, 40])
     with pytest.raises(ValueError):
         attn.rotate_store(None, None, k, k, cache.g_k, cache.g_v, args[5], [40, 40], q_out=q)
+
+
+def test_sample_more_flat_rows_than_places():
+    """More rows that a list does not hold than the workspace has places: the rest take another way to the same token."""
+    rng = np.random.default_rng(3)
+    row = torch.from_numpy((0.1 * rng.standard_normal(9001)).astype(np.float32))
+    x = row.expand(1500, -1).contiguous().cuda()
+    u, top_p = cuda([0.7] * 1500, torch.float32), cuda([0.9] * 1500, torch.float32)
+    token, logprob, kept = B.Sampler()(x, u, top_p=top_p)
+    check_samples(x[:2], u[:2], (token[:2], logprob[:2], kept[:2]), top_p=top_p[:2])
+    assert (token == token[0]).all() and (logprob == logprob[0]).all() and (kept == kept[0]).all()
