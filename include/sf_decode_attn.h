@@ -999,7 +999,7 @@ sf_status sf_sample_workspace(const sf_sample_desc* desc, uint64_t* bytes);
  * Enqueues the draw of a token per row. All pointers are device memory, logits aligned to their elements, workspace to 16
  * bytes, the others to 4: temperature, top_p, min_p (fp32 [num_rows]) and top_k (int32 [num_rows]) may be NULL (T = 1, no
  * cut), logprob and kept (fp32 [num_rows]) too; uniform fp32 and token int32 [num_rows]. Two launches on the stream, three
- * with top_k or min_p, five with top_p; nothing is allocated or kept, so the call can be captured. Calls that share a workspace must not overlap.
+ * with top_k alone, five with top_p or min_p; nothing is allocated or kept, so the call can be captured. Calls that share a workspace must not overlap.
  * SF_ERR_CAPACITY for a workspace smaller than sf_sample_workspace says.
  */
 sf_status sf_sample(const sf_sample_desc* desc, const void* logits, const float* temperature, const int32_t* top_k,

@@ -14,7 +14,7 @@
 // the groups' largest logits bound where that order can end (Bound below): if
 // no more than 4096 entries lie above the bound, only their groups are read again, the
 // entries are sorted in LDS and every cut is a position there. A row left open by
-// that takes one of two ways. A top-p of everything is found by all of the row's chunks at once, in two
+// that takes one of two ways. A top-p of everything, a min-p too, is found by all of the row's chunks at once, in two
 // launches: sums by 2048 equal steps of the logit, then the entries of the step in which the share is
 // reached, which a third one sorts. The rest (a top-k of thousands) is read whole by the third's workgroup.
 // Rows that are done cost those launches a workgroup each that ends at once.
@@ -937,7 +937,7 @@ __global__ __launch_bounds__(kCutThreads) void sample_cut_kernel(SampleArgs a) {
   // left to the launches behind this one
   // (which rows get a place may differ from run to run; what they give does not)
   if (tid == 0) {
-    const uint32_t place = cut_p && !cut_k ? atomicAdd(a.taken, 1u) : uint32_t(a.places);
+    const uint32_t place = cut_k ? uint32_t(a.places) : atomicAdd(a.taken, 1u);
     sh.found = place < uint32_t(a.places) ? int(place) + 1 : -1;
     a.rows[row] = SampleRow{total, 0, top, bound, sh.found, 0};
   }
@@ -1177,7 +1177,7 @@ __device__ __forceinline__ void whole_row(const SampleArgs& a, int row, const Sa
   }
 }
 
-// Top-p rows whose nucleus may be more than the list holds, by three launches over all of the row's chunks:
+// Rows without a top-k that keep more than the list holds, by three launches over all of the row's chunks:
 // sums by equal steps of the logit; the step in which the share is reached, whose entries are
 // listed, with the sums of what lies above it by chunk; the order of the listed ones, which is the cut, and the draw.
 struct Crossing {
@@ -1185,7 +1185,8 @@ struct Crossing {
   uint64_t above;   // the sum before it
 };
 __device__ __forceinline__ double share_of(const SampleArgs& a, int row, double whole) {
-  return fmax(double(a.top_p[row]) * whole, 1.0);   // no share lies before the first, so it always stays
+  const float p = a.top_p ? a.top_p[row] : 1.f;
+  return p < 1.f ? fmax(double(p) * whole, 1.0) : __builtin_inf();   // no share lies before the first, so it always stays
 }
 __device__ __forceinline__ double least_of(const SampleArgs& a, int row) {
   return a.min_p && a.min_p[row] > 0.f ? fmin(double(a.min_p[row]), 1.0) : 0.0;
@@ -1392,7 +1393,7 @@ void launch_chunks(const SampleArgs& a, hipStream_t stream) {
 template <int kType, int kChunk>
 void launch_open(const SampleArgs& a, hipStream_t stream) {
   const dim3 grid{uint32_t(a.num_rows) * uint32_t(a.num_chunks), 1, 1};
-  if (a.top_p) {
+  if (a.top_p || a.min_p) {
     hipLaunchKernelGGL((sample_bins_kernel<kType, kChunk>), grid, dim3(kChunkThreads), 0, stream, a);
     hipLaunchKernelGGL((sample_collect_kernel<kType, kChunk>), grid, dim3(kChunkThreads), 0, stream, a);
   }

@@ -268,7 +268,7 @@ struct SampleRow {
   uint64_t above;    // sum of those before the step in which the share is reached
   float top;         // the row's largest logit
   float bound;       // no entry below it stays
-  int32_t open;      // 0: done; 1 + its place: a top-p to be found by all chunks; -1: any cuts, by one workgroup
+  int32_t open;      // 0: done; 1 + its place: for all of its chunks; -1: any cuts, by one workgroup
   uint32_t listed;   // entries of that step
 };
 struct SampleArgs {

@@ -783,3 +783,17 @@ def test_sample_more_flat_rows_than_places():
     token, logprob, kept = B.Sampler()(x, u, top_p=top_p)
     check_samples(x[:2], u[:2], (token[:2], logprob[:2], kept[:2]), top_p=top_p[:2])
     assert (token == token[0]).all() and (logprob == logprob[0]).all() and (kept == kept[0]).all()
+
+
+@pytest.mark.parametrize("vocab, dtype", [(9001, torch.float32), (50001, torch.bfloat16)])
+def test_sample_min_p_of_a_flat_row(vocab, dtype):
+    """More entries stay than a list holds, with and without a top-p among the rows."""
+    rng = np.random.default_rng(vocab)
+    x = torch.from_numpy((0.3 * rng.standard_normal((6, vocab))).astype(np.float32)).to(dtype)
+    x[4] = x[4] * 10
+    x[5] = 0.0
+    x, u = x.cuda(), cuda([0.0, 0.3, 0.999, 0.5, 0.8, 0.6], torch.float32)
+    for params in (dict(min_p=cuda([0.01, 0.05, 0.2, 0.3, 0.0001, 1.0], torch.float32)),
+                   dict(min_p=cuda([0.3, 0.3, 0.0, 0.4, 0.2, 0.5], torch.float32),
+                        top_p=cuda([1.0, 0.9, 0.9, math.nan, 0.99, 0.5], torch.float32))):
+        check_samples(x, u, B.Sampler()(x, u, **params), **params)
