@@ -29,12 +29,20 @@ int32_t pages_of(int32_t tokens) { return (tokens + kPage - 1) / kPage; }
 int32_t blocks_together(int32_t blocks) { return std::min(blocks, kSharedWaves); }
 int32_t splits_of(int32_t blocks) { return blocks == 1 ? 1 : kSharedWaves / blocks_together(blocks); }
 
-// Cost of a prompt's page, per mille of one that a wave reads for itself: memory
-// gives it once, and a block of rows takes its time on the matrix cores, which in pages
-// of half the bytes is twice as many. Measured, us at 250, 320, 400 and 500 per block: 16 prompts of 2048
-// tokens with 16 members (28/4 heads) 147, 128, 116, 119; one of 32760 with 64 (32/8) 101, 90, 95, 97; one of 4000
-// with 256 200, 181, 179, 182; 8 of 8000 with 8 (40/8, fp8) at 500, 640, 800 and 1000 98, 90, 85, 81.
-int64_t page_cost(int32_t blocks, bool fp8) { return std::max<int64_t>(1000, (fp8 ? 1000 : 400) * int64_t(blocks)); }
+// What a page costs, ns of one wave. One that a wave reads for itself (a prompt of one block, too): its latency, where
+// waves of prompts leave memory to spare. One prompt of 32760 tokens with 64 members (32/8 heads) at 1450, 1700 and
+// 2450: 95, 89 and 93 us; 8 of 8000 with 8 (40/8, fp8) at 900, 1000 and 1300: 84, 81 and 85.
+double own_cost(const sf_attn_desc& d, bool fp8) { return fp8 ? 1000 : d.head_dim == 64 ? 950 : 1700; }
+// Of a prompt whose rows several waves hold: the time of its blocks of rows on their waves' matrix and vector units, at least
+// the staging by eight waves.
+double page_cost(const sf_attn_desc& d, int32_t blocks, bool fp8) {
+  if (blocks == 1) return own_cost(d, fp8);
+  return std::max(2000.0, (fp8 ? 1300 : 980) * (d.head_dim == 64 ? 0.63 : 1.0) * blocks);
+}
+// Own pages take up to kShort times their latency where all bytes at kBytesPerNs take longer than all waves' work;
+// prompts, read ahead further, feel that less. 16 prompts of 2048 tokens with 16 members (28/4; half as much work
+// as bytes) at 1.45 and 1.3: 109 and 102 us.
+constexpr double kShort = 1.3, kBytesPerNs = 5000;
 
 // A group whose prompt is read once.
 struct Prompt {
@@ -52,7 +60,7 @@ struct Prompt {
 struct Track {
   int32_t blocks;
   int64_t pages = 0;
-  int64_t cost = 0;
+  double cost = 0;         // ns of all waves
   int64_t columns = 0;     // runs; blocks > 1: of workgroups
   std::vector<int32_t> prompts;
 };
@@ -76,7 +84,7 @@ struct Scratch {
   std::vector<Unit> units;       // of prompts
   std::vector<int32_t> prompt_of;    // per sequence: index, -1
   std::vector<Unit> own;         // per (sequence, KV head)
-  std::vector<int64_t> start;    // per sequence: first own page
+  std::vector<int64_t> start;    // per sequence: its first place among the own pages'
 };
 
 void put_fields(int32_t* row, int32_t seq0, int32_t source, int32_t kvh, int32_t pb, int32_t pe, int32_t end, int32_t slot,
@@ -147,32 +155,50 @@ sf_status plan(const sf_attn_desc* desc, const int32_t* lens, int32_t num_groups
     }
     p.start = track->pages;
     track->pages += int64_t(pages) * hkv;
-    track->cost += int64_t(pages) * hkv * page_cost(p.blocks, fp8);
+    track->cost += double(pages) * hkv * page_cost(*desc, p.blocks, fp8);
     track->prompts.push_back(int32_t(t.prompts.size()));
     t.prompts.push_back(p);
   }
   // many blocks first: a prompt's blocks then fill whole workgroups
   std::sort(t.tracks.begin(), t.tracks.end(), [](const Track& x, const Track& y) { return x.blocks > y.blocks; });
-  int64_t own_pages = 0, cost = 0;
+  // What sequences have to themselves, end to end: of each (sequence, KV head), kSegmentPages places for its start, then its pages.
+  int64_t own_pages = 0, own_places = 0;
   for (int32_t s = 0; s < n; ++s) {
-    t.start[s] = own_pages;
-    own_pages += int64_t(pages_of(lens[s]) - (t.prompt_of[s] >= 0 ? t.prompts[t.prompt_of[s]].pages : 0)) * hkv;
+    const int32_t pages = pages_of(lens[s]) - (t.prompt_of[s] >= 0 ? t.prompts[t.prompt_of[s]].pages : 0);
+    t.start[s] = own_places;
+    own_pages += int64_t(pages) * hkv;
+    if (pages) own_places += (pages + kSegmentPages) * hkv;
   }
-  cost = (own_pages + kSegmentPages * int64_t(n) * hkv) * 1000;
-  for (const Track& x : t.tracks) cost += x.cost;
+  const double own_work = double(own_places) * own_cost(*desc, fp8);
+  double alone_work = own_work, all_work = own_work, all_pages = double(own_pages);
+  for (const Track& x : t.tracks) {
+    all_work += x.cost;
+    if (x.blocks == 1) alone_work += x.cost;
+    all_pages += double(x.pages);
+  }
+  const double bytes = all_pages * kPage * desc->head_dim * (fp8 ? 2 : 4);
+  const double at_memory = bytes / kBytesPerNs * kSharedWaves * cus;   // ns of all waves
+  const double slower = all_work > 0.0 ? std::min(kShort, std::max(1.0, at_memory / all_work)) : 1.0;
+  for (Track& x : t.tracks)
+    if (x.blocks == 1) x.cost *= slower;
+  const double cost = all_work + alone_work * (slower - 1.0);
   // waves: two per SIMD, fewer rather than thinner runs
-  const int64_t waves = std::max<int64_t>(1, std::min<int64_t>(int64_t(kSharedWaves) * cus, cost / 1000 / least));
+  const int64_t waves = std::max<int64_t>(1, std::min<int64_t>(int64_t(kSharedWaves) * cus, int64_t(cost / (own_cost(*desc, fp8) * least))));
   // Prompts of several blocks take whole workgroups, the first ones; the other
   // waves (prompts of one block, then the sequences' own pages) are spread over the rest.
   int64_t groups = 0, alone = 0;
   for (Track& x : t.tracks) {
-    const double share = double(waves) * double(x.cost) / double(cost);
+    const double share = double(waves) * x.cost / cost;
     if (x.blocks == 1) {
       x.columns = std::max<int64_t>(1, std::min<int64_t>(x.pages, int64_t(share)));
       alone += x.columns;
     } else {
       const int32_t each = (x.blocks + kSharedWaves - 1) / kSharedWaves;
       x.columns = std::max<int64_t>(1, std::min<int64_t>(x.pages, int64_t(share / kSharedWaves / each)));
+      // Runs that end with every KV head's pages spare a second start: 27 for each of 8 KV heads 89 us, 221 for all 8 95.
+      const int64_t units = int64_t(x.prompts.size()) * hkv, over = x.columns % units;
+      const bool alike = x.pages == units * t.prompts[size_t(x.prompts[0])].pages;   // (or none is cut right but by chance)
+      if (alike && over * 32 <= x.columns && x.columns > over) x.columns -= over;
       groups += x.columns * each;
     }
   }
@@ -200,14 +226,14 @@ sf_status plan(const sf_attn_desc* desc, const int32_t* lens, int32_t num_groups
       }
     }
   }
-  const Runs own_runs = {own_pages, own_columns};
+  const Runs own_runs = {own_places, own_columns};
   t.own.resize(size_t(n) * hkv);
   for (int32_t s = 0; s < n; ++s) {
     const bool has_prompt = t.prompt_of[s] >= 0;
     const int32_t pages = pages_of(lens[s]) - (has_prompt ? t.prompts[t.prompt_of[s]].pages : 0);
     for (int32_t h = 0; h < hkv; ++h) {
       Unit& u = t.own[size_t(s) * hkv + h];
-      const int64_t begin = t.start[s] + int64_t(h) * pages;
+      const int64_t begin = t.start[s] + h * (pages + kSegmentPages) + kSegmentPages;
       u.parts = pages ? own_runs.parts(begin, begin + pages) : 0;
       u.base = -1;
       items += u.parts;
@@ -300,25 +326,29 @@ sf_status plan(const sf_attn_desc* desc, const int32_t* lens, int32_t num_groups
           for (int32_t w = 0; w < kSharedWaves; ++w) emit(c, k * kSharedWaves + w % together, w / together);
   }
   if (own_columns > 0) {
-    int64_t page = 0, col = 0;
+    int64_t col = 0;
     int32_t first = item;
+    auto close_until = [&](int64_t place) {
+      for (; col < own_columns && own_runs.at(col + 1) <= place; ++col) {
+        close_worker(first);
+        next_alone();
+        first = item;
+      }
+    };
     for (int32_t s = 0; s < n; ++s) {
       const int32_t skip = t.prompt_of[s] >= 0 ? t.prompts[t.prompt_of[s]].pages : 0;
       const int32_t pages = pages_of(lens[s]) - skip;
       for (int32_t h = 0; h < hkv && pages > 0; ++h) {
         const Unit& u = t.own[size_t(s) * hkv + h];
-        const int64_t begin = page, end = page + pages;
-        for (int32_t part = 0; page < end; ++part) {
+        const int64_t begin = t.start[s] + h * (pages + kSegmentPages) + kSegmentPages, end = begin + pages;
+        int64_t at = begin;
+        close_until(at);
+        for (int32_t part = 0; at < end; ++part) {
           const int64_t stop = std::min(end, own_runs.at(col + 1));
-          put_fields(list + int64_t(item++) * kSharedInts, s, s, h, skip + int32_t(page - begin), skip + int32_t(stop - begin),
+          put_fields(list + int64_t(item++) * kSharedInts, s, s, h, skip + int32_t(at - begin), skip + int32_t(stop - begin),
                      lens[s], u.base < 0 ? -1 : u.base + part * g, 0, g, g);
-          page = stop;
-          if (page == own_runs.at(col + 1)) {
-            close_worker(first);
-            next_alone();
-            first = item;
-            ++col;
-          }
+          at = stop;
+          close_until(at);
         }
       }
     }
