@@ -860,8 +860,9 @@ sf_status sf_route(const sf_cost_model* model, double mu, int32_t min_initial_ve
  * L_s > 0. Members with L_s = 0 get out = 0, lse = -inf.
  *
  * Plan (host only). A prompt's rows, members times g, are taken in blocks of at most 32 (2 tiles of 16): 1 (up to 16 rows),
- * 2, 4 or a multiple of 8 blocks, which walk the same pages side by side; the pages of all prompts with one number of blocks, and those that
- * sequences have to themselves, are each cut into equal runs, one per wave, as many runs as their share of the work.
+ * 2, 4 or a multiple of 8 blocks, which walk the same pages side by side; the pages of all prompts with one number of
+ * blocks, and those that sequences have to themselves (the start of one counts as two pages), are each cut into equal
+ * runs, one per wave, as many runs as their share of the work.
  * Results of runs that end inside a prompt or sequence, and of all prompts, go to the workspace and are joined by a
  * second launch. fp8 = 1: for an fp8 cache, whose pages are half the bytes at the same arithmetic (only the shares go by
  * it: the plan runs over either). Of opts, num_cus and min_chunk_pages (default 4) count.

@@ -1555,9 +1555,8 @@ class DecodeAttention:
         keys and the values into the pages of a bf16 cache (sf_rotary_store, through the runner). rotary: a Rotary, or
         None (nothing turns); q, k_new, v_new: bf16 [T, H, D], parts of wider rows allowed (q may be None). q_lens None is
         a decode step: a row per sequence, of which the running ones' (seq_lens[s] > 0) last token is new (the others' rows
-        of q_out are not written). first_pos: host
-        int32 [B], the first new token's position (default: its index in the cache); new_pages as in store_fp8. Returns the
-        turned queries: q_out (may be q), by default a new tensor."""
+        of q_out are not written). first_pos: host int32 [B], the first new token's position (default: its index in the
+        cache); new_pages as in store_fp8. Returns the turned queries: q_out (may be q), by default a new tensor."""
         desc, lens = self._call_desc(k_pool, block_table, seq_lens, 1.0)
         n = lens.size
         qls, first, pages = (_host_i32(x, name, n) for x, name in ((q_lens, "q_lens"), (first_pos, "first_pos"),
@@ -1692,7 +1691,7 @@ class Sampler:
     def __init__(self, device=None):
         self.device = torch.device("cuda" if device is None else device)
         self._L = lib()
-        self._desc, self._bytes, self._key = sf_sample_desc(), ctypes.c_uint64(), None
+        self._last = (None, None, 0)   # (shape, desc, workspace bytes) of the last call
 
     def __call__(self, logits, uniform, temperature=None, top_k=None, top_p=None, min_p=None, token=None, logprob=None,
                  kept=None, stream=None):
@@ -1705,6 +1704,8 @@ class Sampler:
         if code is None:
             raise ValueError(f"logits must be float32, bfloat16 or float16 (got {logits.dtype})")
         b, v = logits.shape
+        if max(b, v) >= 1 << 31:
+            raise ValueError(f"logits of {b} x {v} are more than a call takes")
         stride = logits.stride(0) if b > 1 else v
         if (v > 1 and logits.stride(1) != 1) or stride < v:
             raise ValueError("a row's logits must be contiguous, and rows must not overlap")
@@ -1714,20 +1715,21 @@ class Sampler:
             if t is not None:
                 _dev(t, name, dtype, (b,))
         key = (b, v, stride, code)
-        desc = self._desc
-        if key != self._key:
-            desc.num_rows, desc.vocab, desc.row_stride, desc.dtype = key
-            _check("sf_sample_workspace", self._L.sf_sample_workspace(ctypes.byref(desc), ctypes.byref(self._bytes)))
-            self._key = key
+        last, desc, size = self._last
+        if key != last:   # kept only once it is known to be good
+            desc, need = sf_sample_desc(*key, 0), ctypes.c_uint64()
+            _check("sf_sample_workspace", self._L.sf_sample_workspace(ctypes.byref(desc), ctypes.byref(need)))
+            size = need.value
+            self._last = (key, desc, size)
         with _on_device(logits.device), torch.cuda.stream(stream) if stream else _HERE:
             made = []
             for t, name, dtype in ((token, "token", torch.int32), (logprob, "logprob", torch.float32), (kept, "kept", torch.float32)):
                 made.append(torch.empty((b,), dtype=dtype, device=logits.device) if t is None else _dev(t, name, dtype, (b,)))
-            workspace = torch.empty((max(16, self._bytes.value),), dtype=torch.uint8, device=logits.device)
+            workspace = torch.empty((max(16, size),), dtype=torch.uint8, device=logits.device)
             _check("sf_sample", self._L.sf_sample(
                 ctypes.byref(desc), logits.data_ptr(), _addr(temperature), _addr(top_k), _addr(top_p), _addr(min_p),
                 uniform.data_ptr(), made[0].data_ptr(), made[1].data_ptr(), made[2].data_ptr(), workspace.data_ptr(),
-                self._bytes.value, stream.cuda_stream if stream else _current_stream(logits.device)))
+                size, stream.cuda_stream if stream else _current_stream(logits.device)))
         return tuple(made)
 
 

@@ -797,3 +797,14 @@ def test_sample_min_p_of_a_flat_row(vocab, dtype):
                    dict(min_p=cuda([0.3, 0.3, 0.0, 0.4, 0.2, 0.5], torch.float32),
                         top_p=cuda([1.0, 0.9, 0.9, math.nan, 0.99, 0.5], torch.float32))):
         check_samples(x, u, B.Sampler()(x, u, **params), **params)
+
+
+def test_sample_after_a_refused_call():
+    """A shape that is refused leaves nothing behind for the next call of the one before it."""
+    S, u = B.Sampler(), cuda([0.3, 0.8], torch.float32)
+    x = torch.randn(2, 1000, generator=torch.Generator().manual_seed(5)).cuda()
+    want = [t.clone() for t in S(x, u)]
+    with pytest.raises(B.SfError):
+        S(torch.zeros(2, (1 << 19) + 1, device="cuda"), u)
+    for a, b in zip(S(x, u), want):
+        assert torch.equal(a, b)
