@@ -449,7 +449,9 @@ __device__ __forceinline__ void draw_row(const SampleArgs& a, int row, Drawn& sh
         sh.top = w.top;
         sh.chunk_top = c.top;
         sh.total = w.total;
-        sh.want = fmin((target - before) / s.weight(c.top), double(c.sum) - 1.0);
+        // (below the sum as a double holds it, which is some thread's end: c.sum - 1 is c.sum again beyond 2^53)
+        const double sum = double(c.sum), below = __builtin_bit_cast(double, __builtin_bit_cast(uint64_t, sum) - 1);
+        sh.want = fmin((target - before) / s.weight(c.top), below);
       }
       chunk = last;
     }
