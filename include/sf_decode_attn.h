@@ -857,7 +857,8 @@ sf_status sf_route(const sf_cost_model* model, double mu, int32_t min_initial_ve
  * shared_lens[i] / 16 entries of the other members' rows are not read. Tokens behind those pages, the rest of the
  * shared ones among them, come from each member's own row. Groups lie one behind the other and cover the batch
  * (group_offsets[0] = 0, group_offsets[num_groups] = num_seqs); shared_lens[i] is at most L_s of every member with
- * L_s > 0. Members with L_s = 0 get out = 0, lse = -inf.
+ * L_s > 0. Members with L_s = 0 get out = 0, lse = -inf. A member's bits follow from its own query, its tokens and the
+ * batch's lengths: what other members' queries hold (or those with L_s = 0, which may be read) does not change them.
  *
  * Plan (host only). A prompt's rows, members times g, are taken in blocks of at most 32 (2 tiles of 16): 1 (up to 16 rows),
  * 2, 4 or a multiple of 8 blocks, which walk the same pages side by side; the pages of all prompts with one number of

@@ -263,7 +263,8 @@ __device__ __forceinline__ float sum8(const float* p) {
 
 // c0, c1: factors of the two pages' scores in log2 units; v0, v1: value scales (fp8).
 // A lane's sum of weights bounds each of them; until one passes the headroom (the first
-// block's does: m is -inf) lanes of a row need not agree on its maximum, and nothing is exchanged.
+// block's does: m is -inf) lanes of a row need not agree on its maximum, and nothing is exchanged. Only the rows
+// that passed it move their reference: a row's bits are its own, whatever the other sequences' rows of its tile hold.
 template <int D, bool kFp8>
 __device__ __forceinline__ Weights weigh(Tile<D>& t, const f32x4& s0, const f32x4& s1, float c0, float c1, float v0, float v1,
                                          int valid, const Lane& l) {
@@ -280,13 +281,17 @@ __device__ __forceinline__ Weights weigh(Tile<D>& t, const f32x4& s0, const f32x
 #pragma unroll
   for (int e = 0; e < 8; ++e) p[e] = exp2_fast(z[e] - t.m);
   float part = sum8(p);
-  if (__any(!(part <= kHeadroom))) {
+  float past = part <= kHeadroom ? 0.f : 1.f;
+  if (__any(past != 0.f)) {
+    past = fmaxf(past, l.across(past, 16));
+    past = fmaxf(past, l.across(past, 32));
+    const bool moves = past != 0.f;   // (every row without a reference so far does)
     float top = fmaxf(fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3])), fmaxf(fmaxf(z[4], z[5]), fmaxf(z[6], z[7])));
     top = fmaxf(top, l.across(top, 16));
     top = fmaxf(top, l.across(top, 32));
-    const float m = fmaxf(t.m, top);
+    const float m = moves ? fmaxf(t.m, top) : t.m;
     const float ref = m == -__builtin_inff() ? 0.f : m;   // no key with a finite score so far
-    const float keep = exp2_fast(t.m - ref);
+    const float keep = moves ? exp2_fast(t.m - ref) : 1.f;
     t.m = m;
     t.sum *= keep;
 #pragma unroll

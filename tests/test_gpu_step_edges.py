@@ -1,10 +1,12 @@
 """GPU tests of a group rollout's step at its edges. Tolerances as in tests/test_gpu_step.py."""
+import math
+
 import numpy as np
 import pytest
 import torch
 
 from paper_2601_12784_amd import binding as B
-from tests.test_gpu_step import check_samples, cuda
+from tests.test_gpu_step import Grouped, check_samples, cuda, randn
 
 pytestmark = pytest.mark.gpu
 
@@ -39,3 +41,35 @@ def test_draws_at_the_border_of_equal_chunks(rows, block, chunks, dtype, cut):
     assert (logprob < 0).all() and (kept == 1).all()
     some = list(range(0, b, 16))
     check_samples(x[some], u[some], (token[some], logprob[some], kept[some]), **{k: t[some] for k, t in params.items()})
+
+
+# ---------------------------------------------------------------------------
+# attention over shared prompts
+# ---------------------------------------------------------------------------
+@pytest.mark.parametrize("hq,hkv,d", [(14, 2, 64), (14, 2, 128)])
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("members", [2, 4, 10, 20])
+def test_a_members_bits_are_its_own(members, fp8, hq, hkv, d):
+    """Rows of several members share a wave. Whatever the others' queries hold, large ones whose references move at
+    many blocks, NaN, infinities, or a place whose sequence has left: every bit of the rest stays."""
+    prefix = 805
+    lens = [prefix + 1 + 7 * s for s in range(members)]
+    if members > 2:
+        lens[2] = 0
+    cache = Grouped(lens, [0, members], [prefix], hkv, d, fp8, seed=members)
+    q = randn(np.random.default_rng(d), members, hq, d)
+    attn = B.DecodeAttention(hq, hkv, d)
+    others = [s for s in range(members) if s % 2 == 0]
+    rest = [s for s in range(members) if s % 2]
+
+    def run(q):
+        lse = torch.empty(members, hq, device="cuda")
+        return attn.shared(q, cache.g_k, cache.g_v, cache.g_bt, lens, [0, members], [prefix], 1.0 / math.sqrt(d), lse=lse, fp8=cache.g_fp8), lse
+
+    out, lse = run(q)
+    cache.check(q, out, lse, 1.0 / math.sqrt(d), hq)
+    for what, value in (("large", q[others] * 40), ("nan", math.nan), ("inf", math.inf)):
+        changed = q.clone()
+        changed[others] = value
+        got, got_lse = run(changed)
+        assert torch.equal(got[rest], out[rest]) and torch.equal(got_lse[rest], lse[rest]), what
