@@ -323,6 +323,15 @@ def _on_device(device):
     return torch.cuda.device(device)
 
 
+def _made_on(stream, device):
+    """Where a call on `stream` makes its tensors: memory of the current stream may still be in use there by what came before."""
+    if stream is None:
+        return _HERE
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(int(stream), device=device)
+    return torch.cuda.stream(stream)
+
+
 def _stream(stream) -> int | None:
     if stream is None:
         return _current_stream()
@@ -1045,7 +1054,8 @@ class ExtendAttention:
         if DEBUG_CHECKS:
             check_block_table(desc, block_table, np.where(qls > 0, lens, 0))
         if out is None:
-            out = torch.empty((rows, self.hq, self.d), dtype=torch.float32, device=self.device)
+            with _made_on(stream, self.device):
+                out = torch.empty((rows, self.hq, self.d), dtype=torch.float32, device=self.device)
         _check_extend(desc, rows, q, k_pool, v_pool, block_table, out, lse, k_new, v_new, fp8)
         info = sf_extend_info()
         tensors = (q, k_pool, v_pool, block_table, out, lse, k_new, v_new, fp8)
@@ -1323,7 +1333,7 @@ class DecodeAttention:
         self._desc_key = None
         self._desc = self._desc_ref = None
         self._stepped = False
-        self._lse = None
+        self._lse, self._old_lse = None, []
         self._host_checked = False   # set by a caller that checked its own host copy
 
     def _runner(self, chunk_pages):
@@ -1403,7 +1413,8 @@ class DecodeAttention:
         b = q.shape[0]
         main = stream.cuda_stream if stream else _current_stream(self.device)
         if out is None:
-            out = torch.empty((b, self.hq, self.d), dtype=torch.float32, device=self.device)
+            with _made_on(stream, self.device):
+                out = torch.empty((b, self.hq, self.d), dtype=torch.float32, device=self.device)
         self._check_tensors(q, k_pool, v_pool, block_table, out, lse, fp8)
         dkey = (b, block_table.shape[1], k_pool.shape[0], float(scale))
         if dkey != self._desc_key:
@@ -1434,7 +1445,9 @@ class DecodeAttention:
             ex.k_new, ex.v_new, ex.new_pages_host = k_new.data_ptr(), v_new.data_ptr(), _host_addr(pages)
             if lse is None and fp8 is None:  # the merge reads lse back: keep one of our own
                 if self._lse is None or self._lse.numel() < b * self.hq:
-                    self._lse = torch.empty(b * self.hq * 5 // 4 + 64, dtype=torch.float32, device=self.device)
+                    self._old_lse.append(self._lse)   # calls on other streams may still write it
+                    with _made_on(stream, self.device):
+                        self._lse = torch.empty(b * self.hq * 5 // 4 + 64, dtype=torch.float32, device=self.device)
                 lse = self._lse[: b * self.hq].view(b, self.hq)
         if fp8 is not None:
             ex.k_scale, ex.v_scale = fp8[0].data_ptr(), fp8[1].data_ptr()
@@ -1534,7 +1547,8 @@ class DecodeAttention:
         start with (host int32 arrays). The result is the plain step's over each sequence's seq_lens[s] tokens. out: fp32
         (default) or bf16 [B, Hq, D]; fp8 = (k_scale, v_scale) of an fp8 cache."""
         if out is None:
-            out = torch.empty((q.shape[0], self.hq, self.d), dtype=torch.float32, device=self.device)
+            with _made_on(stream, self.device):
+                out = torch.empty((q.shape[0], self.hq, self.d), dtype=torch.float32, device=self.device)
         desc, lens = self._call_desc(k_pool, block_table, seq_lens, scale)
         lens, offsets, shared = _host_groups(lens.size, lens, group_offsets, shared_lens)
         _check_step(desc, q, k_pool, v_pool, block_table, out, lse, fp8)

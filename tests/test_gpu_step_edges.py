@@ -6,6 +6,7 @@ import pytest
 import torch
 
 from paper_2601_12784_amd import binding as B
+from tests.test_gpu_cache import Cache
 from tests.test_gpu_step import Grouped, check_samples, cuda, randn
 
 pytestmark = pytest.mark.gpu
@@ -73,3 +74,55 @@ def test_a_members_bits_are_its_own(members, fp8, hq, hkv, d):
         changed[others] = value
         got, got_lse = run(changed)
         assert torch.equal(got[rest], out[rest]) and torch.equal(got_lse[rest], lse[rest]), what
+
+
+# ---------------------------------------------------------------------------
+# tensors that a call makes
+# ---------------------------------------------------------------------------
+def stream_of(t):
+    """The stream whose memory a tensor lies in."""
+    for seg in torch.cuda.memory_snapshot():
+        if seg["address"] <= t.data_ptr() < seg["address"] + seg["total_size"]:
+            return seg["stream"]
+    raise AssertionError("not torch's memory")
+
+
+def test_results_belong_to_the_stream_that_writes_them():
+    """Memory of the current stream may still be read there by what came before: a call on another stream must not
+    take its result from it."""
+    cache = Grouped([200, 130, 161], [0, 3], [128], 2, 64, False, seed=5)
+    table = torch.from_numpy(cache.bt).cuda()
+    lens = np.array(cache.lens, np.int32)
+    q, kv = randn(np.random.default_rng(0), 3, 8, 64), randn(np.random.default_rng(1), 3, 2, 64)
+    attn, extend, side = B.DecodeAttention(8, 2, 64), B.ExtendAttention(8, 2, 64), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    calls = dict(
+        shared=lambda s: attn.shared(q, cache.g_k, cache.g_v, cache.g_bt, lens, [0, 3], [128], 0.1, stream=s),
+        step=lambda s: attn(q, cache.g_k, cache.g_v, table, lens, 0.1, stream=s),
+        append=lambda s: attn(q, cache.g_k, cache.g_v, table, lens, 0.1, stream=s, append=(kv, kv, np.full(3, -1, np.int32))),
+        extend=lambda s: extend(q, cache.g_k, cache.g_v, table, lens, [1, 1, 1], 0.1, stream=s),
+        extend_handle=lambda s: extend(q, cache.g_k, cache.g_v, table, lens, [1, 1, 1], 0.1, stream=s and s.cuda_stream),
+    )
+    for name, call in calls.items():
+        out = call(side)
+        side.synchronize()
+        assert stream_of(out) == side.cuda_stream, name
+        if name == "append":
+            assert stream_of(attn._lse) == side.cuda_stream
+        here = call(None)
+        torch.cuda.synchronize()
+        assert stream_of(here) == torch.cuda.current_stream().cuda_stream and torch.equal(here, out), name
+
+
+def test_an_appending_steps_own_lse_outlives_a_larger_one():
+    """The buffer that a larger batch replaces may still be written by a call on another stream."""
+    attn = B.DecodeAttention(8, 2, 64)
+    buffers = []
+    for n in (1, 100):
+        cache = Cache([20] * n, 2, 64, False, seed=5)
+        q, kv = randn(np.random.default_rng(0), n, 8, 64), randn(np.random.default_rng(1), n, 2, 64)
+        attn(q, cache.g_k, cache.g_v, cache.g_bt, np.full(n, 20, np.int32), 0.1, append=(kv, kv, np.full(n, -1, np.int32)))
+        buffers.append(attn._lse.data_ptr())
+        torch.cuda.synchronize()
+    taken = [torch.empty(8 * 5 // 4 + 64, device="cuda") for _ in range(64)]
+    assert buffers[0] not in [t.data_ptr() for t in taken]
