@@ -932,7 +932,7 @@ sf_status sf_rotary_turns(const double* freq_host, int32_t n, uint64_t* turns_ho
  * Turns the queries and keys of num_tokens tokens, token i by positions[i] (device int32). turns: device, R/2 of them.
  * q, k (bf16, either may be NULL: not turned): head h of token i starts at q + i * q_stride + h * D, in elements, so
  * both may be parts of a wider tensor; outputs likewise. An output may be its own input (same pointer and stride);
- * otherwise it must not overlap an input. Pointers are 16-byte aligned, strides a multiple of 8 and at least the heads'
+ * otherwise it must not overlap an input, and never the other output (not checked here). Pointers are 16-byte aligned, strides a multiple of 8 and at least the heads'
  * num_q_heads * D (num_kv_heads * D). One launch on the stream; nothing is allocated, so it can be captured.
  */
 sf_status sf_rotary(const sf_rotary_desc* rotary, int32_t num_tokens, int32_t num_q_heads, int32_t num_kv_heads,

@@ -767,15 +767,21 @@ def _extent(t):
     return at, at + (sum((n - 1) * s for n, s in zip(t.shape, t.stride())) + 1) * t.element_size() if t.numel() else at
 
 
+def _overlap(a, b):
+    (a0, a1), (b0, b1) = _extent(a), _extent(b)
+    return a0 < b1 and b0 < a1 and not _interleaved(a, b)
+
+
 def _check_turned(x, x_out, name, others):
-    """An output is its input's own place, or overlaps none."""
+    """An output is its input's own place, or overlaps none. (x among the others twice is read by another part of the
+    call, too.)"""
+    others = list(others)
     if x_out.data_ptr() == x.data_ptr() and x_out.stride() == x.stride():
-        others = [t for t in others if t is not x]
-    a, b = _extent(x_out)
-    for t in others:
-        c, e = _extent(t)
-        if a < e and c < b and not _interleaved(x_out, t):
-            raise ValueError(f"{name} overlaps an input")
+        own = next((i for i, t in enumerate(others) if t is x), None)
+        if own is not None:
+            del others[own]
+    if any(_overlap(x_out, t) for t in others):
+        raise ValueError(f"{name} overlaps an input")
 
 
 def _interleaved(a, b):
@@ -1685,8 +1691,8 @@ class Rotary:
             _check_turned(x, out, name + "_out", ins)
             args += [x.data_ptr(), stride, out.data_ptr(), out_stride]
             outs.append(out)
-        if q_out is not None and k_out is not None:
-            _check_turned(q_out, k_out, "k_out", [q_out])
+        if q_out is not None and k_out is not None and _overlap(q_out, k_out):
+            raise ValueError("k_out overlaps q_out")
         device = given.device
         with _on_device(device):
             _check("sf_rotary", lib().sf_rotary(

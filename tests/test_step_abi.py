@@ -470,3 +470,29 @@ def test_outputs_that_overlap_inputs_are_refused():
     y = gpu(7, 4, 64)
     with pytest.raises(ValueError):
         B._check_turned(y[:6], y[1:], "q_out", [y[:6]])
+
+
+def test_outputs_in_place_of_what_is_read_twice_are_refused():
+    """One tensor as queries and keys (or values): turned in place, one part of the call would read what another has written."""
+    x, y, at = gpu(6, 4, 64), gpu(6, 4, 64), gpu(6, dtype=torch.int32)
+    B._check_turned(x, y, "q_out", [x, x])
+    with pytest.raises(ValueError):
+        B._check_turned(x, x, "q_out", [x, x])
+    rotary = B.Rotary(64)
+    for kw in (dict(q_out=x), dict(q_out=y, k_out=x), dict(q_out=x, k_out=y)):
+        with pytest.raises(ValueError, match="overlaps an input"):
+            rotary(x, x, at, **kw)
+    attn = B.DecodeAttention(4, 4, 64, num_cus=256)
+    k_pool, v_pool = gpu(6, 4, 8, 16, 8), gpu(6, 4, 64, 16)
+    for k_new, v_new in ((x, y), (y, x), (x, x)):
+        with pytest.raises(ValueError, match="overlaps an input"):
+            attn.rotate_store(None, x, k_new, v_new, k_pool, v_pool, gpu(6, 1, dtype=torch.int32), [1] * 6, q_out=x)
+
+
+def test_outputs_that_overlap_each_other_are_refused():
+    q, k, at, wide = gpu(6, 4, 64), gpu(6, 4, 64), gpu(6, dtype=torch.int32), gpu(6, 8 * 64)
+    rotary, out = B.Rotary(64), gpu(6, 4, 64)
+    for a, b in ((out, out), (wide[:, :256].view(6, 4, 64), wide[:, 192:448].view(6, 4, 64)), (out, out.view(6, 4, 64))):
+        with pytest.raises(ValueError, match="k_out overlaps q_out"):
+            rotary(q, k, at, q_out=a, k_out=b)
+    assert not B._overlap(wide[:, :256].view(6, 4, 64), wide[:, 256:].view(6, 4, 64))
