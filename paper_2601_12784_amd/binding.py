@@ -1655,11 +1655,13 @@ class Rotary:
 
     def turns_on(self, device):
         """The turns per position as a tensor on the device (uploaded at the first call there)."""
-        t = self._on.get(device.index)
+        index = torch.cuda.current_device() if device.index is None else device.index   # "cuda" is the current one
+        t = self._on.get(index)
         if t is None:
             if torch.cuda.is_current_stream_capturing():
                 raise RuntimeError("a Rotary's first call on a device uploads its frequencies: make it before the capture")
-            t = self._on[device.index] = self._turns.to(device)
+            device = torch.device("cuda", index)
+            t = self._on[index] = self._turns.to(device)
             torch.cuda.current_stream(device).synchronize()   # other streams may be the next to read it
         return t
 

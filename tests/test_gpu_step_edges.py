@@ -7,7 +7,7 @@ import torch
 
 from paper_2601_12784_amd import binding as B
 from tests.test_gpu_cache import Cache
-from tests.test_gpu_step import Grouped, check_samples, cuda, randn
+from tests.test_gpu_step import Grouped, check_samples, check_turned, cuda, randn
 
 pytestmark = pytest.mark.gpu
 
@@ -126,3 +126,23 @@ def test_an_appending_steps_own_lse_outlives_a_larger_one():
         torch.cuda.synchronize()
     taken = [torch.empty(8 * 5 // 4 + 64, device="cuda") for _ in range(64)]
     assert buffers[0] not in [t.data_ptr() for t in taken]
+
+
+# ---------------------------------------------------------------------------
+# rotary positions
+# ---------------------------------------------------------------------------
+def test_a_rotary_made_for_the_current_device_can_be_captured():
+    """device="cuda" uploads the frequencies ahead, where the calls look for them."""
+    q, at = randn(np.random.default_rng(0), 5, 4, 64), torch.arange(5, dtype=torch.int32, device="cuda")
+    rotary = B.Rotary(64, device="cuda")
+    got, stream, graph = torch.empty_like(q), torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=stream):
+        rotary(q, None, at, q_out=got)
+    for _ in range(3):
+        q.copy_(randn(np.random.default_rng(1), 5, 4, 64))
+        graph.replay()
+        torch.cuda.synchronize()
+        check_turned(got, q, range(5), rotary, "replay")
+        assert torch.equal(got, rotary(q, None, at)[0])
+    assert rotary.turns_on(torch.device("cuda")) is rotary.turns_on(q.device)
