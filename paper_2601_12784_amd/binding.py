@@ -263,6 +263,34 @@ def check_block_table(desc: sf_attn_desc, block_table_host, seq_lens) -> None:
         raise SfError(f"sf_check_block_table (sequence {bad.value})", st)
 
 
+def _check_group_pages(desc, block_table, lens, offsets, shared) -> None:
+    """check_block_table for a step of groups: of the shared pages, the first running member's entries count. An entry of
+    another member there is not read; a page that is not the first member's is a mistake all the same."""
+    bt = np.array(block_table.cpu().numpy() if isinstance(block_table, torch.Tensor) else block_table, dtype=np.int32)
+    for i, tokens in enumerate(shared.tolist()):
+        # (offsets out of order or range, members shorter than what they share: the call itself refuses them)
+        a, b = (min(max(int(x), 0), lens.size) for x in offsets[i: i + 2])
+        live, common = [s for s in range(a, b) if lens[s] > 0], max(tokens, 0) // PAGE
+        for s in live[1:]:
+            own, first = bt[s, :common], bt[live[0], :common]
+            if np.any((own != first) & (own >= 0) & (own < desc.num_pages)):
+                raise ValueError(f"sequence {s} does not start with the pages of sequence {live[0]}, of whose group it is")
+            bt[s, :common] = first
+    check_block_table(desc, bt, lens)
+
+
+def _check_stored_pages(desc, block_table, lens, q_lens, new_pages) -> None:
+    """check_block_table for a store: the entries of the new tokens' pages (the earlier ones are not read), less those that
+    the call itself writes."""
+    bt = np.array(block_table.cpu().numpy() if isinstance(block_table, torch.Tensor) else block_table, dtype=np.int32)
+    named = np.zeros(lens.size, bool) if new_pages is None else new_pages >= 0
+    first, end = np.maximum(lens - q_lens, 0) // PAGE, -(-lens.astype(np.int64) // PAGE) - named
+    bt[np.arange(bt.shape[1])[None, :] < first[:, None]] = 0
+    check_block_table(desc, bt, np.where((q_lens > 0) & (end > first), end * PAGE, 0))
+    if new_pages is not None and np.any((new_pages < -1) | (new_pages >= desc.num_pages)):
+        raise ValueError("new_pages holds a page id outside the pool")
+
+
 def status_string(status: int) -> str:
     return lib().sf_status_string(int(status)).decode()
 
@@ -1497,10 +1525,7 @@ class DecodeAttention:
         _dev(v_new, "v_new", torch.bfloat16, (rows, self.hkv, self.d))
         _check_pools(desc.num_pages, self.hkv, self.d, k_pool8, v_pool8, block_table, lens.size, fp8)
         if DEBUG_CHECKS:
-            named = np.zeros(lens.size, bool) if pages is None else pages >= 0
-            check_block_table(desc, block_table, np.where(qls > 0, lens - named, 0))
-            if pages is not None and np.any((pages < -1) | (pages >= desc.num_pages)):
-                raise ValueError("new_pages holds a page id outside the pool")
+            _check_stored_pages(desc, block_table, lens, qls, pages)
         _check("sf_runner_store_fp8", self.L.sf_runner_store_fp8(
             self._runner(None), ctypes.byref(desc), _host_addr(lens), _host_addr(qls), k_new.data_ptr(), v_new.data_ptr(),
             _addr(pages), k_pool8.data_ptr(), v_pool8.data_ptr(), fp8[0].data_ptr(), fp8[1].data_ptr(),
@@ -1559,7 +1584,7 @@ class DecodeAttention:
         lens, offsets, shared = _host_groups(lens.size, lens, group_offsets, shared_lens)
         _check_step(desc, q, k_pool, v_pool, block_table, out, lse, fp8)
         if DEBUG_CHECKS and not self._host_checked:
-            check_block_table(desc, block_table, lens)
+            _check_group_pages(desc, block_table, lens, offsets, shared)
         self._host_checked = False
         k_scale, v_scale = fp8 if fp8 is not None else (None, None)
         _check("sf_runner_shared", self.L.sf_runner_shared(
@@ -1600,10 +1625,7 @@ class DecodeAttention:
             raise ValueError("q_out without q")
         _check_pools(desc.num_pages, self.hkv, self.d, k_pool, v_pool, block_table, n, None)
         if DEBUG_CHECKS and not self._host_checked:
-            named = np.zeros(n, bool) if pages is None else pages >= 0
-            check_block_table(desc, block_table, np.where((lens if qls is None else qls) > 0, lens - named, 0))
-            if pages is not None and np.any((pages < -1) | (pages >= desc.num_pages)):
-                raise ValueError("new_pages holds a page id outside the pool")
+            _check_stored_pages(desc, block_table, lens, (lens > 0).astype(np.int32) if qls is None else qls, pages)
         self._host_checked = False
         _check("sf_runner_rotary_store", self.L.sf_runner_rotary_store(
             self._runner(None), ctypes.byref(desc), rope, _host_addr(lens), _addr(qls), _addr(first), turns, _addr(q), sq,

@@ -146,3 +146,25 @@ def test_a_rotary_made_for_the_current_device_can_be_captured():
         check_turned(got, q, range(5), rotary, "replay")
         assert torch.equal(got, rotary(q, None, at)[0])
     assert rotary.turns_on(torch.device("cuda")) is rotary.turns_on(q.device)
+
+
+def test_debug_checks_accept_what_the_calls_allow(monkeypatch):
+    """Entries of shared pages in the other members' rows stay unfilled: stores and steps do not read them."""
+    monkeypatch.setattr(B, "DEBUG_CHECKS", True)
+    for fp8 in (False, True):
+        lens, offsets, shared = [50, 0, 49, 60, 20], [0, 4, 5], [48, 16]
+        cache = Grouped(lens, offsets, shared, 2, 64, fp8, seed=3)
+        attn = B.DecodeAttention(8, 2, 64)
+        q, kv = randn(np.random.default_rng(0), 5, 8, 64), randn(np.random.default_rng(1), 5, 2, 64)
+        page = int(cache.g_bt[2, 3])
+        cache.g_bt[2, 3] = -1       # a page that the call opens
+        fresh = np.array([-1, -1, page, -1, -1], np.int32)
+        if fp8:
+            attn.store_fp8(kv[:4], kv[:4], cache.g_k, cache.g_v, cache.g_fp8, cache.g_bt, lens, [1, 0, 1, 1, 1], new_pages=fresh)
+        else:
+            attn.rotate_store(B.Rotary(64), q, kv, kv, cache.g_k, cache.g_v, cache.g_bt, lens, new_pages=fresh)
+        attn.shared(q, cache.g_k, cache.g_v, cache.g_bt, lens, offsets, shared, 0.1, fp8=cache.g_fp8)
+        cache.g_bt[3, 0] = page
+        with pytest.raises(ValueError, match="sequence 3 does not start with"):
+            attn.shared(q, cache.g_k, cache.g_v, cache.g_bt, lens, offsets, shared, 0.1, fp8=cache.g_fp8)
+        torch.cuda.synchronize()

@@ -496,3 +496,51 @@ def test_outputs_that_overlap_each_other_are_refused():
         with pytest.raises(ValueError, match="k_out overlaps q_out"):
             rotary(q, k, at, q_out=a, k_out=b)
     assert not B._overlap(wide[:, :256].view(6, 4, 64), wide[:, 256:].view(6, 4, 64))
+
+
+# ---------------------------------------------------------------------------
+# SF_DEBUG_CHECKS: the block-table entries that a call reads
+# ---------------------------------------------------------------------------
+def _refused(check, *args):
+    try:
+        check(*args)
+    except (ValueError, B.SfError):
+        return True
+    return False
+
+
+def test_debug_check_of_shared_pages():
+    lens, offsets, shared = np.array([70, 0, 50, 49, 20], np.int32), np.array([0, 4, 5], np.int32), np.array([48, 16], np.int32)
+    good = np.array([[5, 6, 7, 8, 9], [-1] * 5, [5, 6, 7, 3, -1], [5, 6, 7, 2, -1], [1, 0, -1, -1, -1]], np.int32)
+    desc = B.make_desc(5, 4, 1, 64, 5, 10, 0.1)
+    B._check_group_pages(desc, good, lens, offsets, shared)
+    kept = good.copy()
+    B._check_group_pages(desc, torch.from_numpy(good), lens, offsets, shared)
+    assert np.array_equal(good, kept)
+    for row, col, value, bad in ((2, 1, -1, False), (2, 0, -(1 << 30), False), (3, 2, 10, False),      # not read, and no page
+                                 (2, 1, 4, True), (3, 0, 6, True),                                      # another page than the group's
+                                 (0, 1, -1, True), (0, 2, 10, True), (2, 3, -1, True), (3, 3, 10, True), (4, 1, -5, True), (1, 0, 99, False)):
+        table = good.copy()
+        table[row, col] = value
+        assert _refused(B._check_group_pages, desc, table, lens, offsets, shared) == bad, (row, col, value)
+    # what the call refuses by itself does not get in the way
+    B._check_group_pages(desc, good, lens, np.array([0, 99, 5], np.int32)[[0, 2, 2]], np.array([-4, 16], np.int32))
+
+
+def test_debug_check_of_stored_pages():
+    """A store reads the entries of its new tokens' pages, less those it writes: the others may hold anything."""
+    lens, news = np.array([70, 0, 33, 40], np.int32), np.array([3, 0, 1, 20], np.int32)
+    table = np.full((4, 5), -(1 << 30), np.int32)
+    table[0, 4], table[2, 2], table[3, 1:3] = 8, 7, (5, 6)
+    desc = B.make_desc(4, 4, 1, 64, 5, 10, 0.1)
+    B._check_stored_pages(desc, table, lens, news, None)
+    for row, col in ((0, 4), (2, 2), (3, 1), (3, 2)):
+        for value in (-1, 10):
+            bad = table.copy()
+            bad[row, col] = value
+            assert _refused(B._check_stored_pages, desc, bad, lens, news, None)
+            named = np.full(4, -1, np.int32)
+            named[row] = 9
+            assert _refused(B._check_stored_pages, desc, bad, lens, news, named) == (col == 1)     # its last page is named
+    for value in (-2, 10):
+        assert _refused(B._check_stored_pages, desc, table, lens, news, np.array([-1, -1, value, -1], np.int32))
