@@ -1942,7 +1942,8 @@ class DecodeLoopRunner:
 
     def key_weights(self, q, lse, weights, positions, stream=None):
         """Adds the last step's attention weights (its q and lse, or their rows of the running sequences) to weights.
-        Tokens that no call has weighed start there, and get their positions."""
+        Tokens that no call has weighed start there, and get their positions. q as the step took it: with rotary positions
+        it is turned here as it was there."""
         if self.groups is not None:
             raise ValueError("a loop over groups weighs no keys")
         lens = self.table.prev
@@ -1953,6 +1954,10 @@ class DecodeLoopRunner:
             edges = np.flatnonzero(np.diff(live, prepend=False, append=False)).reshape(-1, 2).tolist()
             with torch.cuda.stream(stream):   # where the rows are read
                 q, lse = (torch.cat([x[a:b] for a, b in edges]) for x in (q, lse))
+        if self.rotary is not None and live.any():
+            with torch.cuda.stream(stream):
+                at = torch.from_numpy((lens - 1 + self.evicted)[live].astype(np.int32)).to(q.device)
+                q, _ = self.rotary(q, None, at, stream=stream)
         held = np.minimum(self.weighed, lens)
         self.attn.key_weights(q, lse, self.k_pool, self.block_table, lens, (lens > 0).astype(np.int32), self.scale, weights,
                               positions=positions, held_lens=held, first_pos=held + self.evicted,

@@ -1,15 +1,18 @@
-"""GPU tests of a group rollout's step at its edges. Tolerances as in tests/test_gpu_step.py."""
+"""GPU tests of a group rollout's step at its edges. Tolerances as in tests/test_gpu_step.py and
+tests/test_gpu_cache.py."""
 import math
 
 import numpy as np
 import pytest
 import torch
 
+from oracle import cache_ref
 from paper_2601_12784_amd import binding as B
-from tests.test_gpu_cache import Cache
-from tests.test_gpu_step import Grouped, check_samples, check_turned, cuda, randn
+from tests.test_gpu_cache import Cache, bits, check, wide
+from tests.test_gpu_step import U, Grouped, check_samples, check_turned, cuda, randn
 
 pytestmark = pytest.mark.gpu
+PAGE = 16
 
 
 @pytest.fixture(scope="module", autouse=True)
@@ -168,3 +171,52 @@ def test_debug_checks_accept_what_the_calls_allow(monkeypatch):
         with pytest.raises(ValueError, match="sequence 3 does not start with"):
             attn.shared(q, cache.g_k, cache.g_v, cache.g_bt, lens, offsets, shared, 0.1, fp8=cache.g_fp8)
         torch.cuda.synchronize()
+
+
+# ---------------------------------------------------------------------------
+# loops
+# ---------------------------------------------------------------------------
+@pytest.mark.parametrize("fp8", [False, True])
+def test_weights_of_a_loop_with_rotary_positions(fp8):
+    """key_weights takes the step's queries as they came and weighs with the turned ones: against 64 bits, with an
+    eviction, a sequence that ends, and rows of the running ones alone."""
+    hq, hkv, d, g = 8, 2, 64, 4
+    rng = np.random.default_rng(6)
+    lens = np.array([40, 24, 9], np.int64)
+    c = Cache([64, 64, 64], hkv, d, fp8, 95)
+    rotary = B.Rotary(d, base=500.0, layout="interleaved")
+    loop = B.DecodeLoopRunner(hq, hkv, d, c.g_k, c.g_v, c.g_bt, c.bt, lens, 0.125, fp8=c.g_fp8, rotary=rotary)
+    w = torch.full((c.n, hkv, PAGE), float("nan"), device="cuda")
+    pos = torch.full((c.n, hkv, PAGE), -1, dtype=torch.int32, device="cuda")
+    for i in range(8):
+        q, kn, vn = randn(rng, 3, hq, d), randn(rng, 3, hkv, d), randn(rng, 3, hkv, d)
+        lse = torch.empty((3, hq), device="cuda")
+        if i:
+            lens = np.where(lens > 0, lens + 1, 0)
+        if i == 5:
+            lens[1] = 0
+        loop.step(q, lens, *((kn, vn) if i else ()), lse=lse)
+        at = np.maximum(lens - 1 + loop.evicted, 0).astype(np.int32)
+        turned = rotary(q, None, torch.from_numpy(at).cuda())[0]
+        check_turned(turned, q, at, rotary, "q")
+        held, before = np.minimum(loop.weighed, lens), w.double().cpu().numpy()
+        rows = torch.from_numpy(np.flatnonzero(lens)).cuda()
+        given = (q[rows], lse[rows]) if i == 6 else (q, lse)
+        loop.key_weights(*given, w, pos)
+        torch.cuda.synchronize()
+        k, ks = (c.g_k.cpu().numpy(), c.g_fp8[0].cpu().numpy()) if fp8 else (bits(c.g_k).reshape(c.k.shape), None)
+        got, qw, lw = w.double().cpu().numpy(), wide(turned), lse.double().cpu().numpy()
+        for s in np.flatnonzero(lens):
+            n = int(lens[s])
+            pages = loop.bt_host[s, : -(-n // PAGE)]
+            for h in range(hkv):
+                heads = slice(h * g, (h + 1) * g)
+                keys = cache_ref.dense(k, ks, pages, h, n, d, False)
+                u, size = cache_ref.key_weights(qw[s: s + 1, heads], lw[s: s + 1, heads], keys, 0.125, n - 1)
+                t = np.arange(n)
+                old = np.where(t < held[s], before[pages[t // PAGE], h, t % PAGE], 0.0)
+                rel = 2 * (d + 8) * U * size + 4 * U * np.abs(lw[s, heads]).max() + 2.0 ** -21 + (g + 4) * U
+                check(got[pages[t // PAGE], h, t % PAGE], old + u, rel * u + 2 * U * (old + u) + 1e-37, f"step {i}")
+        if i == 3:
+            lens = loop.evict(16, w, pos, sinks=2, recent=4).astype(np.int64)
+            assert lens.tolist() == [16, 16, 12]
