@@ -1889,6 +1889,10 @@ class DecodeLoopRunner:
             raise ValueError("every step after the first appends a token: pass k_new and v_new")
         if self.groups is not None and np.any((lens > 0) & (self.table.prev == 0)):
             raise ValueError("a sequence of a group that has left does not start again")
+        if self.groups is not None and attn_events is not None:
+            raise ValueError("a step over groups takes no attn_events")
+        if self.groups is not None and np.any((lens > 0) & (lens < np.repeat(self.groups[1], np.diff(self.groups[0])))):
+            raise ValueError("a member is shorter than its group's shared tokens")
         new_pages = self.table.advance(lens, appending)
         if DEBUG_CHECKS:
             desc = make_desc(lens.size, self.attn.hq, self.attn.hkv, self.attn.d, self.table.bt.shape[1],
@@ -1909,8 +1913,6 @@ class DecodeLoopRunner:
     def _step_stored(self, q, lens, append, out, lse, stream, attn_events):
         """A step of a loop with rotary positions or groups: what is new is turned and stored, then attended to."""
         attn, checked = self.attn, self.attn._host_checked
-        if self.groups is not None and attn_events is not None:
-            raise ValueError("a step over groups takes no attn_events")
         if self.rotary is not None and (append is None or self.fp8 is not None):
             with torch.cuda.stream(stream):
                 at = torch.from_numpy(np.maximum(lens - 1 + self.evicted, 0).astype(np.int32)).to(q.device)

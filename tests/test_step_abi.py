@@ -544,3 +544,18 @@ def test_debug_check_of_stored_pages():
             assert _refused(B._check_stored_pages, desc, bad, lens, news, named) == (col == 1)     # its last page is named
     for value in (-2, 10):
         assert _refused(B._check_stored_pages, desc, table, lens, news, np.array([-1, -1, value, -1], np.int32))
+
+
+def test_a_refused_step_of_a_group_loop_moves_nothing():
+    """The page table goes on only with a step that is taken."""
+    bt = np.array([[3, 1], [3, 2]], np.int32)
+    pools = gpu(6, 2, 8, 16, 8), gpu(6, 2, 64, 16)
+    loop = B.DecodeLoopRunner(4, 2, 64, *pools, gpu(2, 2, dtype=torch.int32), bt, [17, 17], 0.1, num_cus=256, groups=([0, 2], [16]))
+    loop.steps = 1       # (the first one attends alone)
+    free, before = loop.pool.available(), loop.bt_host.copy()
+    for kw in (dict(attn_events=(1, 2)), dict(k_new=None), dict(lens=[15, 18])):
+        a = dict(q=gpu(2, 4, 64), lens=[18, 0], k_new=gpu(2, 2, 64), v_new=gpu(2, 2, 64))
+        a.update(kw)
+        with pytest.raises(ValueError):
+            loop.step(**a)
+        assert loop.pool.available() == free and loop.table.prev.tolist() == [17, 17] and np.array_equal(loop.bt_host, before)
