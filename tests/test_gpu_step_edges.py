@@ -220,3 +220,62 @@ def test_weights_of_a_loop_with_rotary_positions(fp8):
         if i == 3:
             lens = loop.evict(16, w, pos, sinks=2, recent=4).astype(np.int64)
             assert lens.tolist() == [16, 16, 12]
+
+
+@pytest.mark.parametrize("hq,hkv,d", [(14, 2, 64), (28, 4, 128)])
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("members,together", [(4, 2), (10, 4), (20, 8), (40, 8)])
+def test_many_steps_of_a_prompts_walk(members, together, fp8, hq, hkv, d):
+    """Prompts whose rows take two, four, eight and sixteen blocks, walked far enough that the ring of registers and that
+    of LDS come round several times, with an odd number of pages and some own tokens."""
+    prefix = 1205
+    lens = [prefix + 1 + 11 * s % 60 for s in range(members)]
+    cache = Grouped(lens, [0, members], [prefix], hkv, d, fp8, seed=members, spread=0.5 if fp8 else 0.0)
+    opts = B.make_opts(num_cus=2)
+    desc = B.make_desc(members, hq, hkv, d, cache.bt.shape[1], cache.n, 0.1)
+    info, work = B.sf_shared_attn_plan(desc, lens, [0, members], [prefix], opts=opts, fp8=fp8)
+    items = np.asarray(work[16 * info.num_workers: 16 * (info.num_workers + info.num_work)]).reshape(-1, 16)
+    walks = items[items[:, 11] > 0]
+    assert (walks[:, 11] == together).all() and ((walks[:, 6] - walks[:, 5] + 1) // 2 // (8 // together)).max() >= 9
+    q = randn(np.random.default_rng(members), members, hq, d)
+    lse = torch.empty(members, hq, device="cuda")
+    out = B.DecodeAttention(hq, hkv, d, opts=opts).shared(q, cache.g_k, cache.g_v, cache.g_bt, lens, [0, members], [prefix], 0.1, lse=lse, fp8=cache.g_fp8)
+    cache.check(q, out, lse, 0.1, hq)
+
+
+@pytest.mark.parametrize("grouped", [True, False])
+@pytest.mark.parametrize("turned", [True, False])
+def test_what_a_loop_over_fp8_pages_stores(turned, grouped):
+    """Every step's keys and values, turned or as they came, of the running sequences alone, against the oracle's store:
+    all codes and scales, bit for bit."""
+    if not turned and not grouped:
+        pytest.skip("the plain appending step")
+    hq, hkv, d = 8, 2, 64
+    rng = np.random.default_rng(8)
+    prompts, members = [70, 33, 16], [3, 1, 4]
+    lens, offsets = np.repeat(prompts, members).astype(np.int64), np.cumsum([0] + members)
+    c = (Grouped(lens, offsets, prompts, hkv, d, True, seed=13, spare=40, stride_extra=3) if grouped else
+         Cache(lens, hkv, d, True, seed=13, spare=40, stride_extra=3))
+    rotary = B.Rotary(d, base=500.0) if turned else None
+    c.g_bt = torch.from_numpy(c.bt.copy()).cuda()
+    loop = B.DecodeLoopRunner(hq, hkv, d, c.g_k, c.g_v, c.g_bt, c.bt, lens, 0.2, fp8=c.g_fp8, rotary=rotary,
+                              groups=(offsets, prompts) if grouped else None)
+    b = lens.size
+    for step in range(20):
+        q, kn, vn = randn(rng, b, hq, d), randn(rng, b, hkv, d, mult=2.0 ** rng.integers(-3, 3)), randn(rng, b, hkv, d)
+        if step:
+            lens = np.where(lens > 0, lens + 1, 0)
+        for s in {5: (1, 7), 9: (0, 2)}.get(step, ()):
+            lens[s] = 0
+        loop.step(q, lens, *((kn, vn) if step else ()))
+        if step:
+            at = np.maximum(lens - 1, 0)
+            keys = kn if rotary is None else rotary(None, kn, torch.from_numpy(at.astype(np.int32)).cuda())[1]
+            if turned:
+                check_turned(keys, kn, at, rotary, "k")
+            live = np.flatnonzero(lens)
+            c.bt = loop.bt_host
+            cache_ref.store_fp8(bits(keys).reshape(kn.shape)[live], bits(vn).reshape(vn.shape)[live], lens, (lens > 0).astype(int),
+                                c.bt, c.k, c.v, c.ks, c.vs)
+        torch.cuda.synchronize()
+        c.same(f"step {step}", table=False)
