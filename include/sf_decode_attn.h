@@ -751,8 +751,9 @@ sf_status sf_page_pool_release(sf_page_pool* pool, const int32_t* pages, int32_t
  *      in ascending sequence order, recorded in the block table;
  *   3. new_pages[s] = that page, or -1: the array sf_decode_attn_append takes.
  * Appending steps expect lens = prev_lens + 1 for every running sequence.
- * All or nothing: SF_ERR_INVALID_ARG for a length outside [0, 16 * stride]
- * or a page to return that is not in use, SF_ERR_CAPACITY if the pool cannot
+ * All or nothing: SF_ERR_INVALID_ARG for a length outside [0, 16 * stride],
+ * a page to return that is not in use, or a newest token inside a page that
+ * other sequences still hold after 1; SF_ERR_CAPACITY if the pool cannot
  * supply the pages; nothing changes then.
  */
 sf_status sf_page_table_step(sf_page_pool* pool, int32_t* block_table, int32_t stride,

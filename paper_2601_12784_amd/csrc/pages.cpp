@@ -145,6 +145,16 @@ extern "C" sf_status sf_page_table_step(sf_page_pool* pool, int32_t* block_table
   int64_t freed = 0;
   if (!check_pages(pool, gone.data(), int32_t(gone.size()), 1, &freed)) return SF_ERR_INVALID_ARG;
   if (opens > int64_t(pool->stack.size()) + freed) return SF_ERR_CAPACITY;
+  // a new token in a begun page that others go on holding would change what they read
+  bool theirs = false;
+  for (int32_t pg : gone) ++pool->mark[size_t(pg)];
+  for (int32_t s = 0; s < num_seqs && appending && !theirs; ++s) {
+    if (lens[s] <= 0 || (lens[s] - 1) % kPage == 0) continue;
+    const int32_t pg = block_table[int64_t(s) * stride + (lens[s] - 1) / kPage];
+    theirs = pg >= 0 && pg < pool->num_pages && pool->in_use[size_t(pg)] - pool->mark[size_t(pg)] > 1;
+  }
+  for (int32_t pg : gone) pool->mark[size_t(pg)] = 0;
+  if (theirs) return SF_ERR_INVALID_ARG;
   for (int32_t pg : gone) give_back(pool, pg);
   for (int32_t s = 0; s < num_seqs; ++s) {
     const int32_t len = lens[s];

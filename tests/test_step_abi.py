@@ -559,3 +559,26 @@ def test_a_refused_step_of_a_group_loop_moves_nothing():
         with pytest.raises(ValueError):
             loop.step(**a)
         assert loop.pool.available() == free and loop.table.prev.tolist() == [17, 17] and np.array_equal(loop.bt_host, before)
+
+
+def test_no_new_token_goes_into_a_page_that_others_hold():
+    """After a cut into the shared tokens, or where a begun page is shared, the next token would change the others' keys."""
+    t = B.PageTable(12, _table(), [40, 50, 36, 5], ([0, 3, 4], [35, 0]))
+    t.truncate([20, 50, 36, 5])        # the first member's cache ends inside a page of all three
+    free, before = t.pool.available(), t.bt.copy()
+    for lens in ([21, 51, 37, 6], [21, 51, 0, 6]):
+        with pytest.raises(B.SfError):
+            t.advance(lens)
+        assert t.pool.available() == free and np.array_equal(t.bt, before) and t.prev.tolist() == [20, 50, 36, 5]
+    assert t.advance([20, 50, 36, 5], appending=False).tolist() == [-1] * 4      # it may be read
+    t.advance([21, 0, 0, 6])           # the others leave: the page is its own
+    t.advance([22, 0, 0, 0])
+    assert t.pool.available() == 12 - 2
+    # a page of several holders that is begun
+    pool, bt = B.PagePool(4), np.array([[2], [2]], np.int32)
+    pool.claim([2])
+    pool.share([2])
+    lens, new = np.array([5, 5], np.int32), np.zeros(2, np.int32)
+    step = lambda to: B.lib().sf_page_table_step(pool._p, bt.ctypes.data, 1, 2, lens.ctypes.data,  # noqa: E731
+                                                 np.array(to, np.int32).ctypes.data, 1, new.ctypes.data)
+    assert step([6, 6]) == INVALID and step([6, 0]) == OK and pool.available() == 3
