@@ -1146,13 +1146,16 @@ __device__ __forceinline__ void whole_row(const SampleArgs& a, int row, const Sa
     r.load(q < end ? q : r.pieces, x);
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
+      // Selects of values formed for all lanes: with a branch around the weight, hipcc left the weight's bits in
+      // w[i] of lanes that it sent away (ROCm 7.2.0; a draw then fell to an entry below the least weight).
       const uint32_t key = key_of(x[i]);
-      const bool in = x[i] >= bound && key >= cut.key && key != 0 && !(low > 0.0 && s.weight(x[i]) < low);
-      w[i] = in ? s.units(x[i]) : 0;
-      if (in && key == cut.key) {
-        is_tie |= 1u << i;
-        ++mine_ties;
-      }
+      const uint64_t units = s.units(x[i]);
+      bool in = (x[i] >= bound) & (key >= cut.key) & (key != 0);
+      if (low > 0.0) in &= !(s.weight(x[i]) < low);
+      const bool tie = in & (key == cut.key);
+      w[i] = in ? units : 0;
+      is_tie |= uint32_t(tie) << i;
+      mine_ties += tie;
     }
     uint32_t rank = tie + wave_scan(mine_ties) - mine_ties;
 #pragma unroll

@@ -47,6 +47,27 @@ def test_draws_at_the_border_of_equal_chunks(rows, block, chunks, dtype, cut):
     check_samples(x[some], u[some], (token[some], logprob[some], kept[some]), **{k: t[some] for k, t in params.items()})
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("vocab", [4700, 9001, 50000])
+@pytest.mark.parametrize("top_k", [0, 372, 4500])
+def test_a_least_weight_above_the_other_cuts(top_k, vocab, dtype):
+    """min-p is the strictest of three cuts of rows that a list does not hold: no token is lighter."""
+    rng = np.random.default_rng(vocab + top_k)
+    b = 64
+    x = torch.from_numpy(rng.standard_normal((b, vocab)).astype(np.float32)).to(dtype).cuda()
+    u = cuda(rng.random(b), torch.float32)
+    for top_p in (0.9, 0.99, 1.0):
+        params = dict(temperature=torch.full((b,), 3.0, device="cuda"), top_p=torch.full((b,), top_p, device="cuda"),
+                      min_p=cuda(rng.choice([0.2, 0.5, 0.9, 1.0], b), torch.float32))
+        if top_k:
+            params["top_k"] = torch.full((b,), top_k, dtype=torch.int32, device="cuda")
+        token, logprob, kept = B.Sampler()(x, u, **params)
+        weight = torch.exp((x.double() - x.double().amax(1, keepdim=True)) / 3.0).gather(1, token.long()[:, None])[:, 0]
+        assert (weight >= params["min_p"].double() * (1 - 2.0 ** -40)).all(), torch.nonzero(weight < params["min_p"])[:, 0].tolist()
+        some = list(range(0, b, 9))
+        check_samples(x[some], u[some], (token[some], logprob[some], kept[some]), **{k: t[some] for k, t in params.items()})
+
+
 # ---------------------------------------------------------------------------
 # attention over shared prompts
 # ---------------------------------------------------------------------------
