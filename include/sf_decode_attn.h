@@ -942,7 +942,7 @@ sf_status sf_rotary(const sf_rotary_desc* rotary, int32_t num_tokens, int32_t nu
                     void* stream);
 
 /*
- * The same for new tokens, whose turned keys and whose values go straight into the pages of a bf16 cache. The last
+ * The same, to the same bits, for new tokens, whose turned keys and whose values go straight into the pages of a bf16 cache. The last
  * q_lens_host[s] of sequence s' seq_lens_host[s] tokens are new; rows of q [T][Hq][D], k_new and v_new [T][Hkv][D] are
  * theirs, sequence after sequence, with token strides as for sf_rotary. The first new one is at position
  * first_pos_host[s] (NULL: at its index in the cache; a cache that has given up tokens counts on). q_lens_host NULL is a

@@ -60,6 +60,11 @@ struct Pieces {
   u32x4 x, y;
 };
 
+// The turn of a pair, with its two fused products named: left to the compiler, another copy of the loop fused the others,
+// and where the sum nearly cancels a head's bits followed from the launch's shape.
+__device__ __forceinline__ float first_of(float a, float b, const Turn& t) { return __builtin_fmaf(a, t.cos, -(b * t.sin)); }
+__device__ __forceinline__ float second_of(float a, float b, const Turn& t) { return __builtin_fmaf(b, t.cos, a * t.sin); }
+
 // The two pieces' 8 pairs: (x[i], y[i]) in the half layout, neighbours in the
 // interleaved one.
 template <bool kInterleaved>
@@ -70,13 +75,13 @@ __device__ __forceinline__ Pieces turned(const Pieces& p, const Turn* t) {
     if constexpr (kInterleaved) {
       const Turn t0 = t[w], t1 = t[4 + w];
       const float a0 = low(p.x[w]), b0 = high(p.x[w]), a1 = low(p.y[w]), b1 = high(p.y[w]);
-      r.x[w] = pack(a0 * t0.cos - b0 * t0.sin, b0 * t0.cos + a0 * t0.sin);
-      r.y[w] = pack(a1 * t1.cos - b1 * t1.sin, b1 * t1.cos + a1 * t1.sin);
+      r.x[w] = pack(first_of(a0, b0, t0), second_of(a0, b0, t0));
+      r.y[w] = pack(first_of(a1, b1, t1), second_of(a1, b1, t1));
     } else {
       const Turn t0 = t[2 * w], t1 = t[2 * w + 1];
       const float a0 = low(p.x[w]), a1 = high(p.x[w]), b0 = low(p.y[w]), b1 = high(p.y[w]);
-      r.x[w] = pack(a0 * t0.cos - b0 * t0.sin, a1 * t1.cos - b1 * t1.sin);
-      r.y[w] = pack(b0 * t0.cos + a0 * t0.sin, b1 * t1.cos + a1 * t1.sin);
+      r.x[w] = pack(first_of(a0, b0, t0), first_of(a1, b1, t1));
+      r.y[w] = pack(second_of(a0, b0, t0), second_of(a1, b1, t1));
     }
   }
   return r;

@@ -172,6 +172,41 @@ def test_a_rotary_made_for_the_current_device_can_be_captured():
     assert rotary.turns_on(torch.device("cuda")) is rotary.turns_on(q.device)
 
 
+@pytest.mark.parametrize("d,turn", [(64, 64), (64, 32), (128, 128), (128, 96)])
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+def test_storing_and_plain_turns_have_the_same_bits(d, turn, layout):
+    """Pairs whose turn nearly cancels show every rounding of the products: both kernels have to make the same ones."""
+    hq, hkv, t = 28, 4, 3200      # so many pages that a thread takes several heads
+    rng = np.random.default_rng(d + turn)
+    rotary = B.Rotary(d, rotary_dim=turn, layout=layout)
+    first = int(rng.integers(0, 1 << 20))
+    angle = (first + np.arange(t, dtype=np.float64))[:, None, None] * rotary.freq
+    size = rng.uniform(0.5, 2.0, (t, hq + hkv, turn // 2))
+    sign = rng.integers(0, 2, (t, hq + hkv, 1)).astype(bool)
+    # (a, b) ~ (sin, cos): a cos - b sin is near 0; (cos, -sin): b cos + a sin is
+    a, b = (np.where(sign, p, r) * size for p, r in ((np.sin(angle), np.cos(angle)), (np.cos(angle), -np.sin(angle))))
+    x = rng.standard_normal((t, hq + hkv, d))
+    if layout == "half":
+        x[..., : turn // 2], x[..., turn // 2: turn] = a, b
+    else:
+        x[..., 0: turn: 2], x[..., 1: turn: 2] = a, b
+    x = torch.from_numpy(x.astype(np.float32)).to(torch.bfloat16).cuda()
+    q, k = x[:, :hq].contiguous(), x[:, hq:].contiguous()
+    at = torch.arange(first, first + t, dtype=torch.int32, device="cuda")
+    want = rotary(q, k, at)
+    for some in (slice(0, 60), slice(t - 60, t)):
+        check_turned(want[0][some], q[some], at[some].cpu().numpy(), rotary, "q")
+        check_turned(want[1][some], k[some], at[some].cpu().numpy(), rotary, "k")
+    cache = Cache([t], hkv, d, False, seed=1)
+    got = B.DecodeAttention(hq, hkv, d).rotate_store(rotary, q, k, k, cache.g_k, cache.g_v, cache.g_bt, [t], [t], first_pos=[first])
+    assert torch.equal(got, want[0])
+    pages = cache.g_bt[0, : t // PAGE].long()
+    stored = cache.g_k[pages].permute(0, 3, 1, 2, 4).reshape(t, hkv, d)
+    assert torch.equal(stored, want[1])
+    for n in (1, 17):        # few tokens: other shapes of the launch
+        assert all(torch.equal(y[:n], z) for y, z in zip(want, rotary(q[:n].contiguous(), k[:n].contiguous(), at[:n].contiguous())))
+
+
 def test_debug_checks_accept_what_the_calls_allow(monkeypatch):
     """Entries of shared pages in the other members' rows stay unfilled: stores and steps do not read them."""
     monkeypatch.setattr(B, "DEBUG_CHECKS", True)
