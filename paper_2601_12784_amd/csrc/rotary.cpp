@@ -16,7 +16,7 @@ namespace {
 
 constexpr int32_t kMaxTokens = 1 << 30;     // per sequence, as the fp8 store's
 constexpr int64_t kMaxRows = 1 << 23;       // workgroups of 256 threads: 2^32 threads are too many for a launch
-constexpr int32_t kMaxTurned = 1 << 27;     // tokens of a call, 16 to a workgroup
+constexpr int32_t kMaxTurned = 1 << 27;     // tokens of a call, of so many 16 to a workgroup
 constexpr uint64_t kRotaryKey = 0x526f74617279ull;   // tells this plan's info from the fp8 store's
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }

@@ -13,8 +13,10 @@
 // page layout asks for in registers: a thread reads two dims of 16 tokens
 // and writes 2 x 32 contiguous bytes.
 //
-// Measured: 8192 tokens of 32 + 8 heads of 128 37 us = 4.5 TB/s, the tokens of 32 prompts into their
-// pages 228 us = 4.55 TB/s (a copy of 4 GiB here: 4.6). A step's few tokens are bound by the launch (3 us) and the host.
+// Measured: 8192 tokens of 32 + 8 heads of 128 38 us = 4.4 TB/s, the tokens of 32 prompts into their
+// pages 230 us = 4.5 TB/s (a copy of 4 GiB here: 4.6). Few tokens alone are bound by the launch (3 us) and the host; the 512
+// of a step with their store by reads that wait for each other (list row over PCIe, block table, keys, then values: 11 us
+// where the bytes take 2) and by values of 2 bytes 32 bytes apart, as the layout has them.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -208,8 +210,10 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs a, int per_
 template <int D, bool kInterleaved>
 hipError_t launch(const RotaryArgs& a, hipStream_t stream) {
   const int heads = a.num_q_heads + a.num_kv_heads;
-  // tokens that share a workgroup's tile: all of a page's, or in the plain form as many as leave the GPU enough tiles
-  const int per_tile = a.rows ? kPage : a.num_tokens >= 16384 ? 16 : a.num_tokens >= 4096 ? 4 : 1;
+  // tokens that share a workgroup's tile: all of a page's, or in the plain form one, four of many (28 + 4 heads of 128, one,
+  // four and sixteen to a tile: 8192 tokens 31.0, 29.8 and 30.9 us, 17000 54.9, 56.2 and 63.2, 32768 100, 101 and 111),
+  // and sixteen where a launch would have 2^32 threads
+  const int per_tile = a.rows ? kPage : a.num_tokens > 1 << 24 ? 16 : a.num_tokens >= 4096 ? 4 : 1;
   const int64_t tiles = a.rows ? a.num_rows : (int64_t(a.num_tokens) + per_tile - 1) / per_tile;
   // few tiles: their heads are split over workgroups
   const int lanes = kThreads / (D / 16) / (a.rows && a.num_tokens <= a.num_rows ? 1 : per_tile);

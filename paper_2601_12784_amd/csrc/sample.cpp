@@ -23,7 +23,8 @@ sf_status check_sample(const sf_sample_desc* d) {
 }  // namespace
 
 // Elements per workgroup of the first launch: long chunks read with the fewest
-// instructions, short ones give a few rows enough workgroups.
+// instructions, short ones give a few rows enough workgroups. Rows of 131072 bf16 with a top-p, short and long:
+// 8 rows 81 and 85 us, 24 106 and 102, 40 123 and 106, 128 224 and 175 (without cuts 19, 19, 20 and 30, all within 1.3).
 int32_t sf::sample_chunk(const sf_sample_desc& d) {
   return int64_t(d.num_rows) * d.vocab >= int64_t(512) * kSampleChunk ? kSampleChunk : kSampleSmallChunk;
 }

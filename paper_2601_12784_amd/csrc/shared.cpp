@@ -34,7 +34,9 @@ int32_t splits_of(int32_t blocks) { return blocks == 1 ? 1 : kSharedWaves / bloc
 // 2450: 95, 89 and 93 us; 8 of 8000 with 8 (40/8, fp8) at 900, 1000 and 1300: 84, 81 and 85.
 double own_cost(const sf_attn_desc& d, bool fp8) { return fp8 ? 1000 : d.head_dim == 64 ? 950 : 1700; }
 // Of a prompt whose rows several waves hold: the time of its blocks of rows on their waves' matrix and vector units, at least
-// the staging by eight waves.
+// the staging by eight waves. Head dim 64 at 0.45, 0.63 and 1.0 of it (14/2 heads, prompts x members: 16 x 16 of 2048 tokens,
+// 8 x 40 of 4000, 1 x 256 of 4000): 49, 74 and 61 us; 46, 61 and 53; 43, 65 and 47. Own pages there in fp8 at 700, 1000 and
+// 1400: 46, 58 and 45 us; 44, 60 and 45; 46, 67 and 56.
 double page_cost(const sf_attn_desc& d, int32_t blocks, bool fp8) {
   if (blocks == 1) return own_cost(d, fp8);
   return std::max(2000.0, (fp8 ? 1300 : 980) * (d.head_dim == 64 ? 0.63 : 1.0) * blocks);

@@ -207,6 +207,18 @@ def test_storing_and_plain_turns_have_the_same_bits(d, turn, layout):
         assert all(torch.equal(y[:n], z) for y, z in zip(want, rotary(q[:n].contiguous(), k[:n].contiguous(), at[:n].contiguous())))
 
 
+def test_rotary_of_more_tokens_than_a_launch_has_tiles_of_four():
+    """Beyond 2^24 tokens a workgroup takes sixteen of them: the same bits, to the last token."""
+    t = (1 << 24) + 5
+    rotary, q = B.Rotary(64, rotary_dim=32), torch.randn(t, 1, 64, device="cuda", dtype=torch.bfloat16)
+    at = torch.arange(t, dtype=torch.int32, device="cuda")
+    out = rotary(q, None, at)[0]
+    for a in (0, 1 << 23, t - 1000):
+        some = slice(a, a + 1000)
+        assert torch.equal(out[some], rotary(q[some], None, at[some])[0])
+    check_turned(out[-20:], q[-20:], range(t - 20, t), rotary, "q")
+
+
 def test_debug_checks_accept_what_the_calls_allow(monkeypatch):
     """Entries of shared pages in the other members' rows stay unfilled: stores and steps do not read them."""
     monkeypatch.setattr(B, "DEBUG_CHECKS", True)
