@@ -291,7 +291,8 @@ sf_status sf_runner_reserve(sf_runner* runner, uint64_t workspace_bytes, uint64_
  * with any options (chunk_pages too). Takes no more than such steps can use, where
  * sf_runner_reserve, which does not know the lengths, keeps a few MB.
  * SF_ERR_INVALID_ARG for NULL pointers or negative numbers, else as
- * sf_runner_reserve. */
+ * sf_runner_reserve. Steps of groups (sf_runner_shared), whose lists are
+ * longer, and the cache's other calls grow the buffers at their first use. */
 sf_status sf_runner_reserve_batch(sf_runner* runner, const int32_t* seq_lens_host, int32_t num_seqs, void* stream);
 /* The plan of a runner's step (host only, arguments as sf_decode_attn_plan;
  * kind: 0 a plain step, 1 over an fp8 cache, 2 appending). With options that leave the slices to the planner
@@ -904,7 +905,7 @@ sf_status sf_runner_shared(sf_runner* runner, const sf_attn_desc* desc, const in
  *   (a cos - b sin, b cos + a sin) * magnitude,   of the angle t f_i;
  * dims R .. D-1 stay as they are. Queries and keys are bf16, the products are formed in fp32 and rounded once.
  * Frequencies enter as turns: f_i / (2 pi), less whole turns, in units of 2^-64, so t times it, modulo 2^64, is the
- * angle's fraction of a turn, off by at most |t| 2^-65 turns whatever t is.
+ * angle's fraction of a turn, off by less than |t| 2^-64 turns whatever t is, for |f_i| up to 2 pi (|t f_i| 2^-66 beyond).
  * Negative positions turn backwards (which also is the gradient's way through a rotation).
  */
 typedef struct sf_rotary_desc {
@@ -916,7 +917,8 @@ typedef struct sf_rotary_desc {
 
 /* Frequencies of longer contexts than a model was trained on: with r_i = trained_length f_i / (2 pi) turns in the
  * trained length and s = clamp((r_i - low_turns) / (high_turns - low_turns), 0, 1), f_i becomes
- * s f_i + (1 - s) f_i / factor. trained_length = 0: f_i / factor. */
+ * s f_i + (1 - s) f_i / factor. trained_length = 0: f_i / factor. (Configurations whose ramp runs in the pair's index i
+ * instead, between the indexes of two numbers of turns, are another rule: give sf_rotary_turns their frequencies.) */
 typedef struct sf_rotary_scaling {
   double factor;           /* > 0 */
   double trained_length;   /* >= 0 */

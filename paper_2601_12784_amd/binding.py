@@ -1646,7 +1646,8 @@ class Rotary:
     (default: all) turn, in pairs half of rotary_dim apart (layout "half") or of neighbours ("interleaved"), by
     angles of position * freq[i]; freq (radians per position, float64 [rotary_dim / 2]) defaults to base^(-2i / rotary_dim).
     scaling: a dict for contexts longer than the trained one, with factor and, for frequencies that keep their turns in it,
-    original (tokens), low, high (turns; sf_rotary_scaling); its magnitude (default 1) multiplies what is turned."""
+    original (tokens), low, high (turns; sf_rotary_scaling); its magnitude (default 1) multiplies what is turned. Its ramp is
+    linear in the turns; frequencies of a ramp in the pair's index, as some configurations have it, go in as freq."""
 
     def __init__(self, head_dim, rotary_dim=None, base=10000.0, layout="half", scaling=None, freq=None, device=None):
         self.head_dim = int(head_dim)
