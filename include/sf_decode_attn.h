@@ -292,7 +292,8 @@ sf_status sf_runner_reserve(sf_runner* runner, uint64_t workspace_bytes, uint64_
  * sf_runner_reserve, which does not know the lengths, keeps a few MB.
  * SF_ERR_INVALID_ARG for NULL pointers or negative numbers, else as
  * sf_runner_reserve. Steps of groups (sf_runner_shared), whose lists are
- * longer, and the cache's other calls grow the buffers at their first use. */
+ * longer, and the cache's other calls grow the buffers themselves, each slot
+ * of the ring (32) at its first use. */
 sf_status sf_runner_reserve_batch(sf_runner* runner, const int32_t* seq_lens_host, int32_t num_seqs, void* stream);
 /* The plan of a runner's step (host only, arguments as sf_decode_attn_plan;
  * kind: 0 a plain step, 1 over an fp8 cache, 2 appending). With options that leave the slices to the planner

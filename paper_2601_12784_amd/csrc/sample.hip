@@ -21,7 +21,7 @@
 //
 // Measured: 256 rows of 131072 bf16 without cuts 34 + 11 us, where reading them takes 15: an entry
 // costs the first launch some thirty vector instructions (13 of them fp64), which is 25 us of that
-// work alone. 192 rows of 200003 fp32 with mixed cuts (33 us to read): 50 + 58 + 19 + 20 + 23, the second bound by its
+// work alone. 192 rows of 200003 fp32 with mixed cuts (33 us to read): 47 + 62 + 19 + 22 + 23, the second bound by its
 // slowest workgroup (thousands of entries near a cut, read again and sorted). The step forms of the
 // flat rows by one workgroup each instead took 460 us, sorting networks for the lists 120 more.
 #include <hip/hip_runtime.h>
