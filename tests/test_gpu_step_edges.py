@@ -68,6 +68,33 @@ def test_a_least_weight_above_the_other_cuts(top_k, vocab, dtype):
         check_samples(x[some], u[some], (token[some], logprob[some], kept[some]), **{k: t[some] for k, t in params.items()})
 
 
+@pytest.mark.parametrize("vocab", [700, 9001, 50000])
+@pytest.mark.parametrize("cuts", ["min_p", "top_p", "top_k", "all"])
+def test_entries_a_hair_below_the_least_weight(vocab, cuts):
+    """Logits within the margin of the bound that the groups are searched by: their own weights decide, on every way that a
+    row takes."""
+    rng = np.random.default_rng(vocab)
+    b = 24
+    edge = math.log(0.5)
+    x = rng.uniform(-0.6, 0.0, (b, vocab)).astype(np.float32)
+    below, at = rng.random((b, vocab)) < 0.4, rng.random((b, vocab)) < 0.1
+    x[below] = (edge - rng.choice([1e-7, 2e-7, 4e-7, 1e-5], below.sum())).astype(np.float32)
+    x[at] = (edge + rng.choice([6e-8, 1e-6], at.sum())).astype(np.float32)
+    x[:, 5] = 0.0
+    x, u = torch.from_numpy(x).cuda(), cuda(rng.random(b), torch.float32)
+    params = dict(min_p=torch.full((b,), 0.5, device="cuda"))
+    if cuts in ("top_p", "all"):
+        params["top_p"] = cuda(rng.choice([0.9, 0.999], b), torch.float32)
+    if cuts in ("top_k", "all"):
+        params["top_k"] = torch.full((b,), vocab - 50, dtype=torch.int32, device="cuda")
+    got = B.Sampler()(x, u, **params)
+    check_samples(x, u, got, **params)
+    if cuts == "min_p" and vocab == 9001:      # more rows than places: some go by one workgroup
+        many = x.repeat(50, 1), u.repeat(50)
+        more = B.Sampler()(*many, min_p=params["min_p"].repeat(50))
+        assert all(torch.equal(t, g.repeat(50)) for t, g in zip(more, got))
+
+
 # ---------------------------------------------------------------------------
 # attention over shared prompts
 # ---------------------------------------------------------------------------
