@@ -936,8 +936,9 @@ sf_status sf_rotary_turns(const double* freq_host, int32_t n, uint64_t* turns_ho
  * Turns the queries and keys of num_tokens tokens, token i by positions[i] (device int32). turns: device, R/2 of them.
  * q, k (bf16, either may be NULL: not turned): head h of token i starts at q + i * q_stride + h * D, in elements, so
  * both may be parts of a wider tensor; outputs likewise. An output may be its own input (same pointer and stride);
- * otherwise it must not overlap an input, and never the other output (not checked here). Pointers are 16-byte aligned, strides a multiple of 8 and at least the heads'
- * num_q_heads * D (num_kv_heads * D). One launch on the stream; nothing is allocated, so it can be captured.
+ * otherwise it must not overlap an input, and never the other output (not checked here). Pointers are 16-byte aligned,
+ * strides a multiple of 8 and at least the heads' num_q_heads * D (num_kv_heads * D). One launch on the stream; nothing
+ * is allocated, so it can be captured.
  */
 sf_status sf_rotary(const sf_rotary_desc* rotary, int32_t num_tokens, int32_t num_q_heads, int32_t num_kv_heads,
                     const uint64_t* turns, const int32_t* positions, const void* q, int64_t q_stride, void* q_out,
@@ -945,8 +946,8 @@ sf_status sf_rotary(const sf_rotary_desc* rotary, int32_t num_tokens, int32_t nu
                     void* stream);
 
 /*
- * The same, to the same bits, for new tokens, whose turned keys and whose values go straight into the pages of a bf16 cache. The last
- * q_lens_host[s] of sequence s' seq_lens_host[s] tokens are new; rows of q [T][Hq][D], k_new and v_new [T][Hkv][D] are
+ * The same, to the same bits, for new tokens, whose turned keys and whose values go straight into the pages of a bf16
+ * cache. The last q_lens_host[s] of sequence s' seq_lens_host[s] tokens are new; rows of q [T][Hq][D], k_new and v_new [T][Hkv][D] are
  * theirs, sequence after sequence, with token strides as for sf_rotary. The first new one is at position
  * first_pos_host[s] (NULL: at its index in the cache; a cache that has given up tokens counts on). q_lens_host NULL is a
  * decode step: there is a row per sequence, and the last token of each with seq_lens_host[s] > 0 is new; rows of the others
