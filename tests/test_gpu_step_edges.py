@@ -338,13 +338,10 @@ def test_many_steps_of_a_prompts_walk(members, together, fp8, hq, hkv, d):
     cache.check(q, out, lse, 0.1, hq)
 
 
-@pytest.mark.parametrize("grouped", [True, False])
-@pytest.mark.parametrize("turned", [True, False])
+@pytest.mark.parametrize("turned,grouped", [(True, True), (True, False), (False, True)])
 def test_what_a_loop_over_fp8_pages_stores(turned, grouped):
     """Every step's keys and values, turned or as they came, of the running sequences alone, against the oracle's store:
     all codes and scales, bit for bit."""
-    if not turned and not grouped:
-        pytest.skip("the plain appending step")
     hq, hkv, d = 8, 2, 64
     rng = np.random.default_rng(8)
     prompts, members = [70, 33, 16], [3, 1, 4]
